@@ -248,6 +248,99 @@ SPDP_API spdp_status spdp_spmspv_noalloc(const void* tileoffset_dev, const void*
 SPDP_API spdp_status spdp_swiglu_dp(const void* gate_dev, const void* up_dev, int64_t K, float thr, void* x_dev_out,
                            void* mask_dev_out, void* count_dev_out, void* stream);
 
+/* ---- around the projections of a decoder layer ------------------------------------------------------------
+ * The calls of this part take no handle: they run on the current device, which must hold every *_dev pointer, allocate nothing
+ * that outlasts the call, are asynchronous on `stream`, may be captured, and give the same bits for the same arguments.  Calls
+ * with different outputs may overlap.  An output may not overlap an input unless the call says so. */
+
+/* Low-rank adapters of many requests beside a shared projection: Y[n] = base[n] + scale_a * B_a * (A_a * X[n]) with
+ * a = adapter[n] (the paper has no adapters; merging B A into a statically pruned W would fill its zeros, so the adapters of a
+ * packed layer stay beside it).  X is what spdp_spmspv, spdp_spmspv_batch or spdp_spmm got for the same tokens, base what it
+ * wrote; dynamic pruning does not apply to the adapter's own product.
+ *   X_dev        fp16 [N][ldx], ldx >= K, N <= 2^24.
+ *   adapter_dev  int32 [N]; a value outside 0 .. count-1 means no adapter: Y[n] = base[n], bit for bit.
+ *   A_dev, B_dev fp16 [count][rank][K] and [count][M][rank]: row strides lda >= K and ldb >= rank, adapters
+ *                stride_a and stride_b apart (in elements).  1 <= rank <= SPDP_MAX_RANK.
+ *   ranks_dev    int32 [count] or NULL: adapter a has only its first ranks[a] rows of A and columns of B; the others
+ *                are not read.  Values outside 0 .. rank are taken as the nearest of these.
+ *   scales_dev   float [count] or NULL (1).
+ *   base_dev     [N][ldbase] of ydt, ldbase >= M; may be Y_dev itself (with ldbase = ldy): the adapters are then added in place.
+ *   Y_dev        [N][ldy] of ydt, ldy >= M.
+ * Sums in 32 bits; the vector between the two products is rounded to 11 bits for 16-bit results and to 22 for
+ * 32-bit ones (both with the range of 32-bit numbers).  Rows that start on 16-byte boundaries (addresses and strides) are the
+ * fast case.  Launches one kernel. */
+#define SPDP_MAX_RANK 256
+SPDP_API spdp_status spdp_lora(const void* X_dev, int64_t N, int64_t K, int64_t ldx, const void* adapter_dev, const void* A_dev, int64_t lda,
+                      int64_t stride_a, const void* B_dev, int64_t ldb, int64_t stride_b, int64_t count, int rank, const void* ranks_dev,
+                      const void* scales_dev, const void* base_dev, int64_t ldbase, void* Y_dev, int64_t M, int64_t ldy, spdp_ydtype ydt,
+                      void* stream);
+
+/* Norms of the query and key heads and their rotation by positions, in one pass over the output of the q/k projections.
+ * Each head x of head_dim values becomes x / sqrt(mean(x^2) + eps) * weight, then its first 2 * pairs values turn: pair i by the
+ * angle pos[axis of i][n] * inv_freq[i], (a, b) -> (a cos - b sin, b cos + a sin).  Arithmetic in 32 bits, angles in 64, one
+ * rounding to fp16.
+ *   q_dev, k_dev      [N][ldq], [N][ldk] of dt (fp16 or fp32, a projection's output types), N <= 2^24: a token's q_heads
+ *                     (kv_heads) heads one after another.  Either number may be 0 (its pointers are then ignored), not both.
+ *   head_dim          even, 2 .. 256.
+ *   q_weight_dev, k_weight_dev  fp16 [head_dim], or NULL: those heads are not normed.
+ *   pos_dev           int32 [axes][pos_stride], pos_stride >= N: a token's position on each axis (1 axis for text; time, height
+ *                     and width for video).  1 <= axes <= 4.
+ *   sections          HOST int [axes]: the first sections[0] pairs turn by axis 0, the next sections[1] by axis 1, ...; their
+ *                     sum is `pairs`.
+ *   inv_freq_dev      float [pairs], radians per position (whatever scaling of the frequencies is in use is in them).
+ *   pairs             0 .. head_dim / 2; 0: no rotation (pos, axes, sections and inv_freq are ignored).
+ *   adjacent          0: pair i is (x[i], x[i + pairs]); 1: (x[2 i], x[2 i + 1]).
+ *   q_out_dev, k_out_dev  fp16, as q_dev and k_dev; they may be those themselves (same pointer and stride) where dt is fp16.
+ * Launches one kernel. */
+SPDP_API spdp_status spdp_qk_norm_rope(const void* q_dev, int64_t ldq, const void* k_dev, int64_t ldk, spdp_ydtype dt, int64_t N, int q_heads, int kv_heads,
+                              int head_dim, const void* q_weight_dev, const void* k_weight_dev, float eps, const void* pos_dev, int64_t pos_stride,
+                              int axes, const int* sections, const void* inv_freq_dev, int pairs, int adjacent, void* q_out_dev,
+                              int64_t ldq_out, void* k_out_dev, int64_t ldk_out, void* stream);
+
+/* A paged key/value cache held in 4 bits.  A row (one token's key or value of one head, head_dim = 64, 128 or 256 values) is
+ * head_dim codes and one fp16 scale to 32 dimensions, by the rule of the 4-bit Values (spdp_pack_tiled_cbc_q4):
+ *   scale = fp16(max|x| / 7);  code = clamp(rint(x / scale), -7, 7) + 8 (8 where the scale is 0);  it stands for (code - 8) * scale.
+ * Rows must be finite (what Inf or NaN leave is unspecified, within that row).
+ * A page holds page_tokens = P tokens (a power of two, 16 .. 256); for each key head in turn: codes of the keys
+ * [P][head_dim / 2] bytes, codes of the values [P][head_dim / 2], scales of the keys fp16 [P][head_dim / 32], scales of the values
+ * [P][head_dim / 32].  In a row of codes, with G = head_dim / 32, dimension 32 g + 8 c + j (c < 4, j < 8) is bits 4 j .. 4 j + 3 of
+ * 32-bit word c G + g.
+ * A cache is `pages` such pages, 16-byte aligned, in any order; slot s is token s % P of page s / P.
+ * spdp_kv4_page_bytes writes the bytes of a page (host arithmetic). */
+SPDP_API spdp_status spdp_kv4_page_bytes(int kv_heads, int head_dim, int page_tokens, int64_t* bytes_out);
+
+/* Stores N tokens' keys and values into the cache.
+ *   k_dev        fp16 [N][ldk], heads one after another (what spdp_qk_norm_rope leaves), N <= 2^24.
+ *   v_dev        [N][ldv] of vdt; 32-bit values are first rounded to fp16.
+ *   slot_dev     int64 [N]; a slot below 0 or beyond the last page stores nothing.  A slot that occurs twice ends up with either
+ *                token's row, or parts of both.
+ *   k_values_dev_out, v_values_dev_out  fp16 [N][ld...], or NULL: the values that the codes stand for (rounded to fp16), also
+ *                where nothing is stored: a prompt's own attention can then work on the keys and values that later tokens see.
+ * Launches one kernel. */
+SPDP_API spdp_status spdp_kv4_store(const void* k_dev, int64_t ldk, const void* v_dev, int64_t ldv, spdp_ydtype vdt, int64_t N, int kv_heads, int head_dim,
+                           const void* slot_dev, void* cache_dev, int64_t pages, int page_tokens, void* k_values_dev_out, int64_t ldk_values,
+                           void* v_values_dev_out, int64_t ldv_values, void* stream);
+
+/* Attention of one new token for each of B requests over the 4-bit cache, fused with the pruning decision of the projection
+ * behind it (as spdp_swiglu_dp is for a gated MLP): y = softmax(cap * tanh(scale * q k / cap)) v, query head i with key head
+ * i / (q_heads / kv_heads).
+ *   q_dev        fp16 [B][ldq], B <= 4096; q_heads a multiple of kv_heads.
+ *   table_dev    int32 [B][table_stride], table_stride >= table_pages: the pages of each request in order.  The keys of a page
+ *                outside 0 .. pages-1 are left out.
+ *   length_dev   int32 [B]: keys of each request, the new token's own among them (store it first); values below 0 and above
+ *                table_pages * page_tokens count as these.  A request without keys gets zeros.
+ *   cap          > 0: scores are capped; 0: they are not.
+ *   window       > 0: only the last `window` keys count; 0: all do.
+ *   y_dev        fp16 [B][ldy], ldy >= q_heads * head_dim.
+ *   mask_dev_out uint32 [B][mask_stride], mask_stride >= q_heads * head_dim / 32, or NULL: the columns that the o-projection
+ *                should keep, NOT(|y_j| <= thr) on the stored y, for SPDP_DP_MASK (thr is used for nothing else).
+ * What lies in the cache behind a request's last key is never used, whatever it is.  Sums in 32 bits; decoded values and the
+ * softmax's weights are rounded to fp16 for their product.  Launches two kernels; scratch memory (a few MB) comes from the pool
+ * that spdp_spmm describes. */
+SPDP_API spdp_status spdp_attn_kv4(const void* q_dev, int64_t ldq, int64_t B, int q_heads, int kv_heads, int head_dim, const void* cache_dev, int64_t pages,
+                          int page_tokens, const void* table_dev, int64_t table_stride, int64_t table_pages, const void* length_dev, float scale,
+                          float cap, int64_t window, float thr, void* y_dev, int64_t ldy, void* mask_dev_out, int64_t mask_stride, void* stream);
+
 /* Row-tile sharding over several GPUs (the paper names multi-GPU execution as future work, Sec. 6; the
  * natural split of y = W x keeps whole 256-row tiles together, so every rank packs its own rows as
  * an independent Tiled-CBC matrix, x is replicated, and the outputs are disjoint).  This is the split

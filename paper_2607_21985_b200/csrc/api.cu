@@ -157,6 +157,19 @@ spdp_status finish_handle(spdp_matrix* h, cudaStream_t s) {
     return SPDP_OK;
 }
 
+bool misaligned(const void* p, unsigned mask) { return (reinterpret_cast<uintptr_t>(p) & mask) != 0; }
+
+constexpr int64_t kMostSide = int64_t(1) << 30, kMostTokens = int64_t(1) << 24;
+// Elements between rows of at least `row` (below 2^38, so that offsets of all tokens or weights fit 63 bits).
+bool stride_ok(int64_t ld, int64_t row) { return ld >= row && ld <= (int64_t(1) << 38); }
+
+constexpr int kMostCacheHeads = 4096;
+// A cache of 4-bit keys and values that the kernels take.
+bool kv4_shape_ok(int kv_heads, int head_dim, int page_tokens) {
+    return kv_heads >= 1 && kv_heads <= kMostCacheHeads && (head_dim == 64 || head_dim == 128 || head_dim == 256) && page_tokens >= 16 && page_tokens <= 256 &&
+           (page_tokens & (page_tokens - 1)) == 0;
+}
+
 constexpr int kBatchViaSingleCalls = 2;   // spdp_spmspv_batch: up to this many tokens go through the single-vector kernel
 
 // The decode kernel of the handle's Values variant (fp16 values, or 4-bit codes with scales).
@@ -520,6 +533,121 @@ spdp_status spdp_swiglu_dp(const void* gate_dev, const void* up_dev, int64_t K, 
     return launch_swiglu_dp(static_cast<const __half*>(gate_dev), static_cast<const __half*>(up_dev), K, thr,
                             static_cast<__half*>(x_dev_out), static_cast<uint32_t*>(mask_dev_out),
                             static_cast<int*>(count_dev_out), static_cast<cudaStream_t>(stream));
+}
+
+spdp_status spdp_lora(const void* X_dev, int64_t N, int64_t K, int64_t ldx, const void* adapter_dev, const void* A_dev, int64_t lda,
+                      int64_t stride_a, const void* B_dev, int64_t ldb, int64_t stride_b, int64_t count, int rank, const void* ranks_dev,
+                      const void* scales_dev, const void* base_dev, int64_t ldbase, void* Y_dev, int64_t M, int64_t ldy, spdp_ydtype ydt,
+                      void* stream) {
+    if (X_dev == nullptr || adapter_dev == nullptr || A_dev == nullptr || B_dev == nullptr || base_dev == nullptr || Y_dev == nullptr) return SPDP_ERR_INVALID_ARG;
+    if (K < 1 || M < 1 || K > kMostSide || M > kMostSide || rank < 1 || rank > SPDP_MAX_RANK) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    if (N < 1 || N > kMostTokens || count < 1 || count > INT32_MAX) return SPDP_ERR_INVALID_ARG;
+    if (!stride_ok(ldx, K) || !stride_ok(lda, K) || !stride_ok(ldb, rank) || !stride_ok(ldbase, M) || !stride_ok(ldy, M)) return SPDP_ERR_INVALID_ARG;
+    if (count > 1 && (!stride_ok(stride_a, (rank - 1) * lda + K) || !stride_ok(stride_b, (M - 1) * ldb + rank))) return SPDP_ERR_INVALID_ARG;
+    if ((ydt != SPDP_Y_F16 && ydt != SPDP_Y_F32) || (base_dev == Y_dev && N > 1 && ldbase != ldy)) return SPDP_ERR_INVALID_ARG;
+    const unsigned y = ydt == SPDP_Y_F32 ? 3u : 1u;
+    if (misaligned(X_dev, 1u) || misaligned(A_dev, 1u) || misaligned(B_dev, 1u) || misaligned(base_dev, y) || misaligned(Y_dev, y) || misaligned(adapter_dev, 3u) ||
+        misaligned(ranks_dev, 3u) || misaligned(scales_dev, 3u))
+        return SPDP_ERR_INVALID_ARG;
+    LoraCall c = {};
+    c.X = static_cast<const __half*>(X_dev), c.adapter = static_cast<const int32_t*>(adapter_dev), c.A = static_cast<const __half*>(A_dev);
+    c.B = static_cast<const __half*>(B_dev), c.ranks = static_cast<const int32_t*>(ranks_dev), c.scales = static_cast<const float*>(scales_dev);
+    c.base = base_dev, c.Y = Y_dev, c.N = N, c.K = K, c.M = M, c.count = count, c.ldx = ldx, c.lda = lda, c.stride_a = count > 1 ? stride_a : 0, c.ldb = ldb;
+    c.stride_b = count > 1 ? stride_b : 0, c.ldbase = ldbase, c.ldy = ldy, c.rank = rank, c.ydt = ydt;
+    return launch_lora(c, static_cast<cudaStream_t>(stream));
+}
+
+spdp_status spdp_qk_norm_rope(const void* q_dev, int64_t ldq, const void* k_dev, int64_t ldk, spdp_ydtype dt, int64_t N, int q_heads, int kv_heads,
+                              int head_dim, const void* q_weight_dev, const void* k_weight_dev, float eps, const void* pos_dev, int64_t pos_stride,
+                              int axes, const int* sections, const void* inv_freq_dev, int pairs, int adjacent, void* q_out_dev,
+                              int64_t ldq_out, void* k_out_dev, int64_t ldk_out, void* stream) {
+    constexpr int kMostHeads = 1 << 16, kMostAxes = 4;
+    if (head_dim < 2 || head_dim > 256 || head_dim % 2 != 0 || q_heads > kMostHeads || kv_heads > kMostHeads) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    if (N < 1 || N > kMostTokens || q_heads < 0 || kv_heads < 0 || q_heads + kv_heads < 1) return SPDP_ERR_INVALID_ARG;
+    if (dt != SPDP_Y_F16 && dt != SPDP_Y_F32) return SPDP_ERR_INVALID_ARG;
+    if (pairs < 0 || pairs > head_dim / 2 || (adjacent != 0 && adjacent != 1) || !(eps >= 0.0f)) return SPDP_ERR_INVALID_ARG;
+    const unsigned in = dt == SPDP_Y_F32 ? 3u : 1u;
+    const int64_t q_row = static_cast<int64_t>(q_heads) * head_dim, k_row = static_cast<int64_t>(kv_heads) * head_dim;
+    if (q_heads > 0 && (q_dev == nullptr || q_out_dev == nullptr || !stride_ok(ldq, q_row) || !stride_ok(ldq_out, q_row) || misaligned(q_dev, in) ||
+                        misaligned(q_out_dev, 1u) || misaligned(q_weight_dev, 1u) || (q_out_dev == q_dev && (dt != SPDP_Y_F16 || (N > 1 && ldq != ldq_out)))))
+        return SPDP_ERR_INVALID_ARG;
+    if (kv_heads > 0 && (k_dev == nullptr || k_out_dev == nullptr || !stride_ok(ldk, k_row) || !stride_ok(ldk_out, k_row) || misaligned(k_dev, in) ||
+                         misaligned(k_out_dev, 1u) || misaligned(k_weight_dev, 1u) || (k_out_dev == k_dev && (dt != SPDP_Y_F16 || (N > 1 && ldk != ldk_out)))))
+        return SPDP_ERR_INVALID_ARG;
+    if (pairs > 0) {
+        if (pos_dev == nullptr || inv_freq_dev == nullptr || sections == nullptr || axes < 1 || axes > kMostAxes || !stride_ok(pos_stride, N) || misaligned(pos_dev, 3u) ||
+            misaligned(inv_freq_dev, 3u))
+            return SPDP_ERR_INVALID_ARG;
+        int64_t sum = 0;
+        for (int a = 0; a < axes; ++a) {
+            if (sections[a] < 0) return SPDP_ERR_INVALID_ARG;
+            sum += sections[a];
+        }
+        if (sum != pairs) return SPDP_ERR_INVALID_ARG;
+    }
+    HeadsCall c = {};
+    if (q_heads > 0) c.q = q_dev, c.q_out = static_cast<__half*>(q_out_dev), c.q_weight = static_cast<const __half*>(q_weight_dev), c.ldq = ldq, c.ldq_out = ldq_out;
+    if (kv_heads > 0) c.k = k_dev, c.k_out = static_cast<__half*>(k_out_dev), c.k_weight = static_cast<const __half*>(k_weight_dev), c.ldk = ldk, c.ldk_out = ldk_out;
+    if (pairs > 0) {
+        c.pos = static_cast<const int32_t*>(pos_dev), c.inv_freq = static_cast<const float*>(inv_freq_dev);
+        c.sections = sections, c.pos_stride = pos_stride, c.axes = axes;
+    }
+    c.N = N, c.q_heads = q_heads, c.kv_heads = kv_heads, c.head_dim = head_dim, c.pairs = pairs, c.dt = dt, c.eps = eps, c.adjacent = adjacent != 0;
+    return launch_qk_norm_rope(c, static_cast<cudaStream_t>(stream));
+}
+
+spdp_status spdp_kv4_page_bytes(int kv_heads, int head_dim, int page_tokens, int64_t* bytes_out) {
+    if (bytes_out == nullptr) return SPDP_ERR_INVALID_ARG;
+    if (!kv4_shape_ok(kv_heads, head_dim, page_tokens)) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    *bytes_out = static_cast<int64_t>(kv_heads) * page_tokens * (head_dim + head_dim / 8);
+    return SPDP_OK;
+}
+
+spdp_status spdp_kv4_store(const void* k_dev, int64_t ldk, const void* v_dev, int64_t ldv, spdp_ydtype vdt, int64_t N, int kv_heads, int head_dim,
+                           const void* slot_dev, void* cache_dev, int64_t pages, int page_tokens, void* k_values_dev_out, int64_t ldk_values,
+                           void* v_values_dev_out, int64_t ldv_values, void* stream) {
+    if (k_dev == nullptr || v_dev == nullptr || slot_dev == nullptr || cache_dev == nullptr) return SPDP_ERR_INVALID_ARG;
+    if (!kv4_shape_ok(kv_heads, head_dim, page_tokens)) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    const int64_t row = static_cast<int64_t>(kv_heads) * head_dim;
+    if (N < 1 || N > kMostTokens || pages < 1 || pages > INT32_MAX || !stride_ok(ldk, row) || !stride_ok(ldv, row) || (vdt != SPDP_Y_F16 && vdt != SPDP_Y_F32))
+        return SPDP_ERR_INVALID_ARG;
+    if ((k_values_dev_out != nullptr && !stride_ok(ldk_values, row)) || (v_values_dev_out != nullptr && !stride_ok(ldv_values, row))) return SPDP_ERR_INVALID_ARG;
+    if (misaligned(k_dev, 1u) || misaligned(v_dev, vdt == SPDP_Y_F32 ? 3u : 1u) || misaligned(slot_dev, 7u) || misaligned(cache_dev, 15u) ||
+        misaligned(k_values_dev_out, 1u) || misaligned(v_values_dev_out, 1u))
+        return SPDP_ERR_INVALID_ARG;
+    Kv4StoreCall c = {};
+    c.k = static_cast<const __half*>(k_dev), c.v = v_dev, c.slot = static_cast<const int64_t*>(slot_dev), c.cache = static_cast<unsigned char*>(cache_dev);
+    c.k_values = static_cast<__half*>(k_values_dev_out), c.v_values = static_cast<__half*>(v_values_dev_out);
+    c.N = N, c.ldk = ldk, c.ldv = ldv, c.pages = pages;
+    c.ldk_values = k_values_dev_out != nullptr ? ldk_values : 0, c.ldv_values = v_values_dev_out != nullptr ? ldv_values : 0;
+    c.kv_heads = kv_heads, c.head_dim = head_dim, c.page_tokens = page_tokens, c.vdt = vdt;
+    return launch_kv4_store(c, static_cast<cudaStream_t>(stream));
+}
+
+spdp_status spdp_attn_kv4(const void* q_dev, int64_t ldq, int64_t B, int q_heads, int kv_heads, int head_dim, const void* cache_dev, int64_t pages,
+                          int page_tokens, const void* table_dev, int64_t table_stride, int64_t table_pages, const void* length_dev, float scale,
+                          float cap, int64_t window, float thr, void* y_dev, int64_t ldy, void* mask_dev_out, int64_t mask_stride, void* stream) {
+    if (q_dev == nullptr || cache_dev == nullptr || table_dev == nullptr || length_dev == nullptr || y_dev == nullptr) return SPDP_ERR_INVALID_ARG;
+    if (!kv4_shape_ok(kv_heads, head_dim, page_tokens) || q_heads < 1 || q_heads > 16 * kMostCacheHeads || q_heads % kv_heads != 0) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    if (B < 1 || B > 4096) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    const int64_t row = static_cast<int64_t>(q_heads) * head_dim;
+    if (pages < 1 || pages > INT32_MAX || table_pages < 1 || !stride_ok(table_stride, table_pages) || !stride_ok(ldq, row) || !stride_ok(ldy, row) || window < 0)
+        return SPDP_ERR_INVALID_ARG;
+    if (mask_dev_out != nullptr && !stride_ok(mask_stride, row / 32)) return SPDP_ERR_INVALID_ARG;
+    if (!(scale >= -1.0e38f && scale <= 1.0e38f) || !(cap >= 0.0f && cap <= 1.0e38f)) return SPDP_ERR_INVALID_ARG;
+    if (misaligned(q_dev, 1u) || misaligned(cache_dev, 15u) || misaligned(table_dev, 3u) || misaligned(length_dev, 3u) || misaligned(y_dev, 1u) ||
+        misaligned(mask_dev_out, 3u))
+        return SPDP_ERR_INVALID_ARG;
+    // the keys of a request, and the 64-key units of all requests and heads, are counted in 32 bits
+    if (table_pages > INT32_MAX / page_tokens - 64) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    const int64_t triples = kv_heads * static_cast<int64_t>((q_heads / kv_heads + 7) / 8);
+    if (triples * (table_pages * page_tokens / 64 + 2) > INT32_MAX / B) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    Kv4AttnCall c = {};
+    c.q = static_cast<const __half*>(q_dev), c.cache = static_cast<const unsigned char*>(cache_dev), c.table = static_cast<const int32_t*>(table_dev);
+    c.length = static_cast<const int32_t*>(length_dev), c.y = static_cast<__half*>(y_dev), c.mask = static_cast<uint32_t*>(mask_dev_out);
+    c.B = B, c.ldq = ldq, c.ldy = ldy, c.table_stride = table_stride, c.table_pages = table_pages, c.mask_stride = mask_stride, c.pages = pages, c.window = window;
+    c.q_heads = q_heads, c.kv_heads = kv_heads, c.head_dim = head_dim, c.page_tokens = page_tokens, c.scale = scale, c.cap = cap, c.thr = thr;
+    return launch_attn_kv4(c, static_cast<cudaStream_t>(stream));
 }
 
 spdp_status spdp_row_shard(int64_t M, int world, int rank, int64_t* first_row_out, int64_t* rows_out) {

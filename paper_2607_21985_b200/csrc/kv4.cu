@@ -1,0 +1,576 @@
+// A paged key/value cache of 4-bit codes: storing rows (what a q/k/v projection and the rotation left), and the attention of
+// one new token per request over it, whose output is the input of a dynamically pruned o-projection and comes with its keep
+// mask, as spdp_swiglu_dp's does.
+//
+// Layout of the cache (spdp.h): per page and key head the codes of the keys [P][D/2], of the values [P][D/2], the scales of the keys
+// [P][D/32] and of the values [P][D/32].  In a row of codes the dimension 32 g + 8 c + j is nibble j of word c D/32 + g: so the
+// four lanes that share a key in a matrix product's fragment each read one run of 16 bytes (D = 128), and what a lane holds
+// for one step of the product all belongs to one scale.
+#include <mutex>
+
+#include "mma_f16.cuh"
+#include "spdp_internal.h"
+
+namespace spdp {
+namespace {
+
+// ---- storing ----------------------------------------------------------------------------------------------------------------
+
+constexpr int kStoreThreads = 256;
+
+struct StoreParams {
+    const __half* k;
+    const void* v;
+    const int64_t* slot;
+    unsigned char* cache;
+    __half* k_values;
+    __half* v_values;
+    int64_t ldk, ldv, ldk_values, ldv_values, N, pages;
+    int heads, dim, page_shift;
+};
+
+// A lane takes 8 dimensions, four neighbours a scale.  kWide: 16-byte accesses.
+template <typename T, bool kWide>
+__device__ __forceinline__ void store_row(const StoreParams& p, const T* from, int64_t ld, __half* values, int64_t ld_values, bool is_v, int64_t i) {
+    const int per_row = p.dim / 8;                               // lanes of a row: 8, 16 or 32
+    const int64_t row = i / per_row, n = row / p.heads;
+    const bool there = n < p.N;
+    const int h = static_cast<int>(row % p.heads), piece = static_cast<int>(i % per_row), c = piece & 3, g = piece >> 2;
+    float x[8] = {};
+    if (there) dev::load_floats<T, kWide>(from + n * ld + h * p.dim + 8 * piece, x);
+    float top = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (sizeof(T) == 4) x[j] = __half2float(__float2half_rn(x[j]));        // 32-bit rows count as the fp16 row they round to
+        top = fmaxf(top, fabsf(x[j]));
+    }
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+    if (!there) return;
+    const __half scale = __float2half_rn(__fdiv_rn(top, 7.0f));
+    const float s = __half2float(scale);
+    uint32_t word = 0;
+    float step[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        step[j] = s > 0.0f ? fminf(fmaxf(rintf(__fdiv_rn(x[j], s)), -7.0f), 7.0f) : 0.0f;
+        word |= static_cast<uint32_t>(static_cast<int>(step[j]) + 8) << (4 * j);
+    }
+    const int64_t slot = p.slot[n], page = slot >> p.page_shift;
+    if (slot >= 0 && page < p.pages) {
+        const int P = 1 << p.page_shift, groups = p.dim / 32, at = static_cast<int>(slot & (P - 1));
+        const int64_t codes = static_cast<int64_t>(P) * (p.dim / 2), scales = static_cast<int64_t>(P) * groups * 2;
+        unsigned char* head = p.cache + (page * p.heads + h) * 2 * (codes + scales);
+        reinterpret_cast<uint32_t*>(head + (is_v ? codes : 0) + static_cast<int64_t>(at) * (p.dim / 2))[c * groups + g] = word;
+        if (c == 0) reinterpret_cast<__half*>(head + 2 * codes + (is_v ? scales : 0))[at * groups + g] = scale;
+    }
+    if (values != nullptr) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) step[j] *= s;
+        dev::store_halves<kWide>(values + n * ld_values + h * p.dim + 8 * piece, step);
+    }
+}
+
+template <typename V, bool kWide>
+__global__ void __launch_bounds__(kStoreThreads) kv4_store_kernel(const StoreParams p) {
+    dev::programmatic_start();
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kStoreThreads + threadIdx.x;
+    if (blockIdx.y == 0) store_row<__half, kWide>(p, p.k, p.ldk, p.k_values, p.ldk_values, false, i);
+    else store_row<V, kWide>(p, static_cast<const V*>(p.v), p.ldv, p.v_values, p.ldv_values, true, i);
+}
+
+// ---- attention --------------------------------------------------------------------------------------------------------------
+//
+// The keys of all (request, key head, block of query heads) triples, 64 to a unit, stand in one line that is cut into equal runs,
+// one to a CTA: so one long request and many short ones alike occupy the whole GPU, whatever the lengths are, which only
+// the device knows.  A run that holds a triple's every key writes its output; else CTAs leave a partial sum of it, with its
+// maximum and its weight, and a second kernel joins them in the order of the keys.
+//
+// Inside a CTA each warp takes 16 keys at a time.  Scores are K q^T and outputs V^T P^T on mma.sync, with the query heads of
+// the key head as the 8 columns (so that up to 8 heads cost no more than one, and 16 share what was decoded): the codes go from
+// registers through two logical operations per pair into fp16 fragments; the keys' scales multiply the 32-bit sums of their 32
+// dimensions, the values' scales the decoded values (one rounding of 2^-12), and the weights, at most 2^8, are rounded to fp16
+// once (2^-12), as outputs are.  Maxima are only renewed, and sums rescaled, when a score exceeds the old one by 2^8: so that
+// the exchanges between lanes that a maximum takes are rare.
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kUnit = 64;               // keys
+constexpr int kMostRequests = 4096;
+constexpr float kLowest = -1.0e30f;     // stands for "no score yet"
+constexpr float kSlack = 8.0f;
+
+struct AttnParams {
+    const __half* q;
+    const unsigned char* cache;
+    const int32_t* table;
+    const int32_t* length;
+    __half* y;
+    uint32_t* mask;
+    float* sums;                        // [2 CTAs][rows][dim]
+    float2* stats;                      // [2 CTAs][rows]: maximum, weight
+    int* first_unit;                    // [B + 1]
+    int64_t ldq, ldy, table_stride, table_pages, mask_stride, pages;
+    int B, heads, group, row_blocks, page_shift;
+    float scale, cap, cap_inv;          // scores in powers of two
+    int64_t window;
+    float thr;
+};
+
+struct Span {
+    int low, end, units;                // keys of the request: low .. end - 1 (low a multiple of 16), in units
+};
+__device__ __forceinline__ Span span_of(const AttnParams& p, int b) {
+    const int64_t most = p.table_pages << p.page_shift;
+    const int64_t n = p.length[b] < 0 ? 0 : p.length[b] < most ? p.length[b] : most;
+    Span s;
+    s.end = static_cast<int>(n);
+    s.low = p.window > 0 && n > p.window ? static_cast<int>(n - p.window) & ~15 : 0;
+    s.units = (s.end - s.low + kUnit - 1) / kUnit;
+    return s;
+}
+
+// The first unit of every request, into shared memory (all threads; ends with a barrier).
+__device__ void scan_units(const AttnParams& p, int* first, int* warp_sums) {
+    const int each = (p.B + kThreads - 1) / kThreads, b0 = threadIdx.x * each, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    int mine = 0;
+    for (int b = b0; b < b0 + each && b < p.B; ++b) mine += span_of(p, b).units * p.heads * p.row_blocks;
+    int up_to = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int v = __shfl_up_sync(0xFFFFFFFFu, up_to, d);
+        if (lane >= d) up_to += v;
+    }
+    if (lane == 31) warp_sums[w] = up_to;
+    __syncthreads();
+    int at = up_to - mine;
+    for (int i = 0; i < w; ++i) at += warp_sums[i];
+    for (int b = b0; b < b0 + each && b < p.B; ++b) {
+        first[b] = at;
+        at += span_of(p, b).units * p.heads * p.row_blocks;
+    }
+    if (b0 < p.B && b0 + each >= p.B) first[p.B] = at;
+    __syncthreads();
+}
+
+__device__ __forceinline__ uint32_t low_pair(uint32_t w) {       // nibbles 0 and 4 of w, as fp16 numbers minus 8
+    const uint32_t v = (w & 0x000F000Fu) | 0x64006400u;          // 1024 + n
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&v), __half2half2(__ushort_as_half(0x6408)));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t high_pair(uint32_t w) {      // nibbles 1 and 5
+    const uint32_t v = (w & 0x00F000F0u) | 0x54005400u;          // 64 + n
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&v), __half2half2(__ushort_as_half(0x5480)));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+// pair i: nibbles i and i + 4
+__device__ __forceinline__ void pairs_of(uint32_t w, uint32_t (&out)[4]) {
+    out[0] = low_pair(w), out[1] = high_pair(w), out[2] = low_pair(w >> 8), out[3] = high_pair(w >> 8);
+}
+__device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
+    const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ float exp2_of(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// kWords 32-bit words (1, 2, 4 or 8) from an address that is a multiple of their size (16 at most).
+template <int kWords>
+__device__ __forceinline__ void load_words(const unsigned char* at, uint32_t (&w)[kWords]) {
+    if constexpr (kWords == 1) w[0] = *reinterpret_cast<const uint32_t*>(at);
+    else if constexpr (kWords == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(at);
+        w[0] = v.x, w[1] = v.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kWords / 4; ++i) {
+            const uint4 v = reinterpret_cast<const uint4*>(at)[i];
+            w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+        }
+    }
+}
+
+// What a lane (g, c) holds of 16 keys: words of the keys g and g + 8 and their scales; words and scales of the values of keys
+// 2 c, 2 c + 1, 2 c + 8, 2 c + 9, an eighth of a row each.
+template <int kGroups>
+struct Keys {
+    uint32_t k[2][kGroups], v[4][kGroups / 2];
+    uint32_t ks[2][kGroups / 2];
+    uint32_t vs[4][(kGroups + 3) / 4];      // kGroups / 2 scales
+};
+
+template <int kGroups>
+__device__ __forceinline__ void load_keys(Keys<kGroups>& x, const unsigned char* head, int at, int P, int g, int c) {
+    constexpr int kRow = 16 * kGroups;      // bytes of a row of codes
+    const unsigned char* values = head + P * kRow;
+    const unsigned char* k_scales = head + 2 * P * kRow;
+    const unsigned char* v_scales = k_scales + P * 2 * kGroups;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int key = at + g + 8 * i;
+        load_words<kGroups>(head + key * kRow + c * 4 * kGroups, x.k[i]);
+        load_words<kGroups / 2>(k_scales + key * 2 * kGroups, x.ks[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int key = at + 2 * c + (i & 1) + 8 * (i >> 1);
+        load_words<kGroups / 2>(values + key * kRow + g * 2 * kGroups, x.v[i]);
+        const unsigned char* s = v_scales + key * 2 * kGroups + (g & 1) * kGroups;
+        if constexpr (kGroups == 2) x.vs[i][0] = *reinterpret_cast<const uint16_t*>(s);
+        else load_words<kGroups / 4>(s, x.vs[i]);
+    }
+}
+
+// kGroups = D / 32; kCols: blocks of 8 query heads.
+template <int kGroups, int kCols>
+__global__ void __launch_bounds__(kThreads) attn_kernel(const AttnParams p) {
+    constexpr int kDim = 32 * kGroups, kRows = 8 * kCols;
+    extern __shared__ float shared[];
+    float* joined = shared;                                     // [warp][kRows][kDim]
+    float2* warp_stats = reinterpret_cast<float2*>(joined + kWarps * kRows * kDim);      // [warp][kRows]
+    int* warp_sums = reinterpret_cast<int*>(warp_stats + kWarps * kRows);
+    int* first = warp_sums + kWarps;
+    dev::programmatic_start();
+    scan_units(p, first, warp_sums);
+    if (blockIdx.x == 0)
+        for (int b = threadIdx.x; b <= p.B; b += kThreads) p.first_unit[b] = first[b];
+    const int64_t total = first[p.B];
+    const int begin = static_cast<int>(total * blockIdx.x / gridDim.x), stop = static_cast<int>(total * (blockIdx.x + 1) / gridDim.x);
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+    const int P = 1 << p.page_shift;
+    const int64_t head_bytes = static_cast<int64_t>(P) * 36 * kGroups;
+
+    for (int u = begin; u < stop;) {
+        int b = 0;                                              // the last request whose first unit is not behind u: it has units
+        for (int lo = 0, hi = p.B - 1; lo <= hi;) {
+            const int mid = (lo + hi) >> 1;
+            if (first[mid] <= u) b = mid, lo = mid + 1;
+            else hi = mid - 1;
+        }
+        const Span span = span_of(p, b);
+        const int triple = (u - first[b]) / span.units, off = (u - first[b]) % span.units;
+        const int count = min(span.units - off, stop - u);
+        const int h = triple / p.row_blocks, row0 = triple % p.row_blocks * kRows, rows = min(kRows, p.group - row0);
+        const int k0 = span.low + off * kUnit, k1 = min(span.end, k0 + count * kUnit);
+        const int window_low = p.window > 0 && span.end > p.window ? static_cast<int>(span.end - p.window) : 0;
+        const int32_t* table = p.table + b * p.table_stride;
+
+        // the query heads as the products' columns, in the order that the codes' pairs have
+        uint32_t q[kCols][2 * kGroups][2];
+#pragma unroll
+        for (int n = 0; n < kCols; ++n) {
+            const int row = 8 * n + g;
+            const __half* at = p.q + b * p.ldq + static_cast<int64_t>(h * p.group + row0 + row) * kDim + 8 * c;
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+                uint32_t x[4] = {0, 0, 0, 0};
+                if (row < rows) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] = __half_as_ushort(at[32 * i + 2 * j]) | static_cast<uint32_t>(__half_as_ushort(at[32 * i + 2 * j + 1])) << 16;
+                }
+                q[n][2 * i][0] = __byte_perm(x[0], x[2], 0x5410), q[n][2 * i][1] = __byte_perm(x[0], x[2], 0x7632);
+                q[n][2 * i + 1][0] = __byte_perm(x[1], x[3], 0x5410), q[n][2 * i + 1][1] = __byte_perm(x[1], x[3], 0x7632);
+            }
+        }
+        float acc[kCols][2 * kGroups][4] = {};
+        float top[kCols][2], weight[kCols][2];
+#pragma unroll
+        for (int n = 0; n < kCols; ++n) top[n][0] = top[n][1] = kLowest, weight[n][0] = weight[n][1] = 0.0f;
+
+        auto head_of = [&](int key) -> const unsigned char* {   // null: no such keys, or a page that does not exist
+            if (key >= k1) return nullptr;
+            const int64_t page = table[key >> p.page_shift];
+            return page < 0 || page >= p.pages ? nullptr : p.cache + (page * p.heads + h) * head_bytes;
+        };
+        Keys<kGroups> next = {};
+        const unsigned char* ahead = head_of(k0 + 16 * w);
+        if (ahead != nullptr) load_keys<kGroups>(next, ahead, (k0 + 16 * w) & (P - 1), P, g, c);
+        for (int key = k0 + 16 * w; key < k1; key += 16 * kWarps) {
+            Keys<kGroups> x = next;
+            const bool any = ahead != nullptr;
+            const int after = key + 16 * kWarps;
+            ahead = head_of(after);
+            if (ahead != nullptr) load_keys<kGroups>(next, ahead, after & (P - 1), P, g, c);
+            if (!any) continue;
+            // keys that do not count: no score, and a scale of 0 for whatever the page holds there
+            const bool whole = key >= window_low && key + 16 <= k1;
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = key + 2 * c + (i & 1) + 8 * (i >> 1);
+                    if (at < window_low || at >= k1) {
+#pragma unroll
+                        for (int j = 0; j < (kGroups + 3) / 4; ++j) x.vs[i][j] = 0;
+                    }
+                }
+            }
+            float score[kCols][4] = {};
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+                uint32_t lo[4], hi[4];
+                pairs_of(x.k[0][i], lo);
+                pairs_of(x.k[1][i], hi);
+                const float s0 = __half2float(__ushort_as_half(static_cast<unsigned short>(x.ks[0][i / 2] >> (16 * (i & 1)))));
+                const float s1 = __half2float(__ushort_as_half(static_cast<unsigned short>(x.ks[1][i / 2] >> (16 * (i & 1)))));
+#pragma unroll
+                for (int n = 0; n < kCols; ++n) {
+                    float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    dev::mma_f16(d, lo[0], hi[0], lo[1], hi[1], q[n][2 * i][0], q[n][2 * i][1]);
+                    dev::mma_f16(d, lo[2], hi[2], lo[3], hi[3], q[n][2 * i + 1][0], q[n][2 * i + 1][1]);
+                    score[n][0] += d[0] * s0, score[n][1] += d[1] * s0;
+                    score[n][2] += d[2] * s1, score[n][3] += d[3] * s1;
+                }
+            }
+            uint32_t weights[kCols][2];
+#pragma unroll
+            for (int n = 0; n < kCols; ++n) {
+                bool higher = false;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float s = score[n][i] * p.scale;
+                    if (p.cap > 0.0f) {                         // cap * tanh(s / cap) as 1 - 2 / (e^2x + 1), which keeps its limits
+                        const float e = exp2_of(s * p.cap_inv);
+                        s = p.cap * (1.0f - __fdividef(2.0f, e + 1.0f));
+                    }
+                    if (!whole) {
+                        const int at = key + g + 8 * (i >> 1);
+                        if (at < window_low || at >= k1) s = -INFINITY;
+                    }
+                    score[n][i] = s;
+                    higher |= s > top[n][i & 1] + kSlack;
+                }
+                if (__any_sync(0xFFFFFFFFu, higher)) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float m = fmaxf(top[n][i], fmaxf(score[n][i], score[n][2 + i]));
+#pragma unroll
+                        for (int d = 4; d < 32; d *= 2) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+                        const float f = exp2_of(top[n][i] - m);
+                        top[n][i] = m;
+                        weight[n][i] *= f;
+#pragma unroll
+                        for (int j = 0; j < 2 * kGroups; ++j) acc[n][j][i] *= f, acc[n][j][2 + i] *= f;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    score[n][i] = exp2_of(score[n][i] - top[n][i & 1]);
+                    weight[n][i & 1] += score[n][i];
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const __half2 pair = __floats2half2_rn(score[n][2 * i], score[n][2 * i + 1]);
+                    weights[n][i] = transpose8x8(*reinterpret_cast<const uint32_t*>(&pair));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kGroups / 2; ++i) {
+                const uint32_t sel = (i & 1) ? 0x7632 : 0x5410;
+                const uint32_t sab = __byte_perm(x.vs[0][i / 2], x.vs[1][i / 2], sel), scd = __byte_perm(x.vs[2][i / 2], x.vs[3][i / 2], sel);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t take = half ? 0x7632 : 0x5410;
+                    uint32_t ab[4], cd[4];
+                    pairs_of(__byte_perm(x.v[0][i], x.v[1][i], take), ab);
+                    pairs_of(__byte_perm(x.v[2][i], x.v[3][i], take), cd);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) ab[j] = times(ab[j], sab), cd[j] = times(cd[j], scd);
+#pragma unroll
+                    for (int n = 0; n < kCols; ++n) {
+                        dev::mma_f16(acc[n][4 * i + 2 * half], ab[0], ab[1], cd[0], cd[1], weights[n][0], weights[n][1]);
+                        dev::mma_f16(acc[n][4 * i + 2 * half + 1], ab[2], ab[3], cd[2], cd[3], weights[n][0], weights[n][1]);
+                    }
+                }
+            }
+        }
+
+        // the warps' sums, joined
+#pragma unroll
+        for (int n = 0; n < kCols; ++n) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int d = 4; d < 32; d *= 2) weight[n][i] += __shfl_xor_sync(0xFFFFFFFFu, weight[n][i], d);
+                const int row = 8 * n + 2 * c + i;
+                if (g == 0) warp_stats[w * kRows + row] = make_float2(top[n][i], weight[n][i]);
+                float* to = joined + (w * kRows + row) * kDim;
+#pragma unroll
+                for (int j = 0; j < 2 * kGroups; ++j) {
+                    const int word = g * (kGroups / 2) + j / 4;         // of the row's words; its dimensions 2 (j % 4) and the next
+                    const int d = word % kGroups * 32 + word / kGroups * 8 + 2 * (j % 4);
+                    *reinterpret_cast<float2*>(to + d) = make_float2(acc[n][j][i], acc[n][j][2 + i]);
+                }
+            }
+        }
+        __syncthreads();
+        const bool all = count == span.units;
+        const int slot = 2 * blockIdx.x + (u == begin ? 0 : 1);
+        for (int e = threadIdx.x; e < rows * kDim; e += kThreads) {
+            const int row = e / kDim, d = e % kDim;
+            float m = kLowest, sum = 0.0f, wt = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) m = fmaxf(m, warp_stats[i * kRows + row].x);
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) {
+                const float2 st = warp_stats[i * kRows + row];
+                const float f = exp2_of(st.x - m);
+                wt += st.y * f;
+                sum += joined[(i * kRows + row) * kDim + d] * f;
+            }
+            if (all) {
+                const int64_t at = static_cast<int64_t>(h * p.group + row0 + row) * kDim + d;
+                const __half y = __float2half_rn(wt > 0.0f || wt != wt ? sum / wt : 0.0f);
+                p.y[b * p.ldy + at] = y;
+                const unsigned keep = __ballot_sync(0xFFFFFFFFu, !(fabsf(__half2float(y)) <= p.thr));
+                if (p.mask != nullptr && lane == 0) p.mask[b * p.mask_stride + at / 32] = keep;
+            } else {
+                p.sums[(static_cast<int64_t>(slot) * kRows + row) * kDim + d] = sum;
+                if (d == 0) p.stats[slot * kRows + row] = make_float2(m, wt);
+            }
+        }
+        __syncthreads();
+        u += count;
+    }
+}
+
+// Joins the partial sums of a triple that several CTAs have, in the order of its keys.
+template <int kGroups, int kCols>
+__global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnParams p, int ctas) {
+    constexpr int kDim = 32 * kGroups, kRows = 8 * kCols;
+    dev::programmatic_start();
+    const int triples = p.heads * p.row_blocks;
+    const int b = blockIdx.x / triples, triple = blockIdx.x % triples;
+    const int f0 = p.first_unit[b], units = (p.first_unit[b + 1] - f0) / triples;
+    const int64_t total = p.first_unit[p.B];
+    const int h = triple / p.row_blocks, row0 = triple % p.row_blocks * kRows, rows = min(kRows, p.group - row0);
+    int first = 0, last = -1;                                   // CTAs with a part of it
+    const int64_t s0 = f0 + static_cast<int64_t>(triple) * units;
+    if (units > 0) {
+        first = static_cast<int>(((s0 + 1) * ctas - 1) / total);
+        last = static_cast<int>(((s0 + units) * ctas - 1) / total);
+        if (first == last) return;
+    }
+    const bool starts_inside = units > 0 && total * first / ctas < s0;      // the first CTA has other keys before these
+    for (int e = threadIdx.x; e < rows * kDim; e += kThreads) {
+        const int row = e / kDim, d = e % kDim;
+        float m = kLowest, sum = 0.0f, wt = 0.0f;
+        for (int i = first; i <= last; ++i) {
+            const int64_t slot = 2 * i + (i == first && starts_inside ? 1 : 0);
+            const float2 st = p.stats[slot * kRows + row];
+            const float top = fmaxf(m, st.x), f = exp2_of(m - top), fs = exp2_of(st.x - top);
+            sum = sum * f + p.sums[(slot * kRows + row) * kDim + d] * fs;
+            wt = wt * f + st.y * fs;
+            m = top;
+        }
+        const int64_t at = static_cast<int64_t>(h * p.group + row0 + row) * kDim + d;
+        const __half y = __float2half_rn(wt > 0.0f || wt != wt ? sum / wt : 0.0f);
+        p.y[b * p.ldy + at] = y;
+        const unsigned keep = __ballot_sync(0xFFFFFFFFu, !(fabsf(__half2float(y)) <= p.thr));
+        if (p.mask != nullptr && (threadIdx.x & 31) == 0) p.mask[b * p.mask_stride + at / 32] = keep;
+    }
+}
+
+template <int kGroups, int kCols>
+size_t attn_shared_bytes(int B) { return 4u * (kWarps * 8 * kCols * 32 * kGroups + 2 * kWarps * 8 * kCols + kWarps + B + 1); }
+
+template <int kGroups, int kCols>
+spdp_status launch_form(AttnParams p, int device, int sms, cudaStream_t s) {
+    constexpr int kDim = 32 * kGroups, kRows = 8 * kCols;
+    static std::mutex mu;
+    static int resident[64] = {};                               // CTAs of an SM
+    int per_sm;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (resident[device] == 0) {
+            SPDP_CUDA_TRY(cudaFuncSetAttribute(attn_kernel<kGroups, kCols>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               static_cast<int>(attn_shared_bytes<kGroups, kCols>(kMostRequests))));
+            SPDP_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident[device], attn_kernel<kGroups, kCols>, kThreads,
+                                                                        attn_shared_bytes<kGroups, kCols>(64)));
+        }
+        per_sm = resident[device] > 0 ? resident[device] : 1;
+    }
+    const int triples = p.heads * p.row_blocks;
+    // no more CTAs than there can be units
+    const int64_t most = p.B * ((p.table_pages << p.page_shift) + kUnit - 1) / kUnit * triples;
+    const int ctas = static_cast<int>(most < static_cast<int64_t>(per_sm) * sms ? most : per_sm * sms);
+    const size_t sums = 2ull * ctas * kRows * kDim * sizeof(float), stats = 2ull * ctas * kRows * sizeof(float2);
+    void* scratch = nullptr;
+    spdp_status st = scratch_alloc(device, sums + stats + (p.B + 1) * sizeof(int), s, &scratch);
+    if (st != SPDP_OK) return st;
+    p.sums = static_cast<float*>(scratch);
+    p.stats = reinterpret_cast<float2*>(static_cast<char*>(scratch) + sums);
+    p.first_unit = reinterpret_cast<int*>(static_cast<char*>(scratch) + sums + stats);
+    cudaError_t e = launch_programmatic(attn_kernel<kGroups, kCols>, dim3(static_cast<unsigned>(ctas)), kThreads, attn_shared_bytes<kGroups, kCols>(p.B), s, p);
+    if (e == cudaSuccess) e = launch_programmatic(attn_join_kernel<kGroups, kCols>, dim3(static_cast<unsigned>(p.B * triples)), kThreads, 0, s, p, ctas);
+    const cudaError_t freed = cudaFreeAsync(scratch, s);
+    SPDP_CUDA_TRY(e);
+    SPDP_CUDA_TRY(freed);
+    return SPDP_OK;
+}
+
+template <int kGroups>
+spdp_status launch_groups(AttnParams p, int device, int sms, cudaStream_t s) {
+    if (p.group <= 8) {
+        p.row_blocks = 1;
+        return launch_form<kGroups, 1>(p, device, sms, s);
+    }
+    p.row_blocks = (p.group + 15) / 16;
+    return launch_form<kGroups, 2>(p, device, sms, s);
+}
+
+int log2_of(int v) {
+    int s = 0;
+    while ((1 << s) < v) ++s;
+    return s;
+}
+
+}  // namespace
+
+spdp_status launch_kv4_store(const Kv4StoreCall& call, cudaStream_t s) {
+    StoreParams p = {};
+    p.k = call.k, p.v = call.v, p.slot = call.slot, p.cache = call.cache, p.k_values = call.k_values, p.v_values = call.v_values;
+    p.ldk = call.ldk, p.ldv = call.ldv, p.ldk_values = call.ldk_values, p.ldv_values = call.ldv_values, p.N = call.N, p.pages = call.pages;
+    p.heads = call.kv_heads, p.dim = call.head_dim, p.page_shift = log2_of(call.page_tokens);
+    const bool f32 = call.vdt == SPDP_Y_F32;
+    const bool wide = rows_aligned16(p.k, p.ldk, 2) && rows_aligned16(p.v, p.ldv, f32 ? 4 : 2) && rows_aligned16(p.k_values, p.ldk_values, 2) &&
+                      rows_aligned16(p.v_values, p.ldv_values, 2);
+    const int64_t threads = p.N * p.heads * (p.dim / 8);
+    const dim3 grid(static_cast<unsigned>((threads + kStoreThreads - 1) / kStoreThreads), 2);
+    if (f32)
+        SPDP_CUDA_TRY(wide ? launch_programmatic(kv4_store_kernel<float, true>, grid, kStoreThreads, 0, s, p)
+                           : launch_programmatic(kv4_store_kernel<float, false>, grid, kStoreThreads, 0, s, p));
+    else
+        SPDP_CUDA_TRY(wide ? launch_programmatic(kv4_store_kernel<__half, true>, grid, kStoreThreads, 0, s, p)
+                           : launch_programmatic(kv4_store_kernel<__half, false>, grid, kStoreThreads, 0, s, p));
+    return SPDP_OK;
+}
+
+spdp_status launch_attn_kv4(const Kv4AttnCall& call, cudaStream_t s) {
+    int device = 0, sms = 0;
+    const spdp_status st = current_device(&device, &sms);
+    if (st != SPDP_OK) return st;
+    AttnParams p = {};
+    p.q = call.q, p.cache = call.cache, p.table = call.table, p.length = call.length, p.y = call.y, p.mask = call.mask;
+    p.ldq = call.ldq, p.ldy = call.ldy, p.table_stride = call.table_stride, p.table_pages = call.table_pages, p.mask_stride = call.mask_stride, p.pages = call.pages;
+    p.B = static_cast<int>(call.B), p.heads = call.kv_heads, p.group = call.q_heads / call.kv_heads, p.page_shift = log2_of(call.page_tokens);
+    constexpr float kLog2e = 1.4426950408889634f;
+    p.scale = call.scale * kLog2e;
+    p.cap = call.cap * kLog2e;
+    p.cap_inv = call.cap > 0.0f ? 2.0f / call.cap : 0.0f;       // e^(2 s / cap) = 2^(s log2(e) * 2 / cap)
+    p.window = call.window, p.thr = call.thr;
+    switch (call.head_dim) {
+        case 64: return launch_groups<2>(p, device, sms, s);
+        case 128: return launch_groups<4>(p, device, sms, s);
+        default: return launch_groups<8>(p, device, sms, s);
+    }
+}
+
+}  // namespace spdp

@@ -156,6 +156,66 @@ spdp_status launch_fetch(const __half* x, int64_t K, __half* x_out, const uint32
 spdp_status launch_swiglu_dp(const __half* gate, const __half* up, int64_t K, float thr, __half* x_out, uint32_t* mask_out,
                              int* count, cudaStream_t s);
 
+// lora.cu
+// The current device and its number of SMs (asked once a device).
+spdp_status current_device(int* device, int* sms);
+struct LoraCall {
+    const __half* X;
+    const int32_t* adapter;
+    const __half* A;
+    const __half* B;
+    const int32_t* ranks;       // may be null
+    const float* scales;        // may be null
+    const void* base;
+    void* Y;
+    int64_t N, K, M, count, ldx, lda, stride_a, ldb, stride_b, ldbase, ldy;
+    int rank, ydt;
+};
+spdp_status launch_lora(const LoraCall& call, cudaStream_t s);
+
+// heads.cu
+struct HeadsCall {
+    const void* q;
+    const void* k;
+    const __half* q_weight;     // may be null
+    const __half* k_weight;     // may be null
+    const int32_t* pos;
+    const float* inv_freq;
+    __half* q_out;
+    __half* k_out;
+    const int* sections;        // host, [axes], pairs of each axis
+    int64_t N, ldq, ldk, ldq_out, ldk_out, pos_stride;
+    int q_heads, kv_heads, head_dim, pairs, axes, dt;
+    float eps;
+    bool adjacent;
+};
+spdp_status launch_qk_norm_rope(const HeadsCall& call, cudaStream_t s);
+
+// kv4.cu
+struct Kv4StoreCall {
+    const __half* k;
+    const void* v;
+    const int64_t* slot;
+    unsigned char* cache;
+    __half* k_values;           // may be null
+    __half* v_values;           // may be null
+    int64_t N, ldk, ldv, ldk_values, ldv_values, pages;
+    int kv_heads, head_dim, page_tokens, vdt;
+};
+spdp_status launch_kv4_store(const Kv4StoreCall& call, cudaStream_t s);
+struct Kv4AttnCall {
+    const __half* q;
+    const unsigned char* cache;
+    const int32_t* table;
+    const int32_t* length;
+    __half* y;
+    uint32_t* mask;             // may be null
+    int64_t B, ldq, ldy, table_stride, table_pages, mask_stride, pages, window;
+    int q_heads, kv_heads, head_dim, page_tokens;
+    float scale, cap, thr;
+};
+spdp_status launch_attn_kv4(const Kv4AttnCall& call, cudaStream_t s);
+
 // spmm.cu
 spdp_status configure_spmm_kernel();            // per-device kernel attributes; idempotent
 spdp_status launch_spmm(const spdp_matrix* h, const __half* X, int64_t N, int64_t ldx, void* Y, int64_t ldy, int ydt,

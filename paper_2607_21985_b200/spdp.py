@@ -31,6 +31,7 @@ EXPORTS = (
     "spdp_spmspv_host", "spdp_spmspv_noalloc", "spdp_spmspv_batch", "spdp_free", "spdp_get_info", "spdp_export", "spdp_unpack",
     "spdp_active_columns", "spdp_last_device_status", "spdp_set_num_ctas", "spdp_last_cuda_error",
     "spdp_status_string", "spdp_probe_stream_read", "spdp_probe_gather", "spdp_spmm", "spdp_pack_tiled_cbc_q4", "spdp_export_q4", "spdp_row_shard", "spdp_swiglu_dp",
+    "spdp_lora", "spdp_qk_norm_rope", "spdp_kv4_page_bytes", "spdp_kv4_store", "spdp_attn_kv4",
 )
 
 
@@ -79,6 +80,11 @@ def lib():
         L.spdp_pack_tiled_cbc_q4.argtypes = [vp, i64, i64, i64, ci, ci, vp, ctypes.POINTER(vp)]
         L.spdp_export_q4.argtypes = [vp, vp, vp, vp, vp, vp]
         L.spdp_swiglu_dp.argtypes = [vp, vp, i64, cf, vp, vp, vp, vp]
+        L.spdp_lora.argtypes = [vp, i64, i64, i64, vp, vp, i64, i64, vp, i64, i64, i64, ci, vp, vp, vp, i64, vp, i64, i64, ci, vp]
+        L.spdp_qk_norm_rope.argtypes = [vp, i64, vp, i64, ci, i64, ci, ci, ci, vp, vp, cf, vp, i64, ci, ctypes.POINTER(ci), vp, ci, ci, vp, i64, vp, i64, vp]
+        L.spdp_kv4_page_bytes.argtypes = [ci, ci, ci, ctypes.POINTER(i64)]
+        L.spdp_kv4_store.argtypes = [vp, i64, vp, i64, ci, i64, ci, ci, vp, vp, i64, ci, vp, i64, vp, i64, vp]
+        L.spdp_attn_kv4.argtypes = [vp, i64, i64, ci, ci, ci, vp, i64, ci, vp, i64, i64, vp, cf, cf, i64, cf, vp, i64, vp, i64, vp]
         L.spdp_row_shard.argtypes = [i64, ci, ci, ctypes.POINTER(i64), ctypes.POINTER(i64)]
         L.spdp_probe_stream_read.argtypes = [vp, vp]
         L.spdp_probe_gather.argtypes = [vp, vp, ci, cf, vp, vp]
@@ -93,7 +99,7 @@ def lib():
         except ImportError as e:
             raise RuntimeError("the _pycall module is missing: build it with `python -m paper_2607_21985_b200.build`") from e
         # the per-token calls: same entry points, arguments converted in C (csrc/pycall.c)
-        for name in ("spmspv", "spmspv_batch", "spmm", "swiglu_dp"):
+        for name in ("spmspv", "spmspv_batch", "spmm", "swiglu_dp", "lora", "qk_norm_rope", "kv4_store", "attn_kv4"):
             address = ctypes.cast(getattr(L, "spdp_" + name), ctypes.c_void_p).value
             setattr(L, "call_" + name, functools.partial(getattr(_pycall, name), address))
         _lib = L
@@ -106,13 +112,13 @@ def _check(st: int, where: str):
 
 
 _raw_stream = _device = None
-_f16 = _f32 = None          # torch.float16, torch.float32: an import statement in every call costs more than its checks
+_f16 = _f32 = _i32 = _i64 = _u8 = None          # torch.float16, torch.float32, ...: an import statement in every call costs more than its checks
 
 
 def _load_dtypes():
-    global _f16, _f32
+    global _f16, _f32, _i32, _i64, _u8
     import torch
-    _f16, _f32 = torch.float16, torch.float32
+    _f16, _f32, _i32, _i64, _u8 = torch.float16, torch.float32, torch.int32, torch.int64, torch.uint8
 
 
 def _ydt(y):
@@ -310,6 +316,177 @@ def spdp_swiglu_dp(gate, up, thr: float, x_out, mask_out, count_out=None, stream
                                         _stream(stream))
     if st:
         _check(st, "spdp_swiglu_dp")
+
+
+def _vector(t, dtype, n, name):
+    """The address of a contiguous CUDA vector of n values; None stays None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or t.numel() != n:
+        raise ValueError(f"{name} must be a contiguous CUDA {dtype} of {n} values")
+    return t.data_ptr()
+
+
+def _rows(t, n, m, name):
+    """(address, elements between rows) of a CUDA [n][m] whose rows are contiguous."""
+    if t.shape != (n, m) or not t.is_cuda:
+        raise ValueError(f"{name} must be CUDA [{n}][{m}]")
+    ld, one = t.stride()
+    if one != 1 and m > 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return t.data_ptr(), ld if n > 1 else max(ld, m)
+
+
+def _heads(t, n, heads, dim, name):
+    """(address, elements between tokens) of a CUDA [n][heads][dim] whose heads lie one after another."""
+    if t.shape != (n, heads, dim) or not t.is_cuda:
+        raise ValueError(f"{name} must be CUDA [{n}][{heads}][{dim}]")
+    ld, head, one = t.stride()
+    if one != 1 or (head != dim and heads > 1):
+        raise ValueError(f"the heads of a token of {name} must be contiguous")
+    return t.data_ptr(), ld if n > 1 else max(ld, heads * dim)
+
+
+def spdp_lora(X, adapter, A, B, Y, base=None, scales=None, ranks=None, stream=None) -> None:
+    """Y[n] = base[n] + scales[a] * B[a] @ (A[a] @ X[n]) with a = adapter[n] (none outside 0 .. len(A) - 1); base=None adds to
+    Y in place.  X fp16 CUDA [N][K] (rows may be strided; a single token may come as [K], with Y and base [M]), adapter int32 [N],
+    A fp16 [count][rank][K], B fp16 [count][M][rank] (strided in all but the last dimension), Y and base fp16 or fp32 [N][M],
+    scales fp32 [count] (default 1), ranks int32 [count] (default all)."""
+    if base is None:
+        base = Y
+    ydt, xs = _ydt(Y), X.shape
+    if len(xs) == 1:
+        X, Y, base = X.unsqueeze(0), Y.unsqueeze(0), base.unsqueeze(0)
+        xs = X.shape
+    ashape, bshape = A.shape, B.shape
+    if len(xs) != 2 or len(ashape) != 3 or len(bshape) != 3:
+        raise ValueError("X must be [N][K], A [count][rank][K] and B [count][M][rank]")
+    N, K = xs
+    count, rank, k = ashape
+    M = bshape[1]
+    if k != K or bshape[0] != count or bshape[2] != rank:
+        raise ValueError("X must be [N][K], A [count][rank][K] and B [count][M][rank]")
+    if X.dtype is not _f16 or A.dtype is not _f16 or B.dtype is not _f16 or ydt is None or base.dtype is not Y.dtype:
+        raise ValueError("X, A and B must be fp16, Y and base both fp16 or both fp32")
+    (sa, lda, ca), (sb, ldb, cb) = A.stride(), B.stride()
+    if not A.is_cuda or not B.is_cuda or (ca != 1 and K > 1) or (cb != 1 and rank > 1):
+        raise ValueError("A and B must be CUDA tensors with a contiguous last dimension")
+    if rank <= 1:
+        lda = max(lda, K)
+    if M <= 1:
+        ldb = max(ldb, rank)
+    if adapter is None:
+        raise ValueError("adapter is required")
+    x, ldx = _rows(X, N, K, "X")
+    y, ldy = _rows(Y, N, M, "Y")
+    b, ldbase = (y, ldy) if base is Y else _rows(base, N, M, "base")
+    st = (_lib or lib()).call_lora(x, N, K, ldx, _vector(adapter, _i32, N, "adapter"), A.data_ptr(), lda, sa, B.data_ptr(), ldb, sb, count, rank,
+                                   _vector(ranks, _i32, count, "ranks"), _vector(scales, _f32, count, "scales"), b, ldbase, y, M, ldy, ydt, _stream(stream))
+    if st:
+        _check(st, "spdp_lora")
+
+
+def spdp_qk_norm_rope(q, k, q_out, k_out, pos, inv_freq, sections=None, q_weight=None, k_weight=None, eps: float = 1e-6, adjacent: bool = False,
+                      stream=None) -> None:
+    """Norms (where a weight is given) of the heads q [N][q_heads][D] and k [N][kv_heads][D] (fp16 or fp32 CUDA, tokens may be
+    strided, as in the output of one projection for all of them) and their rotation by pos (int32 [N], or [axes][N] with `sections`
+    pairs to each axis) times inv_freq (fp32 [pairs]), into fp16 q_out and k_out (may be q and k).  k and k_out may be None;
+    inv_freq None: no rotation."""
+    dt, qs = _ydt(q), q.shape
+    if len(qs) != 3 or dt is None or q_out.dtype is not _f16 or (k is not None and (len(k.shape) != 3 or k.dtype is not q.dtype or k_out.dtype is not _f16)):
+        raise ValueError("q and k must be [N][heads][D], both fp16 or both fp32, q_out and k_out fp16")
+    N, q_heads, D = qs
+    qp, ldq = _heads(q, N, q_heads, D, "q")
+    qo, ldqo = _heads(q_out, N, q_heads, D, "q_out")
+    if k is None:
+        kv_heads, kp, ldk, ko, ldko = 0, None, 0, None, 0
+    else:
+        kv_heads = k.shape[1]
+        kp, ldk = _heads(k, N, kv_heads, D, "k")
+        ko, ldko = _heads(k_out, N, kv_heads, D, "k_out")
+    if inv_freq is None:
+        pairs = axes = stride = 0
+        at = freq = sections = None
+    else:
+        pairs, dims = inv_freq.numel(), len(pos.shape)
+        freq = _vector(inv_freq, _f32, pairs, "inv_freq")
+        if dims not in (1, 2) or pos.dtype is not _i32 or not pos.is_cuda or pos.shape[-1] != N or (N > 1 and pos.stride(-1) != 1):
+            raise ValueError("pos must be CUDA int32 [N] or [axes][N]")
+        axes = 1 if dims == 1 else pos.shape[0]
+        stride = N if axes <= 1 else pos.stride(0)
+        at = pos.data_ptr()
+        sections = (pairs,) if sections is None and axes == 1 else tuple(sections or ())
+    st = (_lib or lib()).call_qk_norm_rope(qp, ldq, kp, ldk, dt, N, q_heads, kv_heads, D, _vector(q_weight, _f16, D, "q_weight"),
+                                           _vector(k_weight, _f16, D, "k_weight"), eps, at, stride, axes, sections, freq, pairs, 1 if adjacent else 0,
+                                           qo, ldqo, ko, ldko, _stream(stream))
+    if st:
+        _check(st, "spdp_qk_norm_rope")
+
+
+def spdp_kv4_page_bytes(kv_heads: int, head_dim: int, page_tokens: int) -> int:
+    """Bytes of one page of a 4-bit key/value cache; the cache is a uint8 CUDA tensor [pages][that]."""
+    out = ctypes.c_int64(0)
+    _check(lib().spdp_kv4_page_bytes(kv_heads, head_dim, page_tokens, ctypes.byref(out)), "spdp_kv4_page_bytes")
+    return out.value
+
+
+def _cache(cache, kv_heads, dim, page_tokens):
+    """(address, pages) of a cache."""
+    cs = cache.shape
+    if len(cs) != 2 or cache.dtype is not _u8 or not cache.is_cuda or not cache.is_contiguous() or cs[1] != kv_heads * page_tokens * (dim + dim // 8):
+        raise ValueError("cache must be a contiguous CUDA uint8 [pages][spdp_kv4_page_bytes(kv_heads, head_dim, page_tokens)]")
+    return cache.data_ptr(), cs[0]
+
+
+def spdp_kv4_store(k, v, slot, cache, page_tokens: int, k_values=None, v_values=None, stream=None) -> None:
+    """Keys k (fp16 CUDA [N][kv_heads][D]) and values v (fp16 or fp32) into the slots (int64 [N], below 0: not stored) of a 4-bit
+    cache; k_values and v_values (fp16, optional) get what the codes stand for."""
+    vdt, ks = _ydt(v), k.shape
+    if len(ks) != 3 or k.dtype is not _f16 or vdt is None or (k_values is not None and k_values.dtype is not _f16) or \
+            (v_values is not None and v_values.dtype is not _f16):
+        raise ValueError("k must be fp16 [N][kv_heads][D], v fp16 or fp32, k_values and v_values fp16")
+    if slot is None:
+        raise ValueError("slot is required")
+    N, heads, D = ks
+    kp, ldk = _heads(k, N, heads, D, "k")
+    vp, ldv = _heads(v, N, heads, D, "v")
+    at, pages = _cache(cache, heads, D, page_tokens)
+    ko, ldko = (None, 0) if k_values is None else _heads(k_values, N, heads, D, "k_values")
+    vo, ldvo = (None, 0) if v_values is None else _heads(v_values, N, heads, D, "v_values")
+    st = (_lib or lib()).call_kv4_store(kp, ldk, vp, ldv, vdt, N, heads, D, _vector(slot, _i64, N, "slot"), at, pages, page_tokens, ko, ldko, vo, ldvo,
+                                        _stream(stream))
+    if st:
+        _check(st, "spdp_kv4_store")
+
+
+def spdp_attn_kv4(q, cache, page_tokens: int, kv_heads: int, table, length, y, scale: float, cap: float = 0.0, window: int = 0, thr: float = 0.0,
+                  mask=None, stream=None) -> None:
+    """Attention of one token of each request, q fp16 CUDA [B][q_heads][D], over its `length` (int32 [B]) keys in the pages table[b]
+    (int32 [B][pages of a request]) of a 4-bit cache; y fp16 [B][q_heads * D] and, where mask (int32/uint32 [B][>= q_heads * D / 32])
+    is given, the bits of the columns with |y| above thr."""
+    if _f16 is None:
+        _load_dtypes()
+    qs, ts = q.shape, table.shape
+    if len(qs) != 3 or q.dtype is not _f16 or y.dtype is not _f16:
+        raise ValueError("q must be fp16 [B][q_heads][D] and y fp16")
+    if table.dtype is not _i32 or len(ts) != 2 or length is None:
+        raise ValueError("table must be int32 [B][pages] and length int32 [B]")
+    B, q_heads, D = qs
+    qp, ldq = _heads(q, B, q_heads, D, "q")
+    yp, ldy = _rows(y, B, q_heads * D, "y")
+    at, pages = _cache(cache, kv_heads, D, page_tokens)
+    tp, tstride = _rows(table, B, ts[1], "table")
+    mp, mstride = None, 0
+    if mask is not None:
+        if len(mask.shape) != 2 or mask.element_size() != 4:
+            raise ValueError("mask must be 32-bit [B][words]")
+        mp, mstride = _rows(mask, B, mask.shape[1], "mask")
+        if mask.shape[1] < q_heads * D // 32:
+            raise ValueError("mask must hold a bit for each column of y")
+    st = (_lib or lib()).call_attn_kv4(qp, ldq, B, q_heads, kv_heads, D, at, pages, page_tokens, tp, tstride, ts[1], _vector(length, _i32, B, "length"),
+                                       scale, cap, window, thr, yp, ldy, mp, mstride, _stream(stream))
+    if st:
+        _check(st, "spdp_attn_kv4")
 
 
 def spdp_row_shard(M: int, world: int, rank: int):
