@@ -300,7 +300,8 @@ SPDP_API spdp_status spdp_qk_norm_rope(const void* q_dev, int64_t ldq, const voi
 /* A paged key/value cache held in 4 bits.  A row (one token's key or value of one head, head_dim = 64, 128 or 256 values) is
  * head_dim codes and one fp16 scale to 32 dimensions, by the rule of the 4-bit Values (spdp_pack_tiled_cbc_q4):
  *   scale = fp16(max|x| / 7);  code = clamp(rint(x / scale), -7, 7) + 8 (8 where the scale is 0);  it stands for (code - 8) * scale.
- * Rows must be finite (what Inf or NaN leave is unspecified, within that row).
+ * Rows must be finite (what Inf or NaN leave is unspecified, within that row); values of 65492 and more may come to stand for Inf,
+ * which 7 times their scale rounds to in fp16.
  * A page holds page_tokens = P tokens (a power of two, 16 .. 256); for each key head in turn: codes of the keys
  * [P][head_dim / 2] bytes, codes of the values [P][head_dim / 2], scales of the keys fp16 [P][head_dim / 32], scales of the values
  * [P][head_dim / 32].  In a row of codes, with G = head_dim / 32, dimension 32 g + 8 c + j (c < 4, j < 8) is bits 4 j .. 4 j + 3 of

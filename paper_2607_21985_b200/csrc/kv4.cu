@@ -130,6 +130,9 @@ __device__ __forceinline__ Span span_of(const AttnParams& p, int b) {
     return s;
 }
 
+// The first unit of CTA i's run, of `ctas` that share `total` units.
+__device__ __forceinline__ int run_start(int total, int ctas, int i) { return static_cast<int>(static_cast<int64_t>(total) * i / ctas); }
+
 // The first unit of every request, into shared memory (all threads; ends with a barrier).
 __device__ void scan_units(const AttnParams& p, int* first, int* warp_sums) {
     const int each = (p.B + kThreads - 1) / kThreads, b0 = threadIdx.x * each, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
@@ -242,8 +245,9 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnParams p) {
     scan_units(p, first, warp_sums);
     if (blockIdx.x == 0)
         for (int b = threadIdx.x; b <= p.B; b += kThreads) p.first_unit[b] = first[b];
-    const int64_t total = first[p.B];
-    const int begin = static_cast<int>(total * blockIdx.x / gridDim.x), stop = static_cast<int>(total * (blockIdx.x + 1) / gridDim.x);
+    const int total = first[p.B], ctas = min(static_cast<int>(gridDim.x), total);       // so that no CTA between two others has nothing
+    if (static_cast<int>(blockIdx.x) >= ctas) return;
+    const int begin = run_start(total, ctas, blockIdx.x), stop = run_start(total, ctas, blockIdx.x + 1);
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
     const int P = 1 << p.page_shift;
     const int64_t head_bytes = static_cast<int64_t>(P) * 36 * kGroups;
@@ -443,13 +447,13 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnParams p) {
 
 // Joins the partial sums of a triple that several CTAs have, in the order of its keys.
 template <int kGroups, int kCols>
-__global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnParams p, int ctas) {
+__global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnParams p, int most_ctas) {
     constexpr int kDim = 32 * kGroups, kRows = 8 * kCols;
     dev::programmatic_start();
     const int triples = p.heads * p.row_blocks;
     const int b = blockIdx.x / triples, triple = blockIdx.x % triples;
     const int f0 = p.first_unit[b], units = (p.first_unit[b + 1] - f0) / triples;
-    const int64_t total = p.first_unit[p.B];
+    const int total = p.first_unit[p.B], ctas = min(most_ctas, total);
     const int h = triple / p.row_blocks, row0 = triple % p.row_blocks * kRows, rows = min(kRows, p.group - row0);
     int first = 0, last = -1;                                   // CTAs with a part of it
     const int64_t s0 = f0 + static_cast<int64_t>(triple) * units;
@@ -458,7 +462,7 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnParams p,
         last = static_cast<int>(((s0 + units) * ctas - 1) / total);
         if (first == last) return;
     }
-    const bool starts_inside = units > 0 && total * first / ctas < s0;      // the first CTA has other keys before these
+    const bool starts_inside = units > 0 && run_start(total, ctas, first) < s0;      // the first CTA has other keys before these
     for (int e = threadIdx.x; e < rows * kDim; e += kThreads) {
         const int row = e / kDim, d = e % kDim;
         float m = kLowest, sum = 0.0f, wt = 0.0f;
