@@ -109,7 +109,7 @@ struct AttnParams {
     uint32_t* mask;
     float* sums;                        // [2 CTAs][rows][dim]
     float2* stats;                      // [2 CTAs][rows]: maximum, weight
-    int* first_unit;                    // [B + 1]
+    int4* open;                         // [CTAs]: request, triple, last CTA and slot of a triple that begins there and ends elsewhere; -1: none
     int64_t ldq, ldy, table_stride, table_pages, mask_stride, pages;
     int B, heads, group, row_blocks, page_shift;
     float scale, cap, cap_inv;          // scores in powers of two
@@ -201,6 +201,39 @@ __device__ __forceinline__ void load_words(const unsigned char* at, uint32_t (&w
     }
 }
 
+// 16 keys in shared memory, as a warp's asynchronous copies leave them: four runs of the page's head.  The values' rows are 16
+// bytes further apart than in the page, so that a lane's reads of rows 2 c meet other banks than its neighbours'.
+template <int kGroups>
+struct Chunk {
+    static constexpr int kRow = 16 * kGroups, kValueRow = kRow + 16;
+    static constexpr int kValues = 16 * kRow, kKeyScales = kValues + 16 * kValueRow, kValueScales = kKeyScales + 32 * kGroups;
+    static constexpr int kBytes = kValueScales + 32 * kGroups;
+};
+constexpr int kStages = 4;              // chunks of a warp, three of them on their way
+
+__device__ __forceinline__ void copy16(uint32_t to, const unsigned char* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+
+// The keys at .. at + 15 of a page's head into a chunk.
+template <int kGroups>
+__device__ __forceinline__ void copy_chunk(uint32_t to, const unsigned char* head, int at, int P, int lane) {
+    using C = Chunk<kGroups>;
+    const unsigned char* keys = head + at * C::kRow;
+    const unsigned char* values = keys + P * C::kRow;
+#pragma unroll
+    for (int i = 0; i < (C::kRow + 31) / 32; ++i) {
+        const int piece = 32 * i + lane, row = piece / kGroups, part = piece % kGroups;
+        copy16(to + 16 * piece, keys + 16 * piece);
+        copy16(to + C::kValues + row * C::kValueRow + 16 * part, values + 16 * piece);
+    }
+    const unsigned char* scales = head + 2 * P * C::kRow + at * 2 * kGroups;
+    if (lane < 4 * kGroups) {           // 2 kGroups pieces of the keys' scales, as many of the values'
+        const int piece = lane % (2 * kGroups);
+        copy16(to + C::kKeyScales + 16 * lane, scales + 16 * piece + (lane < 2 * kGroups ? 0 : P * 2 * kGroups));
+    }
+}
+
 // What a lane (g, c) holds of 16 keys: words of the keys g and g + 8 and their scales; words and scales of the values of keys
 // 2 c, 2 c + 1, 2 c + 8, 2 c + 9, an eighth of a row each.
 template <int kGroups>
@@ -211,22 +244,18 @@ struct Keys {
 };
 
 template <int kGroups>
-__device__ __forceinline__ void load_keys(Keys<kGroups>& x, const unsigned char* head, int at, int P, int g, int c) {
-    constexpr int kRow = 16 * kGroups;      // bytes of a row of codes
-    const unsigned char* values = head + P * kRow;
-    const unsigned char* k_scales = head + 2 * P * kRow;
-    const unsigned char* v_scales = k_scales + P * 2 * kGroups;
+__device__ __forceinline__ void load_keys(Keys<kGroups>& x, const unsigned char* chunk, int g, int c) {
+    using C = Chunk<kGroups>;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int key = at + g + 8 * i;
-        load_words<kGroups>(head + key * kRow + c * 4 * kGroups, x.k[i]);
-        load_words<kGroups / 2>(k_scales + key * 2 * kGroups, x.ks[i]);
+        load_words<kGroups>(chunk + (g + 8 * i) * C::kRow + c * 4 * kGroups, x.k[i]);
+        load_words<kGroups / 2>(chunk + C::kKeyScales + (g + 8 * i) * 2 * kGroups, x.ks[i]);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int key = at + 2 * c + (i & 1) + 8 * (i >> 1);
-        load_words<kGroups / 2>(values + key * kRow + g * 2 * kGroups, x.v[i]);
-        const unsigned char* s = v_scales + key * 2 * kGroups + (g & 1) * kGroups;
+        const int key = 2 * c + (i & 1) + 8 * (i >> 1);
+        load_words<kGroups / 2>(chunk + C::kValues + key * C::kValueRow + g * 2 * kGroups, x.v[i]);
+        const unsigned char* s = chunk + C::kValueScales + key * 2 * kGroups + (g & 1) * kGroups;
         if constexpr (kGroups == 2) x.vs[i][0] = *reinterpret_cast<const uint16_t*>(s);
         else load_words<kGroups / 4>(s, x.vs[i]);
     }
@@ -234,22 +263,31 @@ __device__ __forceinline__ void load_keys(Keys<kGroups>& x, const unsigned char*
 
 // kGroups = D / 32; kCols: blocks of 8 query heads.
 template <int kGroups, int kCols>
-__global__ void __launch_bounds__(kThreads) attn_kernel(const AttnParams p) {
+__global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 4) attn_kernel(const AttnParams p) {
     constexpr int kDim = 32 * kGroups, kRows = 8 * kCols;
-    extern __shared__ float shared[];
-    float* joined = shared;                                     // [warp][kRows][kDim]
-    float2* warp_stats = reinterpret_cast<float2*>(joined + kWarps * kRows * kDim);      // [warp][kRows]
+    constexpr int kRing = kStages * Chunk<kGroups>::kBytes;     // bytes of a warp
+    static_assert(kRing >= kRows * kDim * 4 && kRing % 16 == 0, "a warp's sums take the place of its chunks");
+    extern __shared__ float4 shared[];
+    unsigned char* rings = reinterpret_cast<unsigned char*>(shared);                    // [warp]: kStages chunks, then sums [kRows][kDim]
+    float2* warp_stats = reinterpret_cast<float2*>(rings + kWarps * kRing);             // [warp][kRows]
     int* warp_sums = reinterpret_cast<int*>(warp_stats + kWarps * kRows);
     int* first = warp_sums + kWarps;
     dev::programmatic_start();
     scan_units(p, first, warp_sums);
-    if (blockIdx.x == 0)
-        for (int b = threadIdx.x; b <= p.B; b += kThreads) p.first_unit[b] = first[b];
+    for (int b = blockIdx.x; b < p.B; b += gridDim.x) {         // requests without keys
+        if (first[b] != first[b + 1]) continue;
+        const int columns = p.heads * p.group * kDim;
+        for (int i = threadIdx.x; i < columns; i += kThreads) p.y[b * p.ldy + i] = __ushort_as_half(0);
+        if (p.mask != nullptr)
+            for (int i = threadIdx.x; i < columns / 32; i += kThreads) p.mask[b * p.mask_stride + i] = 0.0f <= p.thr ? 0u : 0xFFFFFFFFu;
+    }
+    if (threadIdx.x == 0) p.open[blockIdx.x].x = -1;
     const int total = first[p.B], ctas = min(static_cast<int>(gridDim.x), total);       // so that no CTA between two others has nothing
     if (static_cast<int>(blockIdx.x) >= ctas) return;
     const int begin = run_start(total, ctas, blockIdx.x), stop = run_start(total, ctas, blockIdx.x + 1);
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
     const int P = 1 << p.page_shift;
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(rings)) + w * kRing;
     const int64_t head_bytes = static_cast<int64_t>(P) * 36 * kGroups;
 
     for (int u = begin; u < stop;) {
@@ -289,21 +327,31 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnParams p) {
 #pragma unroll
         for (int n = 0; n < kCols; ++n) top[n][0] = top[n][1] = kLowest, weight[n][0] = weight[n][1] = 0.0f;
 
-        auto head_of = [&](int key) -> const unsigned char* {   // null: no such keys, or a page that does not exist
-            if (key >= k1) return nullptr;
-            const int64_t page = table[key >> p.page_shift];
-            return page < 0 || page >= p.pages ? nullptr : p.cache + (page * p.heads + h) * head_bytes;
+        // the warp's chunks: every fourth one of the run.  Each lane knows the page of one of 32 of them, and of one of the next 32
+        const int chunks = ((k1 - k0 + 15) / 16 - w + kWarps - 1) / kWarps;
+        auto page_of = [&](int i) { return i < chunks ? table[(k0 + 16 * (w + kWarps * i)) >> p.page_shift] : -1; };
+        int pages = page_of(lane), pages_after = page_of(32 + lane);
+        unsigned there = 0;                                     // bit j: the chunk that was asked for j chunks ago exists
+        auto ask = [&](int i) {
+            const int64_t page = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
+            const bool ok = page >= 0 && page < p.pages;
+            there = there << 1 | (ok ? 1u : 0u);
+            if (ok)
+                copy_chunk<kGroups>(ring + i % kStages * Chunk<kGroups>::kBytes, p.cache + (page * p.heads + h) * head_bytes,
+                                    (k0 + 16 * (w + kWarps * i)) & (P - 1), P, lane);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if ((i & 31) == 31) pages = pages_after, pages_after = page_of(i + 33 + lane);
         };
-        Keys<kGroups> next = {};
-        const unsigned char* ahead = head_of(k0 + 16 * w);
-        if (ahead != nullptr) load_keys<kGroups>(next, ahead, (k0 + 16 * w) & (P - 1), P, g, c);
-        for (int key = k0 + 16 * w; key < k1; key += 16 * kWarps) {
-            Keys<kGroups> x = next;
-            const bool any = ahead != nullptr;
-            const int after = key + 16 * kWarps;
-            ahead = head_of(after);
-            if (ahead != nullptr) load_keys<kGroups>(next, ahead, after & (P - 1), P, g, c);
-            if (!any) continue;
+        __syncwarp();
+        for (int i = 0; i < kStages - 1; ++i) ask(i);
+        for (int i = 0; i < chunks; ++i) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+            __syncwarp();                                       // all lanes' copies are there, and all have read the chunk before
+            ask(i + kStages - 1);
+            if (!(there >> (kStages - 1) & 1)) continue;        // a page that does not exist
+            const int key = k0 + 16 * (w + kWarps * i);
+            Keys<kGroups> x;
+            load_keys<kGroups>(x, rings + w * kRing + i % kStages * Chunk<kGroups>::kBytes, g, c);
             // keys that do not count: no score, and a scale of 0 for whatever the page holds there
             const bool whole = key >= window_low && key + 16 <= k1;
             if (!whole) {
@@ -397,6 +445,9 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnParams p) {
         }
 
         // the warps' sums, joined
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
+        float* sums = reinterpret_cast<float*>(rings + w * kRing);
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
 #pragma unroll
@@ -405,7 +456,7 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnParams p) {
                 for (int d = 4; d < 32; d *= 2) weight[n][i] += __shfl_xor_sync(0xFFFFFFFFu, weight[n][i], d);
                 const int row = 8 * n + 2 * c + i;
                 if (g == 0) warp_stats[w * kRows + row] = make_float2(top[n][i], weight[n][i]);
-                float* to = joined + (w * kRows + row) * kDim;
+                float* to = sums + row * kDim;
 #pragma unroll
                 for (int j = 0; j < 2 * kGroups; ++j) {
                     const int word = g * (kGroups / 2) + j / 4;         // of the row's words; its dimensions 2 (j % 4) and the next
@@ -427,7 +478,7 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnParams p) {
                 const float2 st = warp_stats[i * kRows + row];
                 const float f = exp2_of(st.x - m);
                 wt += st.y * f;
-                sum += joined[(i * kRows + row) * kDim + d] * f;
+                sum += reinterpret_cast<const float*>(rings + i * kRing)[row * kDim + d] * f;
             }
             if (all) {
                 const int64_t at = static_cast<int64_t>(h * p.group + row0 + row) * kDim + d;
@@ -440,50 +491,63 @@ __global__ void __launch_bounds__(kThreads) attn_kernel(const AttnParams p) {
                 if (d == 0) p.stats[slot * kRows + row] = make_float2(m, wt);
             }
         }
+        if (threadIdx.x == 0 && off == 0 && !all)               // the CTAs with the rest follow this one
+            p.open[blockIdx.x] = make_int4(b, triple, static_cast<int>(((static_cast<int64_t>(u) + span.units) * ctas - 1) / total), slot);
         __syncthreads();
         u += count;
     }
 }
 
-// Joins the partial sums of a triple that several CTAs have, in the order of its keys.
+// Joins the partial sums of the triple that begins in a CTA and ends in another one, in the order of its keys: a row of it to a
+// CTA, whose groups of lanes take every kParts-th sum.
+constexpr int kJoinThreads = 256;
+
 template <int kGroups, int kCols>
-__global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnParams p, int most_ctas) {
-    constexpr int kDim = 32 * kGroups, kRows = 8 * kCols;
+__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParams p) {
+    constexpr int kDim = 32 * kGroups, kRows = 8 * kCols, kLanes = kDim / 4, kParts = kJoinThreads / kLanes;
+    __shared__ float part[kParts][kDim];
+    __shared__ float2 stat[kParts];
     dev::programmatic_start();
-    const int triples = p.heads * p.row_blocks;
-    const int b = blockIdx.x / triples, triple = blockIdx.x % triples;
-    const int f0 = p.first_unit[b], units = (p.first_unit[b + 1] - f0) / triples;
-    const int total = p.first_unit[p.B], ctas = min(most_ctas, total);
-    const int h = triple / p.row_blocks, row0 = triple % p.row_blocks * kRows, rows = min(kRows, p.group - row0);
-    int first = 0, last = -1;                                   // CTAs with a part of it
-    const int64_t s0 = f0 + static_cast<int64_t>(triple) * units;
-    if (units > 0) {
-        first = static_cast<int>(((s0 + 1) * ctas - 1) / total);
-        last = static_cast<int>(((s0 + units) * ctas - 1) / total);
-        if (first == last) return;
+    const int4 open = p.open[blockIdx.x];
+    if (open.x < 0) return;
+    const int b = open.x, h = open.y / p.row_blocks, row = blockIdx.y, head = open.y % p.row_blocks * kRows + row;
+    if (head >= p.group) return;
+    const int at = threadIdx.x % kLanes, mine = threadIdx.x / kLanes, count = open.z - static_cast<int>(blockIdx.x) + 1;
+    float m = kLowest, wt = 0.0f;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int i = mine; i < count; i += kParts) {
+        const int64_t from = (i == 0 ? open.w : 2 * (static_cast<int64_t>(blockIdx.x) + i)) * kRows + row;
+        const float2 st = p.stats[from];
+        const float4 v = *reinterpret_cast<const float4*>(p.sums + from * kDim + 4 * at);
+        const float top = fmaxf(m, st.x), f = exp2_of(m - top), fs = exp2_of(st.x - top);
+        sum.x = sum.x * f + v.x * fs, sum.y = sum.y * f + v.y * fs, sum.z = sum.z * f + v.z * fs, sum.w = sum.w * f + v.w * fs;
+        wt = wt * f + st.y * fs;
+        m = top;
     }
-    const bool starts_inside = units > 0 && run_start(total, ctas, first) < s0;      // the first CTA has other keys before these
-    for (int e = threadIdx.x; e < rows * kDim; e += kThreads) {
-        const int row = e / kDim, d = e % kDim;
-        float m = kLowest, sum = 0.0f, wt = 0.0f;
-        for (int i = first; i <= last; ++i) {
-            const int64_t slot = 2 * i + (i == first && starts_inside ? 1 : 0);
-            const float2 st = p.stats[slot * kRows + row];
-            const float top = fmaxf(m, st.x), f = exp2_of(m - top), fs = exp2_of(st.x - top);
-            sum = sum * f + p.sums[(slot * kRows + row) * kDim + d] * fs;
-            wt = wt * f + st.y * fs;
-            m = top;
-        }
-        const int64_t at = static_cast<int64_t>(h * p.group + row0 + row) * kDim + d;
-        const __half y = __float2half_rn(wt > 0.0f || wt != wt ? sum / wt : 0.0f);
-        p.y[b * p.ldy + at] = y;
-        const unsigned keep = __ballot_sync(0xFFFFFFFFu, !(fabsf(__half2float(y)) <= p.thr));
-        if (p.mask != nullptr && (threadIdx.x & 31) == 0) p.mask[b * p.mask_stride + at / 32] = keep;
+    *reinterpret_cast<float4*>(&part[mine][4 * at]) = sum;
+    if (at == 0) stat[mine] = make_float2(m, wt);
+    __syncthreads();
+    const int d = threadIdx.x;
+    if (d >= kDim) return;
+    float top = kLowest, weight = 0.0f, total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) top = fmaxf(top, stat[i].x);
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+        const float f = exp2_of(stat[i].x - top);
+        weight += stat[i].y * f;
+        total += part[i][d] * f;
     }
+    const int64_t column = static_cast<int64_t>(h * p.group + head) * kDim + d;
+    const __half y = __float2half_rn(weight > 0.0f || weight != weight ? total / weight : 0.0f);
+    p.y[b * p.ldy + column] = y;
+    const unsigned keep = __ballot_sync(0xFFFFFFFFu, !(fabsf(__half2float(y)) <= p.thr));
+    if (p.mask != nullptr && (d & 31) == 0) p.mask[b * p.mask_stride + column / 32] = keep;
 }
 
 template <int kGroups, int kCols>
-size_t attn_shared_bytes(int B) { return 4u * (kWarps * 8 * kCols * 32 * kGroups + 2 * kWarps * 8 * kCols + kWarps + B + 1); }
+size_t attn_shared_bytes(int B) { return kWarps * (kStages * Chunk<kGroups>::kBytes + 8 * kCols * sizeof(float2) + sizeof(int)) + (B + 1) * sizeof(int); }
 
 template <int kGroups, int kCols>
 spdp_status launch_form(AttnParams p, int device, int sms, cudaStream_t s) {
@@ -507,13 +571,13 @@ spdp_status launch_form(AttnParams p, int device, int sms, cudaStream_t s) {
     const int ctas = static_cast<int>(most < static_cast<int64_t>(per_sm) * sms ? most : per_sm * sms);
     const size_t sums = 2ull * ctas * kRows * kDim * sizeof(float), stats = 2ull * ctas * kRows * sizeof(float2);
     void* scratch = nullptr;
-    spdp_status st = scratch_alloc(device, sums + stats + (p.B + 1) * sizeof(int), s, &scratch);
+    spdp_status st = scratch_alloc(device, sums + stats + ctas * sizeof(int4), s, &scratch);
     if (st != SPDP_OK) return st;
     p.sums = static_cast<float*>(scratch);
     p.stats = reinterpret_cast<float2*>(static_cast<char*>(scratch) + sums);
-    p.first_unit = reinterpret_cast<int*>(static_cast<char*>(scratch) + sums + stats);
+    p.open = reinterpret_cast<int4*>(static_cast<char*>(scratch) + sums + stats);
     cudaError_t e = launch_programmatic(attn_kernel<kGroups, kCols>, dim3(static_cast<unsigned>(ctas)), kThreads, attn_shared_bytes<kGroups, kCols>(p.B), s, p);
-    if (e == cudaSuccess) e = launch_programmatic(attn_join_kernel<kGroups, kCols>, dim3(static_cast<unsigned>(p.B * triples)), kThreads, 0, s, p, ctas);
+    if (e == cudaSuccess) e = launch_programmatic(attn_join_kernel<kGroups, kCols>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(p.group < kRows ? p.group : kRows)), kJoinThreads, 0, s, p);
     const cudaError_t freed = cudaFreeAsync(scratch, s);
     SPDP_CUDA_TRY(e);
     SPDP_CUDA_TRY(freed);
