@@ -113,6 +113,7 @@ struct AttnParams {
     int64_t ldq, ldy, table_stride, table_pages, mask_stride, pages;
     int B, heads, group, row_blocks, page_shift;
     float scale, cap, cap_inv;          // scores in powers of two
+    bool wide_q, wide_y;
     int64_t window;
     float thr;
 };
@@ -156,13 +157,19 @@ __device__ void scan_units(const AttnParams& p, int* first, int* warp_sums) {
     __syncthreads();
 }
 
+// (w & mask) | bits as one operation (with two constants in the instruction the compiler makes two of it).
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
+    return r;
+}
 __device__ __forceinline__ uint32_t low_pair(uint32_t w) {       // nibbles 0 and 4 of w, as fp16 numbers minus 8
-    const uint32_t v = (w & 0x000F000Fu) | 0x64006400u;          // 1024 + n
+    const uint32_t v = and_or(w, 0x000F000Fu, 0x64006400u);      // 1024 + n
     const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&v), __half2half2(__ushort_as_half(0x6408)));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 __device__ __forceinline__ uint32_t high_pair(uint32_t w) {      // nibbles 1 and 5
-    const uint32_t v = (w & 0x00F000F0u) | 0x54005400u;          // 64 + n
+    const uint32_t v = and_or(w, 0x00F000F0u, 0x54005400u);      // 64 + n
     const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&v), __half2half2(__ushort_as_half(0x5480)));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
@@ -209,7 +216,7 @@ struct Chunk {
     static constexpr int kValues = 16 * kRow, kKeyScales = kValues + 16 * kValueRow, kValueScales = kKeyScales + 32 * kGroups;
     static constexpr int kBytes = kValueScales + 32 * kGroups;
 };
-constexpr int kStages = 4;              // chunks of a warp, three of them on their way
+constexpr int kStages = 2;              // of a warp, two chunks each: one is read while the other is on its way
 
 __device__ __forceinline__ void copy16(uint32_t to, const unsigned char* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
@@ -234,41 +241,34 @@ __device__ __forceinline__ void copy_chunk(uint32_t to, const unsigned char* hea
     }
 }
 
-// What a lane (g, c) holds of 16 keys: words of the keys g and g + 8 and their scales; words and scales of the values of keys
-// 2 c, 2 c + 1, 2 c + 8, 2 c + 9, an eighth of a row each.
-template <int kGroups>
-struct Keys {
-    uint32_t k[2][kGroups], v[4][kGroups / 2];
-    uint32_t ks[2][kGroups / 2];
-    uint32_t vs[4][(kGroups + 3) / 4];      // kGroups / 2 scales
-};
-
-template <int kGroups>
-__device__ __forceinline__ void load_keys(Keys<kGroups>& x, const unsigned char* chunk, int g, int c) {
-    using C = Chunk<kGroups>;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        load_words<kGroups>(chunk + (g + 8 * i) * C::kRow + c * 4 * kGroups, x.k[i]);
-        load_words<kGroups / 2>(chunk + C::kKeyScales + (g + 8 * i) * 2 * kGroups, x.ks[i]);
-    }
+// Four columns of a request's output and their bits of its mask; 8 neighbouring lanes have the columns of a word.
+__device__ __forceinline__ void store_result(const AttnParams& p, int b, int64_t column, float4 sum, float weight) {
+    const float f[4] = {sum.x, sum.y, sum.z, sum.w};
+    __half y[4];
+    unsigned keep = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int key = 2 * c + (i & 1) + 8 * (i >> 1);
-        load_words<kGroups / 2>(chunk + C::kValues + key * C::kValueRow + g * 2 * kGroups, x.v[i]);
-        const unsigned char* s = chunk + C::kValueScales + key * 2 * kGroups + (g & 1) * kGroups;
-        if constexpr (kGroups == 2) x.vs[i][0] = *reinterpret_cast<const uint16_t*>(s);
-        else load_words<kGroups / 4>(s, x.vs[i]);
+        y[i] = __float2half_rn(weight > 0.0f || weight != weight ? f[i] / weight : 0.0f);
+        keep |= (fabsf(__half2float(y[i])) <= p.thr ? 0u : 1u) << i;
     }
+    __half* to = p.y + b * p.ldy + column;
+    if (p.wide_y) *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(y);
+    else to[0] = y[0], to[1] = y[1], to[2] = y[2], to[3] = y[3];
+    keep <<= 4 * (threadIdx.x & 7);
+    const unsigned mine = 0xFFu << (threadIdx.x & 24);          // the lanes of a word come together
+#pragma unroll
+    for (int d = 1; d < 8; d *= 2) keep |= __shfl_xor_sync(mine, keep, d);
+    if (p.mask != nullptr && (threadIdx.x & 7) == 0) p.mask[b * p.mask_stride + column / 32] = keep;
 }
 
 // kGroups = D / 32; kCols: blocks of 8 query heads.
 template <int kGroups, int kCols>
 __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 4) attn_kernel(const AttnParams p) {
     constexpr int kDim = 32 * kGroups, kRows = 8 * kCols;
-    constexpr int kRing = kStages * Chunk<kGroups>::kBytes;     // bytes of a warp
+    constexpr int kRing = 2 * kStages * Chunk<kGroups>::kBytes; // bytes of a warp
     static_assert(kRing >= kRows * kDim * 4 && kRing % 16 == 0, "a warp's sums take the place of its chunks");
     extern __shared__ float4 shared[];
-    unsigned char* rings = reinterpret_cast<unsigned char*>(shared);                    // [warp]: kStages chunks, then sums [kRows][kDim]
+    unsigned char* rings = reinterpret_cast<unsigned char*>(shared);                    // [warp]: the stages, then sums [kRows][kDim]
     float2* warp_stats = reinterpret_cast<float2*>(rings + kWarps * kRing);             // [warp][kRows]
     int* warp_sums = reinterpret_cast<int*>(warp_stats + kWarps * kRows);
     int* first = warp_sums + kWarps;
@@ -305,140 +305,212 @@ __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 
         const int window_low = p.window > 0 && span.end > p.window ? static_cast<int>(span.end - p.window) : 0;
         const int32_t* table = p.table + b * p.table_stride;
 
-        // the query heads as the products' columns, in the order that the codes' pairs have
+        // the warp's stages: every fourth one of the run.  Each lane knows the page of a chunk of 16 of them, and of the next 16
+        using C = Chunk<kGroups>;
+        const int stages = ((k1 - k0 + 31) / 32 - w + kWarps - 1) / kWarps;
+        auto first_key = [&](int i) { return k0 + 32 * (w + kWarps * i); };
+        auto page_of = [&](int i) {
+            const int key = first_key(i + (lane >> 1)) + 16 * (lane & 1);
+            return key < k1 ? table[key >> p.page_shift] : -1;
+        };
+        int pages = page_of(0), pages_after = page_of(16);
+        unsigned there = 0;                                     // two bits for each stage that was asked for: which of its chunks exist
+        auto ask = [&](int i) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int64_t page = __shfl_sync(0xFFFFFFFFu, pages, 2 * i + j & 31);
+                const bool ok = page >= 0 && page < p.pages;
+                there = there << 1 | (ok ? 1u : 0u);
+                if (ok)
+                    copy_chunk<kGroups>(ring + (i % kStages * 2 + j) * C::kBytes, p.cache + (page * p.heads + h) * head_bytes, (first_key(i) + 16 * j) & (P - 1), P, lane);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if ((i & 15) == 15) pages = pages_after, pages_after = page_of(i + 17);
+        };
+        ask(0);
+
+        // The query heads as the products' columns, in the order that the codes' pairs have.  A code n is taken from its word by
+        // one logical operation, as the subnormal fp16 number n 2^-24 or, four bits up, n 2^-20: the heads are scaled by a power of two
+        // of their own (2^10 <= largest < 2^11, so that it costs no digits) and 2^4 more where the former meet them.  That a code
+        // stands for n - 8 is in what the sums of a scale's 32 dimensions start from.
         uint32_t q[kCols][2 * kGroups][2];
+        float from[kCols][kGroups][2], factor[kCols][2];
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
             const int row = 8 * n + g;
             const __half* at = p.q + b * p.ldq + static_cast<int64_t>(h * p.group + row0 + row) * kDim + 8 * c;
+            float x[kGroups][8], most = 0.0f;
 #pragma unroll
             for (int i = 0; i < kGroups; ++i) {
-                uint32_t x[4] = {0, 0, 0, 0};
-                if (row < rows) {
+                if (row >= rows) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[j] = __half_as_ushort(at[32 * i + 2 * j]) | static_cast<uint32_t>(__half_as_ushort(at[32 * i + 2 * j + 1])) << 16;
-                }
-                q[n][2 * i][0] = __byte_perm(x[0], x[2], 0x5410), q[n][2 * i][1] = __byte_perm(x[0], x[2], 0x7632);
-                q[n][2 * i + 1][0] = __byte_perm(x[1], x[3], 0x5410), q[n][2 * i + 1][1] = __byte_perm(x[1], x[3], 0x7632);
+                    for (int j = 0; j < 8; ++j) x[i][j] = 0.0f;
+                } else if (p.wide_q) dev::load_floats<__half, true>(at + 32 * i, x[i]);
+                else dev::load_floats<__half, false>(at + 32 * i, x[i]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[i][j]));
             }
+            most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+            const int exponent = max(100, min(150, __float_as_int(most) >> 23 & 255));       // of 0, Inf and NaN: a plain number
+            const float up = __int_as_float((127 + 10 + 127 - exponent) << 23), down = __int_as_float((127 + 20 - 10 - 127 + exponent) << 23);
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float f = j & 1 ? up : 16.0f * up;
+                    const __half2 v = __floats2half2_rn(x[i][j] * f, x[i][j + 4] * f);
+                    q[n][2 * i + (j >> 1)][j & 1] = *reinterpret_cast<const uint32_t*>(&v);
+                }
+                float eight[4];
+                dev::mma_f16_from(eight, 0.0f, 0.0f, 0.0f, 0.0f, 0x00080008u, 0x00080008u, 0x00800080u, 0x00800080u, q[n][2 * i][0], q[n][2 * i][1]);
+                dev::mma_f16(eight, 0x00080008u, 0x00080008u, 0x00800080u, 0x00800080u, q[n][2 * i + 1][0], q[n][2 * i + 1][1]);
+                from[n][i][0] = -eight[0], from[n][i][1] = -eight[1];
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) factor[n][i] = p.scale * __shfl_sync(0xFFFFFFFFu, down, 4 * (2 * c + i));
         }
         float acc[kCols][2 * kGroups][4] = {};
         float top[kCols][2], weight[kCols][2];
 #pragma unroll
         for (int n = 0; n < kCols; ++n) top[n][0] = top[n][1] = kLowest, weight[n][0] = weight[n][1] = 0.0f;
 
-        // the warp's chunks: every fourth one of the run.  Each lane knows the page of one of 32 of them, and of one of the next 32
-        const int chunks = ((k1 - k0 + 15) / 16 - w + kWarps - 1) / kWarps;
-        auto page_of = [&](int i) { return i < chunks ? table[(k0 + 16 * (w + kWarps * i)) >> p.page_shift] : -1; };
-        int pages = page_of(lane), pages_after = page_of(32 + lane);
-        unsigned there = 0;                                     // bit j: the chunk that was asked for j chunks ago exists
-        auto ask = [&](int i) {
-            const int64_t page = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
-            const bool ok = page >= 0 && page < p.pages;
-            there = there << 1 | (ok ? 1u : 0u);
-            if (ok)
-                copy_chunk<kGroups>(ring + i % kStages * Chunk<kGroups>::kBytes, p.cache + (page * p.heads + h) * head_bytes,
-                                    (k0 + 16 * (w + kWarps * i)) & (P - 1), P, lane);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            if ((i & 31) == 31) pages = pages_after, pages_after = page_of(i + 33 + lane);
-        };
-        __syncwarp();
-        for (int i = 0; i < kStages - 1; ++i) ask(i);
-        for (int i = 0; i < chunks; ++i) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-            __syncwarp();                                       // all lanes' copies are there, and all have read the chunk before
-            ask(i + kStages - 1);
-            if (!(there >> (kStages - 1) & 1)) continue;        // a page that does not exist
-            const int key = k0 + 16 * (w + kWarps * i);
-            Keys<kGroups> x;
-            load_keys<kGroups>(x, rings + w * kRing + i % kStages * Chunk<kGroups>::kBytes, g, c);
-            // keys that do not count: no score, and a scale of 0 for whatever the page holds there
-            const bool whole = key >= window_low && key + 16 <= k1;
-            if (!whole) {
+        for (int i = 0; i < stages; ++i) {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();                                       // all lanes' copies are there, and all have read the stage before
+            const unsigned have = there;
+            ask(i + 1);
+            if ((have & 3) == 0) continue;                      // pages that do not exist
+            const int key = first_key(i);
+            const unsigned char* stage = rings + w * kRing + i % kStages * 2 * C::kBytes;
+            const bool whole = (have & 3) == 3 && key >= window_low && key + 32 <= k1;
+            auto counts = [&](int at, int j) { return at >= window_low && at < k1 && (have >> (1 - j) & 1); };
+
+            float score[kCols][2][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int at = key + 2 * c + (i & 1) + 8 * (i >> 1);
-                    if (at < window_low || at >= k1) {
+            for (int j = 0; j < 2; ++j) {
+                const unsigned char* chunk = stage + j * C::kBytes;
+                uint32_t k[2][kGroups], ks[2][kGroups / 2];     // keys g and g + 8
 #pragma unroll
-                        for (int j = 0; j < (kGroups + 3) / 4; ++j) x.vs[i][j] = 0;
-                    }
-                }
-            }
-            float score[kCols][4] = {};
-#pragma unroll
-            for (int i = 0; i < kGroups; ++i) {
-                uint32_t lo[4], hi[4];
-                pairs_of(x.k[0][i], lo);
-                pairs_of(x.k[1][i], hi);
-                const float s0 = __half2float(__ushort_as_half(static_cast<unsigned short>(x.ks[0][i / 2] >> (16 * (i & 1)))));
-                const float s1 = __half2float(__ushort_as_half(static_cast<unsigned short>(x.ks[1][i / 2] >> (16 * (i & 1)))));
-#pragma unroll
-                for (int n = 0; n < kCols; ++n) {
-                    float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    dev::mma_f16(d, lo[0], hi[0], lo[1], hi[1], q[n][2 * i][0], q[n][2 * i][1]);
-                    dev::mma_f16(d, lo[2], hi[2], lo[3], hi[3], q[n][2 * i + 1][0], q[n][2 * i + 1][1]);
-                    score[n][0] += d[0] * s0, score[n][1] += d[1] * s0;
-                    score[n][2] += d[2] * s1, score[n][3] += d[3] * s1;
-                }
-            }
-            uint32_t weights[kCols][2];
-#pragma unroll
-            for (int n = 0; n < kCols; ++n) {
-                bool higher = false;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float s = score[n][i] * p.scale;
-                    if (p.cap > 0.0f) {                         // cap * tanh(s / cap) as 1 - 2 / (e^2x + 1), which keeps its limits
-                        const float e = exp2_of(s * p.cap_inv);
-                        s = p.cap * (1.0f - __fdividef(2.0f, e + 1.0f));
-                    }
-                    if (!whole) {
-                        const int at = key + g + 8 * (i >> 1);
-                        if (at < window_low || at >= k1) s = -INFINITY;
-                    }
-                    score[n][i] = s;
-                    higher |= s > top[n][i & 1] + kSlack;
-                }
-                if (__any_sync(0xFFFFFFFFu, higher)) {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float m = fmaxf(top[n][i], fmaxf(score[n][i], score[n][2 + i]));
-#pragma unroll
-                        for (int d = 4; d < 32; d *= 2) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-                        const float f = exp2_of(top[n][i] - m);
-                        top[n][i] = m;
-                        weight[n][i] *= f;
-#pragma unroll
-                        for (int j = 0; j < 2 * kGroups; ++j) acc[n][j][i] *= f, acc[n][j][2 + i] *= f;
-                    }
+                for (int m = 0; m < 2; ++m) {
+                    load_words<kGroups>(chunk + (g + 8 * m) * C::kRow + c * 4 * kGroups, k[m]);
+                    load_words<kGroups / 2>(chunk + C::kKeyScales + (g + 8 * m) * 2 * kGroups, ks[m]);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    score[n][i] = exp2_of(score[n][i] - top[n][i & 1]);
-                    weight[n][i & 1] += score[n][i];
-                }
+                for (int n = 0; n < kCols; ++n) score[n][j][0] = score[n][j][1] = score[n][j][2] = score[n][j][3] = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const __half2 pair = __floats2half2_rn(score[n][2 * i], score[n][2 * i + 1]);
-                    weights[n][i] = transpose8x8(*reinterpret_cast<const uint32_t*>(&pair));
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kGroups / 2; ++i) {
-                const uint32_t sel = (i & 1) ? 0x7632 : 0x5410;
-                const uint32_t sab = __byte_perm(x.vs[0][i / 2], x.vs[1][i / 2], sel), scd = __byte_perm(x.vs[2][i / 2], x.vs[3][i / 2], sel);
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint32_t take = half ? 0x7632 : 0x5410;
-                    uint32_t ab[4], cd[4];
-                    pairs_of(__byte_perm(x.v[0][i], x.v[1][i], take), ab);
-                    pairs_of(__byte_perm(x.v[2][i], x.v[3][i], take), cd);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) ab[j] = times(ab[j], sab), cd[j] = times(cd[j], scd);
+                for (int t = 0; t < kGroups; ++t) {
+                    const float2 s0 = __half22float2(*reinterpret_cast<const __half2*>(&ks[0][t / 2])), s1 = __half22float2(*reinterpret_cast<const __half2*>(&ks[1][t / 2]));
+                    const float f0 = t & 1 ? s0.y : s0.x, f1 = t & 1 ? s1.y : s1.x;
+                    const uint32_t a = k[0][t], b = k[1][t], a8 = a >> 8, b8 = b >> 8;
+                    constexpr uint32_t kLow = 0x000F000Fu, kHigh = 0x00F000F0u;
 #pragma unroll
                     for (int n = 0; n < kCols; ++n) {
-                        dev::mma_f16(acc[n][4 * i + 2 * half], ab[0], ab[1], cd[0], cd[1], weights[n][0], weights[n][1]);
-                        dev::mma_f16(acc[n][4 * i + 2 * half + 1], ab[2], ab[3], cd[2], cd[3], weights[n][0], weights[n][1]);
+                        float d[4];
+                        dev::mma_f16_from(d, from[n][t][0], from[n][t][1], from[n][t][0], from[n][t][1], a & kLow, b & kLow, a & kHigh, b & kHigh, q[n][2 * t][0], q[n][2 * t][1]);
+                        dev::mma_f16(d, a8 & kLow, b8 & kLow, a8 & kHigh, b8 & kHigh, q[n][2 * t + 1][0], q[n][2 * t + 1][1]);
+                        score[n][j][0] += d[0] * f0, score[n][j][1] += d[1] * f0;
+                        score[n][j][2] += d[2] * f1, score[n][j][3] += d[3] * f1;
+                    }
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < kCols; ++n) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) score[n][j][m] *= factor[n][m & 1];
+                }
+                if (p.cap > 0.0f) {                             // cap * tanh(s / cap) as 1 - 2 / (e^2x + 1), which keeps its limits
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) score[n][j][m] = p.cap * (1.0f - __fdividef(2.0f, exp2_of(score[n][j][m] * p.cap_inv) + 1.0f));
+                    }
+                }
+            }
+            if (!whole) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        if (counts(key + 16 * j + g + 8 * m, j)) continue;
+#pragma unroll
+                        for (int n = 0; n < kCols; ++n) score[n][j][2 * m] = score[n][j][2 * m + 1] = -INFINITY;
+                    }
+                }
+            }
+            uint32_t weights[kCols][2][2];
+#pragma unroll
+            for (int n = 0; n < kCols; ++n) {
+                float high[2];
+#pragma unroll
+                for (int m = 0; m < 2; ++m) high[m] = fmaxf(fmaxf(score[n][0][m], score[n][0][2 + m]), fmaxf(score[n][1][m], score[n][1][2 + m]));
+                const bool higher = high[0] > top[n][0] + kSlack || high[1] > top[n][1] + kSlack;
+                if (__any_sync(0xFFFFFFFFu, higher)) {
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        float most = fmaxf(top[n][m], high[m]);
+#pragma unroll
+                        for (int d = 4; d < 32; d *= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+                        const float f = exp2_of(top[n][m] - most);
+                        top[n][m] = most;
+                        weight[n][m] *= f;
+#pragma unroll
+                        for (int t = 0; t < 2 * kGroups; ++t) acc[n][t][m] *= f, acc[n][t][2 + m] *= f;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        score[n][j][m] = exp2_of(score[n][j][m] - top[n][m & 1]);
+                        weight[n][m & 1] += score[n][j][m];
+                    }
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        const __half2 pair = __floats2half2_rn(score[n][j][2 * m], score[n][j][2 * m + 1]);
+                        weights[n][j][m] = transpose8x8(*reinterpret_cast<const uint32_t*>(&pair));
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const unsigned char* chunk = stage + j * C::kBytes;
+                uint32_t v[4][kGroups / 2], vs[4][(kGroups + 3) / 4];       // keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    const int row = 2 * c + (m & 1) + 8 * (m >> 1);
+                    load_words<kGroups / 2>(chunk + C::kValues + row * C::kValueRow + g * 2 * kGroups, v[m]);
+                    const unsigned char* s = chunk + C::kValueScales + row * 2 * kGroups + (g & 1) * kGroups;
+                    if constexpr (kGroups == 2) vs[m][0] = *reinterpret_cast<const uint16_t*>(s);
+                    else load_words<kGroups / 4>(s, vs[m]);
+                }
+                if (!whole) {                                   // keys that do not count, whatever the page holds there
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        if (counts(key + 16 * j + 2 * c + (m & 1) + 8 * (m >> 1), j)) continue;
+#pragma unroll
+                        for (int t = 0; t < (kGroups + 3) / 4; ++t) vs[m][t] = 0;
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < kGroups / 2; ++t) {
+                    const uint32_t sel = t & 1 ? 0x7632 : 0x5410;
+                    const uint32_t sab = __byte_perm(vs[0][t / 2], vs[1][t / 2], sel), scd = __byte_perm(vs[2][t / 2], vs[3][t / 2], sel);
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t take = half ? 0x7632 : 0x5410;
+                        uint32_t ab[4], cd[4];
+                        pairs_of(__byte_perm(v[0][t], v[1][t], take), ab);
+                        pairs_of(__byte_perm(v[2][t], v[3][t], take), cd);
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) ab[m] = times(ab[m], sab), cd[m] = times(cd[m], scd);
+#pragma unroll
+                        for (int n = 0; n < kCols; ++n) {
+                            dev::mma_f16(acc[n][4 * t + 2 * half], ab[0], ab[1], cd[0], cd[1], weights[n][j][0], weights[n][j][1]);
+                            dev::mma_f16(acc[n][4 * t + 2 * half + 1], ab[2], ab[3], cd[2], cd[3], weights[n][j][0], weights[n][j][1]);
+                        }
                     }
                 }
             }
@@ -468,26 +540,24 @@ __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 
         __syncthreads();
         const bool all = count == span.units;
         const int slot = 2 * blockIdx.x + (u == begin ? 0 : 1);
-        for (int e = threadIdx.x; e < rows * kDim; e += kThreads) {
-            const int row = e / kDim, d = e % kDim;
-            float m = kLowest, sum = 0.0f, wt = 0.0f;
+        for (int e = threadIdx.x; e < rows * kDim / 4; e += kThreads) {       // four neighbours to a thread
+            const int row = e / (kDim / 4), d = e % (kDim / 4) * 4;
+            float m = kLowest, wt = 0.0f;
+            float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
             for (int i = 0; i < kWarps; ++i) m = fmaxf(m, warp_stats[i * kRows + row].x);
 #pragma unroll
             for (int i = 0; i < kWarps; ++i) {
                 const float2 st = warp_stats[i * kRows + row];
                 const float f = exp2_of(st.x - m);
+                const float4 v = *reinterpret_cast<const float4*>(rings + i * kRing + (row * kDim + d) * 4);
                 wt += st.y * f;
-                sum += reinterpret_cast<const float*>(rings + i * kRing)[row * kDim + d] * f;
+                sum.x += v.x * f, sum.y += v.y * f, sum.z += v.z * f, sum.w += v.w * f;
             }
             if (all) {
-                const int64_t at = static_cast<int64_t>(h * p.group + row0 + row) * kDim + d;
-                const __half y = __float2half_rn(wt > 0.0f || wt != wt ? sum / wt : 0.0f);
-                p.y[b * p.ldy + at] = y;
-                const unsigned keep = __ballot_sync(0xFFFFFFFFu, !(fabsf(__half2float(y)) <= p.thr));
-                if (p.mask != nullptr && lane == 0) p.mask[b * p.mask_stride + at / 32] = keep;
+                store_result(p, b, static_cast<int64_t>(h * p.group + row0 + row) * kDim + d, sum, wt);
             } else {
-                p.sums[(static_cast<int64_t>(slot) * kRows + row) * kDim + d] = sum;
+                *reinterpret_cast<float4*>(p.sums + (static_cast<int64_t>(slot) * kRows + row) * kDim + d) = sum;
                 if (d == 0) p.stats[slot * kRows + row] = make_float2(m, wt);
             }
         }
@@ -505,7 +575,7 @@ constexpr int kJoinThreads = 256;
 template <int kGroups, int kCols>
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParams p) {
     constexpr int kDim = 32 * kGroups, kRows = 8 * kCols, kLanes = kDim / 4, kParts = kJoinThreads / kLanes;
-    __shared__ float part[kParts][kDim];
+    __shared__ __align__(16) float part[kParts][kDim];
     __shared__ float2 stat[kParts];
     dev::programmatic_start();
     const int4 open = p.open[blockIdx.x];
@@ -528,26 +598,24 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParam
     *reinterpret_cast<float4*>(&part[mine][4 * at]) = sum;
     if (at == 0) stat[mine] = make_float2(m, wt);
     __syncthreads();
-    const int d = threadIdx.x;
+    const int d = 4 * threadIdx.x;
     if (d >= kDim) return;
-    float top = kLowest, weight = 0.0f, total = 0.0f;
+    m = kLowest, wt = 0.0f;
+    sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-    for (int i = 0; i < kParts; ++i) top = fmaxf(top, stat[i].x);
+    for (int i = 0; i < kParts; ++i) m = fmaxf(m, stat[i].x);
 #pragma unroll
     for (int i = 0; i < kParts; ++i) {
-        const float f = exp2_of(stat[i].x - top);
-        weight += stat[i].y * f;
-        total += part[i][d] * f;
+        const float f = exp2_of(stat[i].x - m);
+        const float4 v = *reinterpret_cast<const float4*>(&part[i][d]);
+        wt += stat[i].y * f;
+        sum.x += v.x * f, sum.y += v.y * f, sum.z += v.z * f, sum.w += v.w * f;
     }
-    const int64_t column = static_cast<int64_t>(h * p.group + head) * kDim + d;
-    const __half y = __float2half_rn(weight > 0.0f || weight != weight ? total / weight : 0.0f);
-    p.y[b * p.ldy + column] = y;
-    const unsigned keep = __ballot_sync(0xFFFFFFFFu, !(fabsf(__half2float(y)) <= p.thr));
-    if (p.mask != nullptr && (d & 31) == 0) p.mask[b * p.mask_stride + column / 32] = keep;
+    store_result(p, b, static_cast<int64_t>(h * p.group + head) * kDim + d, sum, wt);
 }
 
 template <int kGroups, int kCols>
-size_t attn_shared_bytes(int B) { return kWarps * (kStages * Chunk<kGroups>::kBytes + 8 * kCols * sizeof(float2) + sizeof(int)) + (B + 1) * sizeof(int); }
+size_t attn_shared_bytes(int B) { return kWarps * (2 * kStages * Chunk<kGroups>::kBytes + 8 * kCols * sizeof(float2) + sizeof(int)) + (B + 1) * sizeof(int); }
 
 template <int kGroups, int kCols>
 spdp_status launch_form(AttnParams p, int device, int sms, cudaStream_t s) {
@@ -634,6 +702,7 @@ spdp_status launch_attn_kv4(const Kv4AttnCall& call, cudaStream_t s) {
     p.cap = call.cap * kLog2e;
     p.cap_inv = call.cap > 0.0f ? 2.0f / call.cap : 0.0f;       // e^(2 s / cap) = 2^(s log2(e) * 2 / cap)
     p.window = call.window, p.thr = call.thr;
+    p.wide_q = rows_aligned16(p.q, p.ldq, 2), p.wide_y = rows_aligned16(p.y, p.ldy, 2);
     switch (call.head_dim) {
         case 64: return launch_groups<2>(p, device, sms, s);
         case 128: return launch_groups<4>(p, device, sms, s);

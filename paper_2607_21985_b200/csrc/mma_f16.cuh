@@ -18,9 +18,17 @@ __device__ __forceinline__ void programmatic_start() {
 // a1/a3), b's column g, and d's rows g (d0, d1) and g + 8 (d2, d3), columns 2 c and 2 c + 1.  Which k a register's pair stands for
 // is the caller's choice, as long as a and b agree: the loads below give a lane whole 16-byte runs of a row.
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The same with sums that start from `from`.
+__device__ __forceinline__ void mma_f16_from(float (&d)[4], float from0, float from1, float from2, float from3, uint32_t a0, uint32_t a1, uint32_t a2,
+                                             uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(from0), "f"(from1), "f"(from2), "f"(from3));
 }
 
 // Elements k .. k + 7 of a row, those from `limit` on as zeros; `wide`: every row starts on a 16-byte boundary and k is a
