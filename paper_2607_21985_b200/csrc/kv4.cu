@@ -109,8 +109,10 @@ struct AttnParams {
     uint32_t* mask;
     float* sums;                        // [2 CTAs][rows][dim]
     float2* stats;                      // [2 CTAs][rows]: maximum, weight
-    int4* open;                         // [CTAs]: request, triple, last CTA and slot of a triple that begins there and ends elsewhere; -1: none
-    int64_t ldq, ldy, table_stride, table_pages, mask_stride, pages;
+    int4* open;                         // triples that several CTAs have: request (-1: none), triple, slot of the first sum, last CTA
+    bool by_triple;                     // a place of `open` for each triple; else for each CTA, of the triple that begins there
+    int64_t ldq, ldy, table_stride, table_pages, mask_stride;
+    unsigned pages;
     int B, heads, group, row_blocks, page_shift;
     float scale, cap, cap_inv;          // scores in powers of two
     bool wide_q, wide_y;
@@ -131,14 +133,19 @@ __device__ __forceinline__ Span span_of(const AttnParams& p, int b) {
     return s;
 }
 
-// The first unit of CTA i's run, of `ctas` that share `total` units.
+// A triple costs what its units do and, for its query heads and its sums, as much as kStart more: it is that long in the line
+// that is cut into runs.  (With 0 a CTA that met many short requests took half as long again as the others.)
+constexpr int kStart = 6;
+__device__ __forceinline__ int triple_length(int units) { return units > 0 ? units + kStart : 0; }
+
+// Where the run of CTA i begins, of `ctas` that share a line of `total`.
 __device__ __forceinline__ int run_start(int total, int ctas, int i) { return static_cast<int>(static_cast<int64_t>(total) * i / ctas); }
 
-// The first unit of every request, into shared memory (all threads; ends with a barrier).
+// Where in the line every request begins, into shared memory (all threads; ends with a barrier).
 __device__ void scan_units(const AttnParams& p, int* first, int* warp_sums) {
     const int each = (p.B + kThreads - 1) / kThreads, b0 = threadIdx.x * each, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     int mine = 0;
-    for (int b = b0; b < b0 + each && b < p.B; ++b) mine += span_of(p, b).units * p.heads * p.row_blocks;
+    for (int b = b0; b < b0 + each && b < p.B; ++b) mine += triple_length(span_of(p, b).units) * p.heads * p.row_blocks;
     int up_to = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -151,7 +158,7 @@ __device__ void scan_units(const AttnParams& p, int* first, int* warp_sums) {
     for (int i = 0; i < w; ++i) at += warp_sums[i];
     for (int b = b0; b < b0 + each && b < p.B; ++b) {
         first[b] = at;
-        at += span_of(p, b).units * p.heads * p.row_blocks;
+        at += triple_length(span_of(p, b).units) * p.heads * p.row_blocks;
     }
     if (b0 < p.B && b0 + each >= p.B) first[p.B] = at;
     __syncthreads();
@@ -222,19 +229,17 @@ __device__ __forceinline__ void copy16(uint32_t to, const unsigned char* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 
-// The keys at .. at + 15 of a page's head into a chunk.
+// 16 keys into a chunk; `keys`: the lane's 16 bytes of the first 512 of their codes, `scales`: the start of their scales.
 template <int kGroups>
-__device__ __forceinline__ void copy_chunk(uint32_t to, const unsigned char* head, int at, int P, int lane) {
+__device__ __forceinline__ void copy_chunk(uint32_t to, const unsigned char* keys, const unsigned char* scales, int P, int lane) {
     using C = Chunk<kGroups>;
-    const unsigned char* keys = head + at * C::kRow;
     const unsigned char* values = keys + P * C::kRow;
 #pragma unroll
     for (int i = 0; i < (C::kRow + 31) / 32; ++i) {
         const int piece = 32 * i + lane, row = piece / kGroups, part = piece % kGroups;
-        copy16(to + 16 * piece, keys + 16 * piece);
-        copy16(to + C::kValues + row * C::kValueRow + 16 * part, values + 16 * piece);
+        copy16(to + 16 * piece, keys + 512 * i);
+        copy16(to + C::kValues + row * C::kValueRow + 16 * part, values + 512 * i);
     }
-    const unsigned char* scales = head + 2 * P * C::kRow + at * 2 * kGroups;
     if (lane < 4 * kGroups) {           // 2 kGroups pieces of the keys' scales, as many of the values'
         const int piece = lane % (2 * kGroups);
         copy16(to + C::kKeyScales + 16 * lane, scales + 16 * piece + (lane < 2 * kGroups ? 0 : P * 2 * kGroups));
@@ -280,26 +285,32 @@ __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 
         for (int i = threadIdx.x; i < columns; i += kThreads) p.y[b * p.ldy + i] = __ushort_as_half(0);
         if (p.mask != nullptr)
             for (int i = threadIdx.x; i < columns / 32; i += kThreads) p.mask[b * p.mask_stride + i] = 0.0f <= p.thr ? 0u : 0xFFFFFFFFu;
+        if (p.by_triple)
+            for (int i = threadIdx.x; i < p.heads * p.row_blocks; i += kThreads) p.open[b * p.heads * p.row_blocks + i].x = -1;
     }
-    if (threadIdx.x == 0) p.open[blockIdx.x].x = -1;
+    if (!p.by_triple && threadIdx.x == 0) p.open[blockIdx.x].x = -1;
     const int total = first[p.B], ctas = min(static_cast<int>(gridDim.x), total);       // so that no CTA between two others has nothing
     if (static_cast<int>(blockIdx.x) >= ctas) return;
     const int begin = run_start(total, ctas, blockIdx.x), stop = run_start(total, ctas, blockIdx.x + 1);
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
     const int P = 1 << p.page_shift;
     const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(rings)) + w * kRing;
-    const int64_t head_bytes = static_cast<int64_t>(P) * 36 * kGroups;
+    const unsigned head_bytes = P * 36 * kGroups, page_bytes = head_bytes * p.heads;
 
+    int pieces = 0;
     for (int u = begin; u < stop;) {
-        int b = 0;                                              // the last request whose first unit is not behind u: it has units
+        int b = 0;                                              // the last request that does not begin behind u: it has keys
         for (int lo = 0, hi = p.B - 1; lo <= hi;) {
             const int mid = (lo + hi) >> 1;
             if (first[mid] <= u) b = mid, lo = mid + 1;
             else hi = mid - 1;
         }
         const Span span = span_of(p, b);
-        const int triple = (u - first[b]) / span.units, off = (u - first[b]) % span.units;
-        const int count = min(span.units - off, stop - u);
+        const int length = triple_length(span.units), triple = (u - first[b]) / length, at = (u - first[b]) % length;
+        const int start = u - at;                               // of the triple
+        const int off = max(0, at - kStart), count = max(0, min(length, stop - start) - kStart) - off;
+        u = min(start + length, stop);
+        if (count <= 0) continue;                               // the run ends before the triple's first unit
         const int h = triple / p.row_blocks, row0 = triple % p.row_blocks * kRows, rows = min(kRows, p.group - row0);
         const int k0 = span.low + off * kUnit, k1 = min(span.end, k0 + count * kUnit);
         const int window_low = p.window > 0 && span.end > p.window ? static_cast<int>(span.end - p.window) : 0;
@@ -315,14 +326,18 @@ __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 
         };
         int pages = page_of(0), pages_after = page_of(16);
         unsigned there = 0;                                     // two bits for each stage that was asked for: which of its chunks exist
+        const unsigned char* cache = p.cache + h * static_cast<int64_t>(head_bytes);
         auto ask = [&](int i) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int64_t page = __shfl_sync(0xFFFFFFFFu, pages, 2 * i + j & 31);
-                const bool ok = page >= 0 && page < p.pages;
+                const unsigned page = __shfl_sync(0xFFFFFFFFu, pages, 2 * i + j & 31);
+                const bool ok = page < p.pages;                 // negative ones are large here
                 there = there << 1 | (ok ? 1u : 0u);
-                if (ok)
-                    copy_chunk<kGroups>(ring + (i % kStages * 2 + j) * C::kBytes, p.cache + (page * p.heads + h) * head_bytes, (first_key(i) + 16 * j) & (P - 1), P, lane);
+                if (ok) {
+                    const unsigned char* head = cache + static_cast<uint64_t>(page) * page_bytes;
+                    const int at = (first_key(i) + 16 * j) & (P - 1);
+                    copy_chunk<kGroups>(ring + (i % kStages * 2 + j) * C::kBytes, head + at * C::kRow + 16 * lane, head + 2 * P * C::kRow + at * 2 * kGroups, P, lane);
+                }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
             if ((i & 15) == 15) pages = pages_after, pages_after = page_of(i + 17);
@@ -332,9 +347,11 @@ __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 
         // The query heads as the products' columns, in the order that the codes' pairs have.  A code n is taken from its word by
         // one logical operation, as the subnormal fp16 number n 2^-24 or, four bits up, n 2^-20: the heads are scaled by a power of two
         // of their own (2^10 <= largest < 2^11, so that it costs no digits) and 2^4 more where the former meet them.  That a code
-        // stands for n - 8 is in what the sums of a scale's 32 dimensions start from.
+        // stands for n - 8 takes a product of its own, of the keys' scales and -8 times the sums of the heads' 32 dimensions: its
+        // columns k hold the scales twice, against the upper and the lower 11 bits of these sums.
         uint32_t q[kCols][2 * kGroups][2];
-        float from[kCols][kGroups][2], factor[kCols][2];
+        uint32_t minus[kCols][2] = {};
+        float factor[kCols][2];
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
             const int row = 8 * n + g;
@@ -362,10 +379,27 @@ __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 
                     const __half2 v = __floats2half2_rn(x[i][j] * f, x[i][j + 4] * f);
                     q[n][2 * i + (j >> 1)][j & 1] = *reinterpret_cast<const uint32_t*>(&v);
                 }
-                float eight[4];
-                dev::mma_f16_from(eight, 0.0f, 0.0f, 0.0f, 0.0f, 0x00080008u, 0x00080008u, 0x00800080u, 0x00800080u, q[n][2 * i][0], q[n][2 * i][1]);
-                dev::mma_f16(eight, 0x00080008u, 0x00080008u, 0x00800080u, 0x00800080u, q[n][2 * i + 1][0], q[n][2 * i + 1][1]);
-                from[n][i][0] = -eight[0], from[n][i][1] = -eight[1];
+            }
+#pragma unroll
+            for (int i = 0; i < kGroups; i += 2) {              // two scales to a register: the word i / 2 of the keys' scales
+                float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[m] += x[i + m][j];
+                    sum[m] += __shfl_xor_sync(0xFFFFFFFFu, sum[m], 1);
+                    sum[m] += __shfl_xor_sync(0xFFFFFFFFu, sum[m], 2);
+                    sum[m] *= -8.0f * up * 0x1p-20f;
+                }
+                const __half2 high = __floats2half2_rn(sum[0], sum[1]);
+                const float2 h2 = __half22float2(high);
+                const __half2 low = __floats2half2_rn(sum[0] - h2.x, sum[1] - h2.y);
+                if (c == i / 2) minus[n][0] = *reinterpret_cast<const uint32_t*>(&high);
+                if (kGroups == 8) {
+                    if (c == i / 2) minus[n][1] = *reinterpret_cast<const uint32_t*>(&low);
+                } else if (c == i / 2 + kGroups / 2) {
+                    minus[n][0] = *reinterpret_cast<const uint32_t*>(&low);
+                }
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) factor[n][i] = p.scale * __shfl_sync(0xFFFFFFFFu, down, 4 * (2 * c + i));
@@ -396,8 +430,12 @@ __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 
                     load_words<kGroups>(chunk + (g + 8 * m) * C::kRow + c * 4 * kGroups, k[m]);
                     load_words<kGroups / 2>(chunk + C::kKeyScales + (g + 8 * m) * 2 * kGroups, ks[m]);
                 }
+                uint32_t both[2];                               // the lane's part of the scales' product
 #pragma unroll
-                for (int n = 0; n < kCols; ++n) score[n][j][0] = score[n][j][1] = score[n][j][2] = score[n][j][3] = 0.0f;
+                for (int m = 0; m < 2; ++m) both[m] = *reinterpret_cast<const uint32_t*>(chunk + C::kKeyScales + (g + 8 * m) * 2 * kGroups + c % (kGroups / 2) * 4);
+#pragma unroll
+                for (int n = 0; n < kCols; ++n)
+                    dev::mma_f16_from(score[n][j], 0.0f, 0.0f, 0.0f, 0.0f, both[0], both[1], kGroups == 8 ? both[0] : 0u, kGroups == 8 ? both[1] : 0u, minus[n][0], minus[n][1]);
 #pragma unroll
                 for (int t = 0; t < kGroups; ++t) {
                     const float2 s0 = __half22float2(*reinterpret_cast<const __half2*>(&ks[0][t / 2])), s1 = __half22float2(*reinterpret_cast<const __half2*>(&ks[1][t / 2]));
@@ -407,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 
 #pragma unroll
                     for (int n = 0; n < kCols; ++n) {
                         float d[4];
-                        dev::mma_f16_from(d, from[n][t][0], from[n][t][1], from[n][t][0], from[n][t][1], a & kLow, b & kLow, a & kHigh, b & kHigh, q[n][2 * t][0], q[n][2 * t][1]);
+                        dev::mma_f16_from(d, 0.0f, 0.0f, 0.0f, 0.0f, a & kLow, b & kLow, a & kHigh, b & kHigh, q[n][2 * t][0], q[n][2 * t][1]);
                         dev::mma_f16(d, a8 & kLow, b8 & kLow, a8 & kHigh, b8 & kHigh, q[n][2 * t + 1][0], q[n][2 * t + 1][1]);
                         score[n][j][0] += d[0] * f0, score[n][j][1] += d[1] * f0;
                         score[n][j][2] += d[2] * f1, score[n][j][3] += d[3] * f1;
@@ -539,7 +577,8 @@ __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 
         }
         __syncthreads();
         const bool all = count == span.units;
-        const int slot = 2 * blockIdx.x + (u == begin ? 0 : 1);
+        const int slot = 2 * blockIdx.x + (pieces > 0 ? 1 : 0); // what is not whole is the first piece of a run or the last
+        ++pieces;
         for (int e = threadIdx.x; e < rows * kDim / 4; e += kThreads) {       // four neighbours to a thread
             const int row = e / (kDim / 4), d = e % (kDim / 4) * 4;
             float m = kLowest, wt = 0.0f;
@@ -561,15 +600,15 @@ __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 
                 if (d == 0) p.stats[slot * kRows + row] = make_float2(m, wt);
             }
         }
-        if (threadIdx.x == 0 && off == 0 && !all)               // the CTAs with the rest follow this one
-            p.open[blockIdx.x] = make_int4(b, triple, static_cast<int>(((static_cast<int64_t>(u) + span.units) * ctas - 1) / total), slot);
+        if (threadIdx.x == 0 && off == 0 && (p.by_triple || !all))        // the CTAs with the rest follow this one
+            p.open[p.by_triple ? b * p.heads * p.row_blocks + triple : blockIdx.x] =
+                make_int4(all ? -1 : b, triple, slot, static_cast<int>(((static_cast<int64_t>(start) + length) * ctas - 1) / total));
         __syncthreads();
-        u += count;
     }
 }
 
-// Joins the partial sums of the triple that begins in a CTA and ends in another one, in the order of its keys: a row of it to a
-// CTA, whose groups of lanes take every kParts-th sum.
+// Joins the partial sums of a triple that several CTAs have, in the order of its keys: a row of it to a CTA, whose groups of lanes
+// take every kParts-th sum.
 constexpr int kJoinThreads = 256;
 
 template <int kGroups, int kCols>
@@ -582,12 +621,12 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParam
     if (open.x < 0) return;
     const int b = open.x, h = open.y / p.row_blocks, row = blockIdx.y, head = open.y % p.row_blocks * kRows + row;
     if (head >= p.group) return;
-    const int at = threadIdx.x % kLanes, mine = threadIdx.x / kLanes, count = open.z - static_cast<int>(blockIdx.x) + 1;
+    const int at = threadIdx.x % kLanes, mine = threadIdx.x / kLanes, count = open.w - open.z / 2 + 1;
     float m = kLowest, wt = 0.0f;
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
     for (int i = mine; i < count; i += kParts) {
-        const int64_t from = (i == 0 ? open.w : 2 * (static_cast<int64_t>(blockIdx.x) + i)) * kRows + row;
+        const int64_t from = (i == 0 ? open.z : 2 * (open.z / 2 + static_cast<int64_t>(i))) * kRows + row;
         const float2 st = p.stats[from];
         const float4 v = *reinterpret_cast<const float4*>(p.sums + from * kDim + 4 * at);
         const float top = fmaxf(m, st.x), f = exp2_of(m - top), fs = exp2_of(st.x - top);
@@ -635,7 +674,7 @@ spdp_status launch_form(AttnParams p, int device, int sms, cudaStream_t s) {
     }
     const int triples = p.heads * p.row_blocks;
     // no more CTAs than there can be units
-    const int64_t most = p.B * ((p.table_pages << p.page_shift) + kUnit - 1) / kUnit * triples;
+    const int64_t most = p.B * (((p.table_pages << p.page_shift) + kUnit - 1) / kUnit) * triples;
     const int ctas = static_cast<int>(most < static_cast<int64_t>(per_sm) * sms ? most : per_sm * sms);
     const size_t sums = 2ull * ctas * kRows * kDim * sizeof(float), stats = 2ull * ctas * kRows * sizeof(float2);
     void* scratch = nullptr;
@@ -643,9 +682,11 @@ spdp_status launch_form(AttnParams p, int device, int sms, cudaStream_t s) {
     if (st != SPDP_OK) return st;
     p.sums = static_cast<float*>(scratch);
     p.stats = reinterpret_cast<float2*>(static_cast<char*>(scratch) + sums);
+    p.by_triple = static_cast<int64_t>(p.B) * triples <= ctas;
+    const int places = p.by_triple ? p.B * triples : ctas;
     p.open = reinterpret_cast<int4*>(static_cast<char*>(scratch) + sums + stats);
     cudaError_t e = launch_programmatic(attn_kernel<kGroups, kCols>, dim3(static_cast<unsigned>(ctas)), kThreads, attn_shared_bytes<kGroups, kCols>(p.B), s, p);
-    if (e == cudaSuccess) e = launch_programmatic(attn_join_kernel<kGroups, kCols>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(p.group < kRows ? p.group : kRows)), kJoinThreads, 0, s, p);
+    if (e == cudaSuccess) e = launch_programmatic(attn_join_kernel<kGroups, kCols>, dim3(static_cast<unsigned>(places), static_cast<unsigned>(p.group < kRows ? p.group : kRows)), kJoinThreads, 0, s, p);
     const cudaError_t freed = cudaFreeAsync(scratch, s);
     SPDP_CUDA_TRY(e);
     SPDP_CUDA_TRY(freed);
@@ -695,7 +736,7 @@ spdp_status launch_attn_kv4(const Kv4AttnCall& call, cudaStream_t s) {
     if (st != SPDP_OK) return st;
     AttnParams p = {};
     p.q = call.q, p.cache = call.cache, p.table = call.table, p.length = call.length, p.y = call.y, p.mask = call.mask;
-    p.ldq = call.ldq, p.ldy = call.ldy, p.table_stride = call.table_stride, p.table_pages = call.table_pages, p.mask_stride = call.mask_stride, p.pages = call.pages;
+    p.ldq = call.ldq, p.ldy = call.ldy, p.table_stride = call.table_stride, p.table_pages = call.table_pages, p.mask_stride = call.mask_stride, p.pages = static_cast<unsigned>(call.pages);
     p.B = static_cast<int>(call.B), p.heads = call.kv_heads, p.group = call.q_heads / call.kv_heads, p.page_shift = log2_of(call.page_tokens);
     constexpr float kLog2e = 1.4426950408889634f;
     p.scale = call.scale * kLog2e;

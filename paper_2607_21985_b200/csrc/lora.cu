@@ -2,17 +2,18 @@
 // token n.  Folding B A into a statically pruned W would fill its zeros, so an adapter of a packed layer has to stay beside it.
 //
 // The work is the bytes: x, base and y once, the weights of the adapters in use; the products are a few times the rank per byte.
-// One launch does both products.  A cluster of 8 CTAs takes 32 consecutive tokens and one adapter among them: each CTA
-// multiplies an eighth of K (its warps split that again), the partial sums meet through distributed shared memory in a fixed
-// order, and each CTA then multiplies the rank-long vectors into its share of the output rows.  So the vectors between the
-// two products never leave the chip, there is no workspace, and x, base and y cross memory once whatever N is.  Where there are
-// few tokens several clusters share a tile: one to an adapter, or, past that, each with a part of the output rows, the
-// (small) first product done by each of them.
-//
 // Both products run on mma.sync with tokens as the 8 columns and weight rows as the 16 rows, fragments loaded straight from
-// memory: a lane holds 8 consecutive elements of a row, the same on both sides.  The vectors between the products are kept
-// in fp16 for the second one, scaled per token by a power of two (so that neither end of the range is lost): one rounding of
-// 2^-12 on a term that is added to a 16-bit result; for 32-bit results a second fp16 number holds what the first one lost.
+// memory: a lane holds 8 consecutive elements of a row, the same on both sides.
+//
+// First product: a cluster of 8 CTAs takes a tile of consecutive tokens and one adapter among them after another; each CTA
+// multiplies an eighth of K (its warps split that again), and the partial sums meet through distributed shared memory in a fixed
+// order.  The vectors between the products are kept in fp16 for the second one, scaled per token by a power of two (so that
+// neither end of the range is lost): one rounding of 2^-11 on a term that is added to a 16-bit result; for 32-bit results a
+// second fp16 number holds what the first one lost.  Second product: a warp takes 64 output rows and the tile's tokens, and asks
+// for base before it multiplies.
+//
+// Few tokens: one launch does both, the clusters keep the vectors and go on to the output rows.  Many: a second kernel with a
+// warp to each block of output, so that the loads of all of them are on their way at once (1024 tokens, 28672 x 8192, rank 16: LORA_TIMES).
 #include <cooperative_groups.h>
 
 #include <mutex>
@@ -25,13 +26,16 @@ namespace cg = cooperative_groups;
 namespace spdp {
 namespace {
 
-constexpr int kTok = 32;            // tokens of a tile: 4 column blocks of 8
-constexpr int kTokPad = 40;         // floats from one rank to the next in shared memory: the fragments' stores meet no bank twice
+constexpr int kMostCols = 4;        // column blocks of 8 tokens in a tile: 1 or 4
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kCluster = 8;
 constexpr int kOut = 64;            // output rows of a warp's block
 constexpr int kBlocksOfCluster = kCluster * kWarps;
+#ifndef SPDP_FUSED
+#define SPDP_FUSED 4
+#endif
+constexpr int kFusedTokens = SPDP_FUSED;     // up to here one launch does both products
 
 struct Params {
     const __half* X;
@@ -44,75 +48,210 @@ struct Params {
     void* Y;
     int64_t ldx, lda, stride_a, ldb, stride_b, ldbase, ldy;
     int N, K, M, count, rank;
-    int per_tile;                   // clusters of a tile
-    bool wide_x, wide_a, wide_b, wide_y;
+    int per_tile;                   // clusters (first or only kernel), CTAs (second) of a tile, among which its adapters are dealt out
+    int align_x, align_a, align_b;  // bytes that every row's address is a multiple of
+    bool wide_y;                    // base and Y: 16
+    // what the first kernel leaves for the second: [N][padded rank] fp16, for 32-bit results twice, and a factor to each token
+    __half* vectors;
+    float* factors;
 };
 
 __host__ __device__ inline int padded_rank(int rank) { return (rank + 31) & ~31; }
 
-template <int kRankTiles>
-struct Layout {                     // shared memory, in floats
+// Shared memory of the first product, in floats.  Rows of kTok + 8 floats: the fragments' stores meet no bank twice.
+template <int kRankTiles, int kCols>
+struct Layout {
+    static constexpr int kTok = 8 * kCols, kPad = kTok + 8;
     static __host__ __device__ int sums(int rank) {
         const int warps = kWarps * 16 * kRankTiles, all = padded_rank(rank);
-        return (warps > all ? warps : all) * kTokPad;
+        return (warps > all ? warps : all) * kPad;
     }
-    static __host__ __device__ int part(int rank) { return padded_rank(rank) * kTokPad; }
+    static __host__ __device__ int part(int rank) { return padded_rank(rank) * kPad; }
     static __host__ __device__ int row(int rank) { return padded_rank(rank) + 8; }       // halves of a token's vector
-    static __host__ __device__ size_t bytes(int rank, bool f32) {
-        return 4u * (sums(rank) + part(rank) + (kWarps + 1) * kTok) + 2u * kTok * row(rank) * (f32 ? 2 : 1);
+    static __host__ __device__ size_t bytes(int rank, bool two) {
+        return 4u * (sums(rank) + part(rank) + (kWarps + 1) * 32) + 2u * kTok * row(rank) * (two ? 2 : 1);
     }
 };
 
-template <typename T>
-__device__ __forceinline__ float as_float(T v) {
-    if constexpr (sizeof(T) == 2) return __half2float(v);
-    else return v;
+// The adapters of a tile's tokens, in the order of their first tokens.  Tokens without one (-1) take base as it is: in place
+// there is nothing to do for them.
+struct Tile {
+    int mine;                       // the lane's token's adapter
+    unsigned same, groups;          // the lanes that share it; the first lane of each adapter
+    __device__ __forceinline__ Tile(const Params& p, int64_t n0, int tokens) {
+        const int lane = threadIdx.x & 31;
+        const bool there = lane < tokens && n0 + lane < p.N;
+        mine = there ? p.adapter[n0 + lane] : -2;
+        if (there && (mine < 0 || mine >= p.count)) mine = -1;
+        same = __match_any_sync(0xFFFFFFFFu, mine);
+        groups = __ballot_sync(0xFFFFFFFFu, lane == __ffs(same) - 1 && (mine >= 0 || (mine == -1 && p.base != p.Y)));
+    }
+    __device__ __forceinline__ int count() const { return __popc(groups); }
+    __device__ __forceinline__ void pick(int d, int& adapter, unsigned& members) const {
+        const int lead = __fns(groups, 0, d + 1);
+        adapter = __shfl_sync(0xFFFFFFFFu, mine, lead);
+        members = __shfl_sync(0xFFFFFFFFu, same, lead);
+    }
+};
+
+__device__ __forceinline__ int rank_of(const Params& p, int a) {
+    const int rank = p.ranks != nullptr ? p.ranks[a] : p.rank;
+    return rank < 0 ? 0 : rank > p.rank ? p.rank : rank;
 }
 
-// o[8] to y, on top of base's eight values; `left` of them exist.
+// Eight values of a row of base, then of Y: in 16-byte accesses (kept as bits, so that they can be asked for early), or one by one.
 template <typename T>
-__device__ __forceinline__ void add_store(const T* base, T* y, const float (&o)[8], int left, bool wide) {
-    if (wide && left >= 8) {
+struct Eight {
+    uint4 bits[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* from) {
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) bits[i] = reinterpret_cast<const uint4*>(from)[i];
+    }
+    // base + f o
+    __device__ __forceinline__ void add_store(T* to, const float (&o)[8], float f) {
         if constexpr (sizeof(T) == 2) {
-            const uint4 b = *reinterpret_cast<const uint4*>(base);
-            const uint32_t in[4] = {b.x, b.y, b.z, b.w};
-            uint32_t out[4];
+            uint32_t w[4] = {bits[0].x, bits[0].y, bits[0].z, bits[0].w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&in[i]));
-                const __half2 r = __floats2half2_rn(f.x + o[2 * i], f.y + o[2 * i + 1]);
-                out[i] = *reinterpret_cast<const uint32_t*>(&r);
+                const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                const __half2 r = __floats2half2_rn(v.x + o[2 * i] * f, v.y + o[2 * i + 1] * f);
+                w[i] = *reinterpret_cast<const uint32_t*>(&r);
             }
-            *reinterpret_cast<uint4*>(y) = make_uint4(out[0], out[1], out[2], out[3]);
+            *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                float4 b = reinterpret_cast<const float4*>(base)[i];
-                b.x += o[4 * i], b.y += o[4 * i + 1], b.z += o[4 * i + 2], b.w += o[4 * i + 3];
-                reinterpret_cast<float4*>(y)[i] = b;
+                float4 v = *reinterpret_cast<const float4*>(&bits[i]);
+                v.x += o[4 * i] * f, v.y += o[4 * i + 1] * f, v.z += o[4 * i + 2] * f, v.w += o[4 * i + 3] * f;
+                reinterpret_cast<float4*>(to)[i] = v;
             }
         }
-        return;
     }
+};
+template <typename T>
+__device__ __forceinline__ void add_store_some(const T* base, T* y, const float (&o)[8], float f, int left) {
+    T in[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left) in[i] = base[i];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        if (i < left) {
-            const float v = as_float(base[i]) + o[i];
-            if constexpr (sizeof(T) == 2) y[i] = __float2half_rn(v);
-            else y[i] = v;
+        if (i >= left) continue;
+        if constexpr (sizeof(T) == 2) y[i] = __float2half_rn(__half2float(in[i]) + o[i] * f);
+        else y[i] = in[i] + o[i] * f;
+    }
+}
+
+// Base to Y as it is, for a warp's block of output rows from m0 on.
+template <typename T>
+__device__ __forceinline__ void copy_block(const Params& p, int64_t n0, unsigned members, int m0) {
+    constexpr int kPieces = kOut * sizeof(T) / 16;               // 16-byte pieces of a token's block
+    const int lane = threadIdx.x & 31;
+    const bool whole = p.wide_y && m0 + kOut <= p.M;
+    for (int t = whole ? lane / kPieces : 0; t < 32; t += whole ? 32 / kPieces : 1) {
+        if (!(members >> t & 1)) continue;
+        const T* from = static_cast<const T*>(p.base) + (n0 + t) * p.ldbase + m0;
+        T* to = static_cast<T*>(p.Y) + (n0 + t) * p.ldy + m0;
+        if (whole) {
+            reinterpret_cast<uint4*>(to)[lane % kPieces] = reinterpret_cast<const uint4*>(from)[lane % kPieces];
+        } else {
+            for (int i = lane; i < kOut && m0 + i < p.M; i += 32) to[i] = from[i];
         }
     }
 }
 
-template <int kRankTiles, typename T>
+// The second product for a warp's block of output rows from m_block on: B t, added to base.  `hi`, `lo`: the tile's vectors, `row`
+// halves apart; `factors`: what undoes their scaling.
+template <typename T, int kCols>
+__device__ __forceinline__ void expand_block(const Params& p, int64_t n0, unsigned members, int a, int rank, int m_block, const __half* hi, const __half* lo, int row,
+                                             const float* factors) {
+    constexpr bool kTwo = sizeof(T) == 4;
+    constexpr int kStep = kCols < 2 ? kCols : 2;                 // column blocks at a time
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const int m0 = m_block + 8 * g, left = p.M - m0;             // a lane's eight consecutive output rows
+    const bool wide = p.wide_y && left >= 8;
+    const T* base = static_cast<const T*>(p.base) + n0 * p.ldbase + m0;
+    T* y = static_cast<T*>(p.Y) + n0 * p.ldy + m0;
+    const __half* B = p.B + a * p.stride_b;
+    // base is asked for ahead of the products: all of it where it is 16-bit, else of the tokens that are next
+    constexpr int kAhead = sizeof(T) == 2 ? kCols : kStep;
+    Eight<T> old[kAhead][2];
+    auto ask = [&](int t0) {
+#pragma unroll
+        for (int t = 0; t < kAhead; ++t) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int n = 8 * (t0 + t) + 2 * c + h;
+                if (wide && (members >> n & 1)) old[t][h].load(base + n * p.ldbase);
+            }
+        }
+    };
+    uint4 v[4][2];
+    auto weights = [&](int k0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i / 2][i % 2] = dev::load8(B + (m0 + i) * p.ldb, k0 + 8 * c, i < left ? rank : 0, p.align_b);
+    };
+    ask(0);
+    weights(0);
+#pragma unroll
+    for (int t0 = 0; t0 < kCols; t0 += kStep) {
+        if (t0 > 0 && t0 % kAhead == 0) ask(t0);
+        if (!(members >> (8 * t0) & 0xFFFFu)) continue;
+        float acc[kStep][4][4] = {};
+        for (int k0 = 0; k0 < rank; k0 += 32) {
+            if (rank > 32 && (k0 > 0 || t0 > 0)) weights(k0);
+#pragma unroll
+            for (int t = 0; t < kStep; ++t) {
+                if (!(members >> (8 * (t0 + t)) & 0xFFu)) continue;
+                const bool member = members >> (8 * (t0 + t) + g) & 1;     // other tokens' vectors may be another adapter's, or nobody's
+                const uint4 none = make_uint4(0, 0, 0, 0);
+                const uint4 x = member ? *reinterpret_cast<const uint4*>(hi + (8 * (t0 + t) + g) * row + k0 + 8 * c) : none;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    dev::mma_f16(acc[t][i], v[i][0].x, v[i][1].x, v[i][0].y, v[i][1].y, x.x, x.y);
+                    dev::mma_f16(acc[t][i], v[i][0].z, v[i][1].z, v[i][0].w, v[i][1].w, x.z, x.w);
+                }
+                if constexpr (kTwo) {
+                    const uint4 z = member ? *reinterpret_cast<const uint4*>(lo + (8 * (t0 + t) + g) * row + k0 + 8 * c) : none;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        dev::mma_f16(acc[t][i], v[i][0].x, v[i][1].x, v[i][0].y, v[i][1].y, z.x, z.y);
+                        dev::mma_f16(acc[t][i], v[i][0].z, v[i][1].z, v[i][0].w, v[i][1].w, z.z, z.w);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < kStep; ++t) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int n = 8 * (t0 + t) + 2 * c + h;
+                if (!(members >> n & 1) || left <= 0) continue;
+                const float down = factors[n];
+                float o[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[2 * i] = acc[t][i][h], o[2 * i + 1] = acc[t][i][2 + h];
+                if (wide) old[(t0 + t) % kAhead][h].add_store(y + n * p.ldy, o, down);
+                else add_store_some(base + n * p.ldbase, y + n * p.ldy, o, down, left);
+            }
+        }
+    }
+}
+
+// kSplit: this kernel ends with the vectors, in memory; else it does the second product too.
+template <int kRankTiles, int kCols, typename T, bool kSplit>
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) lora_kernel(const Params p) {
     constexpr bool kTwo = sizeof(T) == 4;                    // two fp16 numbers for a value of the vectors
-    using L = Layout<kRankTiles>;
+    // steps of 32 k whose loads are on their way at once; a step takes 4 kCols + 8 kRankTiles registers
+    constexpr int kBatch = kCols == 1 ? (kRankTiles == 4 ? 2 : 4) : kRankTiles == 1 ? 2 : 1;
+    using L = Layout<kRankTiles, kCols>;
+    constexpr int kTok = L::kTok, kPad = L::kPad;
     extern __shared__ float4 shared[];
-    float* sums = reinterpret_cast<float*>(shared);          // [warp][16 kRankTiles][kTokPad]; then the vectors [rank][kTokPad]
-    float* part = sums + L::sums(p.rank);                    // [rank][kTokPad], read by the whole cluster
-    float* largest = part + L::part(p.rank);                 // [warp][kTok], [kTok]
-    __half* hi = reinterpret_cast<__half*>(largest + (kWarps + 1) * kTok);   // [kTok][row]
+    float* sums = reinterpret_cast<float*>(shared);          // [warp][16 kRankTiles][kPad]; then the vectors [rank][kPad]
+    float* part = sums + L::sums(p.rank);                    // [rank][kPad], read by the whole cluster
+    float* largest = part + L::part(p.rank);                 // [warp][32], factors [32]
+    float* factors = largest + kWarps * 32;
+    __half* hi = reinterpret_cast<__half*>(factors + 32);    // [kTok][row]
     const int row = L::row(p.rank);
     __half* lo = hi + kTok * row;
 
@@ -121,190 +260,218 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
     const int cta = blockIdx.x % kCluster, z = blockIdx.x / kCluster % p.per_tile;
     const int64_t n0 = static_cast<int64_t>(blockIdx.x / kCluster / p.per_tile) * kTok;
-
-    // the tile's adapters, in the order of their first tokens; -1: tokens without one, which take base as it is
-    const bool there = n0 + lane < p.N;
-    int mine = there ? p.adapter[n0 + lane] : -2;
-    if (there && (mine < 0 || mine >= p.count)) mine = -1;
-    const unsigned same = __match_any_sync(0xFFFFFFFFu, mine);
-    const bool first = lane == __ffs(same) - 1 && (mine >= 0 || (mine == -1 && p.base != p.Y));
-    const unsigned groups = __ballot_sync(0xFFFFFFFFu, first);
-    const int G = __popc(groups);
+    const Tile tile(p, n0, kTok);
+    const int G = tile.count();
     if (G == 0) return;
     // more clusters than adapters: they share an adapter's output rows; else a cluster takes several adapters in turn
-    const int sharers = p.per_tile > G ? (p.per_tile - z % G + G - 1) / G : 1, share = p.per_tile > G ? z / G : 0;
-    const int step = p.per_tile > G ? G : p.per_tile;
+    const bool more = !kSplit && p.per_tile > G;
+    const int sharers = more ? (p.per_tile - z % G + G - 1) / G : 1, share = more ? z / G : 0;
     const int blocks = (p.M + kOut - 1) / kOut;
     if (share * kBlocksOfCluster >= blocks) return;
 
-    for (int d = z % step; d < G; d += p.per_tile) {
-        const int lead = __fns(groups, 0, d + 1);
-        const int a = __shfl_sync(0xFFFFFFFFu, mine, lead);
-        const unsigned members = __shfl_sync(0xFFFFFFFFu, same, lead);
+    for (int d = more ? z % G : z; d < G; d += p.per_tile) {
+        int a;
+        unsigned members;
+        tile.pick(d, a, members);
         const int block0 = (share * kCluster + cta) * kWarps + w;
         if (a < 0) {
-            constexpr int kPieces = kOut * sizeof(T) / 16;   // 16-byte pieces of a token's block
-            for (int b = block0; b < blocks; b += sharers * kBlocksOfCluster) {
-                const int m0 = b * kOut;
-                const bool whole = p.wide_y && m0 + kOut <= p.M;
-                for (int t = whole ? lane / kPieces : 0; t < kTok; t += whole ? 32 / kPieces : 1) {
-                    if (!(members >> t & 1)) continue;
-                    const T* from = static_cast<const T*>(p.base) + (n0 + t) * p.ldbase + m0;
-                    T* to = static_cast<T*>(p.Y) + (n0 + t) * p.ldy + m0;
-                    if (whole) {
-                        reinterpret_cast<uint4*>(to)[lane % kPieces] = reinterpret_cast<const uint4*>(from)[lane % kPieces];
-                    } else {
-                        for (int i = lane; i < kOut && m0 + i < p.M; i += 32) to[i] = from[i];
-                    }
-                }
-            }
+            if constexpr (!kSplit)
+                for (int b = block0; b < blocks; b += sharers * kBlocksOfCluster) copy_block<T>(p, n0, members, b * kOut);
             continue;
         }
-        int rank = p.ranks != nullptr ? p.ranks[a] : p.rank;
-        rank = rank < 0 ? 0 : rank > p.rank ? p.rank : rank;
-        const int prank = padded_rank(rank);
+        const int rank = rank_of(p, a), prank = padded_rank(rank);
 
         // A x over this CTA's eighth of K
         const __half* A = p.A + a * p.stride_a;
         const int steps = (p.K + 31) / 32;
         const int s0 = static_cast<int>(static_cast<int64_t>(steps) * cta / kCluster), s1 = static_cast<int>(static_cast<int64_t>(steps) * (cta + 1) / kCluster);
         for (int r0 = 0; r0 < rank; r0 += 16 * kRankTiles) {
-            float acc[kRankTiles][4][4] = {};
-            for (int s = s0 + w; s < s1; s += kWarps) {
-                const int k = s * 32 + 8 * c;
-                uint4 x[4], v[kRankTiles][2];
+            float acc[kRankTiles][kCols][4] = {};
+            for (int s = s0 + w; s < s1; s += kBatch * kWarps) {
+                uint4 x[kBatch][kCols], v[kBatch][kRankTiles][2];
 #pragma unroll
-                for (int i = 0; i < kRankTiles; ++i) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int r = r0 + 16 * i + 8 * h + g;
-                        v[i][h] = r < rank ? dev::load8(A + r * p.lda, k, p.K, p.wide_a) : make_uint4(0, 0, 0, 0);
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    x[t] = members >> (8 * t + g) & 1 ? dev::load8(p.X + (n0 + 8 * t + g) * p.ldx, k, p.K, p.wide_x) : make_uint4(0, 0, 0, 0);
-                }
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    if (!(members >> (8 * t) & 0xFFu)) continue;
+                for (int j = 0; j < kBatch; ++j) {
+                    const int k = s + j * kWarps < s1 ? (s + j * kWarps) * 32 + 8 * c : p.K;
 #pragma unroll
                     for (int i = 0; i < kRankTiles; ++i) {
-                        dev::mma_f16(acc[i][t], v[i][0].x, v[i][1].x, v[i][0].y, v[i][1].y, x[t].x, x[t].y);
-                        dev::mma_f16(acc[i][t], v[i][0].z, v[i][1].z, v[i][0].w, v[i][1].w, x[t].z, x[t].w);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int r = r0 + 16 * i + 8 * h + g;
+                            v[j][i][h] = dev::load8(A + r * p.lda, k, r < rank ? p.K : 0, p.align_a);
+                        }
+                    }
+#pragma unroll
+                    for (int t = 0; t < kCols; ++t) x[j][t] = dev::load8(p.X + (n0 + 8 * t + g) * p.ldx, k, members >> (8 * t + g) & 1 ? p.K : 0, p.align_x);
+                }
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j) {
+#pragma unroll
+                    for (int t = 0; t < kCols; ++t) {
+                        if (!(members >> (8 * t) & 0xFFu)) continue;
+#pragma unroll
+                        for (int i = 0; i < kRankTiles; ++i) {
+                            dev::mma_f16(acc[i][t], v[j][i][0].x, v[j][i][1].x, v[j][i][0].y, v[j][i][1].y, x[j][t].x, x[j][t].y);
+                            dev::mma_f16(acc[i][t], v[j][i][0].z, v[j][i][1].z, v[j][i][0].w, v[j][i][1].w, x[j][t].z, x[j][t].w);
+                        }
                     }
                 }
             }
 #pragma unroll
             for (int i = 0; i < kRankTiles; ++i) {
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    float* at = sums + (w * 16 * kRankTiles + 16 * i + g) * kTokPad + 8 * t + 2 * c;
+                for (int t = 0; t < kCols; ++t) {
+                    float* at = sums + (w * 16 * kRankTiles + 16 * i + g) * kPad + 8 * t + 2 * c;
                     *reinterpret_cast<float2*>(at) = make_float2(acc[i][t][0], acc[i][t][1]);
-                    *reinterpret_cast<float2*>(at + 8 * kTokPad) = make_float2(acc[i][t][2], acc[i][t][3]);
+                    *reinterpret_cast<float2*>(at + 8 * kPad) = make_float2(acc[i][t][2], acc[i][t][3]);
                 }
             }
             __syncthreads();
-            for (int r = w; r < 16 * kRankTiles && r0 + r < rank; r += kWarps) {
+            for (int e = threadIdx.x; e < 16 * kRankTiles * kTok; e += kThreads) {
+                const int r = e / kTok, n = e % kTok;
                 float sum = 0.0f;
 #pragma unroll
-                for (int i = 0; i < kWarps; ++i) sum += sums[(i * 16 * kRankTiles + r) * kTokPad + lane];
-                part[(r0 + r) * kTokPad + lane] = sum;
+                for (int i = 0; i < kWarps; ++i) sum += sums[(i * 16 * kRankTiles + r) * kPad + n];
+                if (r0 + r < rank) part[(r0 + r) * kPad + n] = sum;
             }
             __syncthreads();
         }
         cluster.sync();
 
         // the whole sums, scaled; the largest of a token decides its power of two
+        constexpr int kRows = kThreads / kTok;               // ranks at a time; a thread keeps its token
+        const int n = threadIdx.x % kTok, r_first = threadIdx.x / kTok;
         const float scale = p.scales != nullptr ? p.scales[a] : 1.0f;
         float top = 0.0f;
-        for (int r = w; r < prank; r += kWarps) {
+        for (int r = r_first; r < prank; r += kRows) {
             float sum = 0.0f;
             if (r < rank) {
 #pragma unroll
-                for (int i = 0; i < kCluster; ++i) sum += cluster.map_shared_rank(part, i)[r * kTokPad + lane];
+                for (int i = 0; i < kCluster; ++i) sum += cluster.map_shared_rank(part, i)[r * kPad + n];
             }
             sum *= scale;
-            sums[r * kTokPad + lane] = sum;
+            sums[r * kPad + n] = sum;
             top = fmaxf(top, fabsf(sum));
         }
-        largest[w * kTok + lane] = top;
+#pragma unroll
+        for (int i = kTok; i < 32; i *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, i));
+        if (lane < kTok) largest[w * 32 + lane] = top;
         asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");    // this CTA has read the others' sums
         __syncthreads();
+        top = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) top = fmaxf(top, largest[i * kTok + lane]);
+        for (int i = 0; i < kWarps; ++i) top = fmaxf(top, largest[i * 32 + n]);
         // 2^14 <= top * up < 2^15 (values that are tiny, infinite or NaN keep a factor that is a plain number)
         const int exponent = max(27, min(254, __float_as_int(top) >> 23 & 255));
         const float up = __int_as_float((127 + 127 + 14 - exponent) << 23);
-        if (w == 0) largest[kWarps * kTok + lane] = __int_as_float((exponent - 14) << 23);
-        for (int r = w; r < prank; r += kWarps) {
-            const float v = sums[r * kTokPad + lane] * up;
+        if (threadIdx.x < kTok) factors[n] = __int_as_float((exponent - 14) << 23);
+        for (int r = r_first; r < prank; r += kRows) {
+            const float v = sums[r * kPad + n] * up;
             const __half h = __float2half_rn(v);
-            hi[lane * row + r] = h;
-            if constexpr (kTwo) lo[lane * row + r] = __float2half_rn(v - __half2float(h));
+            hi[n * row + r] = h;
+            if constexpr (kTwo) lo[n * row + r] = __float2half_rn(v - __half2float(h));
         }
         __syncthreads();
 
-        // B t, added to base
-        const __half* B = p.B + a * p.stride_b;
-        for (int b = block0; b < blocks; b += sharers * kBlocksOfCluster) {
-            const int m0 = b * kOut + 8 * g;                 // a lane's eight consecutive output rows
-            float acc[4][4][4] = {};
-            for (int k0 = 0; k0 < rank; k0 += 32) {
-                uint4 v[4][2];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    v[i / 2][i % 2] = m0 + i < p.M ? dev::load8(B + (m0 + i) * p.ldb, k0 + 8 * c, rank, p.wide_b) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    if (!(members >> (8 * t) & 0xFFu)) continue;
-                    const uint4 x = *reinterpret_cast<const uint4*>(hi + (8 * t + g) * row + k0 + 8 * c);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        dev::mma_f16(acc[t][i], v[i][0].x, v[i][1].x, v[i][0].y, v[i][1].y, x.x, x.y);
-                        dev::mma_f16(acc[t][i], v[i][0].z, v[i][1].z, v[i][0].w, v[i][1].w, x.z, x.w);
-                    }
-                    if constexpr (kTwo) {
-                        const uint4 y = *reinterpret_cast<const uint4*>(lo + (8 * t + g) * row + k0 + 8 * c);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            dev::mma_f16(acc[t][i], v[i][0].x, v[i][1].x, v[i][0].y, v[i][1].y, y.x, y.y);
-                            dev::mma_f16(acc[t][i], v[i][0].z, v[i][1].z, v[i][0].w, v[i][1].w, y.z, y.w);
-                        }
-                    }
-                }
+        if constexpr (kSplit) {
+            // each CTA of the cluster writes an eighth of the tile's vectors
+            const int width = padded_rank(p.rank), pieces = prank / 8;
+            const int64_t all = static_cast<int64_t>(p.N) * width;
+            for (int e = threadIdx.x; e < kCols * pieces; e += kThreads) {
+                const int t = cta * kCols + e / pieces, k = e % pieces * 8;
+                if (!(members >> t & 1)) continue;
+                __half* to = p.vectors + (n0 + t) * width + k;
+                *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(hi + t * row + k);
+                if constexpr (kTwo) *reinterpret_cast<uint4*>(to + all) = *reinterpret_cast<const uint4*>(lo + t * row + k);
             }
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int n = 8 * t + 2 * c + h;
-                    if (!(members >> n & 1) || m0 >= p.M) continue;
-                    const float down = largest[kWarps * kTok + n];
-                    float o[8];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[2 * i] = acc[t][i][h] * down, o[2 * i + 1] = acc[t][i][2 + h] * down;
-                    add_store(static_cast<const T*>(p.base) + (n0 + n) * p.ldbase + m0, static_cast<T*>(p.Y) + (n0 + n) * p.ldy + m0, o, p.M - m0, p.wide_y);
-                }
-            }
+            if (threadIdx.x < kCols && (members >> (cta * kCols + threadIdx.x) & 1)) p.factors[n0 + cta * kCols + threadIdx.x] = factors[cta * kCols + threadIdx.x];
+        } else {
+            for (int b = block0; b < blocks; b += sharers * kBlocksOfCluster)
+                expand_block<T, kCols>(p, n0, members, a, rank, b * kOut, hi, lo, row, factors);
         }
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // nobody reads this CTA's sums any more
     }
 }
 
-template <int kRankTiles, typename T>
-spdp_status launch_form(const Params& p, int grid, cudaStream_t s) {
-    SPDP_CUDA_TRY(launch_programmatic(lora_kernel<kRankTiles, T>, dim3(static_cast<unsigned>(grid)), kThreads, Layout<kRankTiles>::bytes(p.rank, sizeof(T) == 4), s, p));
+// The second product where it has a kernel of its own: a block of output to a warp, the blocks of a tile one after another.
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 2) lora_expand_kernel(const Params p) {
+    constexpr int kTok = 8 * kMostCols;
+    dev::programmatic_start();
+    const int blocks = (p.M + kOut - 1) / kOut, per_row = (blocks + kWarps - 1) / kWarps;
+    const int b = blockIdx.x % per_row * kWarps + (threadIdx.x >> 5), z = blockIdx.x / per_row % p.per_tile;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x / per_row / p.per_tile) * kTok;
+    if (b >= blocks) return;
+    const Tile tile(p, n0, kTok);
+    const int G = tile.count(), width = padded_rank(p.rank);
+    const __half* hi = p.vectors + n0 * width;
+    for (int d = z; d < G; d += p.per_tile) {
+        int a;
+        unsigned members;
+        tile.pick(d, a, members);
+        if (a < 0) copy_block<T>(p, n0, members, b * kOut);
+        else expand_block<T, kMostCols>(p, n0, members, a, rank_of(p, a), b * kOut, hi, hi + static_cast<int64_t>(p.N) * width, width, p.factors + n0);
+    }
+}
+
+template <int kRankTiles, int kCols, typename T, bool kSplit>
+spdp_status launch_form(const Params& p, int tiles, int device, cudaStream_t s) {
+    static std::mutex mu;
+    static bool configured[64] = {};
+    constexpr int kMostRank = kRankTiles == 4 ? SPDP_MAX_RANK : 16 * kRankTiles;
+    using L = Layout<kRankTiles, kCols>;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!configured[device])
+            SPDP_CUDA_TRY(cudaFuncSetAttribute(lora_kernel<kRankTiles, kCols, T, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               static_cast<int>(L::bytes(kMostRank, sizeof(T) == 4))));
+        configured[device] = true;
+    }
+    const dim3 grid(static_cast<unsigned>(tiles) * static_cast<unsigned>(p.per_tile) * kCluster);
+    SPDP_CUDA_TRY(launch_programmatic(lora_kernel<kRankTiles, kCols, T, kSplit>, grid, kThreads, L::bytes(p.rank, sizeof(T) == 4), s, p));
     return SPDP_OK;
 }
 
-template <int kRankTiles>
-spdp_status configure_form(int rank) {
-    SPDP_CUDA_TRY(cudaFuncSetAttribute(lora_kernel<kRankTiles, __half>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(Layout<kRankTiles>::bytes(rank, false))));
-    SPDP_CUDA_TRY(cudaFuncSetAttribute(lora_kernel<kRankTiles, float>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(Layout<kRankTiles>::bytes(rank, true))));
-    return SPDP_OK;
+template <int kCols, typename T, bool kSplit>
+spdp_status launch_rank(const Params& p, int tiles, int device, cudaStream_t s) {
+    if (p.rank <= 16) return launch_form<1, kCols, T, kSplit>(p, tiles, device, s);
+    if (p.rank <= 32) return launch_form<2, kCols, T, kSplit>(p, tiles, device, s);
+    return launch_form<4, kCols, T, kSplit>(p, tiles, device, s);
+}
+
+int64_t between(int64_t v, int64_t low, int64_t high) { return v > high ? high : v < low ? low : v; }
+
+template <typename T>
+spdp_status launch_typed(Params p, int device, int sms, cudaStream_t s) {
+    const int blocks = (p.M + kOut - 1) / kOut, cluster_slots = 2 * sms / kCluster;
+    if (p.N <= kFusedTokens) {
+        // Clusters of a tile: two CTAs per SM in all, no more than there is work for
+        const int64_t most = static_cast<int64_t>(p.N) * ((blocks + kBlocksOfCluster - 1) / kBlocksOfCluster);
+        p.per_tile = static_cast<int>(between(cluster_slots, 1, most));
+        return launch_rank<1, T, false>(p, 1, device, s);
+    }
+    const bool few = p.N <= 64;                              // tiles of 8 tokens
+    const int tok = few ? 8 : 32, tiles = (p.N + tok - 1) / tok, width = padded_rank(p.rank);
+    const size_t vectors = 2ull * p.N * width * (sizeof(T) == 4 ? 2 : 1);
+    void* scratch = nullptr;
+    spdp_status st = scratch_alloc(device, vectors + 4ull * p.N, s, &scratch);
+    if (st != SPDP_OK) return st;
+    p.vectors = static_cast<__half*>(scratch);
+    p.factors = reinterpret_cast<float*>(static_cast<char*>(scratch) + vectors);
+    p.per_tile = static_cast<int>(between(cluster_slots / tiles, 1, tok));
+    st = few ? launch_rank<1, T, true>(p, tiles, device, s) : launch_rank<kMostCols, T, true>(p, tiles, device, s);
+    if (st == SPDP_OK) {
+        const int64_t per_row = (blocks + kWarps - 1) / kWarps, rows = (p.N + 8 * kMostCols - 1) / (8 * kMostCols);
+        p.per_tile = static_cast<int>(between(4 * sms / (per_row * rows), 1, p.N < 32 ? p.N : 32));
+        const int64_t grid = per_row * rows * p.per_tile;
+        const cudaError_t e = grid > INT32_MAX ? cudaErrorInvalidConfiguration
+                                               : launch_programmatic(lora_expand_kernel<T>, dim3(static_cast<unsigned>(grid)), kThreads, 0, s, p);
+        if (e != cudaSuccess) {
+            note_cuda_error(e, "lora_expand_kernel");
+            st = SPDP_ERR_CUDA;
+        }
+    }
+    SPDP_CUDA_TRY(cudaFreeAsync(scratch, s));
+    return st;
 }
 
 }  // namespace
@@ -320,22 +487,9 @@ spdp_status current_device(int* device, int* sms) {
     return SPDP_OK;
 }
 
-static spdp_status configure_lora_kernel(int device) {
-    static std::mutex mu;
-    static bool configured[64] = {};
-    std::lock_guard<std::mutex> lock(mu);
-    if (configured[device]) return SPDP_OK;
-    spdp_status st = configure_form<1>(16);
-    if (st == SPDP_OK) st = configure_form<2>(32);
-    if (st == SPDP_OK) st = configure_form<4>(SPDP_MAX_RANK);
-    configured[device] = st == SPDP_OK;
-    return st;
-}
-
 spdp_status launch_lora(const LoraCall& call, cudaStream_t s) {
     int device = 0, sms = 0;
-    spdp_status st = current_device(&device, &sms);
-    if (st == SPDP_OK) st = configure_lora_kernel(device);
+    const spdp_status st = current_device(&device, &sms);
     if (st != SPDP_OK) return st;
     const int64_t size = call.ydt == SPDP_Y_F32 ? 4 : 2;
     Params p = {};
@@ -343,21 +497,11 @@ spdp_status launch_lora(const LoraCall& call, cudaStream_t s) {
     p.ldx = call.ldx, p.lda = call.lda, p.stride_a = call.stride_a, p.ldb = call.ldb, p.stride_b = call.stride_b, p.ldbase = call.ldbase, p.ldy = call.ldy;
     p.N = static_cast<int>(call.N), p.K = static_cast<int>(call.K), p.M = static_cast<int>(call.M);
     p.count = static_cast<int>(call.count), p.rank = call.rank;
-    p.wide_x = rows_aligned16(call.X, call.ldx, 2);
-    p.wide_a = rows_aligned16(call.A, call.lda | call.stride_a, 2);
-    p.wide_b = rows_aligned16(call.B, call.ldb | call.stride_b, 2);
+    p.align_x = rows_alignment(call.X, call.ldx, 2);
+    p.align_a = rows_alignment(call.A, call.lda | call.stride_a, 2);
+    p.align_b = rows_alignment(call.B, call.ldb | call.stride_b, 2);
     p.wide_y = rows_aligned16(call.base, call.ldbase, size) && rows_aligned16(call.Y, call.ldy, size);
-    // Clusters of a tile: enough for two CTAs per SM, no more than there is work for
-    const int tiles = (p.N + kTok - 1) / kTok, blocks = (p.M + kOut - 1) / kOut;
-    const int64_t most = static_cast<int64_t>(p.N < kTok ? p.N : kTok) * ((blocks + kBlocksOfCluster - 1) / kBlocksOfCluster);
-    int64_t per_tile = 2 * sms / kCluster / tiles;
-    if (per_tile > most) per_tile = most;
-    if (per_tile < 1) per_tile = 1;
-    p.per_tile = static_cast<int>(per_tile);
-    const int grid = static_cast<int>(tiles * per_tile * kCluster);
-    if (call.ydt == SPDP_Y_F32)
-        return p.rank <= 16 ? launch_form<1, float>(p, grid, s) : p.rank <= 32 ? launch_form<2, float>(p, grid, s) : launch_form<4, float>(p, grid, s);
-    return p.rank <= 16 ? launch_form<1, __half>(p, grid, s) : p.rank <= 32 ? launch_form<2, __half>(p, grid, s) : launch_form<4, __half>(p, grid, s);
+    return call.ydt == SPDP_Y_F32 ? launch_typed<float>(p, device, sms, s) : launch_typed<__half>(p, device, sms, s);
 }
 
 }  // namespace spdp

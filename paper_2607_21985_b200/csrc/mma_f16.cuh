@@ -31,10 +31,20 @@ __device__ __forceinline__ void mma_f16_from(float (&d)[4], float from0, float f
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(from0), "f"(from1), "f"(from2), "f"(from3));
 }
 
-// Elements k .. k + 7 of a row, those from `limit` on as zeros; `wide`: every row starts on a 16-byte boundary and k is a
-// multiple of 8.
-__device__ __forceinline__ uint4 load8(const __half* row, int k, int limit, bool wide) {
-    if (wide && k + 8 <= limit) return *reinterpret_cast<const uint4*>(row + k);
+// Elements k .. k + 7 of a row (k a multiple of 8), those from `limit` on as zeros.  `align`: 16, 8, 4 or 2, what every row's
+// address is a multiple of.
+__device__ __forceinline__ uint4 load8(const __half* row, int k, int limit, int align) {
+    if (k + 8 <= limit) {
+        if (align == 16) return *reinterpret_cast<const uint4*>(row + k);
+        if (align == 8) {
+            const uint2 a = *reinterpret_cast<const uint2*>(row + k), b = *reinterpret_cast<const uint2*>(row + k + 4);
+            return make_uint4(a.x, a.y, b.x, b.y);
+        }
+        if (align == 4) {
+            const uint32_t* w = reinterpret_cast<const uint32_t*>(row + k);
+            return make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -90,10 +100,12 @@ __device__ __forceinline__ void store_halves(__half* at, const float (&x)[8]) {
 
 }  // namespace dev
 
-// Whether rows `ld` elements of `size` bytes apart start on 16-byte boundaries.
-inline bool rows_aligned16(const void* p, int64_t ld, int64_t size) {
-    return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * size)) & 15u) == 0;
+// What the addresses of rows `ld` elements of `size` bytes apart are multiples of, 16 at most.
+inline int rows_alignment(const void* p, int64_t ld, int64_t size) {
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * size) | 16u;
+    return static_cast<int>(bits & (~bits + 1));
 }
+inline bool rows_aligned16(const void* p, int64_t ld, int64_t size) { return rows_alignment(p, ld, size) == 16; }
 
 // A launch that may be set up while the kernel before it still runs (programmatic_start() in the kernel waits for it).
 template <typename... Formal, typename... Actual>
