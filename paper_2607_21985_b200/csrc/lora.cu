@@ -30,12 +30,14 @@ constexpr int kMostCols = 4;        // column blocks of 8 tokens in a tile: 1 or
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kCluster = 8;
+constexpr int kExpandWarps = 4;     // of a CTA of the second kernel; three CTAs to an SM, for the registers that its loads take
 constexpr int kOut = 64;            // output rows of a warp's block
 constexpr int kBlocksOfCluster = kCluster * kWarps;
 #ifndef SPDP_FUSED
 #define SPDP_FUSED 4
 #endif
 constexpr int kFusedTokens = SPDP_FUSED;     // up to here one launch does both products
+constexpr int kFewTokens = 64;               // up to here tiles are 8 tokens, for there are more adapters than tiles of 32
 
 struct Params {
     const __half* X;
@@ -49,7 +51,6 @@ struct Params {
     int64_t ldx, lda, stride_a, ldb, stride_b, ldbase, ldy;
     int N, K, M, count, rank;
     int per_tile;                   // clusters (first or only kernel), CTAs (second) of a tile, among which its adapters are dealt out
-    int align_x, align_a, align_b;  // bytes that every row's address is a multiple of
     bool wide_y;                    // base and Y: 16
     // what the first kernel leaves for the second: [N][padded rank] fp16, for 32-bit results twice, and a factor to each token
     __half* vectors;
@@ -88,7 +89,9 @@ struct Tile {
     }
     __device__ __forceinline__ int count() const { return __popc(groups); }
     __device__ __forceinline__ void pick(int d, int& adapter, unsigned& members) const {
-        const int lead = __fns(groups, 0, d + 1);
+        unsigned rest = groups;
+        for (int i = 0; i < d; ++i) rest &= rest - 1;
+        const int lead = __ffs(rest) - 1;
         adapter = __shfl_sync(0xFFFFFFFFu, mine, lead);
         members = __shfl_sync(0xFFFFFFFFu, same, lead);
     }
@@ -160,86 +163,108 @@ __device__ __forceinline__ void copy_block(const Params& p, int64_t n0, unsigned
     }
 }
 
-// The second product for a warp's block of output rows from m_block on: B t, added to base.  `hi`, `lo`: the tile's vectors, `row`
-// halves apart; `factors`: what undoes their scaling.
-template <typename T, int kCols>
-__device__ __forceinline__ void expand_block(const Params& p, int64_t n0, unsigned members, int a, int rank, int m_block, const __half* hi, const __half* lo, int row,
-                                             const float* factors) {
-    constexpr bool kTwo = sizeof(T) == 4;
-    constexpr int kStep = kCols < 2 ? kCols : 2;                 // column blocks at a time
-    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    const int m0 = m_block + 8 * g, left = p.M - m0;             // a lane's eight consecutive output rows
-    const bool wide = p.wide_y && left >= 8;
-    const T* base = static_cast<const T*>(p.base) + n0 * p.ldbase + m0;
-    T* y = static_cast<T*>(p.Y) + n0 * p.ldy + m0;
-    const __half* B = p.B + a * p.stride_b;
-    // base is asked for ahead of the products: all of it where it is 16-bit, else of the tokens that are next
-    constexpr int kAhead = sizeof(T) == 2 ? kCols : kStep;
+// The second product for a warp's block of output rows: B t, added to base.  The loads of base, of the weights and of the
+// vectors are all asked for before the products need them.
+template <typename T, int kCols, int kAlign>
+struct Block {
+    static constexpr bool kTwo = sizeof(T) == 4;
+    static constexpr int kStep = kCols < 2 ? kCols : 2;          // column blocks at a time
+    static constexpr int kAhead = sizeof(T) == 2 ? kCols : kStep;        // of base, 16-bit: all of it
     Eight<T> old[kAhead][2];
-    auto ask = [&](int t0) {
+    const T* base;                                               // at the lane's first token and first output row
+    T* y;
+    int m0, left;                                                // a lane's eight consecutive output rows, how many of them exist
+    bool wide;
+
+    __device__ __forceinline__ Block(const Params& p, int64_t n0, int m_block) {
+        const int lane = threadIdx.x & 31;
+        m0 = m_block + 8 * (lane >> 2), left = p.M - m0;
+        wide = p.wide_y && left >= 8;
+        base = static_cast<const T*>(p.base) + (n0 + 2 * (lane & 3)) * p.ldbase + m0;
+        y = static_cast<T*>(p.Y) + (n0 + 2 * (lane & 3)) * p.ldy + m0;
+    }
+    // Base of the tokens in `mask`, column blocks t0 .. t0 + kAhead - 1.
+    __device__ __forceinline__ void ask(const Params& p, unsigned mask, int t0) {
+        const unsigned mine = wide ? mask >> (2 * (threadIdx.x & 3)) : 0u;
 #pragma unroll
         for (int t = 0; t < kAhead; ++t) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int n = 8 * (t0 + t) + 2 * c + h;
-                if (wide && (members >> n & 1)) old[t][h].load(base + n * p.ldbase);
-            }
+            for (int h = 0; h < 2; ++h)
+                if (mine >> (8 * (t0 + t) + h) & 1) old[t][h].load(base + (8 * (t0 + t) + h) * p.ldbase);
         }
-    };
-    uint4 v[4][2];
-    auto weights = [&](int k0) {
+    }
+    // `hi`, `lo`: the tile's vectors, `row` halves apart; `factors`: what undoes their scaling.  `asked`: ask(p, members or more, 0) was called.
+    __device__ __forceinline__ void add(const Params& p, unsigned members, int a, int rank, const __half* hi, const __half* lo, int row, const float* factors, bool asked) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+        const __half* B = p.B + a * p.stride_b + m0 * p.ldb;
+        uint4 v[4][2];
+        auto weights = [&](int k0) {
+            const __half* at = B;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i / 2][i % 2] = dev::load8(B + (m0 + i) * p.ldb, k0 + 8 * c, i < left ? rank : 0, p.align_b);
-    };
-    ask(0);
-    weights(0);
+            for (int i = 0; i < 8; ++i, at += p.ldb) v[i / 2][i % 2] = dev::load8<kAlign>(at, k0 + 8 * c, i < left ? rank : 0);
+            if (kAlign == 16 && rank % 8 != 0) {                 // what stands behind an adapter's own rank
 #pragma unroll
-    for (int t0 = 0; t0 < kCols; t0 += kStep) {
-        if (t0 > 0 && t0 % kAhead == 0) ask(t0);
-        if (!(members >> (8 * t0) & 0xFFFFu)) continue;
-        float acc[kStep][4][4] = {};
-        for (int k0 = 0; k0 < rank; k0 += 32) {
-            if (rank > 32 && (k0 > 0 || t0 > 0)) weights(k0);
+                for (int i = 0; i < 8; ++i) dev::cut8(v[i / 2][i % 2], k0 + 8 * c, rank);
+            }
+        };
+        const __half* vector = hi + g * row + 8 * c;
+        const int64_t second = lo - hi;
+        uint4 x[kCols];
+        auto vectors = [&](int k0) {                             // other tokens' vectors may be another adapter's, or nobody's
 #pragma unroll
-            for (int t = 0; t < kStep; ++t) {
-                if (!(members >> (8 * (t0 + t)) & 0xFFu)) continue;
-                const bool member = members >> (8 * (t0 + t) + g) & 1;     // other tokens' vectors may be another adapter's, or nobody's
-                const uint4 none = make_uint4(0, 0, 0, 0);
-                const uint4 x = member ? *reinterpret_cast<const uint4*>(hi + (8 * (t0 + t) + g) * row + k0 + 8 * c) : none;
+            for (int t = 0; t < kCols; ++t) {
+                x[t] = make_uint4(0, 0, 0, 0);
+                if (members >> (8 * t + g) & 1) x[t] = *reinterpret_cast<const uint4*>(vector + 8 * t * row + k0);
+            }
+        };
+        if (!asked) ask(p, members, 0);
+        if (rank > 0) weights(0), vectors(0);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    dev::mma_f16(acc[t][i], v[i][0].x, v[i][1].x, v[i][0].y, v[i][1].y, x.x, x.y);
-                    dev::mma_f16(acc[t][i], v[i][0].z, v[i][1].z, v[i][0].w, v[i][1].w, x.z, x.w);
-                }
-                if constexpr (kTwo) {
-                    const uint4 z = member ? *reinterpret_cast<const uint4*>(lo + (8 * (t0 + t) + g) * row + k0 + 8 * c) : none;
+        for (int t0 = 0; t0 < kCols; t0 += kStep) {
+            if (t0 > 0 && t0 % kAhead == 0) ask(p, members, t0);
+            if (!(members >> (8 * t0) & (kStep == 2 ? 0xFFFFu : 0xFFu))) continue;
+            float acc[kStep][4][4] = {};
+            for (int k0 = 0; k0 < rank; k0 += 32) {
+                if (rank > 32 && (k0 > 0 || t0 > 0)) weights(k0), vectors(k0);
+#pragma unroll
+                for (int t = 0; t < kStep; ++t) {
+                    if (!(members >> (8 * (t0 + t)) & 0xFFu)) continue;
+                    uint4 z = make_uint4(0, 0, 0, 0);
+                    if (kTwo && (members >> (8 * (t0 + t) + g) & 1)) z = *reinterpret_cast<const uint4*>(vector + second + 8 * (t0 + t) * row + k0);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        dev::mma_f16(acc[t][i], v[i][0].x, v[i][1].x, v[i][0].y, v[i][1].y, z.x, z.y);
-                        dev::mma_f16(acc[t][i], v[i][0].z, v[i][1].z, v[i][0].w, v[i][1].w, z.z, z.w);
+                        dev::mma_f16(acc[t][i], v[i][0].x, v[i][1].x, v[i][0].y, v[i][1].y, x[t0 + t].x, x[t0 + t].y);
+                        dev::mma_f16(acc[t][i], v[i][0].z, v[i][1].z, v[i][0].w, v[i][1].w, x[t0 + t].z, x[t0 + t].w);
+                    }
+                    if constexpr (kTwo) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            dev::mma_f16(acc[t][i], v[i][0].x, v[i][1].x, v[i][0].y, v[i][1].y, z.x, z.y);
+                            dev::mma_f16(acc[t][i], v[i][0].z, v[i][1].z, v[i][0].w, v[i][1].w, z.z, z.w);
+                        }
                     }
                 }
             }
-        }
 #pragma unroll
-        for (int t = 0; t < kStep; ++t) {
+            for (int t = 0; t < kStep; ++t) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int n = 8 * (t0 + t) + 2 * c + h;
-                if (!(members >> n & 1) || left <= 0) continue;
-                const float down = factors[n];
-                float o[8];
+                for (int h = 0; h < 2; ++h) {
+                    const int n = 8 * (t0 + t) + h;              // behind the lane's first token
+                    if (!(members >> (n + 2 * c) & 1) || left <= 0) continue;
+                    const float down = factors[n + 2 * c];
+                    float o[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[2 * i] = acc[t][i][h], o[2 * i + 1] = acc[t][i][2 + h];
-                if (wide) old[(t0 + t) % kAhead][h].add_store(y + n * p.ldy, o, down);
-                else add_store_some(base + n * p.ldbase, y + n * p.ldy, o, down, left);
+                    for (int i = 0; i < 4; ++i) o[2 * i] = acc[t][i][h], o[2 * i + 1] = acc[t][i][2 + h];
+                    if (wide) old[(t0 + t) % kAhead][h].add_store(y + n * p.ldy, o, down);
+                    else add_store_some(base + n * p.ldbase, y + n * p.ldy, o, down, left);
+                }
             }
         }
     }
-}
+};
 
 // kSplit: this kernel ends with the vectors, in memory; else it does the second product too.
-template <int kRankTiles, int kCols, typename T, bool kSplit>
+template <int kRankTiles, int kCols, typename T, bool kSplit, int kAlign>
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) lora_kernel(const Params p) {
     constexpr bool kTwo = sizeof(T) == 4;                    // two fp16 numbers for a value of the vectors
     // steps of 32 k whose loads are on their way at once; a step takes 4 kCols + 8 kRankTiles registers
@@ -283,6 +308,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
 
         // A x over this CTA's eighth of K
         const __half* A = p.A + a * p.stride_a;
+        const __half* X = p.X + (n0 + g) * p.ldx;
         const int steps = (p.K + 31) / 32;
         const int s0 = static_cast<int>(static_cast<int64_t>(steps) * cta / kCluster), s1 = static_cast<int>(static_cast<int64_t>(steps) * (cta + 1) / kCluster);
         for (int r0 = 0; r0 < rank; r0 += 16 * kRankTiles) {
@@ -292,16 +318,12 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
 #pragma unroll
                 for (int j = 0; j < kBatch; ++j) {
                     const int k = s + j * kWarps < s1 ? (s + j * kWarps) * 32 + 8 * c : p.K;
+                    const __half* at = A + (r0 + g) * p.lda;
 #pragma unroll
-                    for (int i = 0; i < kRankTiles; ++i) {
+                    for (int i = 0; i < 2 * kRankTiles; ++i, at += 8 * p.lda) v[j][i / 2][i % 2] = dev::load8<kAlign>(at, k, r0 + 8 * i + g < rank ? p.K : 0);
+                    at = X;
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int r = r0 + 16 * i + 8 * h + g;
-                            v[j][i][h] = dev::load8(A + r * p.lda, k, r < rank ? p.K : 0, p.align_a);
-                        }
-                    }
-#pragma unroll
-                    for (int t = 0; t < kCols; ++t) x[j][t] = dev::load8(p.X + (n0 + 8 * t + g) * p.ldx, k, members >> (8 * t + g) & 1 ? p.K : 0, p.align_x);
+                    for (int t = 0; t < kCols; ++t, at += 8 * p.ldx) x[j][t] = dev::load8<kAlign>(at, k, members >> (8 * t + g) & 1 ? p.K : 0);
                 }
 #pragma unroll
                 for (int j = 0; j < kBatch; ++j) {
@@ -386,21 +408,24 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
             if (threadIdx.x < kCols && (members >> (cta * kCols + threadIdx.x) & 1)) p.factors[n0 + cta * kCols + threadIdx.x] = factors[cta * kCols + threadIdx.x];
         } else {
             for (int b = block0; b < blocks; b += sharers * kBlocksOfCluster)
-                expand_block<T, kCols>(p, n0, members, a, rank, b * kOut, hi, lo, row, factors);
+                Block<T, kCols, kAlign>(p, n0, b * kOut).add(p, members, a, rank, hi, lo, row, factors, false);
         }
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // nobody reads this CTA's sums any more
     }
 }
 
 // The second product where it has a kernel of its own: a block of output to a warp, the blocks of a tile one after another.
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) lora_expand_kernel(const Params p) {
+template <typename T, int kAlign>
+__global__ void __launch_bounds__(32 * kExpandWarps, 3) lora_expand_kernel(const Params p) {
     constexpr int kTok = 8 * kMostCols;
     dev::programmatic_start();
-    const int blocks = (p.M + kOut - 1) / kOut, per_row = (blocks + kWarps - 1) / kWarps;
-    const int b = blockIdx.x % per_row * kWarps + (threadIdx.x >> 5), z = blockIdx.x / per_row % p.per_tile;
+    const int blocks = (p.M + kOut - 1) / kOut, per_row = (blocks + kExpandWarps - 1) / kExpandWarps;
+    const int b = blockIdx.x % per_row * kExpandWarps + (threadIdx.x >> 5), z = blockIdx.x / per_row % p.per_tile;
     const int64_t n0 = static_cast<int64_t>(blockIdx.x / per_row / p.per_tile) * kTok;
     if (b >= blocks) return;
+    Block<T, kMostCols, kAlign> block(p, n0, b * kOut);
+    const bool early = p.per_tile == 1;                      // base of the whole tile, before it is known whose tokens they are
+    if (early) block.ask(p, p.N - n0 >= kTok ? 0xFFFFFFFFu : (1u << (p.N - n0)) - 1u, 0);
     const Tile tile(p, n0, kTok);
     const int G = tile.count(), width = padded_rank(p.rank);
     const __half* hi = p.vectors + n0 * width;
@@ -409,11 +434,11 @@ __global__ void __launch_bounds__(kThreads, 2) lora_expand_kernel(const Params p
         unsigned members;
         tile.pick(d, a, members);
         if (a < 0) copy_block<T>(p, n0, members, b * kOut);
-        else expand_block<T, kMostCols>(p, n0, members, a, rank_of(p, a), b * kOut, hi, hi + static_cast<int64_t>(p.N) * width, width, p.factors + n0);
+        else block.add(p, members, a, rank_of(p, a), hi, hi + static_cast<int64_t>(p.N) * width, width, p.factors + n0, early && (sizeof(T) == 2 || d == 0));
     }
 }
 
-template <int kRankTiles, int kCols, typename T, bool kSplit>
+template <int kRankTiles, int kCols, typename T, bool kSplit, int kAlign>
 spdp_status launch_form(const Params& p, int tiles, int device, cudaStream_t s) {
     static std::mutex mu;
     static bool configured[64] = {};
@@ -422,49 +447,53 @@ spdp_status launch_form(const Params& p, int tiles, int device, cudaStream_t s) 
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!configured[device])
-            SPDP_CUDA_TRY(cudaFuncSetAttribute(lora_kernel<kRankTiles, kCols, T, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+            SPDP_CUDA_TRY(cudaFuncSetAttribute(lora_kernel<kRankTiles, kCols, T, kSplit, kAlign>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                static_cast<int>(L::bytes(kMostRank, sizeof(T) == 4))));
         configured[device] = true;
     }
     const dim3 grid(static_cast<unsigned>(tiles) * static_cast<unsigned>(p.per_tile) * kCluster);
-    SPDP_CUDA_TRY(launch_programmatic(lora_kernel<kRankTiles, kCols, T, kSplit>, grid, kThreads, L::bytes(p.rank, sizeof(T) == 4), s, p));
+    SPDP_CUDA_TRY(launch_programmatic(lora_kernel<kRankTiles, kCols, T, kSplit, kAlign>, grid, kThreads, L::bytes(p.rank, sizeof(T) == 4), s, p));
     return SPDP_OK;
 }
 
-template <int kCols, typename T, bool kSplit>
+template <int kCols, typename T, bool kSplit, int kAlign>
 spdp_status launch_rank(const Params& p, int tiles, int device, cudaStream_t s) {
-    if (p.rank <= 16) return launch_form<1, kCols, T, kSplit>(p, tiles, device, s);
-    if (p.rank <= 32) return launch_form<2, kCols, T, kSplit>(p, tiles, device, s);
-    return launch_form<4, kCols, T, kSplit>(p, tiles, device, s);
+    if (p.rank <= 16) return launch_form<1, kCols, T, kSplit, kAlign>(p, tiles, device, s);
+    if (p.rank <= 32) return launch_form<2, kCols, T, kSplit, kAlign>(p, tiles, device, s);
+    return launch_form<4, kCols, T, kSplit, kAlign>(p, tiles, device, s);
 }
 
 int64_t between(int64_t v, int64_t low, int64_t high) { return v > high ? high : v < low ? low : v; }
 
 template <typename T>
-spdp_status launch_typed(Params p, int device, int sms, cudaStream_t s) {
+spdp_status launch_typed(Params p, int align, int device, int sms, cudaStream_t s) {
     const int blocks = (p.M + kOut - 1) / kOut, cluster_slots = 2 * sms / kCluster;
-    if (p.N <= kFusedTokens) {
+    if (p.N <= kFusedTokens && align == 16) {
         // Clusters of a tile: two CTAs per SM in all, no more than there is work for
         const int64_t most = static_cast<int64_t>(p.N) * ((blocks + kBlocksOfCluster - 1) / kBlocksOfCluster);
         p.per_tile = static_cast<int>(between(cluster_slots, 1, most));
-        return launch_rank<1, T, false>(p, 1, device, s);
+        return launch_rank<1, T, false, 16>(p, 1, device, s);
     }
-    const bool few = p.N <= 64;                              // tiles of 8 tokens
-    const int tok = few ? 8 : 32, tiles = (p.N + tok - 1) / tok, width = padded_rank(p.rank);
+    const bool few = p.N <= kFewTokens && align == 16;
+    const int tok = few ? 8 : 8 * kMostCols, tiles = (p.N + tok - 1) / tok, width = padded_rank(p.rank);
     const size_t vectors = 2ull * p.N * width * (sizeof(T) == 4 ? 2 : 1);
     void* scratch = nullptr;
     spdp_status st = scratch_alloc(device, vectors + 4ull * p.N, s, &scratch);
     if (st != SPDP_OK) return st;
     p.vectors = static_cast<__half*>(scratch);
     p.factors = reinterpret_cast<float*>(static_cast<char*>(scratch) + vectors);
-    p.per_tile = static_cast<int>(between(cluster_slots / tiles, 1, tok));
-    st = few ? launch_rank<1, T, true>(p, tiles, device, s) : launch_rank<kMostCols, T, true>(p, tiles, device, s);
+    p.per_tile = static_cast<int>(between(cluster_slots / tiles, 1, p.N < tok ? p.N : tok));
+    if (align == 16) st = few ? launch_rank<1, T, true, 16>(p, tiles, device, s) : launch_rank<kMostCols, T, true, 16>(p, tiles, device, s);
+    else st = align == 4 ? launch_rank<kMostCols, T, true, 4>(p, tiles, device, s) : launch_rank<kMostCols, T, true, 2>(p, tiles, device, s);
     if (st == SPDP_OK) {
-        const int64_t per_row = (blocks + kWarps - 1) / kWarps, rows = (p.N + 8 * kMostCols - 1) / (8 * kMostCols);
-        p.per_tile = static_cast<int>(between(4 * sms / (per_row * rows), 1, p.N < 32 ? p.N : 32));
-        const int64_t grid = per_row * rows * p.per_tile;
-        const cudaError_t e = grid > INT32_MAX ? cudaErrorInvalidConfiguration
-                                               : launch_programmatic(lora_expand_kernel<T>, dim3(static_cast<unsigned>(grid)), kThreads, 0, s, p);
+        const int64_t per_row = (blocks + kExpandWarps - 1) / kExpandWarps, rows = (p.N + 8 * kMostCols - 1) / (8 * kMostCols);
+        p.per_tile = static_cast<int>(between(8 * sms / (per_row * rows), 1, p.N < 32 ? p.N : 32));
+        const int64_t size = per_row * rows * p.per_tile;
+        const dim3 grid(static_cast<unsigned>(size));
+        const cudaError_t e = size > INT32_MAX ? cudaErrorInvalidConfiguration
+                              : align == 16    ? launch_programmatic(lora_expand_kernel<T, 16>, grid, 32 * kExpandWarps, 0, s, p)
+                              : align == 4     ? launch_programmatic(lora_expand_kernel<T, 4>, grid, 32 * kExpandWarps, 0, s, p)
+                                               : launch_programmatic(lora_expand_kernel<T, 2>, grid, 32 * kExpandWarps, 0, s, p);
         if (e != cudaSuccess) {
             note_cuda_error(e, "lora_expand_kernel");
             st = SPDP_ERR_CUDA;
@@ -497,11 +526,13 @@ spdp_status launch_lora(const LoraCall& call, cudaStream_t s) {
     p.ldx = call.ldx, p.lda = call.lda, p.stride_a = call.stride_a, p.ldb = call.ldb, p.stride_b = call.stride_b, p.ldbase = call.ldbase, p.ldy = call.ldy;
     p.N = static_cast<int>(call.N), p.K = static_cast<int>(call.K), p.M = static_cast<int>(call.M);
     p.count = static_cast<int>(call.count), p.rank = call.rank;
-    p.align_x = rows_alignment(call.X, call.ldx, 2);
-    p.align_a = rows_alignment(call.A, call.lda | call.stride_a, 2);
-    p.align_b = rows_alignment(call.B, call.ldb | call.stride_b, 2);
     p.wide_y = rows_aligned16(call.base, call.ldbase, size) && rows_aligned16(call.Y, call.ldy, size);
-    return call.ydt == SPDP_Y_F32 ? launch_typed<float>(p, device, sms, s) : launch_typed<__half>(p, device, sms, s);
+    // 16-byte loads where every row of X, A and B starts on such a boundary and has whole pieces; else 4-byte or 2-byte ones
+    int align = 16;
+    for (const int v : {rows_alignment(call.X, call.ldx, 2), rows_alignment(call.A, call.lda | call.stride_a, 2), rows_alignment(call.B, call.ldb | call.stride_b, 2)})
+        if (v < align) align = v;
+    align = align == 16 && call.K % 8 == 0 && call.rank % 8 == 0 ? 16 : align >= 4 ? 4 : 2;
+    return call.ydt == SPDP_Y_F32 ? launch_typed<float>(p, align, device, sms, s) : launch_typed<__half>(p, align, device, sms, s);
 }
 
 }  // namespace spdp

@@ -31,28 +31,39 @@ __device__ __forceinline__ void mma_f16_from(float (&d)[4], float from0, float f
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(from0), "f"(from1), "f"(from2), "f"(from3));
 }
 
-// Elements k .. k + 7 of a row (k a multiple of 8), those from `limit` on as zeros.  `align`: 16, 8, 4 or 2, what every row's
-// address is a multiple of.
-__device__ __forceinline__ uint4 load8(const __half* row, int k, int limit, int align) {
-    if (k + 8 <= limit) {
-        if (align == 16) return *reinterpret_cast<const uint4*>(row + k);
-        if (align == 8) {
-            const uint2 a = *reinterpret_cast<const uint2*>(row + k), b = *reinterpret_cast<const uint2*>(row + k + 4);
-            return make_uint4(a.x, a.y, b.x, b.y);
-        }
-        if (align == 4) {
-            const uint32_t* w = reinterpret_cast<const uint32_t*>(row + k);
-            return make_uint4(w[0], w[1], w[2], w[3]);
-        }
-    }
-    uint32_t w[4];
+// Elements k .. k + 7 of a row (k a multiple of 8) of which those from `limit` on are zeros, without a branch, so that many such
+// loads are on their way at once.  kAlign: 16, 4 or 2 bytes, what every row's address is a multiple of; with 16 the elements up
+// to the next multiple of 8 are read too and come back as they are.
+template <int kAlign>
+__device__ __forceinline__ uint4 load8(const __half* row, int k, int limit) {
+    if constexpr (kAlign == 16) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (k < limit) v = *reinterpret_cast<const uint4*>(row + k);
+        return v;
+    } else {
+        uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = k + 2 * i < limit ? __half_as_ushort(row[k + 2 * i]) : 0u;
-        const uint32_t hi = k + 2 * i + 1 < limit ? __half_as_ushort(row[k + 2 * i + 1]) : 0u;
-        w[i] = lo | (hi << 16);
+        for (int i = 0; i < 4; ++i) {
+            const int at = k + 2 * i;
+            if constexpr (kAlign == 4) {
+                uint32_t both = 0, one = 0;
+                if (at + 1 < limit) both = *reinterpret_cast<const uint32_t*>(row + at);
+                if (at + 1 == limit) one = __half_as_ushort(row[at]);
+                w[i] = both | one;
+            } else {
+                uint32_t lo = 0, hi = 0;
+                if (at < limit) lo = __half_as_ushort(row[at]);
+                if (at + 1 < limit) hi = __half_as_ushort(row[at + 1]);
+                w[i] = lo | (hi << 16);
+            }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Zeros in the elements from `limit` on of what stands for elements k .. k + 7.
+__device__ __forceinline__ void cut8(uint4& v, int k, int limit) {
+    auto keep = [&](int i) { return k + 2 * i + 1 < limit ? 0xFFFFFFFFu : k + 2 * i < limit ? 0x0000FFFFu : 0u; };
+    v.x &= keep(0), v.y &= keep(1), v.z &= keep(2), v.w &= keep(3);
 }
 
 // Eight consecutive values of a row as fp32, in 16-byte loads where the address allows them.
