@@ -51,11 +51,14 @@ struct Params {
     int64_t ldx, lda, stride_a, ldb, stride_b, ldbase, ldy;
     int N, K, M, count, rank;
     int per_tile;                   // clusters (first or only kernel), CTAs (second) of a tile, among which its adapters are dealt out
-    bool wide_y;                    // base and Y: 16
+    int per_row;                    // second kernel: CTAs that share a tile's output rows
+    bool wide_y;                    // base and Y: rows of whole 16-byte pieces, on such boundaries
     // what the first kernel leaves for the second: [N][padded rank] fp16, for 32-bit results twice, and a factor to each token
     __half* vectors;
     float* factors;
 };
+
+int64_t between(int64_t v, int64_t low, int64_t high) { return v > high ? high : v < low ? low : v; }
 
 __host__ __device__ inline int padded_rank(int rank) { return (rank + 31) & ~31; }
 
@@ -102,135 +105,79 @@ __device__ __forceinline__ int rank_of(const Params& p, int a) {
     return rank < 0 ? 0 : rank > p.rank ? p.rank : rank;
 }
 
-// Eight values of a row of base, then of Y: in 16-byte accesses (kept as bits, so that they can be asked for early), or one by one.
+// A warp's block of output: 64 rows, eight to a lane (for two tokens of each column block).  kWide: base and Y are read and
+// written 16 bytes at a time, and a lane's rows are neighbours, 8 g + e; else value by value, and the rows are 8 e + g, so that
+// the lanes' are.
+template <bool kWide>
+__device__ __forceinline__ int row_of(int g, int e) { return kWide ? 8 * g + e : 8 * e + g; }
+
 template <typename T>
-struct Eight {
-    uint4 bits[sizeof(T) / 2];
-    __device__ __forceinline__ void load(const T* from) {
-#pragma unroll
-        for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) bits[i] = reinterpret_cast<const uint4*>(from)[i];
-    }
-    // base + f o
-    __device__ __forceinline__ void add_store(T* to, const float (&o)[8], float f) {
-        if constexpr (sizeof(T) == 2) {
-            uint32_t w[4] = {bits[0].x, bits[0].y, bits[0].z, bits[0].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-                const __half2 r = __floats2half2_rn(v.x + o[2 * i] * f, v.y + o[2 * i + 1] * f);
-                w[i] = *reinterpret_cast<const uint32_t*>(&r);
-            }
-            *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float4 v = *reinterpret_cast<const float4*>(&bits[i]);
-                v.x += o[4 * i] * f, v.y += o[4 * i + 1] * f, v.z += o[4 * i + 2] * f, v.w += o[4 * i + 3] * f;
-                reinterpret_cast<float4*>(to)[i] = v;
-            }
-        }
-    }
-};
+__device__ __forceinline__ T sum_of(T base, float add) {
+    if constexpr (sizeof(T) == 2) return __float2half_rn(__half2float(base) + add);
+    else return base + add;
+}
+// Eight neighbours of Y: base's, at `from` (16-byte aligned, as `to` is), plus f o.
 template <typename T>
-__device__ __forceinline__ void add_store_some(const T* base, T* y, const float (&o)[8], float f, int left) {
-    T in[8];
+__device__ __forceinline__ void add_eight(T* to, const T* from, const float (&o)[8], float f) {
+    union { uint4 bits[sizeof(T) / 2]; T v[8]; } x;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < left) in[i] = base[i];
+    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) x.bits[i] = reinterpret_cast<const uint4*>(from)[i];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (i >= left) continue;
-        if constexpr (sizeof(T) == 2) y[i] = __float2half_rn(__half2float(in[i]) + o[i] * f);
-        else y[i] = in[i] + o[i] * f;
-    }
+    for (int i = 0; i < 8; ++i) x.v[i] = sum_of(x.v[i], o[i] * f);
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) reinterpret_cast<uint4*>(to)[i] = x.bits[i];
 }
 
-// Base to Y as it is, for a warp's block of output rows from m0 on.
+// The second product for a warp's block of output rows from m_block on, added to base.  `hi`, `lo`: the tile's vectors, `row`
+// halves apart; `factors`: what undoes their scaling.  `old`: base's block in shared memory, [token][kOldRow], or null: it is
+// read where it is.  a < 0: base as it is.
 template <typename T>
-__device__ __forceinline__ void copy_block(const Params& p, int64_t n0, unsigned members, int m0) {
-    constexpr int kPieces = kOut * sizeof(T) / 16;               // 16-byte pieces of a token's block
-    const int lane = threadIdx.x & 31;
-    const bool whole = p.wide_y && m0 + kOut <= p.M;
-    for (int t = whole ? lane / kPieces : 0; t < 32; t += whole ? 32 / kPieces : 1) {
-        if (!(members >> t & 1)) continue;
-        const T* from = static_cast<const T*>(p.base) + (n0 + t) * p.ldbase + m0;
-        T* to = static_cast<T*>(p.Y) + (n0 + t) * p.ldy + m0;
-        if (whole) {
-            reinterpret_cast<uint4*>(to)[lane % kPieces] = reinterpret_cast<const uint4*>(from)[lane % kPieces];
-        } else {
-            for (int i = lane; i < kOut && m0 + i < p.M; i += 32) to[i] = from[i];
-        }
-    }
-}
+constexpr int kOldRow = kOut + 16 / static_cast<int>(sizeof(T));     // a token's values of a block, and 16 bytes
 
-// The second product for a warp's block of output rows: B t, added to base.  The loads of base, of the weights and of the
-// vectors are all asked for before the products need them.
-template <typename T, int kCols, int kAlign>
-struct Block {
-    static constexpr bool kTwo = sizeof(T) == 4;
-    static constexpr int kStep = kCols < 2 ? kCols : 2;          // column blocks at a time
-    static constexpr int kAhead = sizeof(T) == 2 ? kCols : kStep;        // of base, 16-bit: all of it
-    Eight<T> old[kAhead][2];
-    const T* base;                                               // at the lane's first token and first output row
-    T* y;
-    int m0, left;                                                // a lane's eight consecutive output rows, how many of them exist
-    bool wide;
-
-    __device__ __forceinline__ Block(const Params& p, int64_t n0, int m_block) {
-        const int lane = threadIdx.x & 31;
-        m0 = m_block + 8 * (lane >> 2), left = p.M - m0;
-        wide = p.wide_y && left >= 8;
-        base = static_cast<const T*>(p.base) + (n0 + 2 * (lane & 3)) * p.ldbase + m0;
-        y = static_cast<T*>(p.Y) + (n0 + 2 * (lane & 3)) * p.ldy + m0;
-    }
-    // Base of the tokens in `mask`, column blocks t0 .. t0 + kAhead - 1.
-    __device__ __forceinline__ void ask(const Params& p, unsigned mask, int t0) {
-        const unsigned mine = wide ? mask >> (2 * (threadIdx.x & 3)) : 0u;
+template <typename T, int kCols, int kAlign, bool kWide>
+__device__ __forceinline__ void expand_block(const Params& p, int64_t n0, unsigned members, int a, int rank, int m_block, const __half* hi, const __half* lo, int row,
+                                             const float* factors, const T* old) {
+    constexpr bool kTwo = sizeof(T) == 4;
+    constexpr int kStep = kCols < 2 ? kCols : 2;                 // column blocks at a time
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const int left = p.M - m_block;                              // rows of the block that exist
+    const T* base = static_cast<const T*>(p.base) + (n0 + 2 * c) * p.ldbase + m_block;
+    T* y = static_cast<T*>(p.Y) + (n0 + 2 * c) * p.ldy + m_block;
+    const bool there = row_of<kWide>(g, 0) < left;               // kWide: M is a multiple of 8, so all eight or none
+    const unsigned all = members, owner = members >> g;          // bit 8 t of owner: column g of block t is a member (others' vectors may be nobody's)
+    members >>= 2 * c;                                           // bit 8 t + h: the lane's tokens
+    uint4 v[4][2], x[kCols];
+    const __half* B = p.B + a * p.stride_b + (m_block + row_of<kWide>(g, 0)) * p.ldb;
+    const int64_t apart = (kWide ? 1 : 8) * p.ldb;
+    auto weights = [&](int k0) {
+        const __half* at = B;
 #pragma unroll
-        for (int t = 0; t < kAhead; ++t) {
+        for (int i = 0; i < 8; ++i, at += apart) v[i / 2][i % 2] = dev::load8<kAlign>(at, k0 + 8 * c, row_of<kWide>(g, i) < left ? rank : 0);
+        if (kAlign == 16 && rank % 8 != 0) {                     // what stands behind an adapter's own rank
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (mine >> (8 * (t0 + t) + h) & 1) old[t][h].load(base + (8 * (t0 + t) + h) * p.ldbase);
+            for (int i = 0; i < 8; ++i) dev::cut8(v[i / 2][i % 2], k0 + 8 * c, rank);
         }
-    }
-    // `hi`, `lo`: the tile's vectors, `row` halves apart; `factors`: what undoes their scaling.  `asked`: ask(p, members or more, 0) was called.
-    __device__ __forceinline__ void add(const Params& p, unsigned members, int a, int rank, const __half* hi, const __half* lo, int row, const float* factors, bool asked) {
-        const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-        const __half* B = p.B + a * p.stride_b + m0 * p.ldb;
-        uint4 v[4][2];
-        auto weights = [&](int k0) {
-            const __half* at = B;
+    };
+    const __half* vector = hi + g * row + 8 * c;
+    auto vectors = [&](int k0) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i, at += p.ldb) v[i / 2][i % 2] = dev::load8<kAlign>(at, k0 + 8 * c, i < left ? rank : 0);
-            if (kAlign == 16 && rank % 8 != 0) {                 // what stands behind an adapter's own rank
+        for (int t = 0; t < kCols; ++t) {
+            x[t] = make_uint4(0, 0, 0, 0);
+            if (owner >> (8 * t) & 1) x[t] = *reinterpret_cast<const uint4*>(vector + 8 * t * row + k0);
+        }
+    };
+    if (a >= 0 && rank > 0) weights(0), vectors(0);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) dev::cut8(v[i / 2][i % 2], k0 + 8 * c, rank);
-            }
-        };
-        const __half* vector = hi + g * row + 8 * c;
-        const int64_t second = lo - hi;
-        uint4 x[kCols];
-        auto vectors = [&](int k0) {                             // other tokens' vectors may be another adapter's, or nobody's
-#pragma unroll
-            for (int t = 0; t < kCols; ++t) {
-                x[t] = make_uint4(0, 0, 0, 0);
-                if (members >> (8 * t + g) & 1) x[t] = *reinterpret_cast<const uint4*>(vector + 8 * t * row + k0);
-            }
-        };
-        if (!asked) ask(p, members, 0);
-        if (rank > 0) weights(0), vectors(0);
-#pragma unroll
-        for (int t0 = 0; t0 < kCols; t0 += kStep) {
-            if (t0 > 0 && t0 % kAhead == 0) ask(p, members, t0);
-            if (!(members >> (8 * t0) & (kStep == 2 ? 0xFFFFu : 0xFFu))) continue;
-            float acc[kStep][4][4] = {};
+    for (int t0 = 0; t0 < kCols; t0 += kStep) {
+        if (!(all >> (8 * t0) & (kStep == 2 ? 0xFFFFu : 0xFFu))) continue;
+        float acc[kStep][4][4] = {};
+        if (a >= 0) {
             for (int k0 = 0; k0 < rank; k0 += 32) {
                 if (rank > 32 && (k0 > 0 || t0 > 0)) weights(k0), vectors(k0);
 #pragma unroll
                 for (int t = 0; t < kStep; ++t) {
-                    if (!(members >> (8 * (t0 + t)) & 0xFFu)) continue;
                     uint4 z = make_uint4(0, 0, 0, 0);
-                    if (kTwo && (members >> (8 * (t0 + t) + g) & 1)) z = *reinterpret_cast<const uint4*>(vector + second + 8 * (t0 + t) * row + k0);
+                    if (kTwo && (owner >> (8 * (t0 + t)) & 1)) z = *reinterpret_cast<const uint4*>(vector + (lo - hi) + 8 * (t0 + t) * row + k0);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         dev::mma_f16(acc[t][i], v[i][0].x, v[i][1].x, v[i][0].y, v[i][1].y, x[t0 + t].x, x[t0 + t].y);
@@ -245,23 +192,43 @@ struct Block {
                     }
                 }
             }
+        }
+        if constexpr (kWide) {
 #pragma unroll
             for (int t = 0; t < kStep; ++t) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int n = 8 * (t0 + t) + h;              // behind the lane's first token
-                    if (!(members >> (n + 2 * c) & 1) || left <= 0) continue;
-                    const float down = factors[n + 2 * c];
+                    if (!there || !(members >> n & 1)) continue;
                     float o[8];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[2 * i] = acc[t][i][h], o[2 * i + 1] = acc[t][i][2 + h];
-                    if (wide) old[(t0 + t) % kAhead][h].add_store(y + n * p.ldy, o, down);
-                    else add_store_some(base + n * p.ldbase, y + n * p.ldy, o, down, left);
+                    for (int e = 0; e < 8; ++e) o[e] = acc[t][e / 2][2 * (e % 2) + h];
+                    const T* from = old != nullptr ? old + (n + 2 * c) * kOldRow<T> + 8 * g : base + n * p.ldbase + 8 * g;
+                    if (a < 0) {
+#pragma unroll
+                        for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) reinterpret_cast<uint4*>(y + n * p.ldy + 8 * g)[i] = reinterpret_cast<const uint4*>(from)[i];
+                    } else {
+                        add_eight(y + n * p.ldy + 8 * g, from, o, factors[n + 2 * c]);
+                    }
                 }
+            }
+        } else {                                                 // all values of base first: a store ends what may be read ahead of it
+            T in[kStep][2][8];
+#pragma unroll
+            for (int e = 0; e < 16 * kStep; ++e) {
+                const int t = e / 16, h = e / 8 % 2, n = 8 * (t0 + t) + h;
+                if ((members >> n & 1) && row_of<kWide>(g, e % 8) < left) in[t][h][e % 8] = base[n * p.ldbase + row_of<kWide>(g, e % 8)];
+            }
+#pragma unroll
+            for (int e = 0; e < 16 * kStep; ++e) {
+                const int t = e / 16, h = e / 8 % 2, n = 8 * (t0 + t) + h;
+                if (!(members >> n & 1) || row_of<kWide>(g, e % 8) >= left) continue;
+                const T b = in[t][h][e % 8];
+                y[n * p.ldy + row_of<kWide>(g, e % 8)] = a < 0 ? b : sum_of(b, acc[t][e % 8 / 2][2 * (e % 2) + h] * factors[n + 2 * c]);
             }
         }
     }
-};
+}
 
 // kSplit: this kernel ends with the vectors, in memory; else it does the second product too.
 template <int kRankTiles, int kCols, typename T, bool kSplit, int kAlign>
@@ -301,7 +268,8 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
         const int block0 = (share * kCluster + cta) * kWarps + w;
         if (a < 0) {
             if constexpr (!kSplit)
-                for (int b = block0; b < blocks; b += sharers * kBlocksOfCluster) copy_block<T>(p, n0, members, b * kOut);
+                for (int b = block0; b < blocks; b += sharers * kBlocksOfCluster)
+                    expand_block<T, kCols, kAlign, true>(p, n0, members, a, 0, b * kOut, hi, lo, row, factors, nullptr);
             continue;
         }
         const int rank = rank_of(p, a), prank = padded_rank(rank);
@@ -408,34 +376,91 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
             if (threadIdx.x < kCols && (members >> (cta * kCols + threadIdx.x) & 1)) p.factors[n0 + cta * kCols + threadIdx.x] = factors[cta * kCols + threadIdx.x];
         } else {
             for (int b = block0; b < blocks; b += sharers * kBlocksOfCluster)
-                Block<T, kCols, kAlign>(p, n0, b * kOut).add(p, members, a, rank, hi, lo, row, factors, false);
+                expand_block<T, kCols, kAlign, true>(p, n0, members, a, rank, b * kOut, hi, lo, row, factors, nullptr);
         }
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // nobody reads this CTA's sums any more
     }
 }
 
-// The second product where it has a kernel of its own: a block of output to a warp, the blocks of a tile one after another.
-template <typename T, int kAlign>
-__global__ void __launch_bounds__(32 * kExpandWarps, 3) lora_expand_kernel(const Params p) {
-    constexpr int kTok = 8 * kMostCols;
+// The second product where it has a kernel of its own: a warp takes blocks of a tile's output one after another, and copies
+// base of the next one to shared memory while it works on one (kWide; else base is read where it is).
+template <typename T, int kAlign, bool kWide>
+__global__ void __launch_bounds__(32 * kExpandWarps, sizeof(T) == 2 ? 4 : 3) lora_expand_kernel(const Params p) {
+    constexpr int kTok = 8 * kMostCols, kPiece = 16 / sizeof(T), kPieces = kOut / kPiece;        // values of 16 bytes, such pieces of a row
+    extern __shared__ float4 shared[];
     dev::programmatic_start();
-    const int blocks = (p.M + kOut - 1) / kOut, per_row = (blocks + kExpandWarps - 1) / kExpandWarps;
-    const int b = blockIdx.x % per_row * kExpandWarps + (threadIdx.x >> 5), z = blockIdx.x / per_row % p.per_tile;
-    const int64_t n0 = static_cast<int64_t>(blockIdx.x / per_row / p.per_tile) * kTok;
-    if (b >= blocks) return;
-    Block<T, kMostCols, kAlign> block(p, n0, b * kOut);
-    const bool early = p.per_tile == 1;                      // base of the whole tile, before it is known whose tokens they are
-    if (early) block.ask(p, p.N - n0 >= kTok ? 0xFFFFFFFFu : (1u << (p.N - n0)) - 1u, 0);
+    const int blocks = (p.M + kOut - 1) / kOut, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int q = blockIdx.x % p.per_row, z = blockIdx.x / p.per_row % p.per_tile;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x / p.per_row / p.per_tile) * kTok;
+    const int tokens = p.N - n0 < kTok ? static_cast<int>(p.N - n0) : kTok;
+    T* olds = reinterpret_cast<T*>(shared) + w * 2 * kTok * kOldRow<T>;          // two blocks
+    auto copy = [&](int b, int to) {
+        if constexpr (kWide) {
+            const T* from = static_cast<const T*>(p.base) + n0 * p.ldbase + b * kOut;
+            const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(olds + to * kTok * kOldRow<T>));
+            if (b < blocks) {
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) {
+                    const int n = i * (32 / kPieces) + lane / kPieces, part = lane % kPieces;
+                    if (n < tokens && b * kOut + part * kPiece < p.M)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + (n * kOldRow<T> + part * kPiece) * static_cast<int>(sizeof(T))),
+                                     "l"(from + n * p.ldbase + part * kPiece) : "memory");
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    };
+    const int b0 = q * kExpandWarps + w, step = p.per_row * kExpandWarps;
+    copy(b0, 0);
     const Tile tile(p, n0, kTok);
     const int G = tile.count(), width = padded_rank(p.rank);
     const __half* hi = p.vectors + n0 * width;
-    for (int d = z; d < G; d += p.per_tile) {
-        int a;
-        unsigned members;
-        tile.pick(d, a, members);
-        if (a < 0) copy_block<T>(p, n0, members, b * kOut);
-        else block.add(p, members, a, rank_of(p, a), hi, hi + static_cast<int64_t>(p.N) * width, width, p.factors + n0, early && (sizeof(T) == 2 || d == 0));
+    int a = -1, rank = 0;
+    unsigned members = 0;
+    if (z < G) {                                                 // most tiles have one adapter: known before the loop
+        tile.pick(z, a, members);
+        rank = a >= 0 ? rank_of(p, a) : 0;
+        for (int b = b0, i = 0; b < blocks; b += step, i ^= 1) {
+            copy(b + step, i ^ 1);
+            if constexpr (kWide) {
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+                __syncwarp();
+            }
+            for (int d = z; d < G; d += p.per_tile) {
+                if (G > p.per_tile) {
+                    tile.pick(d, a, members);
+                    rank = a >= 0 ? rank_of(p, a) : 0;
+                }
+                expand_block<T, kMostCols, kAlign, kWide>(p, n0, members, a, rank, b * kOut, hi, hi + static_cast<int64_t>(p.N) * width, width, p.factors + n0,
+                                                          kWide ? olds + i * kTok * kOldRow<T> : nullptr);
+            }
+            if constexpr (kWide) __syncwarp();                   // all lanes have read the block before it is overwritten
+        }
     }
+    if constexpr (kWide) asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
+template <typename T, int kAlign, bool kWide>
+cudaError_t launch_expand(Params p, int device, int sms, cudaStream_t s) {
+    static std::mutex mu;
+    static bool configured[64] = {};
+    const size_t bytes = kWide ? kExpandWarps * 2 * 8 * kMostCols * kOldRow<T> * sizeof(T) : 0;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!configured[device]) {
+            const cudaError_t e = cudaFuncSetAttribute(lora_expand_kernel<T, kAlign, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+            if (e != cudaSuccess) return e;
+        }
+        configured[device] = true;
+    }
+    // as many CTAs as the GPU holds at once
+    const int64_t tiles = (p.N + 8 * kMostCols - 1) / (8 * kMostCols), most = (p.M + kOut * kExpandWarps - 1) / (kOut * kExpandWarps);
+    const int64_t slots = (sizeof(T) == 2 ? 4 : 3) * static_cast<int64_t>(sms);
+    p.per_row = static_cast<int>(between(slots / tiles, 1, most));
+    p.per_tile = static_cast<int>(between(slots / (tiles * p.per_row), 1, p.N < 32 ? p.N : 32));
+    const int64_t size = tiles * p.per_row * p.per_tile;
+    if (size > INT32_MAX) return cudaErrorInvalidConfiguration;
+    return launch_programmatic(lora_expand_kernel<T, kAlign, kWide>, dim3(static_cast<unsigned>(size)), 32 * kExpandWarps, bytes, s, p);
 }
 
 template <int kRankTiles, int kCols, typename T, bool kSplit, int kAlign>
@@ -463,12 +488,10 @@ spdp_status launch_rank(const Params& p, int tiles, int device, cudaStream_t s) 
     return launch_form<4, kCols, T, kSplit, kAlign>(p, tiles, device, s);
 }
 
-int64_t between(int64_t v, int64_t low, int64_t high) { return v > high ? high : v < low ? low : v; }
-
 template <typename T>
 spdp_status launch_typed(Params p, int align, int device, int sms, cudaStream_t s) {
     const int blocks = (p.M + kOut - 1) / kOut, cluster_slots = 2 * sms / kCluster;
-    if (p.N <= kFusedTokens && align == 16) {
+    if (p.N <= kFusedTokens && align == 16 && p.wide_y) {
         // Clusters of a tile: two CTAs per SM in all, no more than there is work for
         const int64_t most = static_cast<int64_t>(p.N) * ((blocks + kBlocksOfCluster - 1) / kBlocksOfCluster);
         p.per_tile = static_cast<int>(between(cluster_slots, 1, most));
@@ -486,14 +509,9 @@ spdp_status launch_typed(Params p, int align, int device, int sms, cudaStream_t 
     if (align == 16) st = few ? launch_rank<1, T, true, 16>(p, tiles, device, s) : launch_rank<kMostCols, T, true, 16>(p, tiles, device, s);
     else st = align == 4 ? launch_rank<kMostCols, T, true, 4>(p, tiles, device, s) : launch_rank<kMostCols, T, true, 2>(p, tiles, device, s);
     if (st == SPDP_OK) {
-        const int64_t per_row = (blocks + kExpandWarps - 1) / kExpandWarps, rows = (p.N + 8 * kMostCols - 1) / (8 * kMostCols);
-        p.per_tile = static_cast<int>(between(8 * sms / (per_row * rows), 1, p.N < 32 ? p.N : 32));
-        const int64_t size = per_row * rows * p.per_tile;
-        const dim3 grid(static_cast<unsigned>(size));
-        const cudaError_t e = size > INT32_MAX ? cudaErrorInvalidConfiguration
-                              : align == 16    ? launch_programmatic(lora_expand_kernel<T, 16>, grid, 32 * kExpandWarps, 0, s, p)
-                              : align == 4     ? launch_programmatic(lora_expand_kernel<T, 4>, grid, 32 * kExpandWarps, 0, s, p)
-                                               : launch_programmatic(lora_expand_kernel<T, 2>, grid, 32 * kExpandWarps, 0, s, p);
+        const cudaError_t e = align == 16 ? (p.wide_y ? launch_expand<T, 16, true>(p, device, sms, s) : launch_expand<T, 16, false>(p, device, sms, s))
+                              : align == 4 ? (p.wide_y ? launch_expand<T, 4, true>(p, device, sms, s) : launch_expand<T, 4, false>(p, device, sms, s))
+                                           : (p.wide_y ? launch_expand<T, 2, true>(p, device, sms, s) : launch_expand<T, 2, false>(p, device, sms, s));
         if (e != cudaSuccess) {
             note_cuda_error(e, "lora_expand_kernel");
             st = SPDP_ERR_CUDA;
@@ -526,7 +544,7 @@ spdp_status launch_lora(const LoraCall& call, cudaStream_t s) {
     p.ldx = call.ldx, p.lda = call.lda, p.stride_a = call.stride_a, p.ldb = call.ldb, p.stride_b = call.stride_b, p.ldbase = call.ldbase, p.ldy = call.ldy;
     p.N = static_cast<int>(call.N), p.K = static_cast<int>(call.K), p.M = static_cast<int>(call.M);
     p.count = static_cast<int>(call.count), p.rank = call.rank;
-    p.wide_y = rows_aligned16(call.base, call.ldbase, size) && rows_aligned16(call.Y, call.ldy, size);
+    p.wide_y = call.M % 8 == 0 && rows_aligned16(call.base, call.ldbase, size) && rows_aligned16(call.Y, call.ldy, size);
     // 16-byte loads where every row of X, A and B starts on such a boundary and has whole pieces; else 4-byte or 2-byte ones
     int align = 16;
     for (const int v : {rows_alignment(call.X, call.ldx, 2), rows_alignment(call.A, call.lda | call.stride_a, 2), rows_alignment(call.B, call.ldb | call.stride_b, 2)})
