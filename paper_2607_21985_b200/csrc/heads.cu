@@ -54,8 +54,33 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const Params p) 
     __shared__ float2 turn[kMostDim / 2];
     dev::programmatic_start();
     const int64_t n = blockIdx.x;
-    const int half = p.dim / 2;
-    for (int i = threadIdx.x; i < half; i += kThreads) {
+    const int half = p.dim / 2, heads = p.q_heads + p.kv_heads;
+    const int lane = threadIdx.x & (p.lanes - 1), slots = blockDim.x >> p.shift;
+    // The lane's pairs, the same in every head.  Members: neighbours, or as far apart as the pairs that turn; what does not turn is
+    // split in two the same way.
+    int at[kRounds][2], pair[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int i = (r * p.lanes + lane) * kPairs;                // the lane's first pair
+        pair[r] = i < half ? i : -1;
+        if (kAdjacent) at[r][0] = 2 * i, at[r][1] = 2 * i + kPairs;
+        else if (i < p.pairs) at[r][0] = i, at[r][1] = i + p.pairs;
+        else at[r][0] = i + p.pairs, at[r][1] = i + half;
+    }
+    float x[kRounds][2][kPairs];
+    auto fetch = [&](int h) {
+        if (h >= heads) return;
+        const T* from = h < p.q_heads ? static_cast<const T*>(p.q) + n * p.ldq + h * p.dim : static_cast<const T*>(p.k) + n * p.ldk + (h - p.q_heads) * p.dim;
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+                if (pair[r] >= 0) load<T, kPairs>(from + at[r][m], x[r][m]);
+        }
+    };
+    int h = blockIdx.y * slots + (threadIdx.x >> p.shift);
+    fetch(h);                                                       // on its way while the angles are formed
+    for (int i = threadIdx.x; i < half; i += blockDim.x) {
         float2 cs = make_float2(1.0f, 0.0f);
         if (i < p.pairs) {
             int a = 0;
@@ -66,33 +91,27 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const Params p) 
         turn[i] = cs;
     }
     __syncthreads();
-    const int lane = threadIdx.x & (p.lanes - 1), slots = kThreads >> p.shift;
-    for (int h0 = blockIdx.y * slots; h0 < p.q_heads + p.kv_heads; h0 += gridDim.y * slots) {
-        const int h = h0 + (threadIdx.x >> p.shift);
-        const bool there = h < p.q_heads + p.kv_heads, is_q = h < p.q_heads;
-        const int64_t head = static_cast<int64_t>(is_q ? h : h - p.q_heads) * p.dim;
-        const T* from = static_cast<const T*>(is_q ? p.q : p.k) + n * (is_q ? p.ldq : p.ldk) + head;
+    for (int rounds = (heads - blockIdx.y * slots + gridDim.y * slots - 1) / (gridDim.y * slots); rounds > 0; --rounds) {      // the same for all threads
+        const bool is_q = h < p.q_heads;
         const __half* weight = is_q ? p.q_weight : p.k_weight;
-        float x[kRounds][2][kPairs];
-        int at[kRounds][2], pair[kRounds];
-        float squares = 0.0f;
+        float squares = 0.0f, y[kRounds][2][kPairs];
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
-            const int i = (r * p.lanes + lane) * kPairs;            // the lane's first pair
-            pair[r] = there && i < half ? i : -1;
-            // the members: neighbours, or as far apart as the pairs that turn; what does not turn is split in two the same way
-            if (kAdjacent) at[r][0] = 2 * i, at[r][1] = 2 * i + kPairs;
-            else if (i < p.pairs) at[r][0] = i, at[r][1] = i + p.pairs;
-            else at[r][0] = i + p.pairs, at[r][1] = i + half;
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
-                if (pair[r] < 0) continue;
-                load<T, kPairs>(from + at[r][m], x[r][m]);
 #pragma unroll
-                for (int j = 0; j < kPairs; ++j) squares += x[r][m][j] * x[r][m][j];
+                for (int j = 0; j < kPairs; ++j) {
+                    y[r][m][j] = x[r][m][j];
+                    if (h < heads && pair[r] >= 0) squares += y[r][m][j] * y[r][m][j];
+                }
             }
         }
+        __half* to = is_q ? p.q_out + n * p.ldq_out + h * p.dim : p.k_out + n * p.ldk_out + (h - p.q_heads) * p.dim;
+        const bool there = h < heads;
+        h += gridDim.y * slots;
+        fetch(h);
         for (int d = p.lanes / 2; d > 0; d >>= 1) squares += __shfl_xor_sync(0xFFFFFFFFu, squares, d);
+        if (!there) continue;
         if (weight != nullptr) {
             const float inv = 1.0f / sqrtf(squares / p.dim + p.eps);
 #pragma unroll
@@ -103,16 +122,15 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const Params p) 
                     float g[kPairs];
                     load<__half, kPairs>(weight + at[r][m], g);
 #pragma unroll
-                    for (int j = 0; j < kPairs; ++j) x[r][m][j] = x[r][m][j] * inv * g[j];
+                    for (int j = 0; j < kPairs; ++j) y[r][m][j] = y[r][m][j] * inv * g[j];
                 }
             }
         }
-        __half* to = (is_q ? p.q_out + n * p.ldq_out : p.k_out + n * p.ldk_out) + head;
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
             if (pair[r] < 0) continue;
-            // neighbours: a lane's 2 kPairs values are a0 b0 a1 b1 ...; else x[0] holds the first members and x[1] the second
-            float* flat = &x[r][0][0];
+            // neighbours: a lane's 2 kPairs values are a0 b0 a1 b1 ...; else y[0] holds the first members and y[1] the second
+            float* flat = &y[r][0][0];
 #pragma unroll
             for (int j = 0; j < kPairs; ++j) {
                 const float2 cs = turn[pair[r] + j];
@@ -121,22 +139,24 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const Params p) 
                 const float ra = a * cs.x - b * cs.y, rb = b * cs.x + a * cs.y;
                 a = ra, b = rb;
             }
-            store<kPairs>(to + at[r][0], x[r][0]);
-            store<kPairs>(to + at[r][1], x[r][1]);
+            store<kPairs>(to + at[r][0], y[r][0]);
+            store<kPairs>(to + at[r][1], y[r][1]);
         }
     }
 }
 
 template <typename T, int kPairs>
 spdp_status launch_form(const Params& p, bool adjacent, int64_t N, int sms, cudaStream_t s) {
-    const int heads = p.q_heads + p.kv_heads, slots = kThreads >> p.shift;
-    // one CTA takes a token's heads in turn (and its angles once) where the tokens fill the GPU; else they are dealt out
+    // Rounds of a token's heads, with no more threads than make them equal.  One CTA takes them in turn (and the angles once)
+    // where the tokens fill the GPU; else they are dealt out.
+    const int heads = p.q_heads + p.kv_heads, rounds = (heads + (kThreads >> p.shift) - 1) / (kThreads >> p.shift);
+    const int threads = ((heads + rounds - 1) / rounds * p.lanes + 31) / 32 * 32, slots = threads >> p.shift;
     int64_t shares = (heads + slots - 1) / slots;
     const int64_t enough = (8 * sms + N - 1) / N;
     if (shares > enough) shares = enough;
     const dim3 grid(static_cast<unsigned>(N), static_cast<unsigned>(shares));
-    SPDP_CUDA_TRY(adjacent ? launch_programmatic(qk_norm_rope_kernel<T, kPairs, true>, grid, kThreads, 0, s, p)
-                           : launch_programmatic(qk_norm_rope_kernel<T, kPairs, false>, grid, kThreads, 0, s, p));
+    SPDP_CUDA_TRY(adjacent ? launch_programmatic(qk_norm_rope_kernel<T, kPairs, true>, grid, threads, 0, s, p)
+                           : launch_programmatic(qk_norm_rope_kernel<T, kPairs, false>, grid, threads, 0, s, p));
     return SPDP_OK;
 }
 

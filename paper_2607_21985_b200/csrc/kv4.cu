@@ -26,57 +26,90 @@ struct StoreParams {
     __half* k_values;
     __half* v_values;
     int64_t ldk, ldv, ldk_values, ldv_values, N, pages;
-    int heads, dim, page_shift;
+    int heads, dim, page_shift, row_shift;      // pieces of 8 dimensions in a row: 2^row_shift
 };
 
-// A lane takes 8 dimensions, four neighbours a scale.  kWide: 16-byte accesses.
-template <typename T, bool kWide>
-__device__ __forceinline__ void store_row(const StoreParams& p, const T* from, int64_t ld, __half* values, int64_t ld_values, bool is_v, int64_t i) {
-    const int per_row = p.dim / 8;                               // lanes of a row: 8, 16 or 32
-    const int64_t row = i / per_row, n = row / p.heads;
-    const bool there = n < p.N;
-    const int h = static_cast<int>(row % p.heads), piece = static_cast<int>(i % per_row), c = piece & 3, g = piece >> 2;
-    float x[8] = {};
-    if (there) dev::load_floats<T, kWide>(from + n * ld + h * p.dim + 8 * piece, x);
-    float top = 0.0f;
+// x / s, correctly rounded where the quotient is a number of 24 bits (as where a code lies half way between two, which are n +
+// 1/2) and else to within a step: a product with the reciprocal, corrected by its exact remainder (Markstein).  Quotients of fp16
+// numbers that are not half way are 2^-12 and more of their size away from it, so rint() gives what it gives for the true quotient.
+__device__ __forceinline__ float quotient(float x, float s, float reciprocal) {
+    const float q = x * reciprocal;
+    return fmaf(fmaf(-q, s, x), reciprocal, q);
+}
+
+// A thread takes 8 dimensions (a piece; four neighbouring threads a scale) of kTokens tokens, whose loads are on their way at
+// once.  blockDim.x: the pieces of a token, or 256 of them at a time; blockDim.y: tokens.  kWide: 16-byte accesses.
+template <typename T, bool kWide, int kTokens>
+__device__ __forceinline__ void store_rows(const StoreParams& p, const T* from, int64_t ld, __half* values, int64_t ld_values, bool is_v) {
+    const int P = 1 << p.page_shift, groups = p.dim / 32, row_bytes = p.dim / 2;
+    const unsigned head_bytes = P * (p.dim + p.dim / 8), page_bytes = p.heads * head_bytes;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * (kTokens * blockDim.y) + threadIdx.y;
+    const unsigned four = 0xFu << ((threadIdx.y * blockDim.x + threadIdx.x) & 28);      // the lanes of a scale come and go together
+    for (int t = threadIdx.x; t < p.heads << p.row_shift; t += blockDim.x) {
+        float x[kTokens][8];
+        int64_t slot[kTokens];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        if constexpr (sizeof(T) == 4) x[j] = __half2float(__float2half_rn(x[j]));        // 32-bit rows count as the fp16 row they round to
-        top = fmaxf(top, fabsf(x[j]));
-    }
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-    if (!there) return;
-    const __half scale = __float2half_rn(__fdiv_rn(top, 7.0f));
-    const float s = __half2float(scale);
-    uint32_t word = 0;
-    float step[8];
+        for (int j = 0; j < kTokens; ++j) {
+            const int64_t n = n0 + j * blockDim.y;
+            if (n >= p.N) continue;
+            slot[j] = p.slot[n];
+            dev::load_floats<T, kWide>(from + n * ld + 8 * t, x[j]);
+        }
+        const int piece = t & ((1 << p.row_shift) - 1), c = piece & 3, g = piece >> 2;
+        unsigned char* head = p.cache + (t >> p.row_shift) * static_cast<int64_t>(head_bytes);
+        unsigned char* word_at = head + (is_v ? P * row_bytes : 0) + 4 * (c * groups + g);
+        unsigned char* scale_at = head + 2 * P * row_bytes + (is_v ? P * groups * 2 : 0) + 2 * g;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        step[j] = s > 0.0f ? fminf(fmaxf(rintf(__fdiv_rn(x[j], s)), -7.0f), 7.0f) : 0.0f;
-        word |= static_cast<uint32_t>(static_cast<int>(step[j]) + 8) << (4 * j);
-    }
-    const int64_t slot = p.slot[n], page = slot >> p.page_shift;
-    if (slot >= 0 && page < p.pages) {
-        const int P = 1 << p.page_shift, groups = p.dim / 32, at = static_cast<int>(slot & (P - 1));
-        const int64_t codes = static_cast<int64_t>(P) * (p.dim / 2), scales = static_cast<int64_t>(P) * groups * 2;
-        unsigned char* head = p.cache + (page * p.heads + h) * 2 * (codes + scales);
-        reinterpret_cast<uint32_t*>(head + (is_v ? codes : 0) + static_cast<int64_t>(at) * (p.dim / 2))[c * groups + g] = word;
-        if (c == 0) reinterpret_cast<__half*>(head + 2 * codes + (is_v ? scales : 0))[at * groups + g] = scale;
-    }
-    if (values != nullptr) {
+        for (int j = 0; j < kTokens; ++j) {
+            const int64_t n = n0 + j * blockDim.y;
+            if (n >= p.N) continue;
+            float top = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) step[j] *= s;
-        dev::store_halves<kWide>(values + n * ld_values + h * p.dim + 8 * piece, step);
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (sizeof(T) == 4) x[j][e] = __half2float(__float2half_rn(x[j][e]));          // 32-bit rows count as the fp16 row they round to
+                top = fmaxf(top, fabsf(x[j][e]));
+            }
+            top = fmaxf(top, __shfl_xor_sync(four, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(four, top, 2));
+            const __half scale = __float2half_rn(__fdiv_rn(top, 7.0f));
+            const float s = __half2float(scale), reciprocal = s > 0.0f ? __frcp_rn(s) : 0.0f;
+            // Adding 1.5 2^23 + 8 rounds to a whole number, ties to even, and leaves it, 8 more, in the lowest bits
+            constexpr float kWhole = 12582912.0f + 8.0f;
+            constexpr uint32_t kWholeBits = 0x4B400000u;
+            uint32_t word = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float whole = fminf(fmaxf(quotient(x[j][e], s, reciprocal), -7.0f), 7.0f) + kWhole;
+                word += (__float_as_uint(whole) - kWholeBits) << (4 * e);
+                x[j][e] = (whole - kWhole) * s;
+            }
+            const int64_t page = slot[j] >> p.page_shift;
+            if (slot[j] >= 0 && page < p.pages) {
+                const uint64_t first = static_cast<uint64_t>(static_cast<unsigned>(page)) * page_bytes;
+                const unsigned at = static_cast<unsigned>(slot[j]) & (P - 1);
+                *reinterpret_cast<uint32_t*>(word_at + first + at * row_bytes) = word;
+                if (c == 0) *reinterpret_cast<__half*>(scale_at + first + at * groups * 2) = scale;
+            }
+            if (values != nullptr) dev::store_halves<kWide>(values + n * ld_values + 8 * t, x[j]);
+        }
     }
 }
 
-template <typename V, bool kWide>
+template <typename V, bool kWide, int kTokens>
 __global__ void __launch_bounds__(kStoreThreads) kv4_store_kernel(const StoreParams p) {
     dev::programmatic_start();
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * kStoreThreads + threadIdx.x;
-    if (blockIdx.y == 0) store_row<__half, kWide>(p, p.k, p.ldk, p.k_values, p.ldk_values, false, i);
-    else store_row<V, kWide>(p, static_cast<const V*>(p.v), p.ldv, p.v_values, p.ldv_values, true, i);
+    if (blockIdx.y == 0) store_rows<__half, kWide, kTokens>(p, p.k, p.ldk, p.k_values, p.ldk_values, false);
+    else store_rows<V, kWide, kTokens>(p, static_cast<const V*>(p.v), p.ldv, p.v_values, p.ldv_values, true);
+}
+
+template <typename V, bool kWide>
+cudaError_t launch_store(const StoreParams& p, int sms, cudaStream_t s) {
+    const int pieces = p.heads << p.row_shift;
+    const dim3 block(pieces < kStoreThreads ? pieces : kStoreThreads, pieces < kStoreThreads ? kStoreThreads / pieces : 1);
+    // two tokens to a thread where that still fills the GPU
+    const int64_t ctas = (p.N + block.y - 1) / block.y;
+    if (ctas > 8 * sms) return launch_programmatic(kv4_store_kernel<V, kWide, 2>, dim3(static_cast<unsigned>((ctas + 1) / 2), 2), block, 0, s, p);
+    return launch_programmatic(kv4_store_kernel<V, kWide, 1>, dim3(static_cast<unsigned>(ctas), 2), block, 0, s, p);
 }
 
 // ---- attention --------------------------------------------------------------------------------------------------------------
@@ -712,6 +745,9 @@ int log2_of(int v) {
 }  // namespace
 
 spdp_status launch_kv4_store(const Kv4StoreCall& call, cudaStream_t s) {
+    int device = 0, sms = 0;
+    const spdp_status st = current_device(&device, &sms);
+    if (st != SPDP_OK) return st;
     StoreParams p = {};
     p.k = call.k, p.v = call.v, p.slot = call.slot, p.cache = call.cache, p.k_values = call.k_values, p.v_values = call.v_values;
     p.ldk = call.ldk, p.ldv = call.ldv, p.ldk_values = call.ldk_values, p.ldv_values = call.ldv_values, p.N = call.N, p.pages = call.pages;
@@ -719,14 +755,9 @@ spdp_status launch_kv4_store(const Kv4StoreCall& call, cudaStream_t s) {
     const bool f32 = call.vdt == SPDP_Y_F32;
     const bool wide = rows_aligned16(p.k, p.ldk, 2) && rows_aligned16(p.v, p.ldv, f32 ? 4 : 2) && rows_aligned16(p.k_values, p.ldk_values, 2) &&
                       rows_aligned16(p.v_values, p.ldv_values, 2);
-    const int64_t threads = p.N * p.heads * (p.dim / 8);
-    const dim3 grid(static_cast<unsigned>((threads + kStoreThreads - 1) / kStoreThreads), 2);
-    if (f32)
-        SPDP_CUDA_TRY(wide ? launch_programmatic(kv4_store_kernel<float, true>, grid, kStoreThreads, 0, s, p)
-                           : launch_programmatic(kv4_store_kernel<float, false>, grid, kStoreThreads, 0, s, p));
-    else
-        SPDP_CUDA_TRY(wide ? launch_programmatic(kv4_store_kernel<__half, true>, grid, kStoreThreads, 0, s, p)
-                           : launch_programmatic(kv4_store_kernel<__half, false>, grid, kStoreThreads, 0, s, p));
+    p.row_shift = log2_of(p.dim / 8);
+    SPDP_CUDA_TRY(f32 ? (wide ? launch_store<float, true>(p, sms, s) : launch_store<float, false>(p, sms, s))
+                      : (wide ? launch_store<__half, true>(p, sms, s) : launch_store<__half, false>(p, sms, s)));
     return SPDP_OK;
 }
 

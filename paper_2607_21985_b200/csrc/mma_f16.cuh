@@ -120,10 +120,10 @@ inline bool rows_aligned16(const void* p, int64_t ld, int64_t size) { return row
 
 // A launch that may be set up while the kernel before it still runs (programmatic_start() in the kernel waits for it).
 template <typename... Formal, typename... Actual>
-cudaError_t launch_programmatic(void (*kernel)(Formal...), dim3 grid, int threads, size_t shared_bytes, cudaStream_t s, const Actual&... args) {
+cudaError_t launch_programmatic(void (*kernel)(Formal...), dim3 grid, dim3 threads, size_t shared_bytes, cudaStream_t s, const Actual&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.blockDim = threads;
     cfg.dynamicSmemBytes = shared_bytes;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
