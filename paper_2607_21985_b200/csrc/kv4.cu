@@ -6,10 +6,14 @@
 // [P][D/32] and of the values [P][D/32].  In a row of codes the dimension 32 g + 8 c + j is nibble j of word c D/32 + g: so the
 // four lanes that share a key in a matrix product's fragment each read one run of 16 bytes (D = 128), and what a lane holds
 // for one step of the product all belongs to one scale.
+#include <cooperative_groups.h>
+
 #include <mutex>
 
 #include "mma_f16.cuh"
 #include "spdp_internal.h"
+
+namespace cg = cooperative_groups;
 
 namespace spdp {
 namespace {
@@ -299,12 +303,312 @@ __device__ __forceinline__ void store_result(const AttnParams& p, int b, int64_t
     if (p.mask != nullptr && (threadIdx.x & 7) == 0) p.mask[b * p.mask_stride + column / 32] = keep;
 }
 
-// kGroups = D / 32; kCols: blocks of 8 query heads.
+// A CTA's warps over the keys k0 .. k1 - 1 of a triple: a warp's sums [kRows][kDim] end up in its part of `rings`, its maxima and
+// weights in warp_stats [warp][kRows].  kGroups = D / 32; kCols: blocks of 8 query heads.
 template <int kGroups, int kCols>
-__global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 4) attn_kernel(const AttnParams p) {
-    constexpr int kDim = 32 * kGroups, kRows = 8 * kCols;
-    constexpr int kRing = 2 * kStages * Chunk<kGroups>::kBytes; // bytes of a warp
+struct Shape {
+    static constexpr int kDim = 32 * kGroups, kRows = 8 * kCols;
+    static constexpr int kRing = 2 * kStages * Chunk<kGroups>::kBytes;      // bytes of a warp
+    static constexpr int kCtasOfSm = kGroups == 8 ? 2 : kCols == 2 ? 3 : 4; // that the registers are cut for
     static_assert(kRing >= kRows * kDim * 4 && kRing % 16 == 0, "a warp's sums take the place of its chunks");
+};
+
+template <int kGroups, int kCols>
+__device__ __forceinline__ void attend(const AttnParams& p, int b, int h, int row0, int k0, int k1, int end, unsigned char* rings, float2* warp_stats) {
+    using S = Shape<kGroups, kCols>;
+    constexpr int kDim = S::kDim, kRows = S::kRows, kRing = S::kRing;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+    const int P = 1 << p.page_shift, rows = min(kRows, p.group - row0);
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(rings)) + w * kRing;
+    const unsigned head_bytes = P * 36 * kGroups, page_bytes = head_bytes * p.heads;
+    const int window_low = p.window > 0 && end > p.window ? static_cast<int>(end - p.window) : 0;
+    const int32_t* table = p.table + b * p.table_stride;
+
+    // the warp's stages: every fourth one of the run.  Each lane knows the page of a chunk of 16 of them, and of the next 16
+    using C = Chunk<kGroups>;
+    const int stages = ((k1 - k0 + 31) / 32 - w + kWarps - 1) / kWarps;
+    auto first_key = [&](int i) { return k0 + 32 * (w + kWarps * i); };
+    auto page_of = [&](int i) {
+        const int key = first_key(i + (lane >> 1)) + 16 * (lane & 1);
+        return key < k1 ? table[key >> p.page_shift] : -1;
+    };
+    int pages = page_of(0), pages_after = page_of(16);
+    unsigned there = 0;                                     // two bits for each stage that was asked for: which of its chunks exist
+    const unsigned char* cache = p.cache + h * static_cast<int64_t>(head_bytes);
+    auto ask = [&](int i) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const unsigned page = __shfl_sync(0xFFFFFFFFu, pages, 2 * i + j & 31);
+            const bool ok = page < p.pages;                 // negative ones are large here
+            there = there << 1 | (ok ? 1u : 0u);
+            if (ok) {
+                const unsigned char* head = cache + static_cast<uint64_t>(page) * page_bytes;
+                const int at = (first_key(i) + 16 * j) & (P - 1);
+                copy_chunk<kGroups>(ring + (i % kStages * 2 + j) * C::kBytes, head + at * C::kRow + 16 * lane, head + 2 * P * C::kRow + at * 2 * kGroups, P, lane);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if ((i & 15) == 15) pages = pages_after, pages_after = page_of(i + 17);
+    };
+    ask(0);
+
+    // The query heads as the products' columns, in the order that the codes' pairs have.  A code n is taken from its word by
+    // one logical operation, as the subnormal fp16 number n 2^-24 or, four bits up, n 2^-20: the heads are scaled by a power of two
+    // of their own (2^10 <= largest < 2^11, so that it costs no digits) and 2^4 more where the former meet them.  That a code
+    // stands for n - 8 takes a product of its own, of the keys' scales and -8 times the sums of the heads' 32 dimensions: its
+    // columns k hold the scales twice, against the upper and the lower 11 bits of these sums.
+    uint32_t q[kCols][2 * kGroups][2];
+    uint32_t minus[kCols][2] = {};
+    float factor[kCols][2];
+#pragma unroll
+    for (int n = 0; n < kCols; ++n) {
+        const int row = 8 * n + g;
+        const __half* at = p.q + b * p.ldq + static_cast<int64_t>(h * p.group + row0 + row) * kDim + 8 * c;
+        float x[kGroups][8], most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+            if (row >= rows) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[i][j] = 0.0f;
+            } else if (p.wide_q) dev::load_floats<__half, true>(at + 32 * i, x[i]);
+            else dev::load_floats<__half, false>(at + 32 * i, x[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[i][j]));
+        }
+        most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+        const int exponent = max(100, min(150, __float_as_int(most) >> 23 & 255));       // of 0, Inf and NaN: a plain number
+        const float up = __int_as_float((127 + 10 + 127 - exponent) << 23), down = __int_as_float((127 + 20 - 10 - 127 + exponent) << 23);
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float f = j & 1 ? up : 16.0f * up;
+                const __half2 v = __floats2half2_rn(x[i][j] * f, x[i][j + 4] * f);
+                q[n][2 * i + (j >> 1)][j & 1] = *reinterpret_cast<const uint32_t*>(&v);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kGroups; i += 2) {              // two scales to a register: the word i / 2 of the keys' scales
+            float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[m] += x[i + m][j];
+                sum[m] += __shfl_xor_sync(0xFFFFFFFFu, sum[m], 1);
+                sum[m] += __shfl_xor_sync(0xFFFFFFFFu, sum[m], 2);
+                sum[m] *= -8.0f * up * 0x1p-20f;
+            }
+            const __half2 high = __floats2half2_rn(sum[0], sum[1]);
+            const float2 h2 = __half22float2(high);
+            const __half2 low = __floats2half2_rn(sum[0] - h2.x, sum[1] - h2.y);
+            if (c == i / 2) minus[n][0] = *reinterpret_cast<const uint32_t*>(&high);
+            if (kGroups == 8) {
+                if (c == i / 2) minus[n][1] = *reinterpret_cast<const uint32_t*>(&low);
+            } else if (c == i / 2 + kGroups / 2) {
+                minus[n][0] = *reinterpret_cast<const uint32_t*>(&low);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) factor[n][i] = p.scale * __shfl_sync(0xFFFFFFFFu, down, 4 * (2 * c + i));
+    }
+    float acc[kCols][2 * kGroups][4] = {};
+    float top[kCols][2], weight[kCols][2];
+#pragma unroll
+    for (int n = 0; n < kCols; ++n) top[n][0] = top[n][1] = kLowest, weight[n][0] = weight[n][1] = 0.0f;
+
+    for (int i = 0; i < stages; ++i) {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();                                       // all lanes' copies are there, and all have read the stage before
+        const unsigned have = there;
+        ask(i + 1);
+        if ((have & 3) == 0) continue;                      // pages that do not exist
+        const int key = first_key(i);
+        const unsigned char* stage = rings + w * kRing + i % kStages * 2 * C::kBytes;
+        const bool whole = (have & 3) == 3 && key >= window_low && key + 32 <= k1;
+        auto counts = [&](int at, int j) { return at >= window_low && at < k1 && (have >> (1 - j) & 1); };
+
+        float score[kCols][2][4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const unsigned char* chunk = stage + j * C::kBytes;
+            uint32_t k[2][kGroups], ks[2][kGroups / 2];     // keys g and g + 8
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                load_words<kGroups>(chunk + (g + 8 * m) * C::kRow + c * 4 * kGroups, k[m]);
+                load_words<kGroups / 2>(chunk + C::kKeyScales + (g + 8 * m) * 2 * kGroups, ks[m]);
+            }
+            uint32_t both[2];                               // the lane's part of the scales' product
+#pragma unroll
+            for (int m = 0; m < 2; ++m) both[m] = *reinterpret_cast<const uint32_t*>(chunk + C::kKeyScales + (g + 8 * m) * 2 * kGroups + c % (kGroups / 2) * 4);
+#pragma unroll
+            for (int n = 0; n < kCols; ++n)
+                dev::mma_f16_from(score[n][j], 0.0f, 0.0f, 0.0f, 0.0f, both[0], both[1], kGroups == 8 ? both[0] : 0u, kGroups == 8 ? both[1] : 0u, minus[n][0], minus[n][1]);
+#pragma unroll
+            for (int t = 0; t < kGroups; ++t) {
+                const float2 s0 = __half22float2(*reinterpret_cast<const __half2*>(&ks[0][t / 2])), s1 = __half22float2(*reinterpret_cast<const __half2*>(&ks[1][t / 2]));
+                const float f0 = t & 1 ? s0.y : s0.x, f1 = t & 1 ? s1.y : s1.x;
+                const uint32_t a = k[0][t], b = k[1][t], a8 = a >> 8, b8 = b >> 8;
+                constexpr uint32_t kLow = 0x000F000Fu, kHigh = 0x00F000F0u;
+#pragma unroll
+                for (int n = 0; n < kCols; ++n) {
+                    float d[4];
+                    dev::mma_f16_from(d, 0.0f, 0.0f, 0.0f, 0.0f, a & kLow, b & kLow, a & kHigh, b & kHigh, q[n][2 * t][0], q[n][2 * t][1]);
+                    dev::mma_f16(d, a8 & kLow, b8 & kLow, a8 & kHigh, b8 & kHigh, q[n][2 * t + 1][0], q[n][2 * t + 1][1]);
+                    score[n][j][0] += d[0] * f0, score[n][j][1] += d[1] * f0;
+                    score[n][j][2] += d[2] * f1, score[n][j][3] += d[3] * f1;
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < kCols; ++n) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int m = 0; m < 4; ++m) score[n][j][m] *= factor[n][m & 1];
+            }
+            if (p.cap > 0.0f) {                             // cap * tanh(s / cap) as 1 - 2 / (e^2x + 1), which keeps its limits
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) score[n][j][m] = p.cap * (1.0f - __fdividef(2.0f, exp2_of(score[n][j][m] * p.cap_inv) + 1.0f));
+                }
+            }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    if (counts(key + 16 * j + g + 8 * m, j)) continue;
+#pragma unroll
+                    for (int n = 0; n < kCols; ++n) score[n][j][2 * m] = score[n][j][2 * m + 1] = -INFINITY;
+                }
+            }
+        }
+        uint32_t weights[kCols][2][2];
+#pragma unroll
+        for (int n = 0; n < kCols; ++n) {
+            float high[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) high[m] = fmaxf(fmaxf(score[n][0][m], score[n][0][2 + m]), fmaxf(score[n][1][m], score[n][1][2 + m]));
+            const bool higher = high[0] > top[n][0] + kSlack || high[1] > top[n][1] + kSlack;
+            if (__any_sync(0xFFFFFFFFu, higher)) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    float most = fmaxf(top[n][m], high[m]);
+#pragma unroll
+                    for (int d = 4; d < 32; d *= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+                    const float f = exp2_of(top[n][m] - most);
+                    top[n][m] = most;
+                    weight[n][m] *= f;
+#pragma unroll
+                    for (int t = 0; t < 2 * kGroups; ++t) acc[n][t][m] *= f, acc[n][t][2 + m] *= f;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    score[n][j][m] = exp2_of(score[n][j][m] - top[n][m & 1]);
+                    weight[n][m & 1] += score[n][j][m];
+                }
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const __half2 pair = __floats2half2_rn(score[n][j][2 * m], score[n][j][2 * m + 1]);
+                    weights[n][j][m] = transpose8x8(*reinterpret_cast<const uint32_t*>(&pair));
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const unsigned char* chunk = stage + j * C::kBytes;
+            uint32_t v[4][kGroups / 2], vs[4][(kGroups + 3) / 4];       // keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                const int row = 2 * c + (m & 1) + 8 * (m >> 1);
+                load_words<kGroups / 2>(chunk + C::kValues + row * C::kValueRow + g * 2 * kGroups, v[m]);
+                const unsigned char* s = chunk + C::kValueScales + row * 2 * kGroups + (g & 1) * kGroups;
+                if constexpr (kGroups == 2) vs[m][0] = *reinterpret_cast<const uint16_t*>(s);
+                else load_words<kGroups / 4>(s, vs[m]);
+            }
+            if (!whole) {                                   // keys that do not count, whatever the page holds there
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    if (counts(key + 16 * j + 2 * c + (m & 1) + 8 * (m >> 1), j)) continue;
+#pragma unroll
+                    for (int t = 0; t < (kGroups + 3) / 4; ++t) vs[m][t] = 0;
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < kGroups / 2; ++t) {
+                const uint32_t sel = t & 1 ? 0x7632 : 0x5410;
+                const uint32_t sab = __byte_perm(vs[0][t / 2], vs[1][t / 2], sel), scd = __byte_perm(vs[2][t / 2], vs[3][t / 2], sel);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t take = half ? 0x7632 : 0x5410;
+                    uint32_t ab[4], cd[4];
+                    pairs_of(__byte_perm(v[0][t], v[1][t], take), ab);
+                    pairs_of(__byte_perm(v[2][t], v[3][t], take), cd);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) ab[m] = times(ab[m], sab), cd[m] = times(cd[m], scd);
+#pragma unroll
+                    for (int n = 0; n < kCols; ++n) {
+                        dev::mma_f16(acc[n][4 * t + 2 * half], ab[0], ab[1], cd[0], cd[1], weights[n][j][0], weights[n][j][1]);
+                        dev::mma_f16(acc[n][4 * t + 2 * half + 1], ab[2], ab[3], cd[2], cd[3], weights[n][j][0], weights[n][j][1]);
+                    }
+                }
+            }
+        }
+    }
+
+    // the warps' sums, joined
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncwarp();
+    float* sums = reinterpret_cast<float*>(rings + w * kRing);
+#pragma unroll
+    for (int n = 0; n < kCols; ++n) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int d = 4; d < 32; d *= 2) weight[n][i] += __shfl_xor_sync(0xFFFFFFFFu, weight[n][i], d);
+            const int row = 8 * n + 2 * c + i;
+            if (g == 0) warp_stats[w * kRows + row] = make_float2(top[n][i], weight[n][i]);
+            float* to = sums + row * kDim;
+#pragma unroll
+            for (int j = 0; j < 2 * kGroups; ++j) {
+                const int word = g * (kGroups / 2) + j / 4;         // of the row's words; its dimensions 2 (j % 4) and the next
+                const int d = word % kGroups * 32 + word / kGroups * 8 + 2 * (j % 4);
+                *reinterpret_cast<float2*>(to + d) = make_float2(acc[n][j][i], acc[n][j][2 + i]);
+            }
+        }
+    }
+}
+
+// A CTA's sums of four neighbouring dimensions of a row, from its warps'; (maximum, weight) in `stat`.
+template <int kGroups, int kCols>
+__device__ __forceinline__ float4 join_warps(const unsigned char* rings, const float2* warp_stats, int row, int d, float2& stat) {
+    using S = Shape<kGroups, kCols>;
+    float m = kLowest, wt = 0.0f;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) m = fmaxf(m, warp_stats[i * S::kRows + row].x);
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+        const float2 st = warp_stats[i * S::kRows + row];
+        const float f = exp2_of(st.x - m);
+        const float4 v = *reinterpret_cast<const float4*>(rings + i * S::kRing + (row * S::kDim + d) * 4);
+        wt += st.y * f;
+        sum.x += v.x * f, sum.y += v.y * f, sum.z += v.z * f, sum.w += v.w * f;
+    }
+    stat = make_float2(m, wt);
+    return sum;
+}
+
+template <int kGroups, int kCols>
+__global__ void __launch_bounds__(kThreads, Shape<kGroups, kCols>::kCtasOfSm) attn_kernel(const AttnParams p) {
+    using S = Shape<kGroups, kCols>;
+    constexpr int kDim = S::kDim, kRows = S::kRows, kRing = S::kRing;
     extern __shared__ float4 shared[];
     unsigned char* rings = reinterpret_cast<unsigned char*>(shared);                    // [warp]: the stages, then sums [kRows][kDim]
     float2* warp_stats = reinterpret_cast<float2*>(rings + kWarps * kRing);             // [warp][kRows]
@@ -325,11 +629,6 @@ __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 
     const int total = first[p.B], ctas = min(static_cast<int>(gridDim.x), total);       // so that no CTA between two others has nothing
     if (static_cast<int>(blockIdx.x) >= ctas) return;
     const int begin = run_start(total, ctas, blockIdx.x), stop = run_start(total, ctas, blockIdx.x + 1);
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-    const int P = 1 << p.page_shift;
-    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(rings)) + w * kRing;
-    const unsigned head_bytes = P * 36 * kGroups, page_bytes = head_bytes * p.heads;
-
     int pieces = 0;
     for (int u = begin; u < stop;) {
         int b = 0;                                              // the last request that does not begin behind u: it has keys
@@ -346,291 +645,20 @@ __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 
         if (count <= 0) continue;                               // the run ends before the triple's first unit
         const int h = triple / p.row_blocks, row0 = triple % p.row_blocks * kRows, rows = min(kRows, p.group - row0);
         const int k0 = span.low + off * kUnit, k1 = min(span.end, k0 + count * kUnit);
-        const int window_low = p.window > 0 && span.end > p.window ? static_cast<int>(span.end - p.window) : 0;
-        const int32_t* table = p.table + b * p.table_stride;
-
-        // the warp's stages: every fourth one of the run.  Each lane knows the page of a chunk of 16 of them, and of the next 16
-        using C = Chunk<kGroups>;
-        const int stages = ((k1 - k0 + 31) / 32 - w + kWarps - 1) / kWarps;
-        auto first_key = [&](int i) { return k0 + 32 * (w + kWarps * i); };
-        auto page_of = [&](int i) {
-            const int key = first_key(i + (lane >> 1)) + 16 * (lane & 1);
-            return key < k1 ? table[key >> p.page_shift] : -1;
-        };
-        int pages = page_of(0), pages_after = page_of(16);
-        unsigned there = 0;                                     // two bits for each stage that was asked for: which of its chunks exist
-        const unsigned char* cache = p.cache + h * static_cast<int64_t>(head_bytes);
-        auto ask = [&](int i) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const unsigned page = __shfl_sync(0xFFFFFFFFu, pages, 2 * i + j & 31);
-                const bool ok = page < p.pages;                 // negative ones are large here
-                there = there << 1 | (ok ? 1u : 0u);
-                if (ok) {
-                    const unsigned char* head = cache + static_cast<uint64_t>(page) * page_bytes;
-                    const int at = (first_key(i) + 16 * j) & (P - 1);
-                    copy_chunk<kGroups>(ring + (i % kStages * 2 + j) * C::kBytes, head + at * C::kRow + 16 * lane, head + 2 * P * C::kRow + at * 2 * kGroups, P, lane);
-                }
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            if ((i & 15) == 15) pages = pages_after, pages_after = page_of(i + 17);
-        };
-        ask(0);
-
-        // The query heads as the products' columns, in the order that the codes' pairs have.  A code n is taken from its word by
-        // one logical operation, as the subnormal fp16 number n 2^-24 or, four bits up, n 2^-20: the heads are scaled by a power of two
-        // of their own (2^10 <= largest < 2^11, so that it costs no digits) and 2^4 more where the former meet them.  That a code
-        // stands for n - 8 takes a product of its own, of the keys' scales and -8 times the sums of the heads' 32 dimensions: its
-        // columns k hold the scales twice, against the upper and the lower 11 bits of these sums.
-        uint32_t q[kCols][2 * kGroups][2];
-        uint32_t minus[kCols][2] = {};
-        float factor[kCols][2];
-#pragma unroll
-        for (int n = 0; n < kCols; ++n) {
-            const int row = 8 * n + g;
-            const __half* at = p.q + b * p.ldq + static_cast<int64_t>(h * p.group + row0 + row) * kDim + 8 * c;
-            float x[kGroups][8], most = 0.0f;
-#pragma unroll
-            for (int i = 0; i < kGroups; ++i) {
-                if (row >= rows) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[i][j] = 0.0f;
-                } else if (p.wide_q) dev::load_floats<__half, true>(at + 32 * i, x[i]);
-                else dev::load_floats<__half, false>(at + 32 * i, x[i]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[i][j]));
-            }
-            most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
-            most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-            const int exponent = max(100, min(150, __float_as_int(most) >> 23 & 255));       // of 0, Inf and NaN: a plain number
-            const float up = __int_as_float((127 + 10 + 127 - exponent) << 23), down = __int_as_float((127 + 20 - 10 - 127 + exponent) << 23);
-#pragma unroll
-            for (int i = 0; i < kGroups; ++i) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float f = j & 1 ? up : 16.0f * up;
-                    const __half2 v = __floats2half2_rn(x[i][j] * f, x[i][j + 4] * f);
-                    q[n][2 * i + (j >> 1)][j & 1] = *reinterpret_cast<const uint32_t*>(&v);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kGroups; i += 2) {              // two scales to a register: the word i / 2 of the keys' scales
-                float sum[2] = {0.0f, 0.0f};
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) sum[m] += x[i + m][j];
-                    sum[m] += __shfl_xor_sync(0xFFFFFFFFu, sum[m], 1);
-                    sum[m] += __shfl_xor_sync(0xFFFFFFFFu, sum[m], 2);
-                    sum[m] *= -8.0f * up * 0x1p-20f;
-                }
-                const __half2 high = __floats2half2_rn(sum[0], sum[1]);
-                const float2 h2 = __half22float2(high);
-                const __half2 low = __floats2half2_rn(sum[0] - h2.x, sum[1] - h2.y);
-                if (c == i / 2) minus[n][0] = *reinterpret_cast<const uint32_t*>(&high);
-                if (kGroups == 8) {
-                    if (c == i / 2) minus[n][1] = *reinterpret_cast<const uint32_t*>(&low);
-                } else if (c == i / 2 + kGroups / 2) {
-                    minus[n][0] = *reinterpret_cast<const uint32_t*>(&low);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) factor[n][i] = p.scale * __shfl_sync(0xFFFFFFFFu, down, 4 * (2 * c + i));
-        }
-        float acc[kCols][2 * kGroups][4] = {};
-        float top[kCols][2], weight[kCols][2];
-#pragma unroll
-        for (int n = 0; n < kCols; ++n) top[n][0] = top[n][1] = kLowest, weight[n][0] = weight[n][1] = 0.0f;
-
-        for (int i = 0; i < stages; ++i) {
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-            __syncwarp();                                       // all lanes' copies are there, and all have read the stage before
-            const unsigned have = there;
-            ask(i + 1);
-            if ((have & 3) == 0) continue;                      // pages that do not exist
-            const int key = first_key(i);
-            const unsigned char* stage = rings + w * kRing + i % kStages * 2 * C::kBytes;
-            const bool whole = (have & 3) == 3 && key >= window_low && key + 32 <= k1;
-            auto counts = [&](int at, int j) { return at >= window_low && at < k1 && (have >> (1 - j) & 1); };
-
-            float score[kCols][2][4];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const unsigned char* chunk = stage + j * C::kBytes;
-                uint32_t k[2][kGroups], ks[2][kGroups / 2];     // keys g and g + 8
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    load_words<kGroups>(chunk + (g + 8 * m) * C::kRow + c * 4 * kGroups, k[m]);
-                    load_words<kGroups / 2>(chunk + C::kKeyScales + (g + 8 * m) * 2 * kGroups, ks[m]);
-                }
-                uint32_t both[2];                               // the lane's part of the scales' product
-#pragma unroll
-                for (int m = 0; m < 2; ++m) both[m] = *reinterpret_cast<const uint32_t*>(chunk + C::kKeyScales + (g + 8 * m) * 2 * kGroups + c % (kGroups / 2) * 4);
-#pragma unroll
-                for (int n = 0; n < kCols; ++n)
-                    dev::mma_f16_from(score[n][j], 0.0f, 0.0f, 0.0f, 0.0f, both[0], both[1], kGroups == 8 ? both[0] : 0u, kGroups == 8 ? both[1] : 0u, minus[n][0], minus[n][1]);
-#pragma unroll
-                for (int t = 0; t < kGroups; ++t) {
-                    const float2 s0 = __half22float2(*reinterpret_cast<const __half2*>(&ks[0][t / 2])), s1 = __half22float2(*reinterpret_cast<const __half2*>(&ks[1][t / 2]));
-                    const float f0 = t & 1 ? s0.y : s0.x, f1 = t & 1 ? s1.y : s1.x;
-                    const uint32_t a = k[0][t], b = k[1][t], a8 = a >> 8, b8 = b >> 8;
-                    constexpr uint32_t kLow = 0x000F000Fu, kHigh = 0x00F000F0u;
-#pragma unroll
-                    for (int n = 0; n < kCols; ++n) {
-                        float d[4];
-                        dev::mma_f16_from(d, 0.0f, 0.0f, 0.0f, 0.0f, a & kLow, b & kLow, a & kHigh, b & kHigh, q[n][2 * t][0], q[n][2 * t][1]);
-                        dev::mma_f16(d, a8 & kLow, b8 & kLow, a8 & kHigh, b8 & kHigh, q[n][2 * t + 1][0], q[n][2 * t + 1][1]);
-                        score[n][j][0] += d[0] * f0, score[n][j][1] += d[1] * f0;
-                        score[n][j][2] += d[2] * f1, score[n][j][3] += d[3] * f1;
-                    }
-                }
-            }
-#pragma unroll
-            for (int n = 0; n < kCols; ++n) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) score[n][j][m] *= factor[n][m & 1];
-                }
-                if (p.cap > 0.0f) {                             // cap * tanh(s / cap) as 1 - 2 / (e^2x + 1), which keeps its limits
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                        for (int m = 0; m < 4; ++m) score[n][j][m] = p.cap * (1.0f - __fdividef(2.0f, exp2_of(score[n][j][m] * p.cap_inv) + 1.0f));
-                    }
-                }
-            }
-            if (!whole) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        if (counts(key + 16 * j + g + 8 * m, j)) continue;
-#pragma unroll
-                        for (int n = 0; n < kCols; ++n) score[n][j][2 * m] = score[n][j][2 * m + 1] = -INFINITY;
-                    }
-                }
-            }
-            uint32_t weights[kCols][2][2];
-#pragma unroll
-            for (int n = 0; n < kCols; ++n) {
-                float high[2];
-#pragma unroll
-                for (int m = 0; m < 2; ++m) high[m] = fmaxf(fmaxf(score[n][0][m], score[n][0][2 + m]), fmaxf(score[n][1][m], score[n][1][2 + m]));
-                const bool higher = high[0] > top[n][0] + kSlack || high[1] > top[n][1] + kSlack;
-                if (__any_sync(0xFFFFFFFFu, higher)) {
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        float most = fmaxf(top[n][m], high[m]);
-#pragma unroll
-                        for (int d = 4; d < 32; d *= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
-                        const float f = exp2_of(top[n][m] - most);
-                        top[n][m] = most;
-                        weight[n][m] *= f;
-#pragma unroll
-                        for (int t = 0; t < 2 * kGroups; ++t) acc[n][t][m] *= f, acc[n][t][2 + m] *= f;
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        score[n][j][m] = exp2_of(score[n][j][m] - top[n][m & 1]);
-                        weight[n][m & 1] += score[n][j][m];
-                    }
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        const __half2 pair = __floats2half2_rn(score[n][j][2 * m], score[n][j][2 * m + 1]);
-                        weights[n][j][m] = transpose8x8(*reinterpret_cast<const uint32_t*>(&pair));
-                    }
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const unsigned char* chunk = stage + j * C::kBytes;
-                uint32_t v[4][kGroups / 2], vs[4][(kGroups + 3) / 4];       // keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
-#pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    const int row = 2 * c + (m & 1) + 8 * (m >> 1);
-                    load_words<kGroups / 2>(chunk + C::kValues + row * C::kValueRow + g * 2 * kGroups, v[m]);
-                    const unsigned char* s = chunk + C::kValueScales + row * 2 * kGroups + (g & 1) * kGroups;
-                    if constexpr (kGroups == 2) vs[m][0] = *reinterpret_cast<const uint16_t*>(s);
-                    else load_words<kGroups / 4>(s, vs[m]);
-                }
-                if (!whole) {                                   // keys that do not count, whatever the page holds there
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        if (counts(key + 16 * j + 2 * c + (m & 1) + 8 * (m >> 1), j)) continue;
-#pragma unroll
-                        for (int t = 0; t < (kGroups + 3) / 4; ++t) vs[m][t] = 0;
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < kGroups / 2; ++t) {
-                    const uint32_t sel = t & 1 ? 0x7632 : 0x5410;
-                    const uint32_t sab = __byte_perm(vs[0][t / 2], vs[1][t / 2], sel), scd = __byte_perm(vs[2][t / 2], vs[3][t / 2], sel);
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const uint32_t take = half ? 0x7632 : 0x5410;
-                        uint32_t ab[4], cd[4];
-                        pairs_of(__byte_perm(v[0][t], v[1][t], take), ab);
-                        pairs_of(__byte_perm(v[2][t], v[3][t], take), cd);
-#pragma unroll
-                        for (int m = 0; m < 4; ++m) ab[m] = times(ab[m], sab), cd[m] = times(cd[m], scd);
-#pragma unroll
-                        for (int n = 0; n < kCols; ++n) {
-                            dev::mma_f16(acc[n][4 * t + 2 * half], ab[0], ab[1], cd[0], cd[1], weights[n][j][0], weights[n][j][1]);
-                            dev::mma_f16(acc[n][4 * t + 2 * half + 1], ab[2], ab[3], cd[2], cd[3], weights[n][j][0], weights[n][j][1]);
-                        }
-                    }
-                }
-            }
-        }
-
-        // the warps' sums, joined
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        __syncwarp();
-        float* sums = reinterpret_cast<float*>(rings + w * kRing);
-#pragma unroll
-        for (int n = 0; n < kCols; ++n) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-#pragma unroll
-                for (int d = 4; d < 32; d *= 2) weight[n][i] += __shfl_xor_sync(0xFFFFFFFFu, weight[n][i], d);
-                const int row = 8 * n + 2 * c + i;
-                if (g == 0) warp_stats[w * kRows + row] = make_float2(top[n][i], weight[n][i]);
-                float* to = sums + row * kDim;
-#pragma unroll
-                for (int j = 0; j < 2 * kGroups; ++j) {
-                    const int word = g * (kGroups / 2) + j / 4;         // of the row's words; its dimensions 2 (j % 4) and the next
-                    const int d = word % kGroups * 32 + word / kGroups * 8 + 2 * (j % 4);
-                    *reinterpret_cast<float2*>(to + d) = make_float2(acc[n][j][i], acc[n][j][2 + i]);
-                }
-            }
-        }
+        attend<kGroups, kCols>(p, b, h, row0, k0, k1, span.end, rings, warp_stats);
         __syncthreads();
         const bool all = count == span.units;
         const int slot = 2 * blockIdx.x + (pieces > 0 ? 1 : 0); // what is not whole is the first piece of a run or the last
         ++pieces;
         for (int e = threadIdx.x; e < rows * kDim / 4; e += kThreads) {       // four neighbours to a thread
             const int row = e / (kDim / 4), d = e % (kDim / 4) * 4;
-            float m = kLowest, wt = 0.0f;
-            float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-            for (int i = 0; i < kWarps; ++i) m = fmaxf(m, warp_stats[i * kRows + row].x);
-#pragma unroll
-            for (int i = 0; i < kWarps; ++i) {
-                const float2 st = warp_stats[i * kRows + row];
-                const float f = exp2_of(st.x - m);
-                const float4 v = *reinterpret_cast<const float4*>(rings + i * kRing + (row * kDim + d) * 4);
-                wt += st.y * f;
-                sum.x += v.x * f, sum.y += v.y * f, sum.z += v.z * f, sum.w += v.w * f;
-            }
+            float2 stat;
+            const float4 sum = join_warps<kGroups, kCols>(rings, warp_stats, row, d, stat);
             if (all) {
-                store_result(p, b, static_cast<int64_t>(h * p.group + row0 + row) * kDim + d, sum, wt);
+                store_result(p, b, static_cast<int64_t>(h * p.group + row0 + row) * kDim + d, sum, stat.y);
             } else {
                 *reinterpret_cast<float4*>(p.sums + (static_cast<int64_t>(slot) * kRows + row) * kDim + d) = sum;
-                if (d == 0) p.stats[slot * kRows + row] = make_float2(m, wt);
+                if (d == 0) p.stats[slot * kRows + row] = stat;
             }
         }
         if (threadIdx.x == 0 && off == 0 && (p.by_triple || !all))        // the CTAs with the rest follow this one
@@ -638,6 +666,59 @@ __global__ void __launch_bounds__(kThreads, kGroups == 8 ? 2 : kCols == 2 ? 3 : 
                 make_int4(all ? -1 : b, triple, slot, static_cast<int>(((static_cast<int64_t>(start) + length) * ctas - 1) / total));
         __syncthreads();
     }
+}
+
+// The form for few triples of few keys: a cluster of CTAs to a triple, an eighth of its keys each, whose sums meet through
+// distributed shared memory.  No scratch memory, no second kernel.
+constexpr int kCluster = 8;
+
+template <int kGroups, int kCols>
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, Shape<kGroups, kCols>::kCtasOfSm) attn_cluster_kernel(const AttnParams p) {
+    using S = Shape<kGroups, kCols>;
+    constexpr int kDim = S::kDim, kRows = S::kRows, kRing = S::kRing;
+    extern __shared__ float4 shared[];
+    unsigned char* rings = reinterpret_cast<unsigned char*>(shared);
+    float2* warp_stats = reinterpret_cast<float2*>(rings + kWarps * kRing);
+    float2* stats = warp_stats + kWarps * kRows;                // [kRows], read by the whole cluster, as the first warp's sums are
+    dev::programmatic_start();
+    cg::cluster_group cluster = cg::this_cluster();
+    const int cta = blockIdx.x % kCluster, place = blockIdx.x / kCluster, triples = p.heads * p.row_blocks, b = place / triples, triple = place % triples;
+    const int h = triple / p.row_blocks, row0 = triple % p.row_blocks * kRows, rows = min(kRows, p.group - row0);
+    const Span span = span_of(p, b);
+    const int steps = (span.end - span.low + 31) / 32;          // of 32 keys
+    const int k0 = span.low + 32 * (steps * cta / kCluster), k1 = min(span.end, span.low + 32 * (steps * (cta + 1) / kCluster));
+    attend<kGroups, kCols>(p, b, h, row0, k0, k1, span.end, rings, warp_stats);
+    __syncthreads();
+    for (int e = threadIdx.x; e < rows * kDim / 4; e += kThreads) {
+        const int row = e / (kDim / 4), d = e % (kDim / 4) * 4;
+        float2 stat;
+        const float4 sum = join_warps<kGroups, kCols>(rings, warp_stats, row, d, stat);
+        *reinterpret_cast<float4*>(rings + (row * kDim + d) * 4) = sum;      // nobody else reads or writes the first warp's there
+        if (d == 0) stats[row] = stat;
+    }
+    cluster.sync();
+    const int e = cta * kThreads + threadIdx.x;
+    static_assert(kRows * kDim / 4 <= kCluster * kThreads, "a thread of the cluster for every four results");
+    if (e < rows * kDim / 4) {
+        const int row = e / (kDim / 4), d = e % (kDim / 4) * 4;
+        float m = kLowest, wt = 0.0f;
+        float2 st[kCluster];
+        float4 v[kCluster], sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < kCluster; ++i) {
+            st[i] = cluster.map_shared_rank(stats, i)[row];
+            v[i] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(rings, i) + (row * kDim + d) * 4);
+            m = fmaxf(m, st[i].x);
+        }
+#pragma unroll
+        for (int i = 0; i < kCluster; ++i) {
+            const float f = exp2_of(st[i].x - m);
+            wt += st[i].y * f;
+            sum.x += v[i].x * f, sum.y += v[i].y * f, sum.z += v[i].z * f, sum.w += v[i].w * f;
+        }
+        store_result(p, b, static_cast<int64_t>(h * p.group + row0 + row) * kDim + d, sum, wt);
+    }
+    cluster.sync();                                             // nobody reads this CTA's sums any more
 }
 
 // Joins the partial sums of a triple that several CTAs have, in the order of its keys: a row of it to a CTA, whose groups of lanes
@@ -687,7 +768,15 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParam
 }
 
 template <int kGroups, int kCols>
-size_t attn_shared_bytes(int B) { return kWarps * (2 * kStages * Chunk<kGroups>::kBytes + 8 * kCols * sizeof(float2) + sizeof(int)) + (B + 1) * sizeof(int); }
+size_t attn_shared_bytes(int B) { return kWarps * (Shape<kGroups, kCols>::kRing + 8 * kCols * sizeof(float2) + sizeof(int)) + (B + 1) * sizeof(int); }
+
+template <int kGroups, int kCols>
+size_t attn_cluster_bytes() { return kWarps * Shape<kGroups, kCols>::kRing + (kWarps + 1) * 8 * kCols * sizeof(float2); }
+
+// Up to here a cluster to a triple, where all of them fit the GPU at once (64 query and 8 key heads, in a graph, us, cluster against
+// line: 1 request of 1000 keys 12.3 against 17.7, of 8000 18.4 : 25.9, of 16000 26.6 : 27.9; 8 of 1000 18.4 : 23.8, of 8000 32.8 :
+// 38.2).  Beyond, few long requests among short ones are better cut anywhere.
+constexpr int kClusterKeys = 8192;
 
 template <int kGroups, int kCols>
 spdp_status launch_form(AttnParams p, int device, int sms, cudaStream_t s) {
@@ -702,10 +791,18 @@ spdp_status launch_form(AttnParams p, int device, int sms, cudaStream_t s) {
                                                static_cast<int>(attn_shared_bytes<kGroups, kCols>(kMostRequests))));
             SPDP_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident[device], attn_kernel<kGroups, kCols>, kThreads,
                                                                         attn_shared_bytes<kGroups, kCols>(64)));
+            SPDP_CUDA_TRY(cudaFuncSetAttribute(attn_cluster_kernel<kGroups, kCols>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               static_cast<int>(attn_cluster_bytes<kGroups, kCols>())));
         }
         per_sm = resident[device] > 0 ? resident[device] : 1;
     }
     const int triples = p.heads * p.row_blocks;
+    const int64_t longest = p.window > 0 && p.window < p.table_pages << p.page_shift ? p.window : p.table_pages << p.page_shift;
+    if (longest <= kClusterKeys && static_cast<int64_t>(p.B) * triples * kCluster <= static_cast<int64_t>(per_sm) * sms) {
+        SPDP_CUDA_TRY(launch_programmatic(attn_cluster_kernel<kGroups, kCols>, dim3(static_cast<unsigned>(p.B * triples * kCluster)), kThreads,
+                                          attn_cluster_bytes<kGroups, kCols>(), s, p));
+        return SPDP_OK;
+    }
     // no more CTAs than there can be units
     const int64_t most = p.B * (((p.table_pages << p.page_shift) + kUnit - 1) / kUnit) * triples;
     const int ctas = static_cast<int>(most < static_cast<int64_t>(per_sm) * sms ? most : per_sm * sms);

@@ -33,10 +33,7 @@ constexpr int kCluster = 8;
 constexpr int kExpandWarps = 4;     // of a CTA of the second kernel; three CTAs to an SM, for the registers that its loads take
 constexpr int kOut = 64;            // output rows of a warp's block
 constexpr int kBlocksOfCluster = kCluster * kWarps;
-#ifndef SPDP_FUSED
-#define SPDP_FUSED 4
-#endif
-constexpr int kFusedTokens = SPDP_FUSED;     // up to here one launch does both products
+constexpr int kFusedTokens = 4;     // up to here one launch does both products (4096 x 4096, rank 16, 1 token: 6.2 us in a graph, two launches 8.8)
 constexpr int kFewTokens = 64;               // up to here tiles are 8 tokens, for there are more adapters than tiles of 32
 
 struct Params {

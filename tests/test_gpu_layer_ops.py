@@ -335,11 +335,12 @@ def cache_values(cache):
     return 150.0                        # 30 standard deviations' worth of the largest rows: no stored value is larger
 
 
+@pytest.mark.parametrize("columns", [2, 1000])     # of the table behind the longest request's: with 1000 the keys may be too many for one cluster
 @pytest.mark.parametrize("heads,group,D,page,lengths,cap,window", [
     (1, 1, 128, 16, [1], 0.0, 0), (2, 4, 128, 16, [0, 1, 15, 16, 17], 0.0, 0), (1, 8, 64, 32, [63, 64, 65, 0, 130], 0.0, 0), (3, 3, 128, 64, [200, 3, 64, 128], 20.0, 0),
     (1, 9, 128, 16, [100, 33], 0.0, 0), (2, 16, 64, 16, [70, 1, 300], 5.0, 50), (1, 20, 128, 128, [129, 257], 0.0, 1), (2, 2, 256, 256, [40, 300], 0.0, 17),
     (1, 12, 256, 16, [90, 16], 30.0, 0), (1, 33, 64, 16, [50], 0.0, 16), (4, 1, 128, 32, [700, 5, 0, 31, 32, 33, 64, 1], 0.0, 100)])
-def test_attn_kv4(S, heads, group, D, page, lengths, cap, window):
+def test_attn_kv4(S, heads, group, D, page, lengths, cap, window, columns):
     rng = np.random.default_rng(heads * 100 + group + D)
     cache, table, oracle = filled(rng, heads, D, page, lengths)
     B, H = len(lengths), heads * group
@@ -351,7 +352,7 @@ def test_attn_kv4(S, heads, group, D, page, lengths, cap, window):
     words = H * D // 32
     mask = torch.full((B + 1, words + 1), 123, dtype=torch.int32, device="cuda")
     y, scale, thr = y_all[:B, :H * D], 1.3 / np.sqrt(D), 0.05
-    tab = dev(np.concatenate([table, np.full((B, 2), -7, np.int32)], 1))
+    tab = dev(np.concatenate([table, np.full((B, columns), -7, np.int32)], 1))
     S.spdp_attn_kv4(q, cache, page, heads, tab, dev(length), y, scale, cap=cap, window=window, thr=thr, mask=mask[:B])
     torch.cuda.synchronize()
     attn_check(y, q, oracle, table, length, scale, cap, window)
@@ -367,10 +368,12 @@ def test_attn_kv4(S, heads, group, D, page, lengths, cap, window):
     assert torch.equal(first, y)
 
 
-def test_attn_kv4_pages_that_do_not_exist_and_lengths_beyond_the_table(S):
+@pytest.mark.parametrize("columns", [5, 600])
+def test_attn_kv4_pages_that_do_not_exist_and_lengths_beyond_the_table(S, columns):
     rng = np.random.default_rng(8)
     cache, table, oracle = filled(rng, 2, 128, 16, [80, 80, 40])
     table[0, 1], table[0, 3], table[1, :] = -1, 2 ** 31 - 1, len(oracle.raw)
+    table = np.concatenate([table, np.full((3, columns - 5), len(oracle.raw) + 3, np.int32)], 1)
     length = np.array([80, 80, 10 ** 9], np.int32)
     for t in range(40, 80):
         oracle.store(int(table[2, t // 16]) * 16 + t % 16, np.ones((2, 128), np.float16), np.ones((2, 128), np.float16))
@@ -381,7 +384,8 @@ def test_attn_kv4_pages_that_do_not_exist_and_lengths_beyond_the_table(S):
     assert bool((y[1] == 0).all())
 
 
-def test_attn_kv4_scores_of_all_sizes(S):
+@pytest.mark.parametrize("columns", [0, 600])
+def test_attn_kv4_scores_of_all_sizes(S, columns):
     """Scores that grow along the keys, fall, and lie far apart: the running maximum, and weights down to nothing."""
     rng = np.random.default_rng(9)
     heads, D, page, n = 1, 128, 16, 200
@@ -394,7 +398,7 @@ def test_attn_kv4_scores_of_all_sizes(S):
     q = np.zeros((3, 2, D), np.float16)
     q[:, 0, 5], q[:, 1, 5] = 8.0, -3.0
     y = torch.empty(3, 2 * D, dtype=torch.float16, device="cuda")
-    S.spdp_attn_kv4(dev(q), dev(oracle.raw), page, heads, dev(table), dev(np.full(3, n, np.int32)), y, 0.125)
+    S.spdp_attn_kv4(dev(q), dev(oracle.raw), page, heads, dev(np.concatenate([table, np.zeros((3, columns), np.int32)], 1)), dev(np.full(3, n, np.int32)), y, 0.125)
     attn_check(y, dev(q), oracle, table, [n] * 3, 0.125)
 
 
@@ -435,7 +439,35 @@ def test_attn_kv4_long_and_behind_four_gigabytes(S):
         assert bool((err <= bound).all()), (b, float((err - bound).max()))
 
 
-def test_attn_kv4_captured_and_on_streams(S):
+def test_attn_kv4_many_requests(S):
+    """More triples than CTAs, most of one key, some of none, a few long."""
+    heads, group, D, page, B = 4, 2, 64, 16, 700
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    length = torch.randint(0, 4, (B,), generator=gen, device="cuda", dtype=torch.int32)
+    length[::97] = torch.tensor([300, 1, 16, 17, 512, 0, 33, 64], dtype=torch.int32, device="cuda")[:len(length[::97])]
+    each = 32
+    table = torch.randperm(B * each, generator=gen, device="cuda").view(B, each).int()
+    cache = torch.full((B * each, S.spdp_kv4_page_bytes(heads, D, page)), 0xFF, dtype=torch.uint8, device="cuda")
+    kv, vv = (torch.zeros(B, 512, heads, D, dtype=torch.float16, device="cuda") for _ in range(2))
+    t = torch.arange(512, device="cuda")
+    slot = torch.where(t < length[:, None], table[:, t // page].long() * page + t % page, -1).view(-1)
+    k, v = (torch.randn(B * 512, heads, D, generator=gen, device="cuda").half() for _ in range(2))
+    S.spdp_kv4_store(k, v, slot, cache, page, k_values=kv.view(-1, heads, D), v_values=vv.view(-1, heads, D))
+    q = torch.randn(B, heads * group, D, generator=gen, device="cuda").half()
+    y, mask = torch.full((B, heads * group * D), 3.0, dtype=torch.float16, device="cuda"), torch.full((B, heads * group * D // 32), 5, dtype=torch.int32, device="cuda")
+    S.spdp_attn_kv4(q, cache, page, heads, table, length, y, 0.125, mask=mask)
+    score = torch.einsum("bhgd,bthd->bhgt", q.double().view(B, heads, group, D), kv.double()) * 0.125
+    score.masked_fill_((t >= length[:, None])[:, None, None], -torch.inf)
+    p = torch.softmax(score, -1).nan_to_num(0.0)
+    want, spread = (torch.einsum("bhgt,bthd->bhgd", p, x).reshape(B, -1) for x in (vv.double(), vv.double().abs()))
+    reach = 0.125 * q.double().abs().sum(-1).repeat_interleave(D, 1) * 6.0
+    bound = U * want.abs() * 1.01 + (3 * U + 2 * reach * (U + 560 * V) + 2.0 ** -20) * 1.02 * spread + 512 * TINY * 6.0 + TINY       # as in the next test
+    assert bool(((y.double() - want).abs() <= bound).all())
+    assert bool((y[length == 0] == 0).all()) and bool((mask[length == 0] == 0).all())
+
+
+@pytest.mark.parametrize("columns", [0, 600])
+def test_attn_kv4_captured_and_on_streams(S, columns):
     """Two graphs and eager calls, one after another and at once: each call's scratch memory is its own."""
     rng = np.random.default_rng(6)
     cases = []
@@ -443,7 +475,7 @@ def test_attn_kv4_captured_and_on_streams(S):
         cache, table, oracle = filled(rng, 2, 128, 16, [300, 17, 90])
         q, y = dev(rng.standard_normal((3, 8, 128)).astype(np.float16)), torch.empty(3, 1024, dtype=torch.float16, device="cuda")
         length = dev(np.array([300, 17, 90], np.int32))
-        cases.append((q, cache, dev(table), length, y, oracle, table))
+        cases.append((q, cache, dev(np.concatenate([table, np.full((3, columns), -1, np.int32)], 1)), length, y, oracle, table))
 
     def call(c):
         S.spdp_attn_kv4(c[0], c[1], 16, 2, c[2], c[3], c[4], 0.1)
