@@ -265,22 +265,23 @@ constexpr int kStages = 2;              // of a warp, two chunks each: one is re
 __device__ __forceinline__ void copy16(uint32_t to, const unsigned char* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
+__device__ __forceinline__ void copy16_if(bool on, uint32_t to, const unsigned char* from) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.s32 p, %2, 0;\n @p cp.async.cg.shared.global [%0], [%1], 16;\n}" ::"r"(to), "l"(from), "r"(static_cast<int>(on)) : "memory");
+}
 
-// 16 keys into a chunk; `keys`: the lane's 16 bytes of the first 512 of their codes, `scales`: the start of their scales.
+// 16 keys into a chunk.  The lane's addresses: `to`, `keys` of its 16 bytes of the first 512 of their codes and `scale` of its 16
+// bytes of the scales (keys' and values': 4 kGroups lanes have some); `values`: how far behind the keys' codes the values' are;
+// value_to, scale_to: the lane's places for these, from `to`.
 template <int kGroups>
-__device__ __forceinline__ void copy_chunk(uint32_t to, const unsigned char* keys, const unsigned char* scales, int P, int lane) {
+__device__ __forceinline__ void copy_chunk(uint32_t to, const unsigned char* keys, const unsigned char* scale, int values, int value_to, int scale_to, bool has_scale) {
     using C = Chunk<kGroups>;
-    const unsigned char* values = keys + P * C::kRow;
+    constexpr int kRows = 32 / kGroups;             // of 512 bytes
 #pragma unroll
-    for (int i = 0; i < (C::kRow + 31) / 32; ++i) {
-        const int piece = 32 * i + lane, row = piece / kGroups, part = piece % kGroups;
-        copy16(to + 16 * piece, keys + 512 * i);
-        copy16(to + C::kValues + row * C::kValueRow + 16 * part, values + 512 * i);
+    for (int i = 0; i < 512 * kGroups / 1024; ++i) {
+        copy16(to + 512 * i, keys + 512 * i);
+        copy16(to + value_to + kRows * C::kValueRow * i, keys + values + 512 * i);
     }
-    if (lane < 4 * kGroups) {           // 2 kGroups pieces of the keys' scales, as many of the values'
-        const int piece = lane % (2 * kGroups);
-        copy16(to + C::kKeyScales + 16 * lane, scales + 16 * piece + (lane < 2 * kGroups ? 0 : P * 2 * kGroups));
-    }
+    copy16_if(has_scale, to + scale_to, scale);
 }
 
 // Four columns of a request's output and their bits of its mask; 8 neighbouring lanes have the columns of a word.
@@ -319,7 +320,6 @@ __device__ __forceinline__ void attend(const AttnParams& p, int b, int h, int ro
     constexpr int kDim = S::kDim, kRows = S::kRows, kRing = S::kRing;
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
     const int P = 1 << p.page_shift, rows = min(kRows, p.group - row0);
-    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(rings)) + w * kRing;
     const unsigned head_bytes = P * 36 * kGroups, page_bytes = head_bytes * p.heads;
     const int window_low = p.window > 0 && end > p.window ? static_cast<int>(end - p.window) : 0;
     const int32_t* table = p.table + b * p.table_stride;
@@ -327,30 +327,33 @@ __device__ __forceinline__ void attend(const AttnParams& p, int b, int h, int ro
     // the warp's stages: every fourth one of the run.  Each lane knows the page of a chunk of 16 of them, and of the next 16
     using C = Chunk<kGroups>;
     const int stages = ((k1 - k0 + 31) / 32 - w + kWarps - 1) / kWarps;
-    auto first_key = [&](int i) { return k0 + 32 * (w + kWarps * i); };
-    auto page_of = [&](int i) {
-        const int key = first_key(i + (lane >> 1)) + 16 * (lane & 1);
-        return key < k1 ? table[key >> p.page_shift] : -1;
+    int key = k0 + 32 * w, asked = key;                         // the first key of the stage that is worked on, and that is asked for
+    auto page_of = [&](int i) {                                 // of the stages i .. i + 15
+        const int at = k0 + 32 * (w + kWarps * (i + (lane >> 1))) + 16 * (lane & 1);
+        return at < k1 ? table[at >> p.page_shift] : -1;
     };
     int pages = page_of(0), pages_after = page_of(16);
-    unsigned there = 0;                                     // two bits for each stage that was asked for: which of its chunks exist
-    const unsigned char* cache = p.cache + h * static_cast<int64_t>(head_bytes);
+    unsigned there = 0;                                         // two bits for each stage that was asked for: which of its chunks exist
+    const unsigned char* codes = p.cache + h * static_cast<int64_t>(head_bytes) + 16 * lane;
+    const unsigned char* scales = codes + 2 * P * C::kRow + (lane < 2 * kGroups ? 0 : P * 2 * kGroups - 32 * kGroups);
+    const int values = P * C::kRow, value_to = C::kValues + lane / kGroups * C::kValueRow + lane % kGroups * 16 - 16 * lane, scale_to = C::kKeyScales;
+    uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(rings)) + w * kRing + 16 * lane;
+    uint32_t flip = 2 * C::kBytes;                              // to the other stage, and back
     auto ask = [&](int i) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const unsigned page = __shfl_sync(0xFFFFFFFFu, pages, 2 * i + j & 31);
-            const bool ok = page < p.pages;                 // negative ones are large here
+            const bool ok = page < p.pages;                     // negative ones are large here; the first page stands in for what does not exist
             there = there << 1 | (ok ? 1u : 0u);
-            if (ok) {
-                const unsigned char* head = cache + static_cast<uint64_t>(page) * page_bytes;
-                const int at = (first_key(i) + 16 * j) & (P - 1);
-                copy_chunk<kGroups>(ring + (i % kStages * 2 + j) * C::kBytes, head + at * C::kRow + 16 * lane, head + 2 * P * C::kRow + at * 2 * kGroups, P, lane);
-            }
+            const uint64_t first = static_cast<uint64_t>(ok ? page : 0u) * page_bytes;
+            const int at = (asked + 16 * j) & (P - 1);
+            copy_chunk<kGroups>(to + j * C::kBytes, codes + first + at * C::kRow, scales + first + at * 2 * kGroups, values, value_to, scale_to, lane < 4 * kGroups);
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        to += flip, flip = -flip, asked += 32 * kWarps;
         if ((i & 15) == 15) pages = pages_after, pages_after = page_of(i + 17);
     };
-    ask(0);
+    if (stages > 0) ask(0);
+    asm volatile("cp.async.commit_group;" ::: "memory");
 
     // The query heads as the products' columns, in the order that the codes' pairs have.  A code n is taken from its word by
     // one logical operation, as the subnormal fp16 number n 2^-24 or, four bits up, n 2^-20: the heads are scaled by a power of two
@@ -417,14 +420,15 @@ __device__ __forceinline__ void attend(const AttnParams& p, int b, int h, int ro
 #pragma unroll
     for (int n = 0; n < kCols; ++n) top[n][0] = top[n][1] = kLowest, weight[n][0] = weight[n][1] = 0.0f;
 
-    for (int i = 0; i < stages; ++i) {
+    const unsigned char* stage = rings + w * kRing;
+    int other = 2 * C::kBytes;
+    for (int i = 0; i < stages; ++i, key += 32 * kWarps, stage += other, other = -other) {
         asm volatile("cp.async.wait_group 0;" ::: "memory");
-        __syncwarp();                                       // all lanes' copies are there, and all have read the stage before
+        __syncwarp();                                           // all lanes' copies are there, and all have read the stage before
         const unsigned have = there;
-        ask(i + 1);
-        if ((have & 3) == 0) continue;                      // pages that do not exist
-        const int key = first_key(i);
-        const unsigned char* stage = rings + w * kRing + i % kStages * 2 * C::kBytes;
+        if (i + 1 < stages) ask(i + 1);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if ((have & 3) == 0) continue;                          // pages that do not exist
         const bool whole = (have & 3) == 3 && key >= window_low && key + 32 <= k1;
         auto counts = [&](int at, int j) { return at >= window_low && at < k1 && (have >> (1 - j) & 1); };
 
