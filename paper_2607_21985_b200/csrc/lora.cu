@@ -163,7 +163,12 @@ __device__ __forceinline__ void expand_block(const Params& p, int64_t n0, unsign
             if (owner >> (8 * t) & 1) x[t] = *reinterpret_cast<const uint4*>(vector + 8 * t * row + k0);
         }
     };
-    if (a >= 0 && rank > 0) weights(0), vectors(0);
+    float down[kCols][2];
+    if (a >= 0) {
+        if (rank > 0) weights(0), vectors(0);
+#pragma unroll
+        for (int i = 0; i < 2 * kCols; ++i) down[i / 2][i % 2] = members >> (8 * (i / 2) + i % 2) & 1 ? factors[8 * (i / 2) + i % 2 + 2 * c] : 0.0f;
+    }
 #pragma unroll
     for (int t0 = 0; t0 < kCols; t0 += kStep) {
         if (!(all >> (8 * t0) & (kStep == 2 ? 0xFFFFu : 0xFFu))) continue;
@@ -205,7 +210,7 @@ __device__ __forceinline__ void expand_block(const Params& p, int64_t n0, unsign
 #pragma unroll
                         for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) reinterpret_cast<uint4*>(y + n * p.ldy + 8 * g)[i] = reinterpret_cast<const uint4*>(from)[i];
                     } else {
-                        add_eight(y + n * p.ldy + 8 * g, from, o, factors[n + 2 * c]);
+                        add_eight(y + n * p.ldy + 8 * g, from, o, down[t0 + t][h]);
                     }
                 }
             }
@@ -221,7 +226,7 @@ __device__ __forceinline__ void expand_block(const Params& p, int64_t n0, unsign
                 const int t = e / 16, h = e / 8 % 2, n = 8 * (t0 + t) + h;
                 if (!(members >> n & 1) || row_of<kWide>(g, e % 8) >= left) continue;
                 const T b = in[t][h][e % 8];
-                y[n * p.ldy + row_of<kWide>(g, e % 8)] = a < 0 ? b : sum_of(b, acc[t][e % 8 / 2][2 * (e % 2) + h] * factors[n + 2 * c]);
+                y[n * p.ldy + row_of<kWide>(g, e % 8)] = a < 0 ? b : sum_of(b, acc[t][e % 8 / 2][2 * (e % 2) + h] * down[t0 + t][h]);
             }
         }
     }
