@@ -123,19 +123,22 @@ cudaError_t launch_store(const StoreParams& p, int sms, cudaStream_t s) {
 // the device knows.  A run that holds a triple's every key writes its output; else CTAs leave a partial sum of it, with its
 // maximum and its weight, and a second kernel joins them in the order of the keys.
 //
-// Inside a CTA each warp takes 16 keys at a time.  Scores are K q^T and outputs V^T P^T on mma.sync, with the query heads of
-// the key head as the 8 columns (so that up to 8 heads cost no more than one, and 16 share what was decoded): the codes go from
-// registers through two logical operations per pair into fp16 fragments; the keys' scales multiply the 32-bit sums of their 32
-// dimensions, the values' scales the decoded values (one rounding of 2^-12), and the weights, at most 2^8, are rounded to fp16
-// once (2^-12), as outputs are.  Maxima are only renewed, and sums rescaled, when a score exceeds the old one by 2^8: so that
-// the exchanges between lanes that a maximum takes are rare.
+// Inside a CTA each warp takes 32 keys at a time, copied to shared memory one step ahead.  Scores are K q^T and outputs V^T P^T on
+// mma.sync, with the query heads of the key head as the 8 columns (so that up to 8 heads cost no more than one, and 16 share
+// what was decoded).  A key's code n goes into the products as it is: masked out of its word, four bits are a subnormal fp16
+// number, n 2^-24 or n 2^-20, which the products take exactly; that it stands for n - 8 is one more product, of the scales.  So a
+// pair of codes costs one logical operation.  The keys' scales multiply the 32-bit sums of their 32 dimensions.  The values'
+// codes become exact fp16 numbers n - 8, and their scales multiply the softmax's weights, once for the 32 dimensions of a scale,
+// before these are rounded to fp16 (2^-11): the one rounding besides the result's.
+// What bounds it: the chains of a warp's instructions at the 16 warps that the registers allow (issued: 0.6 a cycle and scheduler; ATTN_RATE).
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kUnit = 64;               // keys
 constexpr int kMostRequests = 4096;
 constexpr float kLowest = -1.0e30f;     // stands for "no score yet"
-constexpr float kSlack = 8.0f;
+constexpr float kHeadroom = 12.0f;      // weights are at most 2^(kHeadroom + kSlack), 2^kSlack where the scales are as large as they can be (2^14):
+constexpr float kSlack = 1.5f;          // their products with the scales are below 2^15.5
 
 struct AttnParams {
     const __half* q;
@@ -220,10 +223,6 @@ __device__ __forceinline__ uint32_t high_pair(uint32_t w) {      // nibbles 1 an
 // pair i: nibbles i and i + 4
 __device__ __forceinline__ void pairs_of(uint32_t w, uint32_t (&out)[4]) {
     out[0] = low_pair(w), out[1] = high_pair(w), out[2] = low_pair(w >> 8), out[3] = high_pair(w >> 8);
-}
-__device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
-    const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-    return *reinterpret_cast<const uint32_t*>(&r);
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
     uint32_t r;
@@ -416,7 +415,8 @@ __device__ __forceinline__ void attend(const AttnParams& p, int b, int h, int ro
         for (int i = 0; i < 2; ++i) factor[n][i] = p.scale * __shfl_sync(0xFFFFFFFFu, down, 4 * (2 * c + i));
     }
     float acc[kCols][2 * kGroups][4] = {};
-    float top[kCols][2], weight[kCols][2];
+    float top[kCols][2], weight[kCols][2], headroom = kHeadroom;
+    __half2 scale_limit = __float2half2_rn(exp2f(14.0f - kHeadroom));
 #pragma unroll
     for (int n = 0; n < kCols; ++n) top[n][0] = top[n][1] = kLowest, weight[n][0] = weight[n][1] = 0.0f;
 
@@ -490,26 +490,64 @@ __device__ __forceinline__ void attend(const AttnParams& p, int b, int h, int ro
                 }
             }
         }
-        uint32_t weights[kCols][2][2];
+        // The weights are 2^(score - top), where top is the largest score so far less `headroom`, or up to kSlack less: as large as
+        // fp16 allows for their products with the values' scales, so that small ones keep their digits.  Scales too large for
+        // that much, and scores, renew it.
+        float high[kCols][2];
+        bool renew = false;
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
-            float high[2];
 #pragma unroll
-            for (int m = 0; m < 2; ++m) high[m] = fmaxf(fmaxf(score[n][0][m], score[n][0][2 + m]), fmaxf(score[n][1][m], score[n][1][2 + m]));
-            const bool higher = high[0] > top[n][0] + kSlack || high[1] > top[n][1] + kSlack;
-            if (__any_sync(0xFFFFFFFFu, higher)) {
+            for (int m = 0; m < 2; ++m) {
+                high[n][m] = fmaxf(fmaxf(score[n][0][m], score[n][0][2 + m]), fmaxf(score[n][1][m], score[n][1][2 + m]));
+                renew |= high[n][m] > top[n][m] + (headroom + kSlack);
+            }
+        }
+        uint32_t vs[2][2][kGroups / 2];                         // scales of the values of keys g and g + 8
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                load_words<kGroups / 2>(stage + j * C::kBytes + C::kValueScales + (g + 8 * m) * 2 * kGroups, vs[j][m]);
+                if (!whole && !counts(key + 16 * j + g + 8 * m, j)) {       // whatever the page holds there
+#pragma unroll
+                    for (int t = 0; t < kGroups / 2; ++t) vs[j][m][t] = 0;
+                }
+#pragma unroll
+                for (int t = 0; t < kGroups / 2; ++t) renew |= !__hblt2(*reinterpret_cast<const __half2*>(&vs[j][m][t]), scale_limit);
+            }
+        }
+        if (__any_sync(0xFFFFFFFFu, renew)) {
+            unsigned most = 0;                                  // the largest scale, as its bits
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
 #pragma unroll
                 for (int m = 0; m < 2; ++m) {
-                    float most = fmaxf(top[n][m], high[m]);
 #pragma unroll
-                    for (int d = 4; d < 32; d *= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
-                    const float f = exp2_of(top[n][m] - most);
-                    top[n][m] = most;
+                    for (int t = 0; t < kGroups / 2; ++t) most = max(most, max(vs[j][m][t] & 0x7FFFu, vs[j][m][t] >> 16 & 0x7FFFu));
+                }
+            }
+            most = __reduce_max_sync(0xFFFFFFFFu, most);        // below 2^(its exponent - 14)
+            const float before = headroom;
+            headroom = fminf(headroom, fmaxf(28.0f - static_cast<float>(most >> 10), 0.0f));
+            scale_limit = __float2half2_rn(exp2f(14.0f - headroom));
+#pragma unroll
+            for (int n = 0; n < kCols; ++n) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    float largest = high[n][m];
+#pragma unroll
+                    for (int d = 4; d < 32; d *= 2) largest = fmaxf(largest, __shfl_xor_sync(0xFFFFFFFFu, largest, d));
+                    const float next = fmaxf(top[n][m] + before, largest) - headroom, f = exp2_of(top[n][m] - next);
+                    top[n][m] = next;
                     weight[n][m] *= f;
 #pragma unroll
                     for (int t = 0; t < 2 * kGroups; ++t) acc[n][t][m] *= f, acc[n][t][2 + m] *= f;
                 }
             }
+        }
+#pragma unroll
+        for (int n = 0; n < kCols; ++n) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
 #pragma unroll
@@ -517,50 +555,28 @@ __device__ __forceinline__ void attend(const AttnParams& p, int b, int h, int ro
                     score[n][j][m] = exp2_of(score[n][j][m] - top[n][m & 1]);
                     weight[n][m & 1] += score[n][j][m];
                 }
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    const __half2 pair = __floats2half2_rn(score[n][j][2 * m], score[n][j][2 * m + 1]);
-                    weights[n][j][m] = transpose8x8(*reinterpret_cast<const uint32_t*>(&pair));
-                }
             }
         }
+        const uint32_t mine = g & 1 ? 0x7632 : 0x5410;          // the lane's half of a word: dimensions 4 g .. 4 g + 3 of the scale's 32
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const unsigned char* chunk = stage + j * C::kBytes;
-            uint32_t v[4][kGroups / 2], vs[4][(kGroups + 3) / 4];       // keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+            uint32_t v[4][kGroups];                             // of keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                const int row = 2 * c + (m & 1) + 8 * (m >> 1);
-                load_words<kGroups / 2>(chunk + C::kValues + row * C::kValueRow + g * 2 * kGroups, v[m]);
-                const unsigned char* s = chunk + C::kValueScales + row * 2 * kGroups + (g & 1) * kGroups;
-                if constexpr (kGroups == 2) vs[m][0] = *reinterpret_cast<const uint16_t*>(s);
-                else load_words<kGroups / 4>(s, vs[m]);
-            }
-            if (!whole) {                                   // keys that do not count, whatever the page holds there
+            for (int m = 0; m < 4; ++m)
+                load_words<kGroups>(stage + j * C::kBytes + C::kValues + (2 * c + (m & 1) + 8 * (m >> 1)) * C::kValueRow + (g >> 1) * 4 * kGroups, v[m]);
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    if (counts(key + 16 * j + 2 * c + (m & 1) + 8 * (m >> 1), j)) continue;
+            for (int t = 0; t < kGroups; ++t) {
+                const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&vs[j][0][t / 2])), f1 = __half22float2(*reinterpret_cast<const __half2*>(&vs[j][1][t / 2]));
+                const float s0 = t & 1 ? f0.y : f0.x, s1 = t & 1 ? f1.y : f1.x;
+                uint32_t ab[4], cd[4];
+                pairs_of(__byte_perm(v[0][t], v[1][t], mine), ab);
+                pairs_of(__byte_perm(v[2][t], v[3][t], mine), cd);
 #pragma unroll
-                    for (int t = 0; t < (kGroups + 3) / 4; ++t) vs[m][t] = 0;
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < kGroups / 2; ++t) {
-                const uint32_t sel = t & 1 ? 0x7632 : 0x5410;
-                const uint32_t sab = __byte_perm(vs[0][t / 2], vs[1][t / 2], sel), scd = __byte_perm(vs[2][t / 2], vs[3][t / 2], sel);
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint32_t take = half ? 0x7632 : 0x5410;
-                    uint32_t ab[4], cd[4];
-                    pairs_of(__byte_perm(v[0][t], v[1][t], take), ab);
-                    pairs_of(__byte_perm(v[2][t], v[3][t], take), cd);
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) ab[m] = times(ab[m], sab), cd[m] = times(cd[m], scd);
-#pragma unroll
-                    for (int n = 0; n < kCols; ++n) {
-                        dev::mma_f16(acc[n][4 * t + 2 * half], ab[0], ab[1], cd[0], cd[1], weights[n][j][0], weights[n][j][1]);
-                        dev::mma_f16(acc[n][4 * t + 2 * half + 1], ab[2], ab[3], cd[2], cd[3], weights[n][j][0], weights[n][j][1]);
-                    }
+                for (int n = 0; n < kCols; ++n) {
+                    const __half2 low = __floats2half2_rn(score[n][j][0] * s0, score[n][j][1] * s0), up = __floats2half2_rn(score[n][j][2] * s1, score[n][j][3] * s1);
+                    const uint32_t lo = transpose8x8(*reinterpret_cast<const uint32_t*>(&low)), hi = transpose8x8(*reinterpret_cast<const uint32_t*>(&up));
+                    dev::mma_f16(acc[n][2 * t], ab[0], ab[1], cd[0], cd[1], lo, hi);
+                    dev::mma_f16(acc[n][2 * t + 1], ab[2], ab[3], cd[2], cd[3], lo, hi);
                 }
             }
         }
@@ -581,8 +597,7 @@ __device__ __forceinline__ void attend(const AttnParams& p, int b, int h, int ro
             float* to = sums + row * kDim;
 #pragma unroll
             for (int j = 0; j < 2 * kGroups; ++j) {
-                const int word = g * (kGroups / 2) + j / 4;         // of the row's words; its dimensions 2 (j % 4) and the next
-                const int d = word % kGroups * 32 + word / kGroups * 8 + 2 * (j % 4);
+                const int d = 32 * (j / 2) + 4 * g + 2 * (j % 2);
                 *reinterpret_cast<float2*>(to + d) = make_float2(acc[n][j][i], acc[n][j][2 + i]);
             }
         }

@@ -319,20 +319,16 @@ def filled(rng, heads, D, page, lengths, spare=2):
     return dev(raw), table, cache
 
 
-def attn_check(y, q, cache, table, length, scale, cap=0.0, window=0):
+def attn_check(y, q, cache, table, length, scale, cap=0.0, window=0, most=150.0):
     """Scores: 8 products of 17 additions at 2 v of the sizes and 4 more sums; a cap adds 8 v of itself.  Weights: twice the scores' error, 2^-21 for the exponential, one
-    rounding u and, where small, half of fp16's smallest step against a weight of at least 1; values: one rounding u; the result."""
+    rounding u and, where small, half of fp16's smallest step against a weight of at least 1; values: one rounding u; the result.  `most`: no value is larger (150: 30 standard
+    deviations' worth of the largest rows)."""
     for b in range(len(length)):
         want, spread, reach, keys = O.attention(host(q[b]), cache, table[b], int(length[b]), scale, cap, window)
         ds = (2 * 2 * V * (17 * 16 + 8) * reach + 8 * V * cap + 2.0 ** -21)[:, None]
-        most = np.abs(cache_values(cache)) if keys else 0.0
         bound = U * np.abs(want) * 1.01 + (2 * U + 2 * ds) * 1.01 * spread + keys * TINY * most + TINY
         err = np.abs(host(y[b]).reshape(want.shape) - want)
         assert np.all(err <= bound), (b, int(length[b]), float((err - bound).max()))
-
-
-def cache_values(cache):
-    return 150.0                        # 30 standard deviations' worth of the largest rows: no stored value is larger
 
 
 @pytest.mark.parametrize("columns", [2, 1000])     # of the table behind the longest request's: with 1000 the keys may be too many for one cluster
@@ -400,6 +396,20 @@ def test_attn_kv4_scores_of_all_sizes(S, columns):
     y = torch.empty(3, 2 * D, dtype=torch.float16, device="cuda")
     S.spdp_attn_kv4(dev(q), dev(oracle.raw), page, heads, dev(np.concatenate([table, np.zeros((3, columns), np.int32)], 1)), dev(np.full(3, n, np.int32)), y, 0.125)
     attn_check(y, dev(q), oracle, table, [n] * 3, 0.125)
+
+
+@pytest.mark.parametrize("sizes", [(2e-4,), (6e4,), (1e-3, 3e4), (3e4, 1e-3)])
+def test_attn_kv4_values_of_all_sizes(S, sizes):
+    """Values near both ends of fp16's range; large ones in the second half of the keys, and in the first."""
+    rng = np.random.default_rng(10)
+    heads, D, page, n = 1, 64, 16, 400
+    cache, table, oracle = filled(rng, heads, D, page, [n])
+    for t in range(n):
+        size = sizes[len(sizes) * t // n]
+        oracle.store(int(table[0, t // page]) * page + t % page, rng.standard_normal((1, D)).astype(np.float16), (size * rng.uniform(-1, 1, (1, D))).astype(np.float16))
+    q, y = dev(rng.standard_normal((1, 3, D)).astype(np.float16)), torch.empty(1, 3 * D, dtype=torch.float16, device="cuda")
+    S.spdp_attn_kv4(q, dev(oracle.raw), page, heads, dev(table), dev(np.array([n], np.int32)), y, 0.2)
+    attn_check(y, q, oracle, table, [n], 0.2, most=max(sizes))
 
 
 def plain_attention(q, k, v, scale):
