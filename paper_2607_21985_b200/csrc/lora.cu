@@ -47,12 +47,12 @@ struct Params {
     void* Y;
     int64_t ldx, lda, stride_a, ldb, stride_b, ldbase, ldy;
     int N, K, M, count, rank;
-    int per_tile;                   // clusters (first or only kernel), CTAs (second) of a tile, among which its adapters are dealt out
-    int per_row;                    // second kernel: CTAs that share a tile's output rows
+    int per_window;                 // clusters (first or only kernel), CTAs (second) of a window, among which its work is dealt out
     bool wide_y;                    // base and Y: rows of whole 16-byte pieces, on such boundaries
     // what the first kernel leaves for the second: [N][padded rank] fp16, for 32-bit results twice, and a factor to each token
     __half* vectors;
     float* factors;
+    struct Plan* plans;             // of the windows, for the second kernel
 };
 
 int64_t between(int64_t v, int64_t low, int64_t high) { return v > high ? high : v < low ? low : v; }
@@ -74,28 +74,75 @@ struct Layout {
     }
 };
 
-// The adapters of a tile's tokens, in the order of their first tokens.  Tokens without one (-1) take base as it is: in place
-// there is nothing to do for them.
-struct Tile {
-    int mine;                       // the lane's token's adapter
-    unsigned same, groups;          // the lanes that share it; the first lane of each adapter
-    __device__ __forceinline__ Tile(const Params& p, int64_t n0, int tokens) {
-        const int lane = threadIdx.x & 31;
-        const bool there = lane < tokens && n0 + lane < p.N;
-        mine = there ? p.adapter[n0 + lane] : -2;
-        if (there && (mine < 0 || mine >= p.count)) mine = -1;
-        same = __match_any_sync(0xFFFFFFFFu, mine);
-        groups = __ballot_sync(0xFFFFFFFFu, lane == __ffs(same) - 1 && (mine >= 0 || (mine == -1 && p.base != p.Y)));
-    }
-    __device__ __forceinline__ int count() const { return __popc(groups); }
-    __device__ __forceinline__ void pick(int d, int& adapter, unsigned& members) const {
-        unsigned rest = groups;
-        for (int i = 0; i < d; ++i) rest &= rest - 1;
-        const int lead = __ffs(rest) - 1;
-        adapter = __shfl_sync(0xFFFFFFFFu, mine, lead);
-        members = __shfl_sync(0xFFFFFFFFu, same, lead);
-    }
+// The tokens of a request stand together, those of an adapter need not: 256 consecutive tokens, a window, are brought together by
+// adapter, and a tile is up to kTok tokens of a window that share one.  So 256 tokens that draw from 15 adapters are 15 to 23
+// tiles of 32, not 8 tiles of 13 adapters each.
+constexpr int kWindow = kThreads;
+struct Plan {
+    int tiles;
+    int2 tile[kWindow];             // adapter (-1: none), first place in `order` and 2^16 times the number of tokens
+    unsigned char order[kWindow];   // the window's tokens, by adapter
 };
+
+// The plan of a window with tiles of `tok` tokens, into shared memory (all threads; ends with a barrier); `wide`, if not null, gets
+// the plan with tiles of 32.  Tokens without an adapter take base as it is: in place they are left out.
+__device__ void make_plan(const Params& p, int64_t n0, int tok, Plan& plan, Plan* wide) {
+    __shared__ int2 entries[kWarps][32];                        // of each warp: an adapter, its tokens and (2^8) the first one's lane
+    __shared__ int starts[kWindow], warp_sums[kWarps], warp_entries[kWarps];
+    const int t = threadIdx.x, lane = t & 31, w = t >> 5, tokens = p.N - n0 < kWindow ? static_cast<int>(p.N - n0) : kWindow;
+    int mine = t < tokens ? p.adapter[n0 + t] : -2;
+    if (t < tokens && (mine < 0 || mine >= p.count)) mine = p.base != p.Y ? -1 : -2;
+    const unsigned same = __match_any_sync(0xFFFFFFFFu, mine), below = (1u << lane) - 1u;
+    const int leader = __ffs(same) - 1;
+    const unsigned leaders = __ballot_sync(0xFFFFFFFFu, lane == leader);
+    if (lane == leader) entries[w][__popc(leaders & below)] = make_int2(mine, __popc(same) | lane << 8);
+    if (lane == 0) warp_entries[w] = __popc(leaders);
+    __syncthreads();
+    int all = 0, before = 0, lead = kWindow;                    // tokens that share the adapter, those in front, the first of them
+    for (int i = 0; i < kWarps && 32 * i < tokens; ++i) {
+        for (int j = 0, n = warp_entries[i]; j < n; ++j) {
+            const int2 e = entries[i][j];
+            if (e.x != mine) continue;
+            all += e.y & 255;
+            if (i < w) before += e.y & 255;
+            lead = min(lead, 32 * i + (e.y >> 8));
+        }
+    }
+    before += __popc(same & below);
+    const bool leads = mine != -2 && lead == t;
+    // places, tiles and tiles of 32 of the adapters in front, ten bits each
+    int sum = leads ? all | (all + tok - 1) / tok << 10 | (all + 31) / 32 << 20 : 0;
+    const int own = sum;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int v = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+        if (lane >= d) sum += v;
+    }
+    if (lane == 31) warp_sums[w] = sum;
+    __syncthreads();
+    int front = 0, total = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+        if (i < w) front += warp_sums[i];
+        total += warp_sums[i];
+    }
+    front += sum - own;
+    const int start = front & 1023;
+    if (leads) {
+        starts[t] = start;
+        for (int i = 0, at = front >> 10 & 1023; i * tok < all; ++i) plan.tile[at + i] = make_int2(mine, start + i * tok | min(tok, all - i * tok) << 16);
+        if (wide != nullptr)
+            for (int i = 0, at = front >> 20; 32 * i < all; ++i) wide->tile[at + i] = make_int2(mine, start + 32 * i | min(32, all - 32 * i) << 16);
+    }
+    __syncthreads();
+    if (mine != -2) plan.order[starts[lead] + before] = static_cast<unsigned char>(t);
+    if (t == 0) plan.tiles = total >> 10 & 1023;
+    __syncthreads();
+    if (wide != nullptr) {
+        wide->order[t] = plan.order[t];
+        if (t == 0) wide->tiles = total >> 20;
+    }
+}
 
 __device__ __forceinline__ int rank_of(const Params& p, int a) {
     const int rank = p.ranks != nullptr ? p.ranks[a] : p.rank;
@@ -125,24 +172,20 @@ __device__ __forceinline__ void add_eight(T* to, const T* from, const float (&o)
     for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) reinterpret_cast<uint4*>(to)[i] = x.bits[i];
 }
 
-// The second product for a warp's block of output rows from m_block on, added to base.  `hi`, `lo`: the tile's vectors, `row`
-// halves apart; `factors`: what undoes their scaling.  `old`: base's block in shared memory, [token][kOldRow], or null: it is
-// read where it is.  a < 0: base as it is.
+// The second product for a warp's block of output rows from m_block on, added to base, for the `count` tokens n0 + list[..].
+// `hi`, `lo`: vectors, `row` halves apart, and `factors` that undo their scaling, by place in the list or (kByToken) by token.
+// `old`: base's block in shared memory, [place][kOldRow], or null: it is read where it is.  a < 0: base as it is.
 template <typename T>
 constexpr int kOldRow = kOut + 16 / static_cast<int>(sizeof(T));     // a token's values of a block, and 16 bytes
 
-template <typename T, int kCols, int kAlign, bool kWide>
-__device__ __forceinline__ void expand_block(const Params& p, int64_t n0, unsigned members, int a, int rank, int m_block, const __half* hi, const __half* lo, int row,
-                                             const float* factors, const T* old) {
+template <typename T, int kCols, int kAlign, bool kWide, bool kByToken>
+__device__ __forceinline__ void expand_block(const Params& p, int64_t n0, const unsigned char* list, int count, int a, int rank, int m_block, const __half* hi,
+                                             const __half* lo, int row, const float* factors, const T* old) {
     constexpr bool kTwo = sizeof(T) == 4;
     constexpr int kStep = kCols < 2 ? kCols : 2;                 // column blocks at a time
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int left = p.M - m_block;                              // rows of the block that exist
-    const T* base = static_cast<const T*>(p.base) + (n0 + 2 * c) * p.ldbase + m_block;
-    T* y = static_cast<T*>(p.Y) + (n0 + 2 * c) * p.ldy + m_block;
     const bool there = row_of<kWide>(g, 0) < left;               // kWide: M is a multiple of 8, so all eight or none
-    const unsigned all = members, owner = members >> g;          // bit 8 t of owner: column g of block t is a member (others' vectors may be nobody's)
-    members >>= 2 * c;                                           // bit 8 t + h: the lane's tokens
     uint4 v[4][2], x[kCols];
     const __half* B = p.B + a * p.stride_b + (m_block + row_of<kWide>(g, 0)) * p.ldb;
     const int64_t apart = (kWide ? 1 : 8) * p.ldb;
@@ -155,23 +198,34 @@ __device__ __forceinline__ void expand_block(const Params& p, int64_t n0, unsign
             for (int i = 0; i < 8; ++i) dev::cut8(v[i / 2][i % 2], k0 + 8 * c, rank);
         }
     };
-    const __half* vector = hi + g * row + 8 * c;
+    int token[kCols][2], place[kCols];                           // of the lane's columns 2 c and 2 c + 1; the vector of its column g
+#pragma unroll
+    for (int t = 0; t < kCols; ++t) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) token[t][h] = 8 * t + 2 * c + h < count ? list[8 * t + 2 * c + h] : -1;
+        place[t] = 8 * t + g >= count ? -1 : kByToken ? list[8 * t + g] : 8 * t + g;
+    }
     auto vectors = [&](int k0) {
 #pragma unroll
         for (int t = 0; t < kCols; ++t) {
             x[t] = make_uint4(0, 0, 0, 0);
-            if (owner >> (8 * t) & 1) x[t] = *reinterpret_cast<const uint4*>(vector + 8 * t * row + k0);
+            if (place[t] >= 0) x[t] = *reinterpret_cast<const uint4*>(hi + place[t] * row + k0 + 8 * c);
         }
     };
     float down[kCols][2];
     if (a >= 0) {
         if (rank > 0) weights(0), vectors(0);
 #pragma unroll
-        for (int i = 0; i < 2 * kCols; ++i) down[i / 2][i % 2] = members >> (8 * (i / 2) + i % 2) & 1 ? factors[8 * (i / 2) + i % 2 + 2 * c] : 0.0f;
+        for (int t = 0; t < kCols; ++t) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) down[t][h] = token[t][h] >= 0 ? factors[kByToken ? token[t][h] : 8 * t + 2 * c + h] : 0.0f;
+        }
     }
+    const T* base = static_cast<const T*>(p.base) + n0 * p.ldbase + m_block;
+    T* y = static_cast<T*>(p.Y) + n0 * p.ldy + m_block;
 #pragma unroll
     for (int t0 = 0; t0 < kCols; t0 += kStep) {
-        if (!(all >> (8 * t0) & (kStep == 2 ? 0xFFFFu : 0xFFu))) continue;
+        if (8 * t0 >= count) break;
         float acc[kStep][4][4] = {};
         if (a >= 0) {
             for (int k0 = 0; k0 < rank; k0 += 32) {
@@ -179,7 +233,7 @@ __device__ __forceinline__ void expand_block(const Params& p, int64_t n0, unsign
 #pragma unroll
                 for (int t = 0; t < kStep; ++t) {
                     uint4 z = make_uint4(0, 0, 0, 0);
-                    if (kTwo && (owner >> (8 * (t0 + t)) & 1)) z = *reinterpret_cast<const uint4*>(vector + (lo - hi) + 8 * (t0 + t) * row + k0);
+                    if (kTwo && place[t0 + t] >= 0) z = *reinterpret_cast<const uint4*>(lo + place[t0 + t] * row + k0 + 8 * c);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         dev::mma_f16(acc[t][i], v[i][0].x, v[i][1].x, v[i][0].y, v[i][1].y, x[t0 + t].x, x[t0 + t].y);
@@ -200,17 +254,18 @@ __device__ __forceinline__ void expand_block(const Params& p, int64_t n0, unsign
             for (int t = 0; t < kStep; ++t) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int n = 8 * (t0 + t) + h;              // behind the lane's first token
-                    if (!there || !(members >> n & 1)) continue;
+                    const int n = token[t0 + t][h];
+                    if (!there || n < 0) continue;
                     float o[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) o[e] = acc[t][e / 2][2 * (e % 2) + h];
-                    const T* from = old != nullptr ? old + (n + 2 * c) * kOldRow<T> + 8 * g : base + n * p.ldbase + 8 * g;
+                    T* to = y + n * p.ldy + 8 * g;
+                    const T* from = old != nullptr ? old + (8 * (t0 + t) + 2 * c + h) * kOldRow<T> + 8 * g : base + n * p.ldbase + 8 * g;
                     if (a < 0) {
 #pragma unroll
-                        for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) reinterpret_cast<uint4*>(y + n * p.ldy + 8 * g)[i] = reinterpret_cast<const uint4*>(from)[i];
+                        for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) reinterpret_cast<uint4*>(to)[i] = reinterpret_cast<const uint4*>(from)[i];
                     } else {
-                        add_eight(y + n * p.ldy + 8 * g, from, o, down[t0 + t][h]);
+                        add_eight(to, from, o, down[t0 + t][h]);
                     }
                 }
             }
@@ -218,13 +273,13 @@ __device__ __forceinline__ void expand_block(const Params& p, int64_t n0, unsign
             T in[kStep][2][8];
 #pragma unroll
             for (int e = 0; e < 16 * kStep; ++e) {
-                const int t = e / 16, h = e / 8 % 2, n = 8 * (t0 + t) + h;
-                if ((members >> n & 1) && row_of<kWide>(g, e % 8) < left) in[t][h][e % 8] = base[n * p.ldbase + row_of<kWide>(g, e % 8)];
+                const int t = e / 16, h = e / 8 % 2, n = token[t0 + t][h];
+                if (n >= 0 && row_of<kWide>(g, e % 8) < left) in[t][h][e % 8] = base[n * p.ldbase + row_of<kWide>(g, e % 8)];
             }
 #pragma unroll
             for (int e = 0; e < 16 * kStep; ++e) {
-                const int t = e / 16, h = e / 8 % 2, n = 8 * (t0 + t) + h;
-                if (!(members >> n & 1) || row_of<kWide>(g, e % 8) >= left) continue;
+                const int t = e / 16, h = e / 8 % 2, n = token[t0 + t][h];
+                if (n < 0 || row_of<kWide>(g, e % 8) >= left) continue;
                 const T b = in[t][h][e % 8];
                 y[n * p.ldy + row_of<kWide>(g, e % 8)] = a < 0 ? b : sum_of(b, acc[t][e % 8 / 2][2 * (e % 2) + h] * down[t0 + t][h]);
             }
@@ -252,33 +307,37 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
     dev::programmatic_start();
     cg::cluster_group cluster = cg::this_cluster();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-    const int cta = blockIdx.x % kCluster, z = blockIdx.x / kCluster % p.per_tile;
-    const int64_t n0 = static_cast<int64_t>(blockIdx.x / kCluster / p.per_tile) * kTok;
-    const Tile tile(p, n0, kTok);
-    const int G = tile.count();
-    if (G == 0) return;
-    // more clusters than adapters: they share an adapter's output rows; else a cluster takes several adapters in turn
-    const bool more = !kSplit && p.per_tile > G;
-    const int sharers = more ? (p.per_tile - z % G + G - 1) / G : 1, share = more ? z / G : 0;
+    const int cta = blockIdx.x % kCluster, z = blockIdx.x / kCluster % p.per_window;
+    const int64_t window = blockIdx.x / kCluster / p.per_window, n0 = window * kWindow;
+    __shared__ Plan plan;
+    make_plan(p, n0, kTok, plan, kSplit && cta == 0 && z == 0 ? p.plans + window : nullptr);
+    const int tiles = plan.tiles;
+    if (tiles == 0) return;
+    // more clusters than tiles: they share a tile's output rows; else a cluster takes several tiles in turn
+    const bool more = !kSplit && p.per_window > tiles;
+    const int sharers = more ? (p.per_window - z % tiles + tiles - 1) / tiles : 1, share = more ? z / tiles : 0;
     const int blocks = (p.M + kOut - 1) / kOut;
     if (share * kBlocksOfCluster >= blocks) return;
 
-    for (int d = more ? z % G : z; d < G; d += p.per_tile) {
-        int a;
-        unsigned members;
-        tile.pick(d, a, members);
+    for (int d = more ? z % tiles : z; d < tiles; d += p.per_window) {
+        const int2 tile = plan.tile[d];
+        const int a = tile.x, count = tile.y >> 16;
+        const unsigned char* list = plan.order + (tile.y & 0xFFFF);
         const int block0 = (share * kCluster + cta) * kWarps + w;
         if (a < 0) {
             if constexpr (!kSplit)
                 for (int b = block0; b < blocks; b += sharers * kBlocksOfCluster)
-                    expand_block<T, kCols, kAlign, true>(p, n0, members, a, 0, b * kOut, hi, lo, row, factors, nullptr);
+                    expand_block<T, kCols, kAlign, true, false>(p, n0, list, count, a, 0, b * kOut, hi, lo, row, factors, nullptr);
             continue;
         }
         const int rank = rank_of(p, a), prank = padded_rank(rank);
 
         // A x over this CTA's eighth of K
         const __half* A = p.A + a * p.stride_a;
-        const __half* X = p.X + (n0 + g) * p.ldx;
+        int token[kCols];                                    // the lane's, behind n0
+#pragma unroll
+        for (int t = 0; t < kCols; ++t) token[t] = 8 * t + g < count ? list[8 * t + g] : -1;
+        const __half* X = p.X + n0 * p.ldx;
         const int steps = (p.K + 31) / 32;
         const int s0 = static_cast<int>(static_cast<int64_t>(steps) * cta / kCluster), s1 = static_cast<int>(static_cast<int64_t>(steps) * (cta + 1) / kCluster);
         for (int r0 = 0; r0 < rank; r0 += 16 * kRankTiles) {
@@ -291,15 +350,14 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
                     const __half* at = A + (r0 + g) * p.lda;
 #pragma unroll
                     for (int i = 0; i < 2 * kRankTiles; ++i, at += 8 * p.lda) v[j][i / 2][i % 2] = dev::load8<kAlign>(at, k, r0 + 8 * i + g < rank ? p.K : 0);
-                    at = X;
 #pragma unroll
-                    for (int t = 0; t < kCols; ++t, at += 8 * p.ldx) x[j][t] = dev::load8<kAlign>(at, k, members >> (8 * t + g) & 1 ? p.K : 0);
+                    for (int t = 0; t < kCols; ++t) x[j][t] = dev::load8<kAlign>(X + token[t] * p.ldx, k, token[t] >= 0 ? p.K : 0);
                 }
 #pragma unroll
                 for (int j = 0; j < kBatch; ++j) {
 #pragma unroll
                     for (int t = 0; t < kCols; ++t) {
-                        if (!(members >> (8 * t) & 0xFFu)) continue;
+                        if (8 * t >= count) continue;
 #pragma unroll
                         for (int i = 0; i < kRankTiles; ++i) {
                             dev::mma_f16(acc[i][t], v[j][i][0].x, v[j][i][1].x, v[j][i][0].y, v[j][i][1].y, x[j][t].x, x[j][t].y);
@@ -370,79 +428,185 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
             const int64_t all = static_cast<int64_t>(p.N) * width;
             for (int e = threadIdx.x; e < kCols * pieces; e += kThreads) {
                 const int t = cta * kCols + e / pieces, k = e % pieces * 8;
-                if (!(members >> t & 1)) continue;
-                __half* to = p.vectors + (n0 + t) * width + k;
+                if (t >= count) continue;
+                __half* to = p.vectors + (n0 + list[t]) * width + k;
                 *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(hi + t * row + k);
                 if constexpr (kTwo) *reinterpret_cast<uint4*>(to + all) = *reinterpret_cast<const uint4*>(lo + t * row + k);
             }
-            if (threadIdx.x < kCols && (members >> (cta * kCols + threadIdx.x) & 1)) p.factors[n0 + cta * kCols + threadIdx.x] = factors[cta * kCols + threadIdx.x];
+            const int t = cta * kCols + threadIdx.x;
+            if (threadIdx.x < kCols && t < count) p.factors[n0 + list[t]] = factors[t];
         } else {
             for (int b = block0; b < blocks; b += sharers * kBlocksOfCluster)
-                expand_block<T, kCols, kAlign, true>(p, n0, members, a, rank, b * kOut, hi, lo, row, factors, nullptr);
+                expand_block<T, kCols, kAlign, true, false>(p, n0, list, count, a, rank, b * kOut, hi, lo, row, factors, nullptr);
         }
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // nobody reads this CTA's sums any more
     }
 }
 
-// The second product where it has a kernel of its own: a warp takes blocks of a tile's output one after another, and copies
-// base of the next one to shared memory while it works on one (kWide; else base is read where it is).
-template <typename T, int kAlign, bool kWide>
-__global__ void __launch_bounds__(32 * kExpandWarps, sizeof(T) == 2 ? 4 : 3) lora_expand_kernel(const Params p) {
+template <typename T>
+__host__ __device__ constexpr int expand_ctas_of_sm(bool is_short) { return sizeof(T) == 2 && !is_short ? 4 : 3; }     // that the registers are cut for
+
+// The second product where it has a kernel of its own.  The blocks of all tiles of a window stand in one line, an equal run of
+// them to each warp of the window's CTAs, however many tiles there are.  A warp copies base of the next block to shared
+// memory while it works on one (kWide; else base is read where it is).  kShort: 16-byte loads and ranks up to 32, the usual case;
+// a tile's vectors stay in registers for all its blocks, and the weights of the next block are on their way too.
+template <typename T, int kAlign, bool kWide, bool kShort>
+__global__ void __launch_bounds__(32 * kExpandWarps, expand_ctas_of_sm<T>(kShort)) lora_expand_kernel(const Params p) {
     constexpr int kTok = 8 * kMostCols, kPiece = 16 / sizeof(T), kPieces = kOut / kPiece;        // values of 16 bytes, such pieces of a row
     extern __shared__ float4 shared[];
     dev::programmatic_start();
     const int blocks = (p.M + kOut - 1) / kOut, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const int q = blockIdx.x % p.per_row, z = blockIdx.x / p.per_row % p.per_tile;
-    const int64_t n0 = static_cast<int64_t>(blockIdx.x / p.per_row / p.per_tile) * kTok;
-    const int tokens = p.N - n0 < kTok ? static_cast<int>(p.N - n0) : kTok;
+    const int64_t window = blockIdx.x / p.per_window, n0 = window * kWindow;
+    const int me = blockIdx.x % p.per_window * kExpandWarps + w, width = padded_rank(p.rank);
+    const Plan* plan = p.plans + window;
+    const int64_t units = static_cast<int64_t>(plan->tiles) * blocks;
+    int64_t u = units * me / (p.per_window * kExpandWarps);
+    const int64_t end = units * (me + 1) / (p.per_window * kExpandWarps);
+    if (u >= end) return;
     T* olds = reinterpret_cast<T*>(shared) + w * 2 * kTok * kOldRow<T>;          // two blocks
-    auto copy = [&](int b, int to) {
+    auto copy = [&](int2 tile, int b, int to) {
         if constexpr (kWide) {
+            const unsigned char* list = plan->order + (tile.y & 0xFFFF);
             const T* from = static_cast<const T*>(p.base) + n0 * p.ldbase + b * kOut;
             const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(olds + to * kTok * kOldRow<T>));
-            if (b < blocks) {
 #pragma unroll
-                for (int i = 0; i < kPieces; ++i) {
-                    const int n = i * (32 / kPieces) + lane / kPieces, part = lane % kPieces;
-                    if (n < tokens && b * kOut + part * kPiece < p.M)
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + (n * kOldRow<T> + part * kPiece) * static_cast<int>(sizeof(T))),
-                                     "l"(from + n * p.ldbase + part * kPiece) : "memory");
-                }
+            for (int i = 0; i < kPieces; ++i) {
+                const int n = i * (32 / kPieces) + lane / kPieces, part = lane % kPieces;
+                if (n < tile.y >> 16 && b * kOut + part * kPiece < p.M)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + (n * kOldRow<T> + part * kPiece) * static_cast<int>(sizeof(T))),
+                                 "l"(from + list[n] * p.ldbase + part * kPiece) : "memory");
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
         }
     };
-    const int b0 = q * kExpandWarps + w, step = p.per_row * kExpandWarps;
-    copy(b0, 0);
-    const Tile tile(p, n0, kTok);
-    const int G = tile.count(), width = padded_rank(p.rank);
+    int b = static_cast<int>(u % blocks), d = static_cast<int>(u / blocks);
+    int2 tile = plan->tile[d];
+    copy(tile, b, 0);
+    if constexpr (kWide) asm volatile("cp.async.commit_group;" ::: "memory");
+    int rank = tile.x >= 0 ? rank_of(p, tile.x) : 0;
     const __half* hi = p.vectors + n0 * width;
-    int a = -1, rank = 0;
-    unsigned members = 0;
-    if (z < G) {                                                 // most tiles have one adapter: known before the loop
-        tile.pick(z, a, members);
-        rank = a >= 0 ? rank_of(p, a) : 0;
-        for (int b = b0, i = 0; b < blocks; b += step, i ^= 1) {
-            copy(b + step, i ^ 1);
+    if constexpr (kShort) {
+        constexpr bool kTwo = sizeof(T) == 4;
+        const int g = lane >> 2, c = lane & 3;
+        const __half* lo = hi + static_cast<int64_t>(p.N) * width;
+        int token[kMostCols][2];                                 // of the lane's columns
+        float down[kMostCols][2];
+        uint4 x[kMostCols], z[kTwo ? kMostCols : 1], v[4][2], ahead[4][2];
+        auto enter = [&]() {                                     // a tile
+            const unsigned char* list = plan->order + (tile.y & 0xFFFF);
+            const int count = tile.y >> 16;
+#pragma unroll
+            for (int t = 0; t < kMostCols; ++t) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    token[t][h] = 8 * t + 2 * c + h < count ? list[8 * t + 2 * c + h] : -1;
+                    down[t][h] = token[t][h] >= 0 && tile.x >= 0 ? p.factors[n0 + token[t][h]] : 0.0f;
+                }
+                x[t] = make_uint4(0, 0, 0, 0);
+                if constexpr (kTwo) z[t] = make_uint4(0, 0, 0, 0);
+                if (8 * t + g < count && 8 * c < rank) {
+                    const int at = list[8 * t + g] * width + 8 * c;
+                    x[t] = *reinterpret_cast<const uint4*>(hi + at);
+                    if constexpr (kTwo) z[t] = *reinterpret_cast<const uint4*>(lo + at);
+                }
+            }
+        };
+        auto weights = [&](uint4 (&into)[4][2], int adapter, int its_rank, int block) {
+            const int m0 = block * kOut + 8 * g;
+            const __half* at = p.B + adapter * p.stride_b + m0 * p.ldb;
+#pragma unroll
+            for (int j = 0; j < 8; ++j, at += p.ldb) into[j / 2][j % 2] = dev::load8<16>(at, 8 * c, m0 < p.M ? its_rank : 0);
+        };
+        enter();
+        weights(v, tile.x, rank, b);
+        for (int i = 0; u < end; ++u, i ^= 1) {
+            const bool last = b + 1 == blocks;                   // of its tile
+            int2 next = tile;
+            int next_rank = rank;
+            if (u + 1 < end) {
+                if (last) {
+                    next = plan->tile[d + 1];
+                    next_rank = next.x >= 0 ? rank_of(p, next.x) : 0;
+                }
+                copy(next, last ? 0 : b + 1, i ^ 1);
+                weights(ahead, next.x, next_rank, last ? 0 : b + 1);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            __syncwarp();
+            if (rank % 8 != 0) {                                 // what stands behind an adapter's own rank
+#pragma unroll
+                for (int j = 0; j < 8; ++j) dev::cut8(v[j / 2][j % 2], 8 * c, rank);
+            }
+            const T* old = olds + i * kTok * kOldRow<T> + 8 * g;
+            T* y = static_cast<T*>(p.Y) + n0 * p.ldy + b * kOut + 8 * g;
+            const bool there = b * kOut + 8 * g < p.M;
+#pragma unroll
+            for (int t = 0; t < kMostCols; ++t) {
+                if (8 * t >= tile.y >> 16) break;
+                float acc[4][4] = {};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    dev::mma_f16(acc[j], v[j][0].x, v[j][1].x, v[j][0].y, v[j][1].y, x[t].x, x[t].y);
+                    if constexpr (kTwo) dev::mma_f16(acc[j], v[j][0].x, v[j][1].x, v[j][0].y, v[j][1].y, z[t].x, z[t].y);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    dev::mma_f16(acc[j], v[j][0].z, v[j][1].z, v[j][0].w, v[j][1].w, x[t].z, x[t].w);
+                    if constexpr (kTwo) dev::mma_f16(acc[j], v[j][0].z, v[j][1].z, v[j][0].w, v[j][1].w, z[t].z, z[t].w);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (!there || token[t][h] < 0) continue;
+                    const T* from = old + (8 * t + 2 * c + h) * kOldRow<T>;
+                    T* to = y + token[t][h] * p.ldy;
+                    if (tile.x < 0) {
+#pragma unroll
+                        for (int j = 0; j < static_cast<int>(sizeof(T)) / 2; ++j) reinterpret_cast<uint4*>(to)[j] = reinterpret_cast<const uint4*>(from)[j];
+                    } else {
+                        float o[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) o[e] = acc[e / 2][2 * (e % 2) + h];
+                        add_eight(to, from, o, down[t][h]);
+                    }
+                }
+            }
+            __syncwarp();                                        // all lanes have read the block before it is overwritten
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j / 2][j % 2] = ahead[j / 2][j % 2];
+            if (last) {
+                tile = next, rank = next_rank, ++d, b = 0;
+                if (u + 1 < end) enter();
+            } else {
+                ++b;
+            }
+        }
+    } else {
+        for (int i = 0; u < end; ++u, i ^= 1) {
+            const bool last = b + 1 == blocks;                       // of its tile
+            int2 next = tile;
+            if (u + 1 < end) {
+                if (last) next = plan->tile[d + 1];
+                copy(next, last ? 0 : b + 1, i ^ 1);
+            }
             if constexpr (kWide) {
+                asm volatile("cp.async.commit_group;" ::: "memory");
                 asm volatile("cp.async.wait_group 1;" ::: "memory");
                 __syncwarp();
             }
-            for (int d = z; d < G; d += p.per_tile) {
-                if (G > p.per_tile) {
-                    tile.pick(d, a, members);
-                    rank = a >= 0 ? rank_of(p, a) : 0;
-                }
-                expand_block<T, kMostCols, kAlign, kWide>(p, n0, members, a, rank, b * kOut, hi, hi + static_cast<int64_t>(p.N) * width, width, p.factors + n0,
-                                                          kWide ? olds + i * kTok * kOldRow<T> : nullptr);
+            expand_block<T, kMostCols, kAlign, kWide, true>(p, n0, plan->order + (tile.y & 0xFFFF), tile.y >> 16, tile.x, rank, b * kOut, hi,
+                                                            hi + static_cast<int64_t>(p.N) * width, width, p.factors + n0, kWide ? olds + i * kTok * kOldRow<T> : nullptr);
+            if constexpr (kWide) __syncwarp();                       // all lanes have read the block before it is overwritten
+            if (last) {
+                tile = next, ++d, b = 0;
+                rank = tile.x >= 0 ? rank_of(p, tile.x) : 0;
+            } else {
+                ++b;
             }
-            if constexpr (kWide) __syncwarp();                   // all lanes have read the block before it is overwritten
         }
     }
-    if constexpr (kWide) asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-template <typename T, int kAlign, bool kWide>
+template <typename T, int kAlign, bool kWide, bool kShort>
 cudaError_t launch_expand(Params p, int device, int sms, cudaStream_t s) {
     static std::mutex mu;
     static bool configured[64] = {};
@@ -450,23 +614,21 @@ cudaError_t launch_expand(Params p, int device, int sms, cudaStream_t s) {
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!configured[device]) {
-            const cudaError_t e = cudaFuncSetAttribute(lora_expand_kernel<T, kAlign, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+            const cudaError_t e = cudaFuncSetAttribute(lora_expand_kernel<T, kAlign, kWide, kShort>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
             if (e != cudaSuccess) return e;
         }
         configured[device] = true;
     }
-    // as many CTAs as the GPU holds at once
-    const int64_t tiles = (p.N + 8 * kMostCols - 1) / (8 * kMostCols), most = (p.M + kOut * kExpandWarps - 1) / (kOut * kExpandWarps);
-    const int64_t slots = (sizeof(T) == 2 ? 4 : 3) * static_cast<int64_t>(sms);
-    p.per_row = static_cast<int>(between(slots / tiles, 1, most));
-    p.per_tile = static_cast<int>(between(slots / (tiles * p.per_row), 1, p.N < 32 ? p.N : 32));
-    const int64_t size = tiles * p.per_row * p.per_tile;
+    // as many CTAs as the GPU holds at once, no more than there can be blocks
+    const int64_t windows = (p.N + kWindow - 1) / kWindow, blocks = (p.M + kOut - 1) / kOut, slots = expand_ctas_of_sm<T>(kShort) * static_cast<int64_t>(sms);
+    p.per_window = static_cast<int>(between((slots + windows - 1) / windows, 1, ((p.N < kWindow ? p.N : kWindow) * blocks + kExpandWarps - 1) / kExpandWarps));
+    const int64_t size = windows * p.per_window;
     if (size > INT32_MAX) return cudaErrorInvalidConfiguration;
-    return launch_programmatic(lora_expand_kernel<T, kAlign, kWide>, dim3(static_cast<unsigned>(size)), 32 * kExpandWarps, bytes, s, p);
+    return launch_programmatic(lora_expand_kernel<T, kAlign, kWide, kShort>, dim3(static_cast<unsigned>(size)), 32 * kExpandWarps, bytes, s, p);
 }
 
 template <int kRankTiles, int kCols, typename T, bool kSplit, int kAlign>
-spdp_status launch_form(const Params& p, int tiles, int device, cudaStream_t s) {
+spdp_status launch_form(const Params& p, int windows, int device, cudaStream_t s) {
     static std::mutex mu;
     static bool configured[64] = {};
     constexpr int kMostRank = kRankTiles == 4 ? SPDP_MAX_RANK : 16 * kRankTiles;
@@ -478,16 +640,16 @@ spdp_status launch_form(const Params& p, int tiles, int device, cudaStream_t s) 
                                                static_cast<int>(L::bytes(kMostRank, sizeof(T) == 4))));
         configured[device] = true;
     }
-    const dim3 grid(static_cast<unsigned>(tiles) * static_cast<unsigned>(p.per_tile) * kCluster);
+    const dim3 grid(static_cast<unsigned>(windows) * static_cast<unsigned>(p.per_window) * kCluster);
     SPDP_CUDA_TRY(launch_programmatic(lora_kernel<kRankTiles, kCols, T, kSplit, kAlign>, grid, kThreads, L::bytes(p.rank, sizeof(T) == 4), s, p));
     return SPDP_OK;
 }
 
 template <int kCols, typename T, bool kSplit, int kAlign>
-spdp_status launch_rank(const Params& p, int tiles, int device, cudaStream_t s) {
-    if (p.rank <= 16) return launch_form<1, kCols, T, kSplit, kAlign>(p, tiles, device, s);
-    if (p.rank <= 32) return launch_form<2, kCols, T, kSplit, kAlign>(p, tiles, device, s);
-    return launch_form<4, kCols, T, kSplit, kAlign>(p, tiles, device, s);
+spdp_status launch_rank(const Params& p, int windows, int device, cudaStream_t s) {
+    if (p.rank <= 16) return launch_form<1, kCols, T, kSplit, kAlign>(p, windows, device, s);
+    if (p.rank <= 32) return launch_form<2, kCols, T, kSplit, kAlign>(p, windows, device, s);
+    return launch_form<4, kCols, T, kSplit, kAlign>(p, windows, device, s);
 }
 
 template <typename T>
@@ -496,24 +658,26 @@ spdp_status launch_typed(Params p, int align, int device, int sms, cudaStream_t 
     if (p.N <= kFusedTokens && align == 16 && p.wide_y) {
         // Clusters of a tile: two CTAs per SM in all, no more than there is work for
         const int64_t most = static_cast<int64_t>(p.N) * ((blocks + kBlocksOfCluster - 1) / kBlocksOfCluster);
-        p.per_tile = static_cast<int>(between(cluster_slots, 1, most));
+        p.per_window = static_cast<int>(between(cluster_slots, 1, most));
         return launch_rank<1, T, false, 16>(p, 1, device, s);
     }
     const bool few = p.N <= kFewTokens && align == 16;
-    const int tok = few ? 8 : 8 * kMostCols, tiles = (p.N + tok - 1) / tok, width = padded_rank(p.rank);
-    const size_t vectors = 2ull * p.N * width * (sizeof(T) == 4 ? 2 : 1);
+    const int windows = (p.N + kWindow - 1) / kWindow, width = padded_rank(p.rank);
+    const size_t vectors = 2ull * p.N * width * (sizeof(T) == 4 ? 2 : 1), factors = (4ull * p.N + 15) / 16 * 16;
     void* scratch = nullptr;
-    spdp_status st = scratch_alloc(device, vectors + 4ull * p.N, s, &scratch);
+    spdp_status st = scratch_alloc(device, vectors + factors + windows * sizeof(Plan), s, &scratch);
     if (st != SPDP_OK) return st;
     p.vectors = static_cast<__half*>(scratch);
     p.factors = reinterpret_cast<float*>(static_cast<char*>(scratch) + vectors);
-    p.per_tile = static_cast<int>(between(cluster_slots / tiles, 1, p.N < tok ? p.N : tok));
-    if (align == 16) st = few ? launch_rank<1, T, true, 16>(p, tiles, device, s) : launch_rank<kMostCols, T, true, 16>(p, tiles, device, s);
-    else st = align == 4 ? launch_rank<kMostCols, T, true, 4>(p, tiles, device, s) : launch_rank<kMostCols, T, true, 2>(p, tiles, device, s);
+    p.plans = reinterpret_cast<Plan*>(static_cast<char*>(scratch) + vectors + factors);
+    p.per_window = static_cast<int>(between(cluster_slots / windows, 1, p.N < kWindow ? p.N : kWindow));
+    if (align == 16) st = few ? launch_rank<1, T, true, 16>(p, windows, device, s) : launch_rank<kMostCols, T, true, 16>(p, windows, device, s);
+    else st = align == 4 ? launch_rank<kMostCols, T, true, 4>(p, windows, device, s) : launch_rank<kMostCols, T, true, 2>(p, windows, device, s);
     if (st == SPDP_OK) {
-        const cudaError_t e = align == 16 ? (p.wide_y ? launch_expand<T, 16, true>(p, device, sms, s) : launch_expand<T, 16, false>(p, device, sms, s))
-                              : align == 4 ? (p.wide_y ? launch_expand<T, 4, true>(p, device, sms, s) : launch_expand<T, 4, false>(p, device, sms, s))
-                                           : (p.wide_y ? launch_expand<T, 2, true>(p, device, sms, s) : launch_expand<T, 2, false>(p, device, sms, s));
+        const cudaError_t e = align == 16 && p.wide_y && p.rank <= 32 ? launch_expand<T, 16, true, true>(p, device, sms, s)
+                              : align == 16 ? (p.wide_y ? launch_expand<T, 16, true, false>(p, device, sms, s) : launch_expand<T, 16, false, false>(p, device, sms, s))
+                              : align == 4  ? (p.wide_y ? launch_expand<T, 4, true, false>(p, device, sms, s) : launch_expand<T, 4, false, false>(p, device, sms, s))
+                                            : (p.wide_y ? launch_expand<T, 2, true, false>(p, device, sms, s) : launch_expand<T, 2, false, false>(p, device, sms, s));
         if (e != cudaSuccess) {
             note_cuda_error(e, "lora_expand_kernel");
             st = SPDP_ERR_CUDA;

@@ -40,24 +40,39 @@ __device__ __forceinline__ uint4 load8(const __half* row, int k, int limit) {
         uint4 v = make_uint4(0, 0, 0, 0);
         if (k < limit) v = *reinterpret_cast<const uint4*>(row + k);
         return v;
-    } else {
+    } else if constexpr (kAlign == 4) {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int at = k + 2 * i;
-            if constexpr (kAlign == 4) {
-                uint32_t both = 0, one = 0;
-                if (at + 1 < limit) both = *reinterpret_cast<const uint32_t*>(row + at);
-                if (at + 1 == limit) one = __half_as_ushort(row[at]);
-                w[i] = both | one;
-            } else {
-                uint32_t lo = 0, hi = 0;
-                if (at < limit) lo = __half_as_ushort(row[at]);
-                if (at + 1 < limit) hi = __half_as_ushort(row[at + 1]);
-                w[i] = lo | (hi << 16);
-            }
+            uint32_t both = 0, one = 0;
+            if (at + 1 < limit) both = *reinterpret_cast<const uint32_t*>(row + at);
+            if (at + 1 == limit) one = __half_as_ushort(row[at]);
+            w[i] = both | one;
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        // Three whole words lie inside the eight elements, one or two elements from the first; besides them the first element, and
+        // the second or the last.
+        const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(row + k) >> 1 & 1), side = odd ? k + 7 : k + 1;
+        uint32_t first = 0, other = 0, w[3];
+        if (k < limit) first = __half_as_ushort(row[k]);
+        if (side < limit) other = __half_as_ushort(row[side]);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const int at = k + 2 - odd + 2 * i;
+            uint32_t both = 0, one = 0;
+            if (at + 1 < limit) both = *reinterpret_cast<const uint32_t*>(row + at);
+            if (at + 1 == limit) one = __half_as_ushort(row[at]);
+            w[i] = both | one;
+        }
+        const uint32_t take = odd ? 0x5432 : 0x3210;            // halves (second of a, first of b); or a
+        uint4 v;
+        v.x = __byte_perm(first, odd ? w[0] : other, 0x5410);
+        v.y = __byte_perm(w[0], w[1], take);
+        v.z = __byte_perm(w[1], w[2], take);
+        v.w = __byte_perm(w[2], other, take);
+        return v;
     }
 }
 // Zeros in the elements from `limit` on of what stands for elements k .. k + 7.

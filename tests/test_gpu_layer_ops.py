@@ -126,6 +126,21 @@ def test_lora(S, N, K, M, rank, count, odd_rows, f32):
         first = Z
 
 
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("N,count,run", [(256, 300, 1), (257, 2, 1), (600, 31, 1), (1030, 9, 7), (700, 3, 100), (512, 1, 1), (90, 90, 1)])
+def test_lora_tokens_of_many_adapters(S, N, count, run, f32):
+    """Windows of tokens with as many adapters as tokens, with few that alternate, with runs across their borders."""
+    K, M, rank = 72, 136, 24
+    c = lora_case(N + count, N, K, M, rank, count, f32)
+    c["adapter"] = c["adapter"][::run].repeat_interleave(run)[:N].contiguous()
+    Y = torch.full_like(c["base"], 99.0)
+    S.spdp_lora(Y=Y, **c)
+    lora_check(c, Y, rank)
+    Z = c["base"].clone()
+    S.spdp_lora(**dict(c, Y=Z, base=None))
+    assert torch.equal(Z, Y)
+
+
 @pytest.mark.parametrize("none", [0.0, 1.0])
 def test_lora_all_or_none(S, none):
     c = lora_case(5, 45, 96, 200, 12, 3, none=none, ranks=False)
