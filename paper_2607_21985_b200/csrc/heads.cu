@@ -33,120 +33,143 @@ struct Params {
     float eps;
 };
 
-template <typename T, int kPairs>
-__device__ __forceinline__ void load(const T* at, float (&x)[kPairs]) {
-    if constexpr (kPairs == 8) dev::load_floats<T, true>(at, x);
-    else if constexpr (sizeof(T) == 2) x[0] = __half2float(*at);
-    else x[0] = *at;
+// Sine and cosine of a pair's angle for token n; pairs that do not turn have 0 and 1.
+__device__ __forceinline__ void turn_of(const Params& p, int64_t n, int i, float& sine, float& cosine) {
+    sine = 0.0f, cosine = 1.0f;
+    if (i >= p.pairs) return;
+    int a = 0;
+    while (a < p.axes - 1 && i >= p.ends[a]) ++a;
+    const double turns = static_cast<double>(p.pos[a * p.pos_stride + n]) * static_cast<double>(p.inv_freq[i]) * 0.15915494309189535;  // 1 / (2 pi)
+    sincospif(2.0f * static_cast<float>(turns - rint(turns)), &sine, &cosine);
 }
 
-template <int kPairs>
-__device__ __forceinline__ void store(__half* at, const float (&x)[kPairs]) {
-    if constexpr (kPairs == 8) dev::store_halves<true>(at, x);
-    else *at = __float2half_rn(x[0]);
+// Where the two members of pair i are: neighbours, or as far apart as the pairs that turn; what does not turn is split in two the
+// same way.  (Neighbours: the first values of `count` pairs, and of the second half of these.)
+template <bool kAdjacent>
+__device__ __forceinline__ void members_of(const Params& p, int i, int count, int& first, int& second) {
+    if (kAdjacent) first = 2 * i, second = 2 * i + count;
+    else if (i < p.pairs) first = i, second = i + p.pairs;
+    else first = i + p.pairs, second = i + p.dim / 2;
 }
 
-// kPairs = 8: 16-byte accesses, D / 16 lanes to a head.  kPairs = 1: any even D up to 256 and any alignment, a head takes up to
-// 32 lanes and four rounds of them.
-template <typename T, int kPairs, bool kAdjacent>
-__global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const Params p) {
-    constexpr int kRounds = kPairs == 1 ? kMostDim / 2 / 32 : 1;
-    __shared__ float2 turn[kMostDim / 2];
+// 16-byte accesses: a lane has 8 pairs, D / 16 lanes (rounded up to a power of two) a head.  The sines and cosines of a lane's
+// pairs, the same in every head, stay in its registers.
+template <typename T, bool kAdjacent>
+__global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_wide_kernel(const Params p) {
+    __shared__ __align__(16) float sines[kMostDim / 2], cosines[kMostDim / 2];
     dev::programmatic_start();
     const int64_t n = blockIdx.x;
     const int half = p.dim / 2, heads = p.q_heads + p.kv_heads;
-    const int lane = threadIdx.x & (p.lanes - 1), slots = blockDim.x >> p.shift;
-    // The lane's pairs, the same in every head.  Members: neighbours, or as far apart as the pairs that turn; what does not turn is
-    // split in two the same way.
-    int at[kRounds][2], pair[kRounds];
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-        const int i = (r * p.lanes + lane) * kPairs;                // the lane's first pair
-        pair[r] = i < half ? i : -1;
-        if (kAdjacent) at[r][0] = 2 * i, at[r][1] = 2 * i + kPairs;
-        else if (i < p.pairs) at[r][0] = i, at[r][1] = i + p.pairs;
-        else at[r][0] = i + p.pairs, at[r][1] = i + half;
-    }
-    float x[kRounds][2][kPairs];
+    const int lane = threadIdx.x & (p.lanes - 1), slots = blockDim.x >> p.shift, stride = gridDim.y * slots;
+    const bool mine = 8 * lane < half;
+    int first, second;
+    members_of<kAdjacent>(p, 8 * lane, 8, first, second);
+    float x[2][8];
     auto fetch = [&](int h) {
-        if (h >= heads) return;
+        if (h >= heads || !mine) return;
         const T* from = h < p.q_heads ? static_cast<const T*>(p.q) + n * p.ldq + h * p.dim : static_cast<const T*>(p.k) + n * p.ldk + (h - p.q_heads) * p.dim;
-#pragma unroll
-        for (int r = 0; r < kRounds; ++r) {
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-                if (pair[r] >= 0) load<T, kPairs>(from + at[r][m], x[r][m]);
-        }
+        dev::load_floats<T, true>(from + first, x[0]);
+        dev::load_floats<T, true>(from + second, x[1]);
     };
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[0][j] = x[1][j] = 0.0f;
     int h = blockIdx.y * slots + (threadIdx.x >> p.shift);
     fetch(h);                                                       // on its way while the angles are formed
-    for (int i = threadIdx.x; i < half; i += blockDim.x) {
-        float2 cs = make_float2(1.0f, 0.0f);
-        if (i < p.pairs) {
-            int a = 0;
-            while (a < p.axes - 1 && i >= p.ends[a]) ++a;
-            const double turns = static_cast<double>(p.pos[a * p.pos_stride + n]) * static_cast<double>(p.inv_freq[i]) * 0.15915494309189535;  // 1 / (2 pi)
-            sincospif(2.0f * static_cast<float>(turns - rint(turns)), &cs.y, &cs.x);
-        }
-        turn[i] = cs;
-    }
+    for (int i = threadIdx.x; i < half; i += blockDim.x) turn_of(p, n, i, sines[i], cosines[i]);
     __syncthreads();
-    for (int rounds = (heads - blockIdx.y * slots + gridDim.y * slots - 1) / (gridDim.y * slots); rounds > 0; --rounds) {      // the same for all threads
+    float s[8], c[8];
+    if (mine) {
+        dev::load_floats<float, true>(sines + 8 * lane, s);
+        dev::load_floats<float, true>(cosines + 8 * lane, c);
+    }
+    const float per_value = 1.0f / p.dim;
+    for (int rounds = (heads - blockIdx.y * slots + stride - 1) / stride; rounds > 0; --rounds, h += stride) {     // the same for all threads
+        float squares = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) squares += x[0][j] * x[0][j] + x[1][j] * x[1][j];
+        for (int d = p.lanes / 2; d > 0; d >>= 1) squares += __shfl_xor_sync(0xFFFFFFFFu, squares, d);
+        if (h >= heads || !mine) continue;
         const bool is_q = h < p.q_heads;
         const __half* weight = is_q ? p.q_weight : p.k_weight;
-        float squares = 0.0f, y[kRounds][2][kPairs];
+        float y[2][8];
+        if (weight != nullptr) {
+            const float inv = rsqrtf(squares * per_value + p.eps);
+            dev::load_floats<__half, true>(weight + first, y[0]);
+            dev::load_floats<__half, true>(weight + second, y[1]);
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) {
+            for (int j = 0; j < 8; ++j) y[0][j] *= x[0][j] * inv, y[1][j] *= x[1][j] * inv;
+        } else {
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
+            for (int j = 0; j < 8; ++j) y[0][j] = x[0][j], y[1][j] = x[1][j];
+        }
+        fetch(h + stride);
+        // neighbours: a lane's 16 values are a0 b0 a1 b1 ...; else y[0] holds the first members and y[1] the second
+        float* flat = &y[0][0];
 #pragma unroll
-                for (int j = 0; j < kPairs; ++j) {
-                    y[r][m][j] = x[r][m][j];
-                    if (h < heads && pair[r] >= 0) squares += y[r][m][j] * y[r][m][j];
-                }
-            }
+        for (int j = 0; j < 8; ++j) {
+            float& a = flat[kAdjacent ? 2 * j : j];
+            float& b = flat[kAdjacent ? 2 * j + 1 : 8 + j];
+            const float ra = a * c[j] - b * s[j], rb = b * c[j] + a * s[j];
+            a = ra, b = rb;
         }
         __half* to = is_q ? p.q_out + n * p.ldq_out + h * p.dim : p.k_out + n * p.ldk_out + (h - p.q_heads) * p.dim;
-        const bool there = h < heads;
-        h += gridDim.y * slots;
-        fetch(h);
-        for (int d = p.lanes / 2; d > 0; d >>= 1) squares += __shfl_xor_sync(0xFFFFFFFFu, squares, d);
-        if (!there) continue;
-        if (weight != nullptr) {
-            const float inv = 1.0f / sqrtf(squares / p.dim + p.eps);
-#pragma unroll
-            for (int r = 0; r < kRounds; ++r) {
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    if (pair[r] < 0) continue;
-                    float g[kPairs];
-                    load<__half, kPairs>(weight + at[r][m], g);
-#pragma unroll
-                    for (int j = 0; j < kPairs; ++j) y[r][m][j] = y[r][m][j] * inv * g[j];
-                }
-            }
-        }
+        dev::store_halves<true>(to + first, y[0]);
+        dev::store_halves<true>(to + second, y[1]);
+    }
+}
+
+// Any even D up to 256 and any alignment: a lane has a pair in each of up to four rounds, up to 32 lanes a head.
+template <typename T, bool kAdjacent>
+__global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const Params p) {
+    constexpr int kRounds = kMostDim / 2 / 32;
+    __shared__ float sines[kMostDim / 2], cosines[kMostDim / 2];
+    dev::programmatic_start();
+    const int64_t n = blockIdx.x;
+    const int half = p.dim / 2, heads = p.q_heads + p.kv_heads;
+    const int lane = threadIdx.x & (p.lanes - 1), slots = blockDim.x >> p.shift, stride = gridDim.y * slots;
+    for (int i = threadIdx.x; i < half; i += blockDim.x) turn_of(p, n, i, sines[i], cosines[i]);
+    __syncthreads();
+    int h = blockIdx.y * slots + (threadIdx.x >> p.shift);
+    for (int rounds = (heads - blockIdx.y * slots + stride - 1) / stride; rounds > 0; --rounds, h += stride) {     // the same for all threads
+        const bool there = h < heads, is_q = h < p.q_heads;
+        const T* from = is_q ? static_cast<const T*>(p.q) + n * p.ldq + h * p.dim : static_cast<const T*>(p.k) + n * p.ldk + (h - p.q_heads) * p.dim;
+        const __half* weight = is_q ? p.q_weight : p.k_weight;
+        float x[kRounds][2], squares = 0.0f;
+        int at[kRounds][2];
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
-            if (pair[r] < 0) continue;
-            // neighbours: a lane's 2 kPairs values are a0 b0 a1 b1 ...; else y[0] holds the first members and y[1] the second
-            float* flat = &y[r][0][0];
+            const int i = r * p.lanes + lane;
+            members_of<kAdjacent>(p, i, 1, at[r][0], at[r][1]);
 #pragma unroll
-            for (int j = 0; j < kPairs; ++j) {
-                const float2 cs = turn[pair[r] + j];
-                float& a = flat[kAdjacent ? 2 * j : j];
-                float& b = flat[kAdjacent ? 2 * j + 1 : kPairs + j];
-                const float ra = a * cs.x - b * cs.y, rb = b * cs.x + a * cs.y;
-                a = ra, b = rb;
+            for (int m = 0; m < 2; ++m) {
+                x[r][m] = 0.0f;
+                if (there && i < half) {
+                    if constexpr (sizeof(T) == 2) x[r][m] = __half2float(from[at[r][m]]);
+                    else x[r][m] = from[at[r][m]];
+                }
+                squares += x[r][m] * x[r][m];
             }
-            store<kPairs>(to + at[r][0], y[r][0]);
-            store<kPairs>(to + at[r][1], y[r][1]);
+        }
+        for (int d = p.lanes / 2; d > 0; d >>= 1) squares += __shfl_xor_sync(0xFFFFFFFFu, squares, d);
+        if (!there) continue;
+        const float inv = rsqrtf(squares / p.dim + p.eps);
+        __half* to = is_q ? p.q_out + n * p.ldq_out + h * p.dim : p.k_out + n * p.ldk_out + (h - p.q_heads) * p.dim;
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const int i = r * p.lanes + lane;
+            if (i >= half) continue;
+            if (weight != nullptr) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) x[r][m] = x[r][m] * inv * __half2float(weight[at[r][m]]);
+            }
+            to[at[r][0]] = __float2half_rn(x[r][0] * cosines[i] - x[r][1] * sines[i]);
+            to[at[r][1]] = __float2half_rn(x[r][1] * cosines[i] + x[r][0] * sines[i]);
         }
     }
 }
 
-template <typename T, int kPairs>
-spdp_status launch_form(const Params& p, bool adjacent, int64_t N, int sms, cudaStream_t s) {
+template <typename T>
+spdp_status launch_form(const Params& p, bool wide, bool adjacent, int64_t N, int sms, cudaStream_t s) {
     // Rounds of a token's heads, with no more threads than make them equal.  One CTA takes them in turn (and the angles once)
     // where the tokens fill the GPU; else they are dealt out.
     const int heads = p.q_heads + p.kv_heads, rounds = (heads + (kThreads >> p.shift) - 1) / (kThreads >> p.shift);
@@ -155,8 +178,9 @@ spdp_status launch_form(const Params& p, bool adjacent, int64_t N, int sms, cuda
     const int64_t enough = (8 * sms + N - 1) / N;
     if (shares > enough) shares = enough;
     const dim3 grid(static_cast<unsigned>(N), static_cast<unsigned>(shares));
-    SPDP_CUDA_TRY(adjacent ? launch_programmatic(qk_norm_rope_kernel<T, kPairs, true>, grid, threads, 0, s, p)
-                           : launch_programmatic(qk_norm_rope_kernel<T, kPairs, false>, grid, threads, 0, s, p));
+    SPDP_CUDA_TRY(launch_programmatic(wide ? (adjacent ? qk_norm_rope_wide_kernel<T, true> : qk_norm_rope_wide_kernel<T, false>)
+                                           : (adjacent ? qk_norm_rope_kernel<T, true> : qk_norm_rope_kernel<T, false>),
+                                      grid, threads, 0, s, p));
     return SPDP_OK;
 }
 
@@ -178,9 +202,7 @@ spdp_status launch_qk_norm_rope(const HeadsCall& call, cudaStream_t s) {
     const bool wide = rows && call.head_dim % 16 == 0 && (call.adjacent || call.pairs % 8 == 0);
     const int needed = wide ? call.head_dim / 16 : call.head_dim / 2;
     for (p.lanes = 1, p.shift = 0; p.lanes < needed && p.lanes < 32; p.lanes *= 2) ++p.shift;
-    if (size == 4)
-        return wide ? launch_form<float, 8>(p, call.adjacent, call.N, sms, s) : launch_form<float, 1>(p, call.adjacent, call.N, sms, s);
-    return wide ? launch_form<__half, 8>(p, call.adjacent, call.N, sms, s) : launch_form<__half, 1>(p, call.adjacent, call.N, sms, s);
+    return size == 4 ? launch_form<float>(p, wide, call.adjacent, call.N, sms, s) : launch_form<__half>(p, wide, call.adjacent, call.N, sms, s);
 }
 
 }  // namespace spdp
