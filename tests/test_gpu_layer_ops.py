@@ -23,7 +23,11 @@ def S():
         pytest.skip("needs a CUDA device")
     from paper_2607_21985_b200 import spdp
     spdp.lib()
-    return spdp
+    yield spdp
+    # what the captured calls' graphs had stays with the driver until it is asked for: other tests look at free memory
+    import ctypes
+    torch.cuda.synchronize()
+    assert ctypes.CDLL("libcudart.so.12").cudaDeviceGraphMemTrim(torch.cuda.current_device()) == 0
 
 
 def dev(a):
