@@ -78,11 +78,26 @@ struct Layout {
 // adapter, and a tile is up to kTok tokens of a window that share one.  So 256 tokens that draw from 15 adapters are 15 to 23
 // tiles of 32, not 8 tiles of 13 adapters each.
 constexpr int kWindow = kThreads;
-struct Plan {
-    int tiles;
-    int2 tile[kWindow];             // adapter (-1: none), first place in `order` and 2^16 times the number of tokens
-    unsigned char order[kWindow];   // the window's tokens, by adapter
+struct Tile {
+    int adapter;                    // -1: none
+    unsigned bits;                  // first place in `order`, 9 bits; tokens, 6 bits; rank
+    __device__ __forceinline__ int first() const { return bits & 511; }
+    __device__ __forceinline__ int count() const { return bits >> 9 & 63; }
+    __device__ __forceinline__ int rank() const { return bits >> 15; }
 };
+__device__ __forceinline__ Tile make_tile(int adapter, int first, int count, int rank) {
+    return {adapter, static_cast<unsigned>(first | count << 9 | rank << 15)};
+}
+struct __align__(128) Plan {
+    int tiles;
+    unsigned char order[kWindow];   // the window's tokens, by adapter
+    Tile tile[kWindow];
+};
+
+__device__ __forceinline__ int rank_of(const Params& p, int a) {
+    const int rank = p.ranks != nullptr ? p.ranks[a] : p.rank;
+    return rank < 0 ? 0 : rank > p.rank ? p.rank : rank;
+}
 
 // The plan of a window with tiles of `tok` tokens, into shared memory (all threads; ends with a barrier); `wide`, if not null, gets
 // the plan with tiles of 32.  Tokens without an adapter take base as it is: in place they are left out.
@@ -92,6 +107,7 @@ __device__ void make_plan(const Params& p, int64_t n0, int tok, Plan& plan, Plan
     const int t = threadIdx.x, lane = t & 31, w = t >> 5, tokens = p.N - n0 < kWindow ? static_cast<int>(p.N - n0) : kWindow;
     int mine = t < tokens ? p.adapter[n0 + t] : -2;
     if (t < tokens && (mine < 0 || mine >= p.count)) mine = p.base != p.Y ? -1 : -2;
+    const int rank = mine >= 0 ? rank_of(p, mine) : 0;
     const unsigned same = __match_any_sync(0xFFFFFFFFu, mine), below = (1u << lane) - 1u;
     const int leader = __ffs(same) - 1;
     const unsigned leaders = __ballot_sync(0xFFFFFFFFu, lane == leader);
@@ -130,9 +146,9 @@ __device__ void make_plan(const Params& p, int64_t n0, int tok, Plan& plan, Plan
     const int start = front & 1023;
     if (leads) {
         starts[t] = start;
-        for (int i = 0, at = front >> 10 & 1023; i * tok < all; ++i) plan.tile[at + i] = make_int2(mine, start + i * tok | min(tok, all - i * tok) << 16);
+        for (int i = 0, at = front >> 10 & 1023; i * tok < all; ++i) plan.tile[at + i] = make_tile(mine, start + i * tok, min(tok, all - i * tok), rank);
         if (wide != nullptr)
-            for (int i = 0, at = front >> 20; 32 * i < all; ++i) wide->tile[at + i] = make_int2(mine, start + 32 * i | min(32, all - 32 * i) << 16);
+            for (int i = 0, at = front >> 20; 32 * i < all; ++i) wide->tile[at + i] = make_tile(mine, start + 32 * i, min(32, all - 32 * i), rank);
     }
     __syncthreads();
     if (mine != -2) plan.order[starts[lead] + before] = static_cast<unsigned char>(t);
@@ -142,11 +158,6 @@ __device__ void make_plan(const Params& p, int64_t n0, int tok, Plan& plan, Plan
         wide->order[t] = plan.order[t];
         if (t == 0) wide->tiles = total >> 20;
     }
-}
-
-__device__ __forceinline__ int rank_of(const Params& p, int a) {
-    const int rank = p.ranks != nullptr ? p.ranks[a] : p.rank;
-    return rank < 0 ? 0 : rank > p.rank ? p.rank : rank;
 }
 
 // A warp's block of output: 64 rows, eight to a lane (for two tokens of each column block).  kWide: base and Y are read and
@@ -320,9 +331,9 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
     if (share * kBlocksOfCluster >= blocks) return;
 
     for (int d = more ? z % tiles : z; d < tiles; d += p.per_window) {
-        const int2 tile = plan.tile[d];
-        const int a = tile.x, count = tile.y >> 16;
-        const unsigned char* list = plan.order + (tile.y & 0xFFFF);
+        const Tile tile = plan.tile[d];
+        const int a = tile.adapter, count = tile.count(), rank = tile.rank(), prank = padded_rank(rank);
+        const unsigned char* list = plan.order + tile.first();
         const int block0 = (share * kCluster + cta) * kWarps + w;
         if (a < 0) {
             if constexpr (!kSplit)
@@ -330,7 +341,6 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
                     expand_block<T, kCols, kAlign, true, false>(p, n0, list, count, a, 0, b * kOut, hi, lo, row, factors, nullptr);
             continue;
         }
-        const int rank = rank_of(p, a), prank = padded_rank(rank);
 
         // A x over this CTA's eighth of K
         const __half* A = p.A + a * p.stride_a;
@@ -457,32 +467,33 @@ __global__ void __launch_bounds__(32 * kExpandWarps, expand_ctas_of_sm<T>(kShort
     dev::programmatic_start();
     const int blocks = (p.M + kOut - 1) / kOut, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int64_t window = blockIdx.x / p.per_window, n0 = window * kWindow;
-    const int me = blockIdx.x % p.per_window * kExpandWarps + w, width = padded_rank(p.rank);
+    const int me = blockIdx.x % p.per_window * kExpandWarps + w, warps = p.per_window * kExpandWarps, width = padded_rank(p.rank);
     const Plan* plan = p.plans + window;
-    const int64_t units = static_cast<int64_t>(plan->tiles) * blocks;
-    int64_t u = units * me / (p.per_window * kExpandWarps);
-    const int64_t end = units * (me + 1) / (p.per_window * kExpandWarps);
+    const unsigned units = static_cast<unsigned>(plan->tiles) * static_cast<unsigned>(blocks), each = units / warps, more = units % warps;
+    unsigned u = me * each + min(static_cast<unsigned>(me), more);
+    const unsigned end = u + each + (me < static_cast<int>(more) ? 1 : 0);
     if (u >= end) return;
     T* olds = reinterpret_cast<T*>(shared) + w * 2 * kTok * kOldRow<T>;          // two blocks
-    auto copy = [&](int2 tile, int b, int to) {
+    auto copy = [&](Tile tile, int b, int to) {
         if constexpr (kWide) {
-            const unsigned char* list = plan->order + (tile.y & 0xFFFF);
+            const unsigned char* list = plan->order + tile.first();
+            const int count = tile.count();
             const T* from = static_cast<const T*>(p.base) + n0 * p.ldbase + b * kOut;
             const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(olds + to * kTok * kOldRow<T>));
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
                 const int n = i * (32 / kPieces) + lane / kPieces, part = lane % kPieces;
-                if (n < tile.y >> 16 && b * kOut + part * kPiece < p.M)
+                if (n < count && b * kOut + part * kPiece < p.M)
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + (n * kOldRow<T> + part * kPiece) * static_cast<int>(sizeof(T))),
                                  "l"(from + list[n] * p.ldbase + part * kPiece) : "memory");
             }
         }
     };
     int b = static_cast<int>(u % blocks), d = static_cast<int>(u / blocks);
-    int2 tile = plan->tile[d];
+    Tile tile = plan->tile[d];
     copy(tile, b, 0);
     if constexpr (kWide) asm volatile("cp.async.commit_group;" ::: "memory");
-    int rank = tile.x >= 0 ? rank_of(p, tile.x) : 0;
+    int rank = tile.rank();
     const __half* hi = p.vectors + n0 * width;
     if constexpr (kShort) {
         constexpr bool kTwo = sizeof(T) == 4;
@@ -492,14 +503,14 @@ __global__ void __launch_bounds__(32 * kExpandWarps, expand_ctas_of_sm<T>(kShort
         float down[kMostCols][2];
         uint4 x[kMostCols], z[kTwo ? kMostCols : 1], v[4][2], ahead[4][2];
         auto enter = [&]() {                                     // a tile
-            const unsigned char* list = plan->order + (tile.y & 0xFFFF);
-            const int count = tile.y >> 16;
+            const unsigned char* list = plan->order + tile.first();
+            const int count = tile.count();
 #pragma unroll
             for (int t = 0; t < kMostCols; ++t) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     token[t][h] = 8 * t + 2 * c + h < count ? list[8 * t + 2 * c + h] : -1;
-                    down[t][h] = token[t][h] >= 0 && tile.x >= 0 ? p.factors[n0 + token[t][h]] : 0.0f;
+                    down[t][h] = token[t][h] >= 0 && tile.adapter >= 0 ? p.factors[n0 + token[t][h]] : 0.0f;
                 }
                 x[t] = make_uint4(0, 0, 0, 0);
                 if constexpr (kTwo) z[t] = make_uint4(0, 0, 0, 0);
@@ -517,18 +528,14 @@ __global__ void __launch_bounds__(32 * kExpandWarps, expand_ctas_of_sm<T>(kShort
             for (int j = 0; j < 8; ++j, at += p.ldb) into[j / 2][j % 2] = dev::load8<16>(at, 8 * c, m0 < p.M ? its_rank : 0);
         };
         enter();
-        weights(v, tile.x, rank, b);
+        weights(v, tile.adapter, rank, b);
         for (int i = 0; u < end; ++u, i ^= 1) {
             const bool last = b + 1 == blocks;                   // of its tile
-            int2 next = tile;
-            int next_rank = rank;
+            Tile next = tile;
             if (u + 1 < end) {
-                if (last) {
-                    next = plan->tile[d + 1];
-                    next_rank = next.x >= 0 ? rank_of(p, next.x) : 0;
-                }
+                if (last) next = plan->tile[d + 1];
                 copy(next, last ? 0 : b + 1, i ^ 1);
-                weights(ahead, next.x, next_rank, last ? 0 : b + 1);
+                weights(ahead, next.adapter, next.rank(), last ? 0 : b + 1);
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
             asm volatile("cp.async.wait_group 1;" ::: "memory");
@@ -542,7 +549,7 @@ __global__ void __launch_bounds__(32 * kExpandWarps, expand_ctas_of_sm<T>(kShort
             const bool there = b * kOut + 8 * g < p.M;
 #pragma unroll
             for (int t = 0; t < kMostCols; ++t) {
-                if (8 * t >= tile.y >> 16) break;
+                if (8 * t >= tile.count()) break;
                 float acc[4][4] = {};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -559,7 +566,7 @@ __global__ void __launch_bounds__(32 * kExpandWarps, expand_ctas_of_sm<T>(kShort
                     if (!there || token[t][h] < 0) continue;
                     const T* from = old + (8 * t + 2 * c + h) * kOldRow<T>;
                     T* to = y + token[t][h] * p.ldy;
-                    if (tile.x < 0) {
+                    if (tile.adapter < 0) {
 #pragma unroll
                         for (int j = 0; j < static_cast<int>(sizeof(T)) / 2; ++j) reinterpret_cast<uint4*>(to)[j] = reinterpret_cast<const uint4*>(from)[j];
                     } else {
@@ -574,7 +581,7 @@ __global__ void __launch_bounds__(32 * kExpandWarps, expand_ctas_of_sm<T>(kShort
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j / 2][j % 2] = ahead[j / 2][j % 2];
             if (last) {
-                tile = next, rank = next_rank, ++d, b = 0;
+                tile = next, rank = next.rank(), ++d, b = 0;
                 if (u + 1 < end) enter();
             } else {
                 ++b;
@@ -583,7 +590,7 @@ __global__ void __launch_bounds__(32 * kExpandWarps, expand_ctas_of_sm<T>(kShort
     } else {
         for (int i = 0; u < end; ++u, i ^= 1) {
             const bool last = b + 1 == blocks;                       // of its tile
-            int2 next = tile;
+            Tile next = tile;
             if (u + 1 < end) {
                 if (last) next = plan->tile[d + 1];
                 copy(next, last ? 0 : b + 1, i ^ 1);
@@ -593,12 +600,12 @@ __global__ void __launch_bounds__(32 * kExpandWarps, expand_ctas_of_sm<T>(kShort
                 asm volatile("cp.async.wait_group 1;" ::: "memory");
                 __syncwarp();
             }
-            expand_block<T, kMostCols, kAlign, kWide, true>(p, n0, plan->order + (tile.y & 0xFFFF), tile.y >> 16, tile.x, rank, b * kOut, hi,
+            expand_block<T, kMostCols, kAlign, kWide, true>(p, n0, plan->order + tile.first(), tile.count(), tile.adapter, rank, b * kOut, hi,
                                                             hi + static_cast<int64_t>(p.N) * width, width, p.factors + n0, kWide ? olds + i * kTok * kOldRow<T> : nullptr);
             if constexpr (kWide) __syncwarp();                       // all lanes have read the block before it is overwritten
             if (last) {
                 tile = next, ++d, b = 0;
-                rank = tile.x >= 0 ? rank_of(p, tile.x) : 0;
+                rank = tile.rank();
             } else {
                 ++b;
             }
@@ -663,7 +670,7 @@ spdp_status launch_typed(Params p, int align, int device, int sms, cudaStream_t 
     }
     const bool few = p.N <= kFewTokens && align == 16;
     const int windows = (p.N + kWindow - 1) / kWindow, width = padded_rank(p.rank);
-    const size_t vectors = 2ull * p.N * width * (sizeof(T) == 4 ? 2 : 1), factors = (4ull * p.N + 15) / 16 * 16;
+    const size_t vectors = (2ull * p.N * width * (sizeof(T) == 4 ? 2 : 1) + 127) / 128 * 128, factors = (4ull * p.N + 127) / 128 * 128;
     void* scratch = nullptr;
     spdp_status st = scratch_alloc(device, vectors + factors + windows * sizeof(Plan), s, &scratch);
     if (st != SPDP_OK) return st;
