@@ -249,9 +249,10 @@ SPDP_API spdp_status spdp_swiglu_dp(const void* gate_dev, const void* up_dev, in
                            void* mask_dev_out, void* count_dev_out, void* stream);
 
 /* ---- around the projections of a decoder layer ------------------------------------------------------------
- * The calls of this part take no handle: they run on the current device, which must hold every *_dev pointer, allocate nothing
- * that outlasts the call, are asynchronous on `stream`, may be captured, and give the same bits for the same arguments.  Calls
- * with different outputs may overlap.  An output may not overlap an input unless the call says so. */
+ * The calls of this part take no handle: they run on the current device, which must hold every *_dev pointer, are asynchronous
+ * on `stream`, may be captured, and give the same bits for the same arguments.  Two of them take scratch memory, stream-ordered from
+ * the pool that spdp_spmm describes (SPDP_ERR_ALLOC where there is none); each call has its own.  Calls with different outputs may
+ * overlap.  An output may not overlap an input unless the call says so. */
 
 /* Low-rank adapters of many requests beside a shared projection: Y[n] = base[n] + scale_a * B_a * (A_a * X[n]) with
  * a = adapter[n] (the paper has no adapters; merging B A into a statically pruned W would fill its zeros, so the adapters of a
@@ -267,8 +268,9 @@ SPDP_API spdp_status spdp_swiglu_dp(const void* gate_dev, const void* up_dev, in
  *   base_dev     [N][ldbase] of ydt, ldbase >= M; may be Y_dev itself (with ldbase = ldy): the adapters are then added in place.
  *   Y_dev        [N][ldy] of ydt, ldy >= M.
  * Sums in 32 bits; the vector between the two products is rounded to 11 bits for 16-bit results and to 22 for
- * 32-bit ones (both with the range of 32-bit numbers).  Rows that start on 16-byte boundaries (addresses and strides) are the
- * fast case.  Launches one kernel. */
+ * 32-bit ones (both with the range of 32-bit numbers).  The tokens of an adapter need not stand together.  The fast case: rows
+ * that start on 16-byte boundaries (addresses and strides), K, M and rank multiples of 8.  Launches one kernel for up to 4 tokens
+ * and else two, with scratch memory (2 * rank + 13 bytes for each token, 4 * rank + 13 with 32-bit results). */
 #define SPDP_MAX_RANK 256
 SPDP_API spdp_status spdp_lora(const void* X_dev, int64_t N, int64_t K, int64_t ldx, const void* adapter_dev, const void* A_dev, int64_t lda,
                       int64_t stride_a, const void* B_dev, int64_t ldb, int64_t stride_b, int64_t count, int rank, const void* ranks_dev,
@@ -335,9 +337,9 @@ SPDP_API spdp_status spdp_kv4_store(const void* k_dev, int64_t ldk, const void* 
  *   y_dev        fp16 [B][ldy], ldy >= q_heads * head_dim.
  *   mask_dev_out uint32 [B][mask_stride], mask_stride >= q_heads * head_dim / 32, or NULL: the columns that the o-projection
  *                should keep, NOT(|y_j| <= thr) on the stored y, for SPDP_DP_MASK (thr is used for nothing else).
- * What lies in the cache behind a request's last key is never used, whatever it is.  Sums in 32 bits; decoded values and the
- * softmax's weights are rounded to fp16 for their product.  Launches two kernels; scratch memory (a few MB) comes from the pool
- * that spdp_spmm describes. */
+ * What lies in the cache behind a request's last key is never used, whatever it is.  Sums in 32 bits; the softmax's weights, times
+ * the scales of the values, are rounded to fp16 for their product with these.  Where the requests are few and table_pages (or the
+ * window) says that they are short, the call launches one kernel; else two, with scratch memory (a few MB). */
 SPDP_API spdp_status spdp_attn_kv4(const void* q_dev, int64_t ldq, int64_t B, int q_heads, int kv_heads, int head_dim, const void* cache_dev, int64_t pages,
                           int page_tokens, const void* table_dev, int64_t table_stride, int64_t table_pages, const void* length_dev, float scale,
                           float cap, int64_t window, float thr, void* y_dev, int64_t ldy, void* mask_dev_out, int64_t mask_stride, void* stream);

@@ -540,6 +540,20 @@ def test_attn_kv4_captured_and_on_streams(S, columns):
     del graphs
 
 
+def test_tensors_of_another_device_are_refused(S, monkeypatch):
+    """The calls run on the current device: tensors of another one are refused before anything is launched."""
+    c = lora_case(1, 4, 64, 64, 8, 2)
+    x = torch.zeros(4, 2, 64, dtype=torch.float16, device="cuda")
+    cache = torch.zeros(2, S.spdp_kv4_page_bytes(2, 64, 16), dtype=torch.uint8, device="cuda")
+    i32 = torch.zeros(4, dtype=torch.int32, device="cuda")
+    S.spdp_lora(Y=c["base"].clone(), **c)
+    monkeypatch.setattr(S, "_device", lambda: torch.cuda.device_count())
+    for call in (lambda: S.spdp_lora(Y=c["base"].clone(), **c), lambda: S.spdp_qk_norm_rope(x, None, x, None, None, None),
+                 lambda: S.spdp_kv4_store(x, x, i32.long(), cache, 16), lambda: S.spdp_attn_kv4(x, cache, 16, 2, i32[:, None], i32, x.view(4, -1), 1.0)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+
+
 # ---- together ---------------------------------------------------------------------------------------------------------------
 
 def test_decode_steps_of_an_attention_block(S):
