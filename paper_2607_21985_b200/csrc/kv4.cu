@@ -34,8 +34,9 @@ struct StoreParams {
 };
 
 // x / s, correctly rounded where the quotient is a number of 24 bits (as where a code lies half way between two, which are n +
-// 1/2) and else to within a step: a product with the reciprocal, corrected by its exact remainder (Markstein).  Quotients of fp16
-// numbers that are not half way are 2^-12 and more of their size away from it, so rint() gives what it gives for the true quotient.
+// 1/2) and else to within a step: a product with the reciprocal (to within a step itself), corrected by its exact remainder
+// (Markstein).  Quotients of fp16 numbers that are not half way are 2^-12 and more of their size away from it, and sevenths 2^-15
+// and more away from the middle of two fp16 numbers, so rounding gives what it gives for the true quotient.
 __device__ __forceinline__ float quotient(float x, float s, float reciprocal) {
     const float q = x * reciprocal;
     return fmaf(fmaf(-q, s, x), reciprocal, q);
@@ -67,26 +68,42 @@ __device__ __forceinline__ void store_rows(const StoreParams& p, const T* from, 
         for (int j = 0; j < kTokens; ++j) {
             const int64_t n = n0 + j * blockDim.y;
             if (n >= p.N) continue;
+            if constexpr (sizeof(T) == 4) {                      // 32-bit rows count as the fp16 row they round to
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float2 f = __half22float2(__floats2half2_rn(x[j][e], x[j][e + 1]));
+                    x[j][e] = f.x, x[j][e + 1] = f.y;
+                }
+            }
             float top = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if constexpr (sizeof(T) == 4) x[j][e] = __half2float(__float2half_rn(x[j][e]));          // 32-bit rows count as the fp16 row they round to
-                top = fmaxf(top, fabsf(x[j][e]));
-            }
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[j][e]));
             top = fmaxf(top, __shfl_xor_sync(four, top, 1));
             top = fmaxf(top, __shfl_xor_sync(four, top, 2));
-            const __half scale = __float2half_rn(__fdiv_rn(top, 7.0f));
-            const float s = __half2float(scale), reciprocal = s > 0.0f ? __frcp_rn(s) : 0.0f;
+            const __half scale = __float2half_rn(quotient(top, 7.0f, 1.0f / 7.0f));
+            const float s = __half2float(scale);
+            float reciprocal;
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(reciprocal) : "f"(s));
+            if (!(s > 0.0f)) reciprocal = 0.0f;
             // Adding 1.5 2^23 + 8 rounds to a whole number, ties to even, and leaves it, 8 more, in the lowest bits
             constexpr float kWhole = 12582912.0f + 8.0f;
             constexpr uint32_t kWholeBits = 0x4B400000u;
-            uint32_t word = 0;
+            float q[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q[e] = quotient(x[j][e], s, reciprocal);
+            if (!(s >= 0x1p-14f && s < 0x1p15f)) {               // else 7 (1 + 2^-11) at most; a subnormal scale may be far off a seventh
+#pragma unroll
+                for (int e = 0; e < 8; ++e) q[e] = fminf(fmaxf(q[e], -7.0f), 7.0f);
+            }
+            uint32_t word = 0, offset = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float whole = fminf(fmaxf(quotient(x[j][e], s, reciprocal), -7.0f), 7.0f) + kWhole;
-                word += (__float_as_uint(whole) - kWholeBits) << (4 * e);
+                const float whole = q[e] + kWhole;
+                word += __float_as_uint(whole) << (4 * e);
+                offset += kWholeBits << (4 * e);
                 x[j][e] = (whole - kWhole) * s;
             }
+            word -= offset;
             const int64_t page = slot[j] >> p.page_shift;
             if (slot[j] >= 0 && page < p.pages) {
                 const uint64_t first = static_cast<uint64_t>(static_cast<unsigned>(page)) * page_bytes;
