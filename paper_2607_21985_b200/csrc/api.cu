@@ -638,10 +638,11 @@ spdp_status spdp_attn_kv4(const void* q_dev, int64_t ldq, int64_t B, int q_heads
     if (misaligned(q_dev, 1u) || misaligned(cache_dev, 15u) || misaligned(table_dev, 3u) || misaligned(length_dev, 3u) || misaligned(y_dev, 1u) ||
         misaligned(mask_dev_out, 3u))
         return SPDP_ERR_INVALID_ARG;
-    // the keys of a request, and the 64-key units of all requests and heads, are counted in 32 bits
+    // the keys of a request, and the 64-key units of all requests and heads with what the kernel adds to each (7 at most, a part of
+    // a unit among them), are counted in 32 bits
     if (table_pages > INT32_MAX / page_tokens - 64) return SPDP_ERR_UNSUPPORTED_SHAPE;
     const int64_t triples = kv_heads * static_cast<int64_t>((q_heads / kv_heads + 7) / 8);
-    if (triples * (table_pages * page_tokens / 64 + 4) > INT32_MAX / B) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    if (triples * (table_pages * page_tokens / 64 + 8) > INT32_MAX / B) return SPDP_ERR_UNSUPPORTED_SHAPE;
     Kv4AttnCall c = {};
     c.q = static_cast<const __half*>(q_dev), c.cache = static_cast<const unsigned char*>(cache_dev), c.table = static_cast<const int32_t*>(table_dev);
     c.length = static_cast<const int32_t*>(length_dev), c.y = static_cast<__half*>(y_dev), c.mask = static_cast<uint32_t*>(mask_dev_out);

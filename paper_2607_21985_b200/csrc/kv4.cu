@@ -192,7 +192,7 @@ __device__ __forceinline__ Span span_of(const AttnParams& p, int b) {
 
 // A triple costs what its units do and, for its query heads and its sums, as much as kStart more: it is that long in the line
 // that is cut into runs.  (With 0 a CTA that met many short requests took half as long again as the others.)
-constexpr int kStart = 6;
+constexpr int kStart = 6;               // spdp_attn_kv4 counts on 7 at most when it checks that a line's length fits 32 bits
 __device__ __forceinline__ int triple_length(int units) { return units > 0 ? units + kStart : 0; }
 
 // Where the run of CTA i begins, of `ctas` that share a line of `total`.

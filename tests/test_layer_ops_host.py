@@ -81,6 +81,13 @@ def test_attn_kv4_refuses(L, change, status):
     assert L.spdp_attn_kv4(*dict(ATTN, **change).values()) == status
 
 
+def test_attn_kv4_refuses_more_units_than_32_bits_count(L):
+    """2^24 pairs of a request and a key head of up to 124 units of 64 keys; with 6 more to each, as the kernel counts, above 2^31."""
+    many = dict(ATTN, B=4096, q_heads=4096, kv_heads=4096, dim=64, ldq=1 << 18, ldy=1 << 18, mask_stride=1 << 13, table_pages=495, table_stride=495)
+    assert 4096 * 4096 * (124 + 6) >= 2 ** 31
+    assert L.spdp_attn_kv4(*many.values()) == SHAPE
+
+
 def test_page_bytes(L):
     for heads, dim, page in ((1, 64, 16), (8, 128, 64), (3, 256, 256), (12, 128, 32)):
         assert spdp.spdp_kv4_page_bytes(heads, dim, page) == heads * page * 2 * (dim // 2 + dim // 32 * 2)
