@@ -8,6 +8,7 @@
 // for one step of the product all belongs to one scale.
 #include <cooperative_groups.h>
 
+#include <cfloat>
 #include <mutex>
 
 #include "mma_f16.cuh"
@@ -905,7 +906,7 @@ spdp_status launch_attn_kv4(const Kv4AttnCall& call, cudaStream_t s) {
     constexpr float kLog2e = 1.4426950408889634f;
     p.scale = call.scale * kLog2e;
     p.cap = call.cap * kLog2e;
-    p.cap_inv = call.cap > 0.0f ? 2.0f / call.cap : 0.0f;       // e^(2 s / cap) = 2^(s log2(e) * 2 / cap)
+    p.cap_inv = call.cap > 0.0f ? fminf(2.0f / call.cap, FLT_MAX) : 0.0f;      // e^(2 s / cap) = 2^(s log2(e) * 2 / cap); never Inf, for a score may be 0
     p.window = call.window, p.thr = call.thr;
     p.wide_q = rows_aligned16(p.q, p.ldq, 2), p.wide_y = rows_aligned16(p.y, p.ldy, 2);
     switch (call.head_dim) {

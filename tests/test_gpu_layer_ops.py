@@ -431,6 +431,16 @@ def test_attn_kv4_values_of_all_sizes(S, sizes):
     attn_check(y, q, oracle, table, [n], 0.2, most=max(sizes))
 
 
+@pytest.mark.parametrize("columns", [0, 600])
+def test_attn_kv4_caps_that_leave_nothing_of_the_scores(S, columns):
+    """A cap whose reciprocal is beyond 32 bits: all scores are 0 or as good as 0, whether the products are 0 or not."""
+    rng = np.random.default_rng(11)
+    cache, table, oracle = filled(rng, 1, 64, 16, [40])
+    q, y = dev(np.stack([np.zeros(64), rng.standard_normal(64)])[None].astype(np.float16)), torch.empty(1, 128, dtype=torch.float16, device="cuda")
+    S.spdp_attn_kv4(q, cache, 16, 1, dev(np.concatenate([table, np.zeros((1, columns), np.int32)], 1)), dev(np.array([40], np.int32)), y, 0.1, cap=1e-40)
+    attn_check(y, q * 0, oracle, table, [40], 0.1)
+
+
 def plain_attention(q, k, v, scale):
     """In 64 bits on the device: q [H][D], k and v [kv heads][keys][D]."""
     z = torch.einsum("hgd,htd->hgt", q.double().unflatten(0, (k.shape[0], -1)), k) * scale
