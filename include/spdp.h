@@ -332,7 +332,8 @@ SPDP_API spdp_status spdp_kv4_store(const void* k_dev, int64_t ldk, const void* 
  *                outside 0 .. pages-1 are left out.
  *   length_dev   int32 [B]: keys of each request, the new token's own among them (store it first); values below 0 and above
  *                table_pages * page_tokens count as these.  A request without keys gets zeros.
- *   cap          > 0: scores are capped; 0: they are not.
+ *   scale        between -10^16 and 10^16.
+ *   cap          > 0 (10^38 at most): scores are capped; 0: they are not.
  *   window       > 0: only the last `window` keys count; 0: all do.
  *   y_dev        fp16 [B][ldy], ldy >= q_heads * head_dim.
  *   mask_dev_out uint32 [B][mask_stride], mask_stride >= q_heads * head_dim / 32, or NULL: the columns that the o-projection

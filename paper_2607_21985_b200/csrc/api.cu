@@ -634,7 +634,8 @@ spdp_status spdp_attn_kv4(const void* q_dev, int64_t ldq, int64_t B, int q_heads
     if (pages < 1 || pages > INT32_MAX || table_pages < 1 || !stride_ok(table_stride, table_pages) || !stride_ok(ldq, row) || !stride_ok(ldy, row) || window < 0)
         return SPDP_ERR_INVALID_ARG;
     if (mask_dev_out != nullptr && !stride_ok(mask_stride, row / 32)) return SPDP_ERR_INVALID_ARG;
-    if (!(scale >= -1.0e38f && scale <= 1.0e38f) || !(cap >= 0.0f && cap <= 1.0e38f)) return SPDP_ERR_INVALID_ARG;
+    // products are below 2^41, so scores stay below the 10^30 that stands for "no score yet" in the kernel
+    if (!(scale >= -1.0e16f && scale <= 1.0e16f) || !(cap >= 0.0f && cap <= 1.0e38f)) return SPDP_ERR_INVALID_ARG;
     if (misaligned(q_dev, 1u) || misaligned(cache_dev, 15u) || misaligned(table_dev, 3u) || misaligned(length_dev, 3u) || misaligned(y_dev, 1u) ||
         misaligned(mask_dev_out, 3u))
         return SPDP_ERR_INVALID_ARG;

@@ -88,6 +88,11 @@ def test_attn_kv4_refuses_more_units_than_32_bits_count(L):
     assert L.spdp_attn_kv4(*many.values()) == SHAPE
 
 
+@pytest.mark.parametrize("scale", [1.1e16, -1.1e16, 1e38])
+def test_attn_kv4_refuses_scales_beyond_its_scores(L, scale):
+    assert L.spdp_attn_kv4(*dict(ATTN, scale=scale).values()) == INVALID
+
+
 def test_page_bytes(L):
     for heads, dim, page in ((1, 64, 16), (8, 128, 64), (3, 256, 256), (12, 128, 32)):
         assert spdp.spdp_kv4_page_bytes(heads, dim, page) == heads * page * 2 * (dim // 2 + dim // 32 * 2)
