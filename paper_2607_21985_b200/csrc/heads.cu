@@ -7,6 +7,9 @@
 // serve all heads.  An angle is formed in 64 bits and in turns, so that whole turns drop out exactly: at position 10^6 a 32-bit
 // angle is off by up to 0.03.  A lane holds both members of its pairs; 8 pairs to a lane where alignment lets it load 16 bytes
 // at once, so 8 lanes share a head of 128 and the sum of squares takes 3 exchanges.
+//
+// 4096 tokens of 64 and 8 heads of 128 from 32-bit rows: 39 us, 226 MB at 5.8 TB/s.  2547 of 32 and 8 heads of 256, 16-bit: 35 us, 49
+// with one kernel for every alignment, whose sines and cosines came from shared memory for each head.
 #include "mma_f16.cuh"
 #include "spdp_internal.h"
 

@@ -5,15 +5,21 @@
 // Both products run on mma.sync with tokens as the 8 columns and weight rows as the 16 rows, fragments loaded straight from
 // memory: a lane holds 8 consecutive elements of a row, the same on both sides.
 //
-// First product: a cluster of 8 CTAs takes a tile of consecutive tokens and one adapter among them after another; each CTA
-// multiplies an eighth of K (its warps split that again), and the partial sums meet through distributed shared memory in a fixed
-// order.  The vectors between the products are kept in fp16 for the second one, scaled per token by a power of two (so that
-// neither end of the range is lost): one rounding of 2^-11 on a term that is added to a 16-bit result; for 32-bit results a
-// second fp16 number holds what the first one lost.  Second product: a warp takes 64 output rows and the tile's tokens, and asks
-// for base before it multiplies.
+// Tokens are brought together by adapter, 256 of them (a window) at a time, into tiles of up to 32 (8 where the tokens are few)
+// that share one: the plan of a window.
 //
-// Few tokens: one launch does both, the clusters keep the vectors and go on to the output rows.  Many: a second kernel with a
-// warp to each block of output, so that the loads of all of them are on their way at once (1024 tokens, 28672 x 8192, rank 16: LORA_TIMES).
+// First product: a cluster of 8 CTAs to a tile; each CTA multiplies an eighth of K (its warps split that again), and the partial
+// sums meet through distributed shared memory in a fixed order.  The vectors between the products are kept in fp16 for the second
+// one, scaled per token by a power of two (so that neither end of the range is lost): one rounding of 2^-11 on a term that is
+// added to a 16-bit result; for 32-bit results a second fp16 number holds what the first one lost.
+//
+// Second product, a kernel of its own: the blocks of 64 output rows of all tiles stand in one line that is dealt out evenly to the
+// warps, base comes to shared memory one block ahead.  For up to 4 tokens one launch does both products: the clusters keep the
+// vectors and go on to the output rows (4096 x 4096, rank 16, 1 token, in a graph: 6.2 us, two launches 8.8).
+//
+// 1024 tokens of 28672 x 8192, rank 16, 16-bit results: 42 us of which the first kernel takes 13 and the second 28 (base and Y at 4.2
+// TB/s); the first is bound by its chain (plan, two rounds of loads, exchange of the sums), the second by the waits between the
+// steps of a block at the 11 warps that its registers allow.  8 tokens of rank 64: 17 us, the same chain twice.
 #include <cooperative_groups.h>
 
 #include <mutex>
@@ -30,11 +36,11 @@ constexpr int kMostCols = 4;        // column blocks of 8 tokens in a tile: 1 or
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kCluster = 8;
-constexpr int kExpandWarps = 4;     // of a CTA of the second kernel; three CTAs to an SM, for the registers that its loads take
+constexpr int kExpandWarps = 4;     // of a CTA of the second kernel
 constexpr int kOut = 64;            // output rows of a warp's block
 constexpr int kBlocksOfCluster = kCluster * kWarps;
-constexpr int kFusedTokens = 4;     // up to here one launch does both products (4096 x 4096, rank 16, 1 token: 6.2 us in a graph, two launches 8.8)
-constexpr int kFewTokens = 64;               // up to here tiles are 8 tokens, for there are more adapters than tiles of 32
+constexpr int kFusedTokens = 4;     // up to here one launch does both products
+constexpr int kFewTokens = 64;      // up to here tiles are 8 tokens, for there are more adapters than tiles of 32
 
 struct Params {
     const __half* X;
