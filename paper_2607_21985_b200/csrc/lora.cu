@@ -6,12 +6,13 @@
 // memory: a lane holds 8 consecutive elements of a row, the same on both sides.
 //
 // Tokens are brought together by adapter, 256 of them (a window) at a time, into tiles of up to 32 (8 where the tokens are few)
-// that share one: the plan of a window.
+// that share one: the plan of a window, laid out on the device.
 //
-// First product: a cluster of 8 CTAs to a tile; each CTA multiplies an eighth of K (its warps split that again), and the partial
-// sums meet through distributed shared memory in a fixed order.  The vectors between the products are kept in fp16 for the second
-// one, scaled per token by a power of two (so that neither end of the range is lost): one rounding of 2^-11 on a term that is
-// added to a 16-bit result; for 32-bit results a second fp16 number holds what the first one lost.
+// First product: a cluster of 8 CTAs to a tile, or to as many tiles as bring all of them into one round; each of a tile's CTAs
+// multiplies its share of K (its warps split that again), and the partial sums meet through distributed shared memory in a fixed
+// order.  The vectors between the products are kept in fp16 for the second one, scaled per token by a power of two (so that neither
+// end of the range is lost): one rounding of 2^-11 on a term that is added to a 16-bit result; for 32-bit results a second fp16
+// number holds what the first one lost.
 //
 // Second product, a kernel of its own: the blocks of 64 output rows of all tiles stand in one line that is dealt out evenly to the
 // warps, base comes to shared memory one block ahead.  For up to 4 tokens one launch does both products: the clusters keep the
@@ -40,7 +41,9 @@ constexpr int kExpandWarps = 4;     // of a CTA of the second kernel
 constexpr int kOut = 64;            // output rows of a warp's block
 constexpr int kBlocksOfCluster = kCluster * kWarps;
 constexpr int kFusedTokens = 4;     // up to here one launch does both products
-constexpr int kFewTokens = 64;      // up to here tiles are 8 tokens, for there are more adapters than tiles of 32
+// Up to here tiles of the first product are 8 tokens, which loads further ahead; beyond, 32 that read A once (4 adapters of rank 16:
+// 512 tokens of 8192 x 28672 equal, 1024 39 against 41 us; 8 of rank 64, 500 tokens of 8192 x 8192 27 against 30, 128 18 : 24).
+constexpr int kFewTokens = 512;
 
 struct Params {
     const __half* X;
@@ -106,7 +109,9 @@ __device__ __forceinline__ int rank_of(const Params& p, int a) {
 }
 
 // The plan of a window with tiles of `tok` tokens, into shared memory (all threads; ends with a barrier); `wide`, if not null, gets
-// the plan with tiles of 32.  Tokens without an adapter take base as it is: in place they are left out.
+// the plan with tiles of 32.  Tokens without an adapter take base as it is: in place they are left out, and in `plan` unless it is
+// for both products (kBare).
+template <bool kBare>
 __device__ void make_plan(const Params& p, int64_t n0, int tok, Plan& plan, Plan* wide) {
     __shared__ int2 entries[kWarps][32];                        // of each warp: an adapter, its tokens and (2^8) the first one's lane
     __shared__ int starts[kWindow], warp_sums[kWarps], warp_entries[kWarps];
@@ -133,7 +138,8 @@ __device__ void make_plan(const Params& p, int64_t n0, int tok, Plan& plan, Plan
     before += __popc(same & below);
     const bool leads = mine != -2 && lead == t;
     // places, tiles and tiles of 32 of the adapters in front, ten bits each
-    int sum = leads ? all | (all + tok - 1) / tok << 10 | (all + 31) / 32 << 20 : 0;
+    const int here = kBare || mine >= 0 ? all : 0;
+    int sum = leads ? all | (here + tok - 1) / tok << 10 | (all + 31) / 32 << 20 : 0;
     const int own = sum;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -152,7 +158,7 @@ __device__ void make_plan(const Params& p, int64_t n0, int tok, Plan& plan, Plan
     const int start = front & 1023;
     if (leads) {
         starts[t] = start;
-        for (int i = 0, at = front >> 10 & 1023; i * tok < all; ++i) plan.tile[at + i] = make_tile(mine, start + i * tok, min(tok, all - i * tok), rank);
+        for (int i = 0, at = front >> 10 & 1023; i * tok < here; ++i) plan.tile[at + i] = make_tile(mine, start + i * tok, min(tok, all - i * tok), rank);
         if (wide != nullptr)
             for (int i = 0, at = front >> 20; 32 * i < all; ++i) wide->tile[at + i] = make_tile(mine, start + 32 * i, min(32, all - 32 * i), rank);
     }
@@ -327,7 +333,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
     const int cta = blockIdx.x % kCluster, z = blockIdx.x / kCluster % p.per_window;
     const int64_t window = blockIdx.x / kCluster / p.per_window, n0 = window * kWindow;
     __shared__ Plan plan;
-    make_plan(p, n0, kTok, plan, kSplit && cta == 0 && z == 0 ? p.plans + window : nullptr);
+    make_plan<!kSplit>(p, n0, kTok, plan, kSplit && cta == 0 && z == 0 ? p.plans + window : nullptr);
     const int tiles = plan.tiles;
     if (tiles == 0) return;
     // more clusters than tiles: they share a tile's output rows; else a cluster takes several tiles in turn
@@ -335,27 +341,34 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
     const int sharers = more ? (p.per_window - z % tiles + tiles - 1) / tiles : 1, share = more ? z / tiles : 0;
     const int blocks = (p.M + kOut - 1) / kOut;
     if (share * kBlocksOfCluster >= blocks) return;
+    // kSplit: where there are more tiles than clusters, a cluster takes 2, 4 or 8 at a time, with fewer CTAs to each (256 tokens with
+    // adapters of their own, rank 16, 4096 x 11008: 64 -> 51 us; 2048 that share 8: 38.7 -> 34.3)
+    static_assert(kCluster == 8, "CTAs of a tile: 1 << shift");
+    int shift = 3;
+    if constexpr (kSplit)
+        while (shift > 0 && tiles > p.per_window << (3 - shift)) --shift;
+    const int sharing = 1 << shift, at_once = kCluster >> shift, mate = cta & (sharing - 1);
 
-    for (int d = more ? z % tiles : z; d < tiles; d += p.per_window) {
-        const Tile tile = plan.tile[d];
+    for (int d0 = more ? z % tiles : z * at_once; d0 < tiles; d0 += p.per_window * at_once) {
+        const int d = d0 + (cta >> shift);
+        const Tile tile = d < tiles ? plan.tile[d] : make_tile(-1, 0, 0, 0);
         const int a = tile.adapter, count = tile.count(), rank = tile.rank(), prank = padded_rank(rank);
         const unsigned char* list = plan.order + tile.first();
         const int block0 = (share * kCluster + cta) * kWarps + w;
-        if (a < 0) {
-            if constexpr (!kSplit)
-                for (int b = block0; b < blocks; b += sharers * kBlocksOfCluster)
-                    expand_block<T, kCols, kAlign, true, false>(p, n0, list, count, a, 0, b * kOut, hi, lo, row, factors, nullptr);
+        if (!kSplit && a < 0) {                              // the same for the whole cluster
+            for (int b = block0; b < blocks; b += sharers * kBlocksOfCluster)
+                expand_block<T, kCols, kAlign, true, false>(p, n0, list, count, a, 0, b * kOut, hi, lo, row, factors, nullptr);
             continue;
         }
 
-        // A x over this CTA's eighth of K
+        // A x over this CTA's share of K (a < 0: its rank is 0, and it only keeps step with the cluster)
         const __half* A = p.A + a * p.stride_a;
         int token[kCols];                                    // the lane's, behind n0
 #pragma unroll
         for (int t = 0; t < kCols; ++t) token[t] = 8 * t + g < count ? list[8 * t + g] : -1;
         const __half* X = p.X + n0 * p.ldx;
         const int steps = (p.K + 31) / 32;
-        const int s0 = static_cast<int>(static_cast<int64_t>(steps) * cta / kCluster), s1 = static_cast<int>(static_cast<int64_t>(steps) * (cta + 1) / kCluster);
+        const int s0 = steps * mate >> shift, s1 = steps * (mate + 1) >> shift;
         for (int r0 = 0; r0 < rank; r0 += 16 * kRankTiles) {
             float acc[kRankTiles][kCols][4] = {};
             for (int s = s0 + w; s < s1; s += kBatch * kWarps) {
@@ -406,13 +419,17 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
         // the whole sums, scaled; the largest of a token decides its power of two
         constexpr int kRows = kThreads / kTok;               // ranks at a time; a thread keeps its token
         const int n = threadIdx.x % kTok, r_first = threadIdx.x / kTok;
-        const float scale = p.scales != nullptr ? p.scales[a] : 1.0f;
+        const float scale = p.scales != nullptr && a >= 0 ? p.scales[a] : 1.0f;
         float top = 0.0f;
         for (int r = r_first; r < prank; r += kRows) {
             float sum = 0.0f;
             if (r < rank) {
+                if (sharing == kCluster) {
 #pragma unroll
-                for (int i = 0; i < kCluster; ++i) sum += cluster.map_shared_rank(part, i)[r * kPad + n];
+                    for (int i = 0; i < kCluster; ++i) sum += cluster.map_shared_rank(part, i)[r * kPad + n];
+                } else {
+                    for (int i = cta - mate; i < cta - mate + sharing; ++i) sum += cluster.map_shared_rank(part, i)[r * kPad + n];
+                }
             }
             sum *= scale;
             sums[r * kPad + n] = sum;
@@ -439,18 +456,18 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
         __syncthreads();
 
         if constexpr (kSplit) {
-            // each CTA of the cluster writes an eighth of the tile's vectors
-            const int width = padded_rank(p.rank), pieces = prank / 8;
+            // each of the tile's CTAs writes as many of its vectors
+            const int width = padded_rank(p.rank), pieces = prank / 8, mine = kTok >> shift;
             const int64_t all = static_cast<int64_t>(p.N) * width;
-            for (int e = threadIdx.x; e < kCols * pieces; e += kThreads) {
-                const int t = cta * kCols + e / pieces, k = e % pieces * 8;
+            for (int e = threadIdx.x; e < mine * pieces; e += kThreads) {
+                const int t = mate * mine + e / pieces, k = e % pieces * 8;
                 if (t >= count) continue;
                 __half* to = p.vectors + (n0 + list[t]) * width + k;
                 *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(hi + t * row + k);
                 if constexpr (kTwo) *reinterpret_cast<uint4*>(to + all) = *reinterpret_cast<const uint4*>(lo + t * row + k);
             }
-            const int t = cta * kCols + threadIdx.x;
-            if (threadIdx.x < kCols && t < count) p.factors[n0 + list[t]] = factors[t];
+            const int t = mate * mine + threadIdx.x;
+            if (threadIdx.x < mine && t < count) p.factors[n0 + list[t]] = factors[t];
         } else {
             for (int b = block0; b < blocks; b += sharers * kBlocksOfCluster)
                 expand_block<T, kCols, kAlign, true, false>(p, n0, list, count, a, rank, b * kOut, hi, lo, row, factors, nullptr);
@@ -674,7 +691,7 @@ spdp_status launch_typed(Params p, int align, int device, int sms, cudaStream_t 
         p.per_window = static_cast<int>(between(cluster_slots, 1, most));
         return launch_rank<1, T, false, 16>(p, 1, device, s);
     }
-    const bool few = p.N <= kFewTokens && align == 16;
+    const bool few = p.N <= kFewTokens;
     const int windows = (p.N + kWindow - 1) / kWindow, width = padded_rank(p.rank);
     const size_t vectors = (2ull * p.N * width * (sizeof(T) == 4 ? 2 : 1) + 127) / 128 * 128, factors = (4ull * p.N + 127) / 128 * 128;
     void* scratch = nullptr;
@@ -685,6 +702,7 @@ spdp_status launch_typed(Params p, int align, int device, int sms, cudaStream_t 
     p.plans = reinterpret_cast<Plan*>(static_cast<char*>(scratch) + vectors + factors);
     p.per_window = static_cast<int>(between(cluster_slots / windows, 1, p.N < kWindow ? p.N : kWindow));
     if (align == 16) st = few ? launch_rank<1, T, true, 16>(p, windows, device, s) : launch_rank<kMostCols, T, true, 16>(p, windows, device, s);
+    else if (few) st = align == 4 ? launch_rank<1, T, true, 4>(p, windows, device, s) : launch_rank<1, T, true, 2>(p, windows, device, s);
     else st = align == 4 ? launch_rank<kMostCols, T, true, 4>(p, windows, device, s) : launch_rank<kMostCols, T, true, 2>(p, windows, device, s);
     if (st == SPDP_OK) {
         const cudaError_t e = align == 16 && p.wide_y && p.rank <= 32 ? launch_expand<T, 16, true, true>(p, device, sms, s)
