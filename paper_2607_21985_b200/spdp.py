@@ -112,13 +112,13 @@ def _check(st: int, where: str):
 
 
 _raw_stream = _device = None
-_f16 = _f32 = _i32 = _i64 = _u8 = None          # torch.float16, torch.float32, ...: an import statement in every call costs more than its checks
+_f16 = _f32 = None          # torch.float16, torch.float32: an import statement in every call costs more than its checks
 
 
 def _load_dtypes():
-    global _f16, _f32, _i32, _i64, _u8
+    global _f16, _f32
     import torch
-    _f16, _f32, _i32, _i64, _u8 = torch.float16, torch.float32, torch.int32, torch.int64, torch.uint8
+    _f16, _f32 = torch.float16, torch.float32
 
 
 def _ydt(y):
@@ -329,71 +329,12 @@ def spdp_swiglu_dp(gate, up, thr: float, x_out, mask_out, count_out=None, stream
         _check(st, "spdp_swiglu_dp")
 
 
-def _vector(t, dtype, n, name, here):
-    """The address of a contiguous vector of n values on the device `here`; None stays None."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.get_device() != here or not t.is_contiguous() or t.numel() != n:
-        raise ValueError(f"{name} must be a contiguous CUDA {dtype} of {n} values on the current device")
-    return t.data_ptr()
-
-
-def _rows(t, n, m, name, here):
-    """(address, elements between rows) of an [n][m] on the device `here` whose rows are contiguous."""
-    if t.shape != (n, m) or t.get_device() != here:
-        raise ValueError(f"{name} must be CUDA [{n}][{m}] on the current device")
-    ld, one = t.stride()
-    if one != 1 and m > 1:
-        raise ValueError(f"the last dimension of {name} must be contiguous")
-    return t.data_ptr(), ld if n > 1 else max(ld, m)
-
-
-def _heads(t, n, heads, dim, name, here):
-    """(address, elements between tokens) of an [n][heads][dim] on the device `here` whose heads lie one after another."""
-    if t.shape != (n, heads, dim) or t.get_device() != here:
-        raise ValueError(f"{name} must be CUDA [{n}][{heads}][{dim}] on the current device")
-    ld, head, one = t.stride()
-    if one != 1 or (head != dim and heads > 1):
-        raise ValueError(f"the heads of a token of {name} must be contiguous")
-    return t.data_ptr(), ld if n > 1 else max(ld, heads * dim)
-
-
 def spdp_lora(X, adapter, A, B, Y, base=None, scales=None, ranks=None, stream=None) -> None:
     """Y[n] = base[n] + scales[a] * B[a] @ (A[a] @ X[n]) with a = adapter[n] (none outside 0 .. len(A) - 1); base=None adds to
     Y in place.  X fp16 CUDA [N][K] (rows may be strided; a single token may come as [K], with Y and base [M]), adapter int32 [N],
     A fp16 [count][rank][K], B fp16 [count][M][rank] (strided in all but the last dimension), Y and base fp16 or fp32 [N][M],
     scales fp32 [count] (default 1), ranks int32 [count] (default all)."""
-    if base is None:
-        base = Y
-    ydt, xs = _ydt(Y), X.shape
-    if len(xs) == 1:
-        X, Y, base = X.unsqueeze(0), Y.unsqueeze(0), base.unsqueeze(0)
-        xs = X.shape
-    ashape, bshape = A.shape, B.shape
-    if len(xs) != 2 or len(ashape) != 3 or len(bshape) != 3:
-        raise ValueError("X must be [N][K], A [count][rank][K] and B [count][M][rank]")
-    N, K = xs
-    count, rank, k = ashape
-    M = bshape[1]
-    if k != K or bshape[0] != count or bshape[2] != rank:
-        raise ValueError("X must be [N][K], A [count][rank][K] and B [count][M][rank]")
-    if X.dtype is not _f16 or A.dtype is not _f16 or B.dtype is not _f16 or ydt is None or base.dtype is not Y.dtype:
-        raise ValueError("X, A and B must be fp16, Y and base both fp16 or both fp32")
-    (sa, lda, ca), (sb, ldb, cb) = A.stride(), B.stride()
-    here = _here()
-    if A.get_device() != here or B.get_device() != here or (ca != 1 and K > 1) or (cb != 1 and rank > 1):
-        raise ValueError("A and B must be CUDA tensors on the current device with a contiguous last dimension")
-    if rank <= 1:
-        lda = max(lda, K)
-    if M <= 1:
-        ldb = max(ldb, rank)
-    if adapter is None:
-        raise ValueError("adapter is required")
-    x, ldx = _rows(X, N, K, "X", here)
-    y, ldy = _rows(Y, N, M, "Y", here)
-    b, ldbase = (y, ldy) if base is Y else _rows(base, N, M, "base", here)
-    st = (_lib or lib()).call_lora(x, N, K, ldx, _vector(adapter, _i32, N, "adapter", here), A.data_ptr(), lda, sa, B.data_ptr(), ldb, sb, count, rank,
-                                   _vector(ranks, _i32, count, "ranks", here), _vector(scales, _f32, count, "scales", here), b, ldbase, y, M, ldy, ydt, _stream(stream))
+    st = (_lib or lib()).call_lora(_here(), X, adapter, A, B, Y, base, scales, ranks, stream)
     if st:
         _check(st, "spdp_lora")
 
@@ -404,34 +345,7 @@ def spdp_qk_norm_rope(q, k, q_out, k_out, pos, inv_freq, sections=None, q_weight
     strided, as in the output of one projection for all of them) and their rotation by pos (int32 [N], or [axes][N] with `sections`
     pairs to each axis) times inv_freq (fp32 [pairs]), into fp16 q_out and k_out (may be q and k).  k and k_out may be None;
     inv_freq None: no rotation."""
-    dt, qs = _ydt(q), q.shape
-    if len(qs) != 3 or dt is None or q_out.dtype is not _f16 or (k is not None and (len(k.shape) != 3 or k.dtype is not q.dtype or k_out.dtype is not _f16)):
-        raise ValueError("q and k must be [N][heads][D], both fp16 or both fp32, q_out and k_out fp16")
-    N, q_heads, D = qs
-    here = _here()
-    qp, ldq = _heads(q, N, q_heads, D, "q", here)
-    qo, ldqo = _heads(q_out, N, q_heads, D, "q_out", here)
-    if k is None:
-        kv_heads, kp, ldk, ko, ldko = 0, None, 0, None, 0
-    else:
-        kv_heads = k.shape[1]
-        kp, ldk = _heads(k, N, kv_heads, D, "k", here)
-        ko, ldko = _heads(k_out, N, kv_heads, D, "k_out", here)
-    if inv_freq is None:
-        pairs = axes = stride = 0
-        at = freq = sections = None
-    else:
-        pairs, dims = inv_freq.numel(), len(pos.shape)
-        freq = _vector(inv_freq, _f32, pairs, "inv_freq", here)
-        if dims not in (1, 2) or pos.dtype is not _i32 or pos.get_device() != here or pos.shape[-1] != N or (N > 1 and pos.stride(-1) != 1):
-            raise ValueError("pos must be CUDA int32 [N] or [axes][N] on the current device")
-        axes = 1 if dims == 1 else pos.shape[0]
-        stride = N if axes <= 1 else pos.stride(0)
-        at = pos.data_ptr()
-        sections = (pairs,) if sections is None and axes == 1 else tuple(sections or ())
-    st = (_lib or lib()).call_qk_norm_rope(qp, ldq, kp, ldk, dt, N, q_heads, kv_heads, D, _vector(q_weight, _f16, D, "q_weight", here),
-                                           _vector(k_weight, _f16, D, "k_weight", here), eps, at, stride, axes, sections, freq, pairs, 1 if adjacent else 0,
-                                           qo, ldqo, ko, ldko, _stream(stream))
+    st = (_lib or lib()).call_qk_norm_rope(_here(), q, k, q_out, k_out, pos, inv_freq, sections, q_weight, k_weight, eps, 1 if adjacent else 0, stream)
     if st:
         _check(st, "spdp_qk_norm_rope")
 
@@ -443,32 +357,10 @@ def spdp_kv4_page_bytes(kv_heads: int, head_dim: int, page_tokens: int) -> int:
     return out.value
 
 
-def _cache(cache, kv_heads, dim, page_tokens, here):
-    """(address, pages) of a cache."""
-    cs = cache.shape
-    if len(cs) != 2 or cache.dtype is not _u8 or cache.get_device() != here or not cache.is_contiguous() or cs[1] != kv_heads * page_tokens * (dim + dim // 8):
-        raise ValueError("cache must be a contiguous CUDA uint8 [pages][spdp_kv4_page_bytes(kv_heads, head_dim, page_tokens)]")
-    return cache.data_ptr(), cs[0]
-
-
 def spdp_kv4_store(k, v, slot, cache, page_tokens: int, k_values=None, v_values=None, stream=None) -> None:
     """Keys k (fp16 CUDA [N][kv_heads][D]) and values v (fp16 or fp32) into the slots (int64 [N], below 0: not stored) of a 4-bit
     cache; k_values and v_values (fp16, optional) get what the codes stand for."""
-    vdt, ks = _ydt(v), k.shape
-    if len(ks) != 3 or k.dtype is not _f16 or vdt is None or (k_values is not None and k_values.dtype is not _f16) or \
-            (v_values is not None and v_values.dtype is not _f16):
-        raise ValueError("k must be fp16 [N][kv_heads][D], v fp16 or fp32, k_values and v_values fp16")
-    if slot is None:
-        raise ValueError("slot is required")
-    N, heads, D = ks
-    here = _here()
-    kp, ldk = _heads(k, N, heads, D, "k", here)
-    vp, ldv = _heads(v, N, heads, D, "v", here)
-    at, pages = _cache(cache, heads, D, page_tokens, here)
-    ko, ldko = (None, 0) if k_values is None else _heads(k_values, N, heads, D, "k_values", here)
-    vo, ldvo = (None, 0) if v_values is None else _heads(v_values, N, heads, D, "v_values", here)
-    st = (_lib or lib()).call_kv4_store(kp, ldk, vp, ldv, vdt, N, heads, D, _vector(slot, _i64, N, "slot", here), at, pages, page_tokens, ko, ldko, vo, ldvo,
-                                        _stream(stream))
+    st = (_lib or lib()).call_kv4_store(_here(), k, v, slot, cache, page_tokens, k_values, v_values, stream)
     if st:
         _check(st, "spdp_kv4_store")
 
@@ -478,28 +370,7 @@ def spdp_attn_kv4(q, cache, page_tokens: int, kv_heads: int, table, length, y, s
     """Attention of one token of each request, q fp16 CUDA [B][q_heads][D], over its `length` (int32 [B]) keys in the pages table[b]
     (int32 [B][pages of a request]) of a 4-bit cache; y fp16 [B][q_heads * D] and, where mask (int32/uint32 [B][>= q_heads * D / 32])
     is given, the bits of the columns with |y| above thr."""
-    if _f16 is None:
-        _load_dtypes()
-    qs, ts = q.shape, table.shape
-    if len(qs) != 3 or q.dtype is not _f16 or y.dtype is not _f16:
-        raise ValueError("q must be fp16 [B][q_heads][D] and y fp16")
-    if table.dtype is not _i32 or len(ts) != 2 or length is None:
-        raise ValueError("table must be int32 [B][pages] and length int32 [B]")
-    B, q_heads, D = qs
-    here = _here()
-    qp, ldq = _heads(q, B, q_heads, D, "q", here)
-    yp, ldy = _rows(y, B, q_heads * D, "y", here)
-    at, pages = _cache(cache, kv_heads, D, page_tokens, here)
-    tp, tstride = _rows(table, B, ts[1], "table", here)
-    mp, mstride = None, 0
-    if mask is not None:
-        if len(mask.shape) != 2 or mask.element_size() != 4:
-            raise ValueError("mask must be 32-bit [B][words]")
-        mp, mstride = _rows(mask, B, mask.shape[1], "mask", here)
-        if mask.shape[1] < q_heads * D // 32:
-            raise ValueError("mask must hold a bit for each column of y")
-    st = (_lib or lib()).call_attn_kv4(qp, ldq, B, q_heads, kv_heads, D, at, pages, page_tokens, tp, tstride, ts[1], _vector(length, _i32, B, "length", here),
-                                       scale, cap, window, thr, yp, ldy, mp, mstride, _stream(stream))
+    st = (_lib or lib()).call_attn_kv4(_here(), q, cache, page_tokens, kv_heads, table, length, y, scale, cap, window, thr, mask, stream)
     if st:
         _check(st, "spdp_attn_kv4")
 

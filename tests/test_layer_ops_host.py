@@ -102,7 +102,7 @@ def test_page_bytes(L):
     assert L.spdp_kv4_page_bytes(1, 128, 16, None) == INVALID
 
 
-@pytest.mark.parametrize("name,n", [("lora", 22), ("qk_norm_rope", 24), ("kv4_store", 17), ("attn_kv4", 22)])
+@pytest.mark.parametrize("name,n", [("lora", 10), ("qk_norm_rope", 13), ("kv4_store", 9), ("attn_kv4", 14)])
 def test_wrong_arguments_raise(L, name, n):
     call = getattr(L, "call_" + name)
     with pytest.raises(TypeError):
@@ -111,24 +111,85 @@ def test_wrong_arguments_raise(L, name, n):
         call("x", *[0] * (n - 1))
     with pytest.raises((TypeError, OverflowError)):
         call(1 << 70, *[0] * (n - 1))
+    with pytest.raises(TypeError, match="torch tensor"):
+        call(*[0] * n)
 
 
-def test_arguments_arrive(L):
-    """A callback in place of each entry point sees what was passed, in its order."""
+HOST = -1            # "the current device" of calls on tensors in the host's memory, which the library never sees: a callback stands in for it
+
+
+def arrived(L, name, *args):
+    """What the entry point gets from a call on host tensors."""
     from paper_2607_21985_b200 import _pycall
-    for name, defaults in (("lora", LORA), ("kv4_store", STORE), ("attn_kv4", ATTN), ("qk_norm_rope", HEADS)):
-        entry = getattr(L, "spdp_" + name)
-        seen = []
-        plain = lambda v: tuple(v[i] for i in range(3)) if isinstance(v, ctypes.POINTER(ctypes.c_int)) else v      # read while the call lasts
-        cb = ctypes.CFUNCTYPE(ctypes.c_int, *entry.argtypes)(lambda *a: seen.append([plain(v) for v in a]) or -3)
-        args = list(range(1, len(entry.argtypes) + 1))
-        if name == "qk_norm_rope":
-            args[14], args[15] = 3, (7, 8, 9)
-        assert getattr(_pycall, name)(ctypes.cast(cb, ctypes.c_void_p).value, *args) == -3
-        assert seen == [args]
-    with pytest.raises(TypeError):
-        args[15] = (7, 8)
-        _pycall.qk_norm_rope(1, *args)
+    seen = []
+    plain = lambda v: [v[i] for i in range(3)] if isinstance(v, ctypes.POINTER(ctypes.c_int)) and v else None if isinstance(v, ctypes.POINTER(ctypes.c_int)) else v
+    cb = ctypes.CFUNCTYPE(ctypes.c_int, *getattr(L, "spdp_" + name).argtypes)(lambda *a: seen.append([plain(v) for v in a]) or -3)      # read while the call lasts
+    assert getattr(_pycall, name)(ctypes.cast(cb, ctypes.c_void_p).value, HOST, *args) == -3
+    return seen[0]
+
+
+class StreamLike:
+    cuda_stream = 99
+
+
+def test_tensors_arrive_lora(L):
+    import torch
+    x, y, base = torch.zeros(5, 9).half()[:, 1:8], torch.zeros(5, 12)[:, :11], torch.zeros(5, 11)
+    A, B = torch.zeros(3, 4, 10).half()[:, :2, :7], torch.zeros(3, 11, 6).half()[:, :, 2:4]
+    adapter, scales, ranks = torch.zeros(5, dtype=torch.int32), torch.zeros(3), torch.zeros(3, dtype=torch.int32)
+    p = lambda *t: [v.data_ptr() for v in t]
+    assert arrived(L, "lora", x, adapter, A, B, y, base, scales, ranks, StreamLike()) == \
+        p(x) + [5, 7, 9] + p(adapter, A) + [10, 40] + p(B) + [6, 66, 3, 2] + p(ranks, scales, base) + [11] + p(y) + [11, 12, 1, 99]
+    one = torch.zeros(7).half()
+    got = arrived(L, "lora", one, adapter[:1], A, B, y[0].half(), None, None, None, 5)
+    assert got[:4] == [one.data_ptr(), 1, 7, 7] and got[13:15] == [None, None] and got[15] == got[17] and got[16] == 11 and got[18:] == [11, 11, 0, 5]
+    assert arrived(L, "lora", torch.nn.Parameter(x.contiguous()), adapter, A, B, y, y, None, None, 0)[1:4] == [5, 7, 7]
+
+
+def test_tensors_arrive_heads(L):
+    import torch
+    qkv = torch.zeros(6, 5 * 64).half()
+    q, k = qkv[:, :192].unflatten(1, (3, 64)), qkv[:, 192:].unflatten(1, (2, 64))
+    qo, ko = torch.zeros(6, 3, 64).half(), torch.zeros(6, 2, 64).half()
+    pos, freq, w = torch.zeros(3, 8, dtype=torch.int32)[:, :6], torch.zeros(24), torch.zeros(64).half()
+    p = lambda *t: [v.data_ptr() for v in t]
+    assert arrived(L, "qk_norm_rope", q, k, qo, ko, pos, freq, [7, 8, 9], w, None, 0.5, 1, 3) == \
+        p(q) + [320] + p(k) + [320, 0, 6, 3, 2, 64] + p(w) + [None, 0.5] + p(pos) + [8, 3, [7, 8, 9]] + p(freq) + [24, 1] + p(qo) + [192] + p(ko) + [128, 3]
+    got = arrived(L, "qk_norm_rope", q.float(), None, qo, None, pos[1], freq, None, None, None, 0.0, 0, 3)
+    assert got[2:9] == [None, 0, 1, 6, 3, 0, 64] and got[13:16] == [6, 1, [24, 0, 0]] and got[20:23] == [192, None, 0]
+    assert arrived(L, "qk_norm_rope", q, None, qo, None, None, None, None, None, None, 0.0, 0, 3)[12:18] == [None, 0, 0, None, None, 0]
+    for sections in ((7, 8), None, 5, (1, 2, "x")):
+        with pytest.raises(TypeError):
+            arrived(L, "qk_norm_rope", q, None, qo, None, pos, freq, sections, None, None, 0.0, 0, 3)
+
+
+def test_tensors_arrive_cache(L):
+    import torch
+    p = lambda *t: [v.data_ptr() for v in t]
+    k, v = torch.zeros(4, 3, 64).half(), torch.zeros(4, 200)[:, :192].unflatten(1, (3, 64))
+    cache, slot, kv = torch.zeros(9, 3 * 16 * 72, dtype=torch.uint8), torch.zeros(4, dtype=torch.int64), torch.zeros(4, 6, 64).half()[:, :3]
+    assert arrived(L, "kv4_store", k, v, slot, cache, 16, kv, None, 8) == \
+        p(k) + [192] + p(v) + [200, 1, 4, 3, 64] + p(slot, cache) + [9, 16] + p(kv) + [384, None, 0, 8]
+    q, y = torch.zeros(4, 6, 64).half(), torch.zeros(4, 400).half()[:, :384]
+    table, length, mask = torch.zeros(4, 7, dtype=torch.int32)[:, :5], torch.zeros(4, dtype=torch.int32), torch.zeros(4, 13, dtype=torch.uint32)
+    assert arrived(L, "attn_kv4", q, cache, 16, 3, table, length, y, 0.25, 2.0, 17, 0.5, mask, 8) == \
+        p(q) + [384, 4, 6, 3, 64] + p(cache) + [9, 16] + p(table) + [7, 5] + p(length) + [0.25, 2.0, 17, 0.5] + p(y) + [400] + p(mask) + [13, 8]
+    assert arrived(L, "attn_kv4", q, cache, 16, 3, table, length, y, 0.25, 0, 0, 0, None, 8)[18:] == [400, None, 0, 8]
+
+
+def test_tensors_keep_their_references(L):
+    import sys
+
+    import torch
+    h, i = torch.zeros(2, 4).half(), torch.zeros(2, dtype=torch.int32)
+    A, B, y = torch.zeros(1, 3, 4).half(), torch.zeros(1, 5, 3).half(), torch.zeros(2, 5).half()
+    things = (h, i, A, B, y, type(h), None)
+    before = [sys.getrefcount(t) for t in things[:5]]
+    for _ in range(50):
+        arrived(L, "lora", h, i, A, B, y, None, None, None, 0)
+        with pytest.raises(ValueError):
+            arrived(L, "lora", h, i, A, B, h, None, None, None, 0)
+    assert [sys.getrefcount(t) for t in things[:5]] == before
 
 
 def test_binding_refuses_tensors():
@@ -149,6 +210,41 @@ def test_binding_refuses_tensors():
     with pytest.raises(ValueError):
         spdp.spdp_attn_kv4(x, torch.zeros(1, 16 * 3 * 72, dtype=torch.uint8), 16, 3, torch.zeros(2, 1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32),
                            x.view(2, -1), 1.0)
+
+
+def test_tensors_are_refused_one_by_one(L):
+    import torch
+
+    from paper_2607_21985_b200 import _pycall
+    h = lambda *n: torch.zeros(*n).half()
+    i = lambda *n: torch.zeros(*n, dtype=torch.int32)
+    sets = {
+        "lora": ([h(4, 8), i(4), h(2, 3, 8), h(2, 5, 3), h(4, 5), h(4, 5), torch.zeros(2), i(2), 0],
+                 {0: (h(4, 9), h(4, 8).float(), h(4, 16)[:, ::2], h(1, 1, 4, 8), h(1)[0]), 1: (None, i(3), i(4).long(), i(8)[::2]), 2: (h(2, 3, 9), h(3, 8), h(2, 3, 16)[:, :, ::2]),
+                  3: (h(1, 5, 3), h(2, 5, 4), h(2, 5, 6)[:, :, ::2]), 4: (h(4, 6), h(3, 5), h(4, 5).double(), h(5)), 5: (h(4, 5).float(), h(3, 5), h(5, 4).t()), 6: (torch.zeros(3), h(2)),
+                  7: (i(1), torch.zeros(2))}),
+        "qk_norm_rope": ([h(4, 3, 64), h(4, 2, 64), h(4, 3, 64), h(4, 2, 64), i(4), torch.zeros(8), None, h(64), h(64), 0.0, 0, 0],
+                         {0: (h(4, 192), h(4, 3, 64).double(), h(4, 6, 64)[:, ::2], h(4, 3, 128)[:, :, ::2]), 1: (h(3, 2, 64), h(4, 2, 32), h(4, 2, 64).float()),
+                          2: (h(4, 3, 64).float(), h(4, 2, 64)), 3: (h(4, 2, 64).float(), h(4, 3, 64)), 4: (i(5), i(4).long(), i(8)[::2], i(1, 1, 4)),
+                          5: (torch.zeros(16)[::2], h(8)), 7: (h(63), torch.zeros(64)), 8: (h(128)[::2],)}),
+        "kv4_store": ([h(4, 3, 64), h(4, 3, 64), torch.zeros(4, dtype=torch.int64), torch.zeros(2, 3 * 16 * 72, dtype=torch.uint8), 16, h(4, 3, 64), h(4, 3, 64), 0],
+                      {0: (h(4, 3, 64).float(), h(4, 64)), 1: (h(4, 3, 64).double(), h(4, 2, 64)), 2: (None, i(4), torch.zeros(3, dtype=torch.int64)),
+                       3: (torch.zeros(2, 3 * 16 * 72 + 1, dtype=torch.uint8), torch.zeros(3 * 16 * 72, dtype=torch.uint8), torch.zeros(2, 3 * 16 * 72, dtype=torch.int8)),
+                       4: (32,), 5: (h(4, 3, 32), h(4, 3, 64).float()), 6: (h(3, 3, 64), h(4, 3, 64).float())}),
+        "attn_kv4": ([h(4, 6, 64), torch.zeros(2, 3 * 16 * 72, dtype=torch.uint8), 16, 3, i(4, 5), i(4), h(4, 384), 0.1, 0.0, 0, 0.0, i(4, 12), 0],
+                     {0: (h(4, 384), h(4, 6, 64).float()), 1: (torch.zeros(2, 3 * 16 * 72 * 2, dtype=torch.uint8)[:, ::2],), 3: (2,), 4: (i(3, 5), i(20), i(4, 10)[:, ::2], i(4, 5).long()),
+                      5: (None, i(5), i(4).float()), 6: (h(4, 383), h(4, 384).float(), h(3, 384)), 11: (i(4, 11), i(3, 12), i(4, 12).long(), i(48), i(4, 24)[:, ::2])})}
+    for name, (args, changes) in sets.items():
+        arrived(L, name, *args)
+        with pytest.raises(ValueError, match="current device"):
+            getattr(_pycall, name)(1, 0, *args)
+        for at, values in changes.items():
+            for v in values:
+                with pytest.raises(ValueError):
+                    arrived(L, name, *args[:at], v, *args[at + 1:])
+            if torch.is_tensor(args[at]):
+                with pytest.raises(TypeError, match="torch tensor"):
+                    arrived(L, name, *args[:at], [1.0], *args[at + 1:])
 
 
 def test_oracle_codes_by_hand():
