@@ -269,8 +269,8 @@ SPDP_API spdp_status spdp_swiglu_dp(const void* gate_dev, const void* up_dev, in
  *   Y_dev        [N][ldy] of ydt, ldy >= M.
  * Sums in 32 bits; the vector between the two products is rounded to 11 bits for 16-bit results and to 22 for
  * 32-bit ones (both with the range of 32-bit numbers).  The tokens of an adapter need not stand together.  The fast case: rows
- * that start on 16-byte boundaries (addresses and strides), K, M and rank multiples of 8.  Launches one kernel for up to 4 tokens
- * and else two, with scratch memory (2 * rank + 13 bytes for each token, 4 * rank + 13 with 32-bit results). */
+ * that start on 16-byte boundaries (addresses and strides), K, M and rank multiples of 8.  Launches one kernel for up to 16 tokens
+ * in the fast case and else two, with scratch memory (2 * rank + 13 bytes for each token, 4 * rank + 13 with 32-bit results). */
 #define SPDP_MAX_RANK 256
 SPDP_API spdp_status spdp_lora(const void* X_dev, int64_t N, int64_t K, int64_t ldx, const void* adapter_dev, const void* A_dev, int64_t lda,
                       int64_t stride_a, const void* B_dev, int64_t ldb, int64_t stride_b, int64_t count, int rank, const void* ranks_dev,

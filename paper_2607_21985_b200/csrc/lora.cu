@@ -15,12 +15,12 @@
 // number holds what the first one lost.
 //
 // Second product, a kernel of its own: the blocks of 64 output rows of all tiles stand in one line that is dealt out evenly to the
-// warps, base comes to shared memory one block ahead.  For up to 4 tokens one launch does both products: the clusters keep the
-// vectors and go on to the output rows (4096 x 4096, rank 16, 1 token, in a graph: 6.2 us, two launches 8.8).
+// warps, base comes to shared memory one block ahead.  For up to 16 tokens one launch does both products: the clusters keep
+// the vectors and go on to the output rows.
 //
 // 1024 tokens of 28672 x 8192, rank 16, 16-bit results: 42 us of which the first kernel takes 13 and the second 28 (base and Y at 4.2
 // TB/s); the first is bound by its chain (plan, two rounds of loads, exchange of the sums), the second by the waits between the
-// steps of a block at the 11 warps that its registers allow.  8 tokens of rank 64: 17 us, the same chain twice.
+// steps of a block at the 11 warps that its registers allow.  8 tokens of rank 64: 13.7 us, two such chains.
 #include <cooperative_groups.h>
 
 #include <mutex>
@@ -40,7 +40,10 @@ constexpr int kCluster = 8;
 constexpr int kExpandWarps = 4;     // of a CTA of the second kernel
 constexpr int kOut = 64;            // output rows of a warp's block
 constexpr int kBlocksOfCluster = kCluster * kWarps;
-constexpr int kFusedTokens = 4;     // up to here one launch does both products
+// Up to here one launch does both products, though clusters that share a tile all compute its vectors (us, one launch against two: 8
+// tokens of rank 16, 4096 x 4096, 6.4 : 8.7; 16 of rank 64, 28672 x 8192, 15.7 : 20.0, of rank 256 53 : 61; 32 of rank 16, 11008 x 4096,
+// 13.0 : 11.3).
+constexpr int kFusedTokens = 16;
 // Up to here tiles of the first product are 8 tokens, which loads further ahead; beyond, 32 that read A once (4 adapters of rank 16:
 // 512 tokens of 8192 x 28672 equal, 1024 39 against 41 us; 8 of rank 64, 500 tokens of 8192 x 8192 27 against 30, 128 18 : 24).
 constexpr int kFewTokens = 512;

@@ -105,7 +105,8 @@ def lora_check(c, Y, rank):
 
 
 SIZES = [(1, 1, 1, 1, 1), (1, 64, 64, 8, 1), (1, 4096, 256, 16, 3), (2, 31, 4200, 17, 2), (8, 257, 130, 5, 4), (9, 1000, 65, 32, 9), (33, 100, 65, 20, 3), (32, 512, 4097, 16, 32),
-         (70, 1000, 300, 64, 5), (5, 300, 77, 100, 2), (3, 40, 9, 256, 2), (300, 128, 1, 1, 2), (40, 8200, 70, 33, 4), (2100, 64, 96, 16, 7), (64, 2048, 640, 128, 64)]
+         (70, 1000, 300, 64, 5), (5, 300, 77, 100, 2), (3, 40, 9, 256, 2), (300, 128, 1, 1, 2), (40, 8200, 70, 33, 4), (2100, 64, 96, 16, 7), (64, 2048, 640, 128, 64),
+         (8, 256, 4608, 64, 8), (16, 1024, 640, 32, 3), (13, 64, 8200, 256, 2), (16, 2048, 64, 16, 30), (4, 320, 20000, 24, 2), (17, 512, 128, 8, 5), (512, 96, 64, 72, 300), (513, 96, 64, 40, 300)]
 
 
 @pytest.mark.parametrize("f32", [False, True])
