@@ -807,6 +807,78 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParam
     store_result(p, b, static_cast<int64_t>(h * p.group + head) * kDim + d, sum, wt);
 }
 
+// The same for few triples of many sums each, where it is all latency: the first kAhead sums of a group are asked for together with
+// all maxima.
+constexpr int kJoinFew = 16;            // sums of a triple from which on this form is taken (64 and 8 heads, us: 1 request of
+                                        // 131072 keys 48.0, 56.2 with the other; 48 requests of up to 16384 121.8, 108.2)
+constexpr int kJoinChunk = kJoinThreads;                        // sums whose maxima and weights are in shared memory at a time
+
+template <int kGroups, int kCols>
+__global__ void __launch_bounds__(kJoinThreads) attn_join_few_kernel(const AttnParams p) {
+    constexpr int kDim = 32 * kGroups, kRows = 8 * kCols, kLanes = kDim / 4, kParts = kJoinThreads / kLanes, kAhead = 12;
+    __shared__ __align__(16) float part[kParts][kDim];
+    __shared__ float2 stats[kJoinChunk];
+    __shared__ float warp_tops[kJoinThreads / 32], weights[kParts];
+    dev::programmatic_start();
+    const int4 open = p.open[blockIdx.x];
+    if (open.x < 0) return;
+    const int b = open.x, h = open.y / p.row_blocks, row = blockIdx.y, head = open.y % p.row_blocks * kRows + row;
+    if (head >= p.group) return;
+    const int at = threadIdx.x % kLanes, mine = threadIdx.x / kLanes, count = open.w - open.z / 2 + 1;
+    auto place = [&](int i) { return (i == 0 ? open.z : 2 * (open.z / 2 + static_cast<int64_t>(i))) * kRows + row; };
+    auto sum_at = [&](int i) { return *reinterpret_cast<const float4*>(p.sums + place(i) * kDim + 4 * at); };
+    float4 ahead[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+        if (mine + j * kParts < count) ahead[j] = sum_at(mine + j * kParts);
+    float m = kLowest, wt = 0.0f;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto add = [&](float4 v, float2 st) {
+        const float f = exp2_of(st.x - m);
+        sum.x += v.x * f, sum.y += v.y * f, sum.z += v.z * f, sum.w += v.w * f;
+        wt += st.y * f;
+    };
+    for (int i0 = 0; i0 < count; i0 += kJoinChunk) {
+        const int n = min(kJoinChunk, count - i0);
+        float top = m;
+        for (int i = threadIdx.x; i < n; i += kJoinThreads) {
+            stats[i] = p.stats[place(i0 + i)];
+            top = fmaxf(top, stats[i].x);
+        }
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+        if (threadIdx.x % 32 == 0) warp_tops[threadIdx.x / 32] = top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kJoinThreads / 32; ++i) top = fmaxf(top, warp_tops[i]);
+        const float f = exp2_of(m - top);
+        sum.x *= f, sum.y *= f, sum.z *= f, sum.w *= f, wt *= f, m = top;
+        int i = mine;
+        if (i0 == 0) {
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j, i += kParts)
+                if (i < n) add(ahead[j], stats[i]);
+        }
+#pragma unroll 4
+        for (; i < n; i += kParts) add(sum_at(i0 + i), stats[i]);
+        __syncthreads();                                        // before the next maxima take their place
+    }
+    *reinterpret_cast<float4*>(&part[mine][4 * at]) = sum;
+    if (at == 0) weights[mine] = wt;
+    __syncthreads();
+    const int d = 4 * threadIdx.x;
+    if (d >= kDim) return;
+    wt = 0.0f;
+    sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+        const float4 v = *reinterpret_cast<const float4*>(&part[i][d]);
+        wt += weights[i];
+        sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+    }
+    store_result(p, b, static_cast<int64_t>(h * p.group + head) * kDim + d, sum, wt);
+}
+
 template <int kGroups, int kCols>
 size_t attn_shared_bytes(int B) { return kWarps * (Shape<kGroups, kCols>::kRing + 8 * kCols * sizeof(float2) + sizeof(int)) + (B + 1) * sizeof(int); }
 
@@ -856,7 +928,7 @@ spdp_status launch_form(AttnParams p, int device, int sms, cudaStream_t s) {
     const int places = p.by_triple ? p.B * triples : ctas;
     p.open = reinterpret_cast<int4*>(static_cast<char*>(scratch) + sums + stats);
     cudaError_t e = launch_programmatic(attn_kernel<kGroups, kCols>, dim3(static_cast<unsigned>(ctas)), kThreads, attn_shared_bytes<kGroups, kCols>(p.B), s, p);
-    if (e == cudaSuccess) e = launch_programmatic(attn_join_kernel<kGroups, kCols>, dim3(static_cast<unsigned>(places), static_cast<unsigned>(p.group < kRows ? p.group : kRows)), kJoinThreads, 0, s, p);
+    if (e == cudaSuccess) e = launch_programmatic(ctas >= kJoinFew * places ? attn_join_few_kernel<kGroups, kCols> : attn_join_kernel<kGroups, kCols>, dim3(static_cast<unsigned>(places), static_cast<unsigned>(p.group < kRows ? p.group : kRows)), kJoinThreads, 0, s, p);
     const cudaError_t freed = cudaFreeAsync(scratch, s);
     SPDP_CUDA_TRY(e);
     SPDP_CUDA_TRY(freed);

@@ -479,6 +479,32 @@ def test_attn_kv4_long_and_behind_four_gigabytes(S):
         assert bool((err <= bound).all()), (b, float((err - bound).max()))
 
 
+@pytest.mark.parametrize("D,group,n", [(64, 1, 60001), (128, 8, 60000), (256, 9, 40007)])
+def test_attn_kv4_one_head_on_the_whole_gpu(S, D, group, n):
+    """Every CTA has a part of the one triple: hundreds of partial sums."""
+    page, gen = 128, torch.Generator(device="cuda").manual_seed(D)
+    pages = -(-n // page)
+    cache = torch.full((pages, S.spdp_kv4_page_bytes(1, D, page)), 0xFF, dtype=torch.uint8, device="cuda")
+    table = torch.randperm(pages, generator=gen, device="cuda")[None].int()
+    t = torch.arange(n, device="cuda")
+    k, v = (torch.randn(n, 1, D, generator=gen, device="cuda").half() for _ in range(2))
+    v[: n // 2] *= 4.0
+    kv, vv = torch.empty_like(k), torch.empty_like(v)
+    S.spdp_kv4_store(k, v, table[0, t // page].long() * page + t % page, cache, page, k_values=kv, v_values=vv)
+    q, y = torch.randn(1, group, D, generator=gen, device="cuda").half(), torch.empty(1, group * D, dtype=torch.float16, device="cuda")
+    S.spdp_attn_kv4(q, cache, page, 1, table, torch.tensor([n], dtype=torch.int32, device="cuda"), y, 0.3)
+    ks, vs = kv.double().transpose(0, 1), vv.double().transpose(0, 1)
+    want, spread = plain_attention(q[0], ks, vs, 0.3), plain_attention(q[0], ks, vs.abs(), 0.3)
+    # as in the test above: keys are below 6, values below 24
+    reach = 0.3 * (q[0].double().abs().sum(-1) * 6.0)[:, None]
+    bound = U * want.abs() * 1.01 + (3 * U + 2 * reach * (U + 560 * V) + 2.0 ** -20) * 1.02 * spread + n * TINY * 24.0 + TINY
+    err = (y[0].double().view_as(want) - want).abs()
+    assert bool((err <= bound).all()), float((err - bound).max())
+    again = torch.empty_like(y)
+    S.spdp_attn_kv4(q, cache, page, 1, table, torch.tensor([n], dtype=torch.int32, device="cuda"), again, 0.3)
+    assert torch.equal(y, again)
+
+
 def test_attn_kv4_many_requests(S):
     """More triples than CTAs, most of one key, some of none, a few long."""
     heads, group, D, page, B = 4, 2, 64, 16, 700
