@@ -479,15 +479,15 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
     }
 }
 
-template <typename T>
-__host__ __device__ constexpr int expand_ctas_of_sm(bool all_columns) { return sizeof(T) == 2 && !all_columns ? 4 : 3; }     // that the registers are cut for
+// What its registers are cut for (at 4 the forms for odd rows spill: 500 tokens, rank 20, 4001 x 4098, 30.5 us against 20.8).
+constexpr int kExpandCtasOfSm = 3;
 
 // The second product where it has a kernel of its own.  The blocks of all tiles of a window stand in one line, an equal run of
 // them to each warp of the window's CTAs, however many tiles there are.  A warp copies base of the next block to shared
 // memory while it works on one (kWide; else base is read where it is).  kShort: 16-byte loads and ranks up to 32, the usual case;
 // a tile's vectors stay in registers for all its blocks, and the weights of the next block are on their way too.
 template <typename T, int kAlign, bool kWide, bool kShort>
-__global__ void __launch_bounds__(32 * kExpandWarps, expand_ctas_of_sm<T>(kShort || (kAlign == 16 && kWide))) lora_expand_kernel(const Params p) {
+__global__ void __launch_bounds__(32 * kExpandWarps, kExpandCtasOfSm) lora_expand_kernel(const Params p) {
     constexpr int kTok = 8 * kMostCols, kPiece = 16 / sizeof(T), kPieces = kOut / kPiece;        // values of 16 bytes, such pieces of a row
     extern __shared__ float4 shared[];
     dev::programmatic_start();
@@ -653,7 +653,7 @@ cudaError_t launch_expand(Params p, int device, int sms, cudaStream_t s) {
         configured[device] = true;
     }
     // as many CTAs as the GPU holds at once, no more than there can be blocks
-    const int64_t windows = (p.N + kWindow - 1) / kWindow, blocks = (p.M + kOut - 1) / kOut, slots = expand_ctas_of_sm<T>(kShort || (kAlign == 16 && kWide)) * static_cast<int64_t>(sms);
+    const int64_t windows = (p.N + kWindow - 1) / kWindow, blocks = (p.M + kOut - 1) / kOut, slots = kExpandCtasOfSm * static_cast<int64_t>(sms);
     p.per_window = static_cast<int>(between((slots + windows - 1) / windows, 1, ((p.N < kWindow ? p.N : kWindow) * blocks + kExpandWarps - 1) / kExpandWarps));
     const int64_t size = windows * p.per_window;
     if (size > INT32_MAX) return cudaErrorInvalidConfiguration;
