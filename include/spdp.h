@@ -328,8 +328,8 @@ SPDP_API spdp_status spdp_kv4_store(const void* k_dev, int64_t ldk, const void* 
  * behind it (as spdp_swiglu_dp is for a gated MLP): y = softmax(cap * tanh(scale * q k / cap)) v, query head i with key head
  * i / (q_heads / kv_heads).
  *   q_dev        fp16 [B][ldq], B <= 4096; q_heads a multiple of kv_heads.
- *   table_dev    int32 [B][table_stride], table_stride >= table_pages: the pages of each request in order.  The keys of a page
- *                outside 0 .. pages-1 are left out.
+ *   table_dev    int32 [B][table_stride], table_stride >= table_pages: the pages of each request in order, table_pages * page_tokens
+ *                <= 2^31 - 8193.  The keys of a page outside 0 .. pages-1 are left out.
  *   length_dev   int32 [B]: keys of each request, the new token's own among them (store it first); values below 0 and above
  *                table_pages * page_tokens count as these.  A request without keys gets zeros.
  *   scale        between -10^16 and 10^16.

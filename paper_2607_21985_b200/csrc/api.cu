@@ -639,9 +639,9 @@ spdp_status spdp_attn_kv4(const void* q_dev, int64_t ldq, int64_t B, int q_heads
     if (misaligned(q_dev, 1u) || misaligned(cache_dev, 15u) || misaligned(table_dev, 3u) || misaligned(length_dev, 3u) || misaligned(y_dev, 1u) ||
         misaligned(mask_dev_out, 3u))
         return SPDP_ERR_INVALID_ARG;
-    // the keys of a request, and the 64-key units of all requests and heads with what the kernel adds to each (7 at most, a part of
-    // a unit among them), are counted in 32 bits
-    if (table_pages > INT32_MAX / page_tokens - 64) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    // the keys of a request (the kernel looks up to 4200 of them ahead of its last one), and the 64-key units of all requests and heads
+    // with what the kernel adds to each (7 at most, a part of a unit among them), are counted in 32 bits
+    if (table_pages > (INT32_MAX - 8192) / page_tokens) return SPDP_ERR_UNSUPPORTED_SHAPE;
     const int64_t triples = kv_heads * static_cast<int64_t>((q_heads / kv_heads + 7) / 8);
     if (triples * (table_pages * page_tokens / 64 + 8) > INT32_MAX / B) return SPDP_ERR_UNSUPPORTED_SHAPE;
     Kv4AttnCall c = {};

@@ -1,0 +1,40 @@
+"""The operators around the projections, without a GPU: refusals at the ends of what the calls take."""
+import pytest
+
+from paper_2607_21985_b200 import build, spdp
+from test_layer_ops_host import ATTN, F, INVALID, SHAPE
+
+INT32_MAX = 2 ** 31 - 1
+
+
+@pytest.fixture(scope="module")
+def L():
+    build.build()
+    return spdp.lib()
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+def test_attn_kv4_refuses_keys_too_near_the_end_of_32_bits(L, page):
+    """The kernel forms the numbers of keys up to 32 stages of 128 behind the stage for which it asks for pages, and a stage behind a run's end: within 8192 of
+    the last key, which have to fit 32 bits too."""
+    pages = (INT32_MAX - 8192) // page + 1
+    one = dict(ATTN, B=1, q_heads=1, kv_heads=1, dim=64, page=page)
+    assert (pages * page // 64 + 8) <= INT32_MAX            # not refused for its units
+    for more in (0, 1, 63, 600):
+        assert L.spdp_attn_kv4(*dict(one, table_pages=pages + more, table_stride=pages + more).values()) == SHAPE
+
+
+def test_attn_kv4_looks_no_further_ahead_than_what_is_refused():
+    """The kernel's arithmetic followed in whole numbers: the largest key number that is formed for any run whose last key is the largest that is taken."""
+    worst = 0
+    for run in (*range(1, 600), *range(2000, 2200), 8191, 8192, 8193, 100000, 100001):      # keys of the run; it ends at k1 = 0
+        k0 = -run
+        for w in range(4):
+            stages = ((run + 31) // 32 - w + 3) // 4
+            page_of = lambda i: max(k0 + 32 * (w + 4 * (i + lane // 2)) + 16 * (lane & 1) for lane in range(32))
+            worst = max(worst, page_of(0), page_of(16))
+            for i in range(max(stages, 0)):
+                worst = max(worst, k0 + 32 * w + 128 * (i + 1) + 32)                        # the stage behind, and its end
+                if i % 16 == 15:
+                    worst = max(worst, page_of(i + 17))
+    assert 4000 < worst < 8192
