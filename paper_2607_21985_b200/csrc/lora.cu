@@ -454,7 +454,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 2) 
             const float v = sums[r * kPad + n] * up;
             const __half h = __float2half_rn(v);
             hi[n * row + r] = h;
-            if constexpr (kTwo) lo[n * row + r] = __float2half_rn(v - __half2float(h));
+            if constexpr (kTwo) lo[n * row + r] = __float2half_rn(isinf(v) ? 0.0f : v - __half2float(h));      // Inf loses nothing
         }
         __syncthreads();
 

@@ -69,3 +69,36 @@ def test_attn_kv4_nan_of_a_head_is_its_own(S, columns, cap):
     capped = cap if cap else 1e38                   # the same bound without a cap
     capped_check(torch.cat([y[0, :128], y[0, 192:]])[None], clean, oracle, table[:1], [100], 0.125, capped, 150.0)
     capped_check(y[1:], q[1:], oracle, table[1:], [20], 0.125, capped, 150.0)
+
+
+# ---- adapters ---------------------------------------------------------------------------------------------------------------
+
+def same_kind(got, want):
+    """NaN, Inf and -Inf where `want` (64 bits) has them, finite elsewhere."""
+    got = got.double().cpu().numpy()
+    return np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isposinf(got), np.isposinf(want)) and np.array_equal(np.isneginf(got), np.isneginf(want))
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("N,K,M,rank,odd", [(1, 64, 72, 1, True), (4, 64, 72, 8, False), (16, 128, 200, 40, False), (40, 64, 72, 16, False), (40, 64, 72, 64, False), (40, 65, 71, 5, True),
+                                            (600, 64, 72, 8, False), (600, 64, 72, 72, False), (7, 66, 70, 34, True)])
+def test_lora_infinite_vectors_between_the_products(S, N, K, M, rank, odd, f32):
+    """An infinite x makes a token's vector infinite: its results are Inf, -Inf or NaN as the formula has them, the other tokens' finite."""
+    rng = np.random.default_rng(N + K + rank)
+    one = lambda *s: (rng.choice([-1.0, 1.0], s) * rng.uniform(0.1, 1.0, s)).astype(np.float16)      # no zeros, so that Inf stays Inf
+    X, A, B = one(N, K), one(2, rank, K) / np.float16(8), one(2, M, rank)
+    B[0] = np.abs(B[0])
+    B[0, M // 2:] *= -1.0                                   # adapter 0: every term of a result has the same sign
+    A[0] = np.abs(A[0])
+    B[1, 3] = 0.0
+    bad = rng.permutation(N)[:max(1, N // 3)]
+    X[bad, rng.integers(0, K, len(bad))] = rng.choice([np.inf, -np.inf], len(bad))
+    adapter = np.arange(N, dtype=np.int32) % 2
+    scales = np.array([0.5, -2.0], np.float32)
+    base = rng.standard_normal((N, M)).astype(np.float32)
+    Y = torch.empty(N, M, dtype=torch.float32 if f32 else torch.float16, device="cuda")
+    S.spdp_lora(dev(X), dev(adapter), dev(A), dev(B), Y, base=dev(base).to(Y.dtype), scales=dev(scales))
+    with np.errstate(invalid="ignore"):
+        t = np.stack([(A[a].astype(np.float64) * X[n].astype(np.float64)).sum(-1) for n, a in enumerate(adapter)])
+        want = np.stack([base[n] + float(scales[a]) * (B[a].astype(np.float64) * t[n]).sum(-1) for n, a in enumerate(adapter)])
+    assert np.isinf(want).any() and same_kind(Y, want)
