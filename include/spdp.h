@@ -261,7 +261,8 @@ SPDP_API spdp_status spdp_swiglu_dp(const void* gate_dev, const void* up_dev, in
  *   X_dev        fp16 [N][ldx], ldx >= K, N <= 2^24.
  *   adapter_dev  int32 [N]; a value outside 0 .. count-1 means no adapter: Y[n] = base[n], bit for bit.
  *   A_dev, B_dev fp16 [count][rank][K] and [count][M][rank]: row strides lda >= K and ldb >= rank, adapters
- *                stride_a and stride_b apart (in elements).  1 <= rank <= SPDP_MAX_RANK.
+ *                stride_a and stride_b apart (in elements): one after another, row between row, or (0) one A or B for all.
+ *                1 <= rank <= SPDP_MAX_RANK.
  *   ranks_dev    int32 [count] or NULL: adapter a has only its first ranks[a] rows of A and columns of B; the others
  *                are not read.  Values outside 0 .. rank are taken as the nearest of these.
  *   scales_dev   float [count] or NULL (1).

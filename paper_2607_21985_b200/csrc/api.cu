@@ -163,6 +163,16 @@ constexpr int64_t kMostSide = int64_t(1) << 30, kMostTokens = int64_t(1) << 24;
 // Elements between rows of at least `row` (below 2^38, so that offsets of all tokens or weights fit 63 bits).
 bool stride_ok(int64_t ld, int64_t row) { return ld >= row && ld <= (int64_t(1) << 38); }
 
+// `count` weights of `rows` rows of `row` elements, none over another: one after another, row between row, or (0 apart) one for all.  Their last
+// element is within 2^60 of the first.
+bool weights_ok(int64_t count, int64_t apart, int64_t rows, int64_t ld, int64_t row) {
+    constexpr int64_t kMostReach = int64_t(1) << 60;
+    if (!stride_ok(ld, row) || rows - 1 > kMostReach / ld) return false;
+    if (count == 1 || apart == 0) return true;
+    if (!stride_ok(apart, row) || count - 1 > kMostReach / apart) return false;
+    return (rows - 1) * ld + row <= apart || (count - 1) * apart + row <= ld;
+}
+
 constexpr int kMostCacheHeads = 4096;
 // A cache of 4-bit keys and values that the kernels take.
 bool kv4_shape_ok(int kv_heads, int head_dim, int page_tokens) {
@@ -542,8 +552,8 @@ spdp_status spdp_lora(const void* X_dev, int64_t N, int64_t K, int64_t ldx, cons
     if (X_dev == nullptr || adapter_dev == nullptr || A_dev == nullptr || B_dev == nullptr || base_dev == nullptr || Y_dev == nullptr) return SPDP_ERR_INVALID_ARG;
     if (K < 1 || M < 1 || K > kMostSide || M > kMostSide || rank < 1 || rank > SPDP_MAX_RANK) return SPDP_ERR_UNSUPPORTED_SHAPE;
     if (N < 1 || N > kMostTokens || count < 1 || count > INT32_MAX) return SPDP_ERR_INVALID_ARG;
-    if (!stride_ok(ldx, K) || !stride_ok(lda, K) || !stride_ok(ldb, rank) || !stride_ok(ldbase, M) || !stride_ok(ldy, M)) return SPDP_ERR_INVALID_ARG;
-    if (count > 1 && (!stride_ok(stride_a, (rank - 1) * lda + K) || !stride_ok(stride_b, (M - 1) * ldb + rank))) return SPDP_ERR_INVALID_ARG;
+    if (!stride_ok(ldx, K) || !stride_ok(ldbase, M) || !stride_ok(ldy, M) || !weights_ok(count, stride_a, rank, lda, K) || !weights_ok(count, stride_b, M, ldb, rank))
+        return SPDP_ERR_INVALID_ARG;
     if ((ydt != SPDP_Y_F16 && ydt != SPDP_Y_F32) || (base_dev == Y_dev && N > 1 && ldbase != ldy)) return SPDP_ERR_INVALID_ARG;
     const unsigned y = ydt == SPDP_Y_F32 ? 3u : 1u;
     if (misaligned(X_dev, 1u) || misaligned(A_dev, 1u) || misaligned(B_dev, 1u) || misaligned(base_dev, y) || misaligned(Y_dev, y) || misaligned(adapter_dev, 3u) ||

@@ -332,7 +332,8 @@ def spdp_swiglu_dp(gate, up, thr: float, x_out, mask_out, count_out=None, stream
 def spdp_lora(X, adapter, A, B, Y, base=None, scales=None, ranks=None, stream=None) -> None:
     """Y[n] = base[n] + scales[a] * B[a] @ (A[a] @ X[n]) with a = adapter[n] (none outside 0 .. len(A) - 1); base=None adds to
     Y in place.  X fp16 CUDA [N][K] (rows may be strided; a single token may come as [K], with Y and base [M]), adapter int32 [N],
-    A fp16 [count][rank][K], B fp16 [count][M][rank] (strided in all but the last dimension), Y and base fp16 or fp32 [N][M],
+    A fp16 [count][rank][K], B fp16 [count][M][rank] (strided in all but the last dimension: one adapter after another, row between
+    row, or one expanded for all), Y and base fp16 or fp32 [N][M],
     scales fp32 [count] (default 1), ranks int32 [count] (default all)."""
     st = (_lib or lib()).call_lora(_here(), X, adapter, A, B, Y, base, scales, ranks, stream)
     if st:

@@ -102,3 +102,22 @@ def test_lora_infinite_vectors_between_the_products(S, N, K, M, rank, odd, f32):
         t = np.stack([(A[a].astype(np.float64) * X[n].astype(np.float64)).sum(-1) for n, a in enumerate(adapter)])
         want = np.stack([base[n] + float(scales[a]) * (B[a].astype(np.float64) * t[n]).sum(-1) for n, a in enumerate(adapter)])
     assert np.isinf(want).any() and same_kind(Y, want)
+
+
+@pytest.mark.parametrize("N,rank", [(5, 16), (60, 16), (60, 64), (60, 20), (5, 7)])
+@pytest.mark.parametrize("shared", ["none", "A", "B", "both"])
+def test_lora_adapters_between_one_another(S, N, rank, shared):
+    """Adapters whose rows stand between each other's (weights kept as [rank][count][K] and [M][count][rank]), and one A or B for all: the same bits as from copies."""
+    rng = np.random.default_rng(N + rank)
+    count, K, M = 3, 128, 200
+    X, adapter = dev(rng.standard_normal((N, K)).astype(np.float16)), dev(rng.integers(-1, count + 1, N).astype(np.int32))
+    A, B = dev(rng.standard_normal((rank, count, K)).astype(np.float16)).permute(1, 0, 2), dev(rng.standard_normal((M, count, rank)).astype(np.float16)).permute(1, 0, 2)
+    if shared in ("A", "both"):
+        A = A[1:2].expand(count, rank, K)
+    if shared in ("B", "both"):
+        B = B[1:2].expand(count, M, rank)
+    base = dev(rng.standard_normal((N, M)).astype(np.float32)).half()
+    Y, Z = torch.empty_like(base), torch.empty_like(base)
+    S.spdp_lora(X, adapter, A, B, Y, base=base)
+    S.spdp_lora(X, adapter, A.contiguous(), B.contiguous(), Z, base=base)
+    assert torch.equal(Y, Z)

@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2607_21985_b200 import build, spdp
-from test_layer_ops_host import ATTN, F, INVALID, SHAPE
+from test_layer_ops_host import ATTN, INVALID, LORA, SHAPE
 
 INT32_MAX = 2 ** 31 - 1
 
@@ -38,3 +38,13 @@ def test_attn_kv4_looks_no_further_ahead_than_what_is_refused():
                 if i % 16 == 15:
                     worst = max(worst, page_of(i + 17))
     assert 4000 < worst < 8192
+
+
+@pytest.mark.parametrize("change", [
+    dict(lda=191, stride_a=64), dict(lda=192, stride_a=63), dict(lda=192, stride_a=65), dict(lda=192, stride_a=1), dict(ldb=23, stride_b=8), dict(ldb=24, stride_b=7), dict(ldb=24, stride_b=9),
+    dict(stride_a=-64), dict(stride_b=-1), dict(stride_a=1 << 50), dict(stride_b=1 << 50),
+    dict(count=2 ** 31 - 1, stride_a=1 << 38, stride_b=1 << 38), dict(count=1, M=1 << 30, ldbase=1 << 30, ldy=1 << 30, ldb=1 << 35),        # 2^69 and 2^65 elements
+    dict(M=1 << 30, ldbase=1 << 30, ldy=1 << 30, ldb=1 << 35), dict(M=1 << 30, ldbase=1 << 30, ldy=1 << 30, ldb=1 << 34, stride_b=1 << 34)])
+def test_lora_refuses_adapters_that_overlap_or_cannot_exist(L, change):
+    """Adapters one after another, or row between row, or all the same; whose last element is within 2^60 of the first."""
+    assert L.spdp_lora(*dict(LORA, **change).values()) == INVALID
