@@ -151,12 +151,12 @@ typedef struct {
     int (*stream)(int32_t, int32_t, void**);
 } dl_table;
 enum { DL_CPU = 1, DL_CUDA = 2, MOST_DIMS = 3 };
-typedef enum { OTHER, F16, F32, I32, I64, U8 } kind_t;
+typedef enum { OTHER, F16, F32, I32, U32, I64, U8 } kind_t;
 
 typedef struct {
     char* p;
     int64_t size[MOST_DIMS], step[MOST_DIMS];
-    int ndim, bits, device;                     /* device: as get_device() has it, -1 for the host's memory */
+    int ndim, device;                           /* device: as get_device() has it, -1 for the host's memory */
     kind_t kind;
 } tensor;
 
@@ -197,10 +197,10 @@ static int look(PyObject* o, const char* name, tensor* t) {
         return 0;
     }
     t->p = (char*)d.data + d.byte_offset;
-    t->ndim = d.ndim, t->bits = d.lanes == 1 ? d.bits : 0;
+    t->ndim = d.ndim;
     t->device = d.device_type == DL_CUDA ? d.device_id : d.device_type == DL_CPU ? -1 : -3;
     t->kind = d.lanes != 1 ? OTHER : d.code == 2 ? (d.bits == 16 ? F16 : d.bits == 32 ? F32 : OTHER) : d.code == 0 ? (d.bits == 32 ? I32 : d.bits == 64 ? I64 : OTHER) :
-              d.code == 1 && d.bits == 8 ? U8 : OTHER;
+              d.code == 1 ? (d.bits == 8 ? U8 : d.bits == 32 ? U32 : OTHER) : OTHER;
     int64_t dense = 1;
     for (int i = d.ndim - 1; i >= 0; --i) {
         t->size[i] = d.shape[i];
@@ -466,8 +466,8 @@ static PyObject* call_attn_kv4(PyObject* self, PyObject* const* a, Py_ssize_t n)
         return NULL;
     if (a[13] != Py_None) {
         if (!look(a[13], "mask", &mask)) return NULL;
-        if (mask.ndim != 2 || mask.bits != 32) {
-            refuse("mask must be 32-bit [B][words]");
+        if (mask.ndim != 2 || (mask.kind != I32 && mask.kind != U32)) {
+            refuse("mask must be 32-bit integers, int32 or uint32 [B][words]");
             return NULL;
         }
         if (!rows(&mask, B, mask.size[1], "mask", here, &mask_stride)) return NULL;

@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2607_21985_b200 import build, spdp
-from test_layer_ops_host import ATTN, INVALID, LORA, SHAPE
+from test_layer_ops_host import ATTN, INVALID, LORA, SHAPE, arrived
 
 INT32_MAX = 2 ** 31 - 1
 
@@ -48,3 +48,15 @@ def test_attn_kv4_looks_no_further_ahead_than_what_is_refused():
 def test_lora_refuses_adapters_that_overlap_or_cannot_exist(L, change):
     """Adapters one after another, or row between row, or all the same; whose last element is within 2^60 of the first."""
     assert L.spdp_lora(*dict(LORA, **change).values()) == INVALID
+
+
+def test_attn_kv4_takes_no_mask_but_32_bit_integers(L):
+    import torch
+    args = [torch.zeros(4, 6, 64).half(), torch.zeros(2, 3 * 16 * 72, dtype=torch.uint8), 16, 3, torch.zeros(4, 5, dtype=torch.int32), torch.zeros(4, dtype=torch.int32),
+            torch.zeros(4, 384).half(), 0.1, 0.0, 0, 0.0]
+    for dtype in (torch.int32, torch.uint32):
+        mask = torch.zeros(4, 13, dtype=dtype)
+        assert arrived(L, "attn_kv4", *args, mask, 0)[19:21] == [mask.data_ptr(), 13]
+    for dtype in (torch.float32, torch.int16, torch.uint8, torch.float64, torch.bool):
+        with pytest.raises(ValueError, match="32-bit"):
+            arrived(L, "attn_kv4", *args, torch.zeros(4, 13, dtype=dtype), 0)
