@@ -86,6 +86,7 @@ __global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_wide_kernel(const Pa
         dev::load_floats<float, true>(cosines + 8 * lane, c);
     }
     const float per_value = 1.0f / p.dim;
+    const int turning = p.pairs - 8 * lane;                         // of the lane's pairs; the rest stay as they are (an Inf next to 0 turns would leave NaN)
     for (int rounds = (heads - blockIdx.y * slots + stride - 1) / stride; rounds > 0; --rounds, h += stride) {     // the same for all threads
         float squares = 0.0f;
 #pragma unroll
@@ -110,6 +111,7 @@ __global__ void __launch_bounds__(kThreads, 4) qk_norm_rope_wide_kernel(const Pa
         float* flat = &y[0][0];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
+            if (!(kAdjacent ? j < turning : turning > 0)) continue;
             float& a = flat[kAdjacent ? 2 * j : j];
             float& b = flat[kAdjacent ? 2 * j + 1 : 8 + j];
             const float ra = a * c[j] - b * s[j], rb = b * c[j] + a * s[j];
@@ -165,8 +167,9 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const Params p) 
 #pragma unroll
                 for (int m = 0; m < 2; ++m) x[r][m] = x[r][m] * inv * __half2float(weight[at[r][m]]);
             }
-            to[at[r][0]] = __float2half_rn(x[r][0] * cosines[i] - x[r][1] * sines[i]);
-            to[at[r][1]] = __float2half_rn(x[r][1] * cosines[i] + x[r][0] * sines[i]);
+            const bool turns = i < p.pairs;
+            to[at[r][0]] = __float2half_rn(turns ? x[r][0] * cosines[i] - x[r][1] * sines[i] : x[r][0]);
+            to[at[r][1]] = __float2half_rn(turns ? x[r][1] * cosines[i] + x[r][0] * sines[i] : x[r][1]);
         }
     }
 }

@@ -121,3 +121,36 @@ def test_lora_adapters_between_one_another(S, N, rank, shared):
     S.spdp_lora(X, adapter, A, B, Y, base=base)
     S.spdp_lora(X, adapter, A.contiguous(), B.contiguous(), Z, base=base)
     assert torch.equal(Y, Z)
+
+
+# ---- head norms and rotation ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("pad", [0, 3])            # rows on 16-byte boundaries, and anywhere
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("D,pairs,adjacent", [(128, 0, False), (128, 0, True), (128, 16, False), (128, 10, True), (256, 40, False), (64, 31, True), (96, 8, False), (128, 64, False)])
+def test_qk_norm_rope_values_that_do_not_turn_stay(S, D, pairs, adjacent, f32, pad):
+    """Inf, NaN, the largest numbers and -0 where nothing turns come out as they are and reach no other value; where a pair turns by an angle of 0 beside them, the formula."""
+    N, H = 5, 3
+    rng = np.random.default_rng(D + pairs)
+    x = rng.standard_normal((N, H, D)).astype(np.float16)
+    rest = np.arange(2 * pairs, D)
+    for n in range(N):
+        for h in range(H):
+            some = rng.permutation(rest)[:5]
+            x[n, h, some] = np.array([np.inf, -np.inf, np.nan, -0.0, 65504], np.float16)[:len(some)]
+    x[0, 0, 2 * pairs:] = -0.0
+    if pairs:
+        x[1, 1, 0] = np.inf                          # turns with its partner, and with no other
+    wide = torch.zeros(N, H * D + pad, dtype=torch.float32 if f32 else torch.float16, device="cuda")
+    q = wide[:, :H * D].unflatten(1, (H, D))
+    q.copy_(dev(x))
+    out = torch.empty(N, H * D + pad, dtype=torch.float16, device="cuda")[:, :H * D].unflatten(1, (H, D))
+    pos, freq = torch.arange(N, dtype=torch.int32, device="cuda"), torch.rand(pairs, device="cuda") if pairs else None
+    S.spdp_qk_norm_rope(q, None, out, None, pos, freq, adjacent=adjacent)
+    got, want = out.cpu().numpy(), x[..., 2 * pairs:]
+    bits = got[..., 2 * pairs:].view(np.uint16)
+    assert np.array_equal(np.isnan(got[..., 2 * pairs:]), np.isnan(want)) and np.array_equal(bits[~np.isnan(want)], want.view(np.uint16)[~np.isnan(want)])
+    if pairs:
+        touched = np.zeros((N, H, D), bool)
+        touched[1, 1, [0, 1 if adjacent else pairs]] = True
+        assert np.isfinite(got[..., :2 * pairs][~touched[..., :2 * pairs]]).all()
