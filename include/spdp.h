@@ -264,14 +264,15 @@ SPDP_API spdp_status spdp_swiglu_dp(const void* gate_dev, const void* up_dev, in
  *                stride_a and stride_b apart (in elements): one after another, row between row, or (0) one A or B for all.
  *                1 <= rank <= SPDP_MAX_RANK.
  *   ranks_dev    int32 [count] or NULL: adapter a has only its first ranks[a] rows of A and columns of B; the others
- *                are not read.  Values outside 0 .. rank are taken as the nearest of these.
+ *                do not count, whatever they hold.  Values outside 0 .. rank are taken as the nearest of these.
  *   scales_dev   float [count] or NULL (1).
  *   base_dev     [N][ldbase] of ydt, ldbase >= M; may be Y_dev itself (with ldbase = ldy): the adapters are then added in place.
  *   Y_dev        [N][ldy] of ydt, ldy >= M.
- * Sums in 32 bits; the vector between the two products is rounded to 11 bits for 16-bit results and to 22 for
- * 32-bit ones (both with the range of 32-bit numbers).  The tokens of an adapter need not stand together.  The fast case: rows
- * that start on 16-byte boundaries (addresses and strides), K, M and rank multiples of 8.  Launches one kernel for up to 16 tokens
- * in the fast case and else two, with scratch memory (2 * rank + 13 bytes for each token, 4 * rank + 13 with 32-bit results). */
+ * Sums in 32 bits; the vector between the two products is rounded to 11 bits for 16-bit results and to 22 for 32-bit ones (below 2^-28
+ * and 2^-17 of a token's largest to fewer, within 2^-39 of that), with the range of 32-bit numbers.  The tokens of an adapter need
+ * not stand together.  The fast case: rows that start on 16-byte boundaries (addresses and strides), K, M and rank multiples of 8.
+ * Launches one kernel for up to 16 tokens in the fast case and else two, with scratch memory: for each token 4 bytes and 2 (with 32-bit
+ * results 4) times the rank rounded up to a multiple of 32; for each started 256 tokens 2432 bytes; 255 bytes at most between. */
 #define SPDP_MAX_RANK 256
 SPDP_API spdp_status spdp_lora(const void* X_dev, int64_t N, int64_t K, int64_t ldx, const void* adapter_dev, const void* A_dev, int64_t lda,
                       int64_t stride_a, const void* B_dev, int64_t ldb, int64_t stride_b, int64_t count, int rank, const void* ranks_dev,
@@ -280,8 +281,9 @@ SPDP_API spdp_status spdp_lora(const void* X_dev, int64_t N, int64_t K, int64_t 
 
 /* Norms of the query and key heads and their rotation by positions, in one pass over the output of the q/k projections.
  * Each head x of head_dim values becomes x / sqrt(mean(x^2) + eps) * weight, then its first 2 * pairs values turn: pair i by the
- * angle pos[axis of i][n] * inv_freq[i], (a, b) -> (a cos - b sin, b cos + a sin).  Arithmetic in 32 bits, angles in 64, one
- * rounding to fp16.
+ * angle pos[axis of i][n] * inv_freq[i], (a, b) -> (a cos - b sin, b cos + a sin); values that do not turn stay.  Arithmetic in 32
+ * bits, angles in 64, one rounding to fp16.  (A normed head's sum of squares, and their mean plus eps, have to be in the range of 32-bit
+ * numbers: a concern for 32-bit rows beyond 10^18, and for heads of zeros or below 10^-18 with an eps of 0.)
  *   q_dev, k_dev      [N][ldq], [N][ldk] of dt (fp16 or fp32, a projection's output types), N <= 2^24: a token's q_heads
  *                     (kv_heads) heads one after another.  Either number may be 0 (its pointers are then ignored), not both.
  *   head_dim          even, 2 .. 256.
@@ -339,6 +341,8 @@ SPDP_API spdp_status spdp_kv4_store(const void* k_dev, int64_t ldk, const void* 
  *   y_dev        fp16 [B][ldy], ldy >= q_heads * head_dim.
  *   mask_dev_out uint32 [B][mask_stride], mask_stride >= q_heads * head_dim / 32, or NULL: the columns that the o-projection
  *                should keep, NOT(|y_j| <= thr) on the stored y, for SPDP_DP_MASK (thr is used for nothing else).
+ * Refused as SPDP_ERR_UNSUPPORTED_SHAPE besides: B * kv_heads * (query heads of a key head / 8, rounded up) * (table_pages * page_tokens / 64 + 8) of
+ * 2^31 and more.
  * What lies in the cache behind a request's last key is never used, whatever it is.  Sums in 32 bits; the softmax's weights, times
  * the scales of the values, are rounded to fp16 for their product with these.  Where the requests are few and table_pages (or the
  * window) says that they are short, the call launches one kernel; else two, with scratch memory (a few MB). */

@@ -195,7 +195,8 @@ __device__ __forceinline__ Span span_of(const AttnParams& p, int b) {
 }
 
 // A triple costs what its units do and, for its query heads and its sums, as much as kStart more: it is that long in the line
-// that is cut into runs.  (With 0 a CTA that met many short requests took half as long again as the others.)
+// that is cut into runs.  (Us with 0, 3 and 6, 64 and 8 heads: 48 requests of 1 to 16384 keys 153, 143, 134; 256 of 1 to 1024 131, 85, 79; 128
+// with heads of 64, lengths to 4096 even in their logarithm, 77, 48, 44; 16 of up to 8192 50, 42, 42.)
 constexpr int kStart = 6;               // spdp_attn_kv4 counts on 7 at most when it checks that a line's length fits 32 bits
 __device__ __forceinline__ int triple_length(int units) { return units > 0 ? units + kStart : 0; }
 
@@ -838,8 +839,10 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParam
 
 // The same for few triples of many sums each, where it is all latency: the first kAhead sums of a group are asked for together with
 // all maxima.
-constexpr int kJoinFew = 16;            // sums of a triple from which on this form is taken (64 and 8 heads, us: 1 request of
-                                        // 131072 keys 48.0, 56.2 with the other; 48 requests of up to 16384 121.8, 108.2)
+// CTAs to a triple from which on this form is taken (us with it and with the other, requests of 16384 keys, 64 and 8 heads: 74 CTAs
+// 23.8 : 25.9, 37 28.0 : 30.0, 25 33.0 : 34.0, 18 38.2 : 38.2, 15 44.3 : 42.3, 9 58.7 : 54.6, 1.5 240.9 : 219; 16 and 1 heads: 592 CTAs 21.8 :
+// 26.3, 37 34.1 : 36.1, 25 44.3 : 42.3, 12 64.9 : 60.7).
+constexpr int kJoinFew = 16;
 constexpr int kJoinChunk = kJoinThreads;                        // sums whose maxima and weights are in shared memory at a time
 
 template <int kGroups, int kCols>
@@ -915,8 +918,9 @@ template <int kGroups, int kCols>
 size_t attn_cluster_bytes() { return kWarps * Shape<kGroups, kCols>::kRing + (kWarps + 1) * 8 * kCols * sizeof(float2); }
 
 // Up to here a cluster to a triple, where all of them fit the GPU at once (64 query and 8 key heads, in a graph, us, cluster against
-// line: 1 request of 1000 keys 12.3 against 17.7, of 8000 18.4 : 25.9, of 16000 26.6 : 27.9; 8 of 1000 18.4 : 23.8, of 8000 32.8 :
-// 38.2).  Beyond, few long requests among short ones are better cut anywhere.
+// line: 1 request of 1000 keys 10.2 against 15.6, of 8000 18.4 : 21.8, of 12000 20.5 : 23.8, of 16000 24.6 : 23.9, of 32000 38.9 : 27.9; 2 of
+// 8000 22.5 : 23.8, of 12000 26.6 : 26.0; 9 of 8000 38.9 : 40.2, of 12000 51.2 : 48.4, the others of a sixteenth of it 24.6 : 27.9).  What
+// decides is the longest that the table allows: a request's own length is only known on the device.
 constexpr int kClusterKeys = 8192;
 
 template <int kGroups, int kCols>

@@ -334,7 +334,11 @@ def spdp_lora(X, adapter, A, B, Y, base=None, scales=None, ranks=None, stream=No
     Y in place.  X fp16 CUDA [N][K] (rows may be strided; a single token may come as [K], with Y and base [M]), adapter int32 [N],
     A fp16 [count][rank][K], B fp16 [count][M][rank] (strided in all but the last dimension: one adapter after another, row between
     row, or one expanded for all), Y and base fp16 or fp32 [N][M],
-    scales fp32 [count] (default 1), ranks int32 [count] (default all)."""
+    scales fp32 [count] (default 1), ranks int32 [count] (default all).
+
+    This call and the three around it look at their tensors through DLPack's exchange table (`__dlpack_c_exchange_api__` of the tensor's
+    type, as PyTorch 2.11 has it); without it they raise TypeError, and lib().spdp_lora and its like take the same addresses and
+    sizes as numbers."""
     st = (_lib or lib()).call_lora(_here(), X, adapter, A, B, Y, base, scales, ranks, stream)
     if st:
         _check(st, "spdp_lora")
