@@ -417,18 +417,20 @@ def _own(s):
     op = case["op"]
     if op in ("serve", "compact"):
         table, ref = s["table"], s["ref"]
+        if "numbers" not in s:                              # the calls write 32-bit numbers, the plain form's are 64-bit ones: these have them in their lower halves
+            s["numbers"] = torch.zeros(2, dtype=torch.int64, device="cuda")
+            s["halves"] = [n.view(torch.int32)[:1] for n in s["numbers"].split(1)]
+            s["wholes"] = list(s["numbers"].unbind())
         table.copy_(s["table0"]), ref.copy_(s["ref0"])
         if op == "compact":
             spdp.spdp_kv_pages_free(ref, table, s["done"], s["zeros"], s["ends"])
-            spdp.spdp_kv_pages_compact(s["cache"], ref, table, s["live"])
-            return dict(table=table, ref=ref, live=s["live"].squeeze(0), cache=s["cache"])
+            spdp.spdp_kv_pages_compact(s["cache"], ref, table, s["halves"][0])
+            return dict(table=table, ref=ref, live=s["wholes"][0], cache=s["cache"])
         spdp.spdp_kv_pages_copy(s["cache"], s["src"], s["dst"])
         spdp.spdp_kv_pages_free(ref, table, s["done"], s["zeros"], s["ends"])
-        if s["grow"].numel():
-            spdp.spdp_kv_pages_take(ref, table, s["grow"], s["grow_from"], s["grow_to"], s["short"])
-        if s["child"].numel():
-            spdp.spdp_kv_pages_fork(s["cache"], ref, table, case["page"], s["parent"], s["child"], s["fork_length"], s["fork_short"])
-        return dict(table=table, ref=ref, short=s["short"].squeeze(0), fork_short=s["fork_short"].squeeze(0), cache=s["cache"])
+        spdp.spdp_kv_pages_take(ref, table, s["grow"], s["grow_from"], s["grow_to"], s["halves"][0])
+        spdp.spdp_kv_pages_fork(s["cache"], ref, table, case["page"], s["parent"], s["child"], s["fork_length"], s["halves"][1])
+        return dict(table=table, ref=ref, short=s["wholes"][0], fork_short=s["wholes"][1], cache=s["cache"])
     first = None if op == "step" else s["first"]
     spdp.spdp_kv8_store(s["k"], s["v"], s["cache"], case["page"], s["table"], s["length"], first=first, k_values=s["k_values"], v_values=s["v_values"])
     stored = dict(k=s["k_values"], v=s["v_values"])
