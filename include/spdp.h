@@ -350,6 +350,97 @@ SPDP_API spdp_status spdp_attn_kv4(const void* q_dev, int64_t ldq, int64_t B, in
                           int page_tokens, const void* table_dev, int64_t table_stride, int64_t table_pages, const void* length_dev, float scale,
                           float cap, int64_t window, float thr, void* y_dev, int64_t ldy, void* mask_dev_out, int64_t mask_stride, void* stream);
 
+/* A paged key/value cache held in 8 bits, with a scale to every 16 tokens of a head.  A page holds page_tokens = P tokens (a power of
+ * two, 16 .. 256): for each key head in turn P / 16 cells, one to 16 tokens.  A cell, with D = head_dim = 64, 128 or 256, is 32 D + 16
+ * bytes: codes of the keys [D / 64][16 tokens][64 dimensions]; codes of the values, where token r and dimension d is byte
+ * 512 (d / 32) + 64 (d % 8) + 16 (r % 8 / 2) + 4 (d % 32 / 8) + 2 (r / 8) + r % 2; the scale of the keys and that of the values (32-bit
+ * floats); 8 bytes of zeros.  A code is an e4m3 number (1 sign, 4 exponent and 3 mantissa bits) and stands for itself times its
+ * scale, which is a power of two: the smallest from 2^-15 up with max|x| <= 448 scale, over what the cell holds of its side.  So
+ *   code = e4m3(x / scale), rounded once, ties to even, and what it stands for is an fp16 number.
+ * Values are first brought between -61440 and 61440 (Inf too; NaN becomes one of the two).
+ * A cache is `pages` such pages, 16-byte aligned, in any order.
+ * spdp_kv8_page_bytes writes the bytes of a page, kv_heads * P * (2 D + 1) (host arithmetic). */
+SPDP_API spdp_status spdp_kv8_page_bytes(int kv_heads, int head_dim, int page_tokens, int64_t* bytes_out);
+
+/* Stores the keys and values of N tokens of B requests (B <= 4096) behind those that the requests have.
+ *   k_dev        fp16 [N][ldk], heads one after another (what spdp_qk_norm_rope leaves), N <= 2^24.
+ *   v_dev        [N][ldv] of vdt; 32-bit values are first rounded to fp16.
+ *   first_dev    int32 [B + 1], ascending: the tokens first[b] .. first[b + 1] - 1 are request b's, in order (numbers below 0 and above N
+ *                count as these; tokens of no request are passed over); NULL: N = B and token b is request b's.
+ *   table_dev    int32 [B][table_stride], table_stride >= table_pages: the pages of each request in order, table_pages * page_tokens
+ *                <= 2^31 - 8193.  Tokens of a page outside 0 .. pages-1 are not stored.  No page that is stored to may occur twice.
+ *   length_dev   int32 [B]: tokens of each request with the new ones: its last new token becomes number length - 1 (values below 0 and
+ *                above table_pages * page_tokens count as these; new tokens that then have numbers below 0 are passed over).
+ *   k_values_dev_out, v_values_dev_out  fp16 [N][ld...], or NULL: the values that the codes of the new tokens stand for, also where
+ *                they are not stored.  Rows of tokens that are passed over stay as they were.
+ * A cell's first token makes the rest of it zeros.  One that joins a cell whose scale is too small for it makes the scale grow, and
+ * the codes of the tokens before are rounded again (those that stand for less than 2^-6 of the new scale change, by half a step of
+ * 2^-9 of it at most).  Launches one kernel. */
+SPDP_API spdp_status spdp_kv8_store(const void* k_dev, int64_t ldk, const void* v_dev, int64_t ldv, spdp_ydtype vdt, int64_t N, int kv_heads, int head_dim, int64_t B,
+                           const void* first_dev, const void* table_dev, int64_t table_stride, int64_t table_pages, const void* length_dev, void* cache_dev,
+                           int64_t pages, int page_tokens, void* k_values_dev_out, int64_t ldk_values, void* v_values_dev_out, int64_t ldv_values, void* stream);
+
+/* Attention of N new tokens of B requests over the 8-bit cache (store them first), fused with the pruning decision of the projection behind
+ * it: y = softmax(cap * tanh(scale * q k / cap)) v, query head i with key head i / (q_heads / kv_heads), for single tokens, a few
+ * of each request, and prompts or pieces of them, also mixed in a call.
+ *   q_dev        fp16 [N][ldq]; q_heads a multiple of kv_heads.
+ *   first_dev, table_dev, length_dev  as for spdp_kv8_store: request b's last token first[b + 1] - 1 is its key number length[b] - 1, and
+ *                a token sees the keys up to its own number.  The keys of a page outside 0 .. pages-1 are left out.
+ *   scale        between -10^16 and 10^16.
+ *   cap          > 0 (10^38 at most): scores are capped; 0: they are not.
+ *   window       > 0: a token sees only the last `window` keys up to its own, and the request's first `sinks` keys (those of them that are not
+ *                behind it); 0: all keys up to its own.  Pages that no token sees may be missing from the table.
+ *   y_dev        fp16 [N][ldy], ldy >= q_heads * head_dim.  A token that sees no key gets zeros; tokens of no request stay as they were.
+ *   mask_dev_out uint32 [N][mask_stride], mask_stride >= q_heads * head_dim / 32, or NULL: the columns that the o-projection
+ *                should keep, NOT(|y_j| <= thr) on the stored y, for SPDP_DP_MASK (thr is used for nothing else).
+ * Refused as SPDP_ERR_UNSUPPORTED_SHAPE besides: N * q_heads of 2^31 and more, and B * kv_heads * (rows / 8, rounded up) * (table_pages * page_tokens
+ * / 64 + 8) of 2^31 and more, with rows the query heads of a key head times N (times 1 where first_dev is NULL).
+ * What lies in the cache behind a request's last key is never used, whatever it is.  Sums in 32 bits; the softmax's weights, times the
+ * scales of the values, are rounded to fp16 for their product with these.  Launches one to four kernels, with scratch memory (up to
+ * some tens of MB) unless the requests are few and short. */
+SPDP_API spdp_status spdp_attn_kv8(const void* q_dev, int64_t ldq, int64_t N, int q_heads, int kv_heads, int head_dim, int64_t B, const void* first_dev, const void* cache_dev,
+                          int64_t pages, int page_tokens, const void* table_dev, int64_t table_stride, int64_t table_pages, const void* length_dev, float scale, float cap,
+                          int64_t window, int64_t sinks, float thr, void* y_dev, int64_t ldy, void* mask_dev_out, int64_t mask_stride, void* stream);
+
+/* The pages of a cache (4-bit, 8-bit, or any whose pages are a multiple of 16 bytes) between steps.  The state is the caller's, on the
+ * device, and every call changes it in stream order, so all of this may be captured together with the steps that use the pages:
+ *   ref_dev      int32 [pages] (1 <= pages <= 2^28): how many entries of the table name the page; 0 or less: the page is free.
+ *   table_dev    int32 [rows][table_stride], table_stride >= table_pages, rows <= 2^24: a request's pages in order, -1 where there is none.
+ *                rows * table_pages < 2^31.
+ *   cache_dev    `layers` caches of `pages` pages each, layer_stride bytes apart (a multiple of 16, >= pages * page_bytes; ignored for one layer); all share
+ *                the table.  16-byte aligned.
+ * A call names n <= 4096 rows (or pairs) by int32 [n] arrays on the device; rows outside 0 .. rows-1 are passed over, entries are cut
+ * to 0 .. table_pages.  n = 0 does nothing (an output of a number gets 0). */
+
+/* Entries from[i] .. to[i] - 1 of row[i] each get a free page, whatever they held: the lowest free page to the first entry of row[0], and so on.
+ * Those for which there is none get -1; short_dev_out (int32 [1], or NULL) gets their number.  No entry may be named twice.  One kernel. */
+SPDP_API spdp_status spdp_kv_pages_take(void* ref_dev, int64_t pages, void* table_dev, int64_t rows, int64_t table_stride, int64_t table_pages, const void* row_dev,
+                           const void* from_dev, const void* to_dev, int64_t n, void* short_dev_out, void* stream);
+
+/* Entries from[i] .. to[i] - 1 of row[i] give their pages back and become -1 (those that name none too).  A finished request frees 0 ..
+ * table_pages; one with a window frees what lies between its first tokens and the window.  One kernel. */
+SPDP_API spdp_status spdp_kv_pages_free(void* ref_dev, int64_t pages, void* table_dev, int64_t rows, int64_t table_stride, int64_t table_pages, const void* row_dev,
+                           const void* from_dev, const void* to_dev, int64_t n, void* stream);
+
+/* Row child[i] becomes a request with the first length[i] tokens of row parent[i]: full pages (of page_tokens, a power of two, 1 .. 2^16) are shared, a last,
+ * partly filled one is copied to a free page (the lowest to the first i) in all layers.  Entries behind these stay as they were.  Where the parent
+ * has no page the child gets -1; so it does where there is no free page for a copy, and short_dev_out (int32 [1], or NULL) gets
+ * the number of these.  Children are distinct rows that are no parents, whose first entries name no pages.  Two kernels, some KB of scratch memory. */
+SPDP_API spdp_status spdp_kv_pages_fork(void* cache_dev, int layers, int64_t layer_stride, int64_t page_bytes, void* ref_dev, int64_t pages, void* table_dev, int64_t rows,
+                           int64_t table_stride, int64_t table_pages, int page_tokens, const void* parent_dev, const void* child_dev, const void* length_dev, int64_t n,
+                           void* short_dev_out, void* stream);
+
+/* Page src[i] to page dst[i] in all layers.  Pairs of which one is outside 0 .. pages-1 are passed over.  What is a destination may be nothing
+ * else in the call.  One kernel. */
+SPDP_API spdp_status spdp_kv_pages_copy(void* cache_dev, int layers, int64_t layer_stride, int64_t page_bytes, int64_t pages, const void* src_dev, const void* dst_dev, int64_t n,
+                           void* stream);
+
+/* Brings the pages in use together: with `live` of them, the i-th free page below `live` gets the i-th page in use from `live` on, in all layers, counts and table
+ * entries (of all rows) with it.  live_dev_out (int32 [1], or NULL) gets their number: the pages from there on are free.  Three
+ * kernels, 8 bytes of scratch memory to a page. */
+SPDP_API spdp_status spdp_kv_pages_compact(void* cache_dev, int layers, int64_t layer_stride, int64_t page_bytes, void* ref_dev, int64_t pages, void* table_dev, int64_t rows,
+                           int64_t table_stride, int64_t table_pages, void* live_dev_out, void* stream);
+
 /* Row-tile sharding over several GPUs (the paper names multi-GPU execution as future work, Sec. 6; the
  * natural split of y = W x keeps whole 256-row tiles together, so every rank packs its own rows as
  * an independent Tiled-CBC matrix, x is replicated, and the outputs are disjoint).  This is the split

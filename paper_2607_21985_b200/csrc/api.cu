@@ -173,11 +173,33 @@ bool weights_ok(int64_t count, int64_t apart, int64_t rows, int64_t ld, int64_t 
     return (rows - 1) * ld + row <= apart || (count - 1) * apart + row <= ld;
 }
 
-constexpr int kMostCacheHeads = 4096;
+constexpr int kMostCacheHeads = 4096, kMostRequests = 4096;
+constexpr int64_t kMostPages = int64_t(1) << 28;
+constexpr int64_t kMostKeys = INT32_MAX - 8192;         // of a request: the kernels look some thousands ahead of its last one
 // A cache of 4-bit keys and values that the kernels take.
 bool kv4_shape_ok(int kv_heads, int head_dim, int page_tokens) {
     return kv_heads >= 1 && kv_heads <= kMostCacheHeads && (head_dim == 64 || head_dim == 128 || head_dim == 256) && page_tokens >= 16 && page_tokens <= 256 &&
            (page_tokens & (page_tokens - 1)) == 0;
+}
+
+// The arguments that the calls on pages share.
+spdp_status pages_call(KvPagesCall* c, void* ref, int64_t pages, void* table, int64_t rows, int64_t table_stride, int64_t table_pages, const void* a, const void* b, const void* d,
+                       int64_t n, void* number_out) {
+    if (ref == nullptr || table == nullptr || (n > 0 && (a == nullptr || b == nullptr || d == nullptr))) return SPDP_ERR_INVALID_ARG;
+    if (pages < 1 || rows < 1 || table_pages < 1 || n < 0 || n > kMostRequests || !stride_ok(table_stride, table_pages)) return SPDP_ERR_INVALID_ARG;
+    if (misaligned(ref, 3u) || misaligned(table, 3u) || misaligned(a, 3u) || misaligned(b, 3u) || misaligned(d, 3u) || misaligned(number_out, 3u)) return SPDP_ERR_INVALID_ARG;
+    if (pages > kMostPages || rows > kMostTokens || table_pages > INT32_MAX / rows) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    c->ref = static_cast<int32_t*>(ref), c->table = static_cast<int32_t*>(table), c->short_out = static_cast<int32_t*>(number_out);
+    c->row = static_cast<const int32_t*>(a), c->from = static_cast<const int32_t*>(b), c->to = static_cast<const int32_t*>(d);
+    c->pages = pages, c->rows = rows, c->table_stride = table_stride, c->table_pages = table_pages, c->n = n;
+    return SPDP_OK;
+}
+spdp_status pages_cache(KvPagesCall* c, void* cache, int layers, int64_t layer_stride, int64_t page_bytes, int64_t pages) {
+    if (cache == nullptr || misaligned(cache, 15u) || layers < 1 || page_bytes < 16 || page_bytes % 16 != 0 || pages < 1) return SPDP_ERR_INVALID_ARG;
+    if (pages > kMostPages || layers > 65536 || page_bytes > int64_t(1) << 32) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    if (layers > 1 && (layer_stride < pages * page_bytes || layer_stride % 16 != 0 || layer_stride > (int64_t(1) << 62) / layers)) return SPDP_ERR_INVALID_ARG;
+    c->cache = static_cast<unsigned char*>(cache), c->layers = layers, c->layer_stride = layers > 1 ? layer_stride : 0, c->page_bytes = page_bytes, c->pages = pages;
+    return SPDP_OK;
 }
 
 constexpr int kBatchViaSingleCalls = 2;   // spdp_spmspv_batch: up to this many tokens go through the single-vector kernel
@@ -660,6 +682,110 @@ spdp_status spdp_attn_kv4(const void* q_dev, int64_t ldq, int64_t B, int q_heads
     c.B = B, c.ldq = ldq, c.ldy = ldy, c.table_stride = table_stride, c.table_pages = table_pages, c.mask_stride = mask_stride, c.pages = pages, c.window = window;
     c.q_heads = q_heads, c.kv_heads = kv_heads, c.head_dim = head_dim, c.page_tokens = page_tokens, c.scale = scale, c.cap = cap, c.thr = thr;
     return launch_attn_kv4(c, static_cast<cudaStream_t>(stream));
+}
+
+spdp_status spdp_kv8_page_bytes(int kv_heads, int head_dim, int page_tokens, int64_t* bytes_out) {
+    if (bytes_out == nullptr) return SPDP_ERR_INVALID_ARG;
+    if (!kv4_shape_ok(kv_heads, head_dim, page_tokens)) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    *bytes_out = static_cast<int64_t>(kv_heads) * page_tokens * (2 * head_dim + 1);
+    return SPDP_OK;
+}
+
+spdp_status spdp_kv8_store(const void* k_dev, int64_t ldk, const void* v_dev, int64_t ldv, spdp_ydtype vdt, int64_t N, int kv_heads, int head_dim, int64_t B,
+                           const void* first_dev, const void* table_dev, int64_t table_stride, int64_t table_pages, const void* length_dev, void* cache_dev,
+                           int64_t pages, int page_tokens, void* k_values_dev_out, int64_t ldk_values, void* v_values_dev_out, int64_t ldv_values, void* stream) {
+    if (k_dev == nullptr || v_dev == nullptr || table_dev == nullptr || length_dev == nullptr || cache_dev == nullptr) return SPDP_ERR_INVALID_ARG;
+    if (!kv4_shape_ok(kv_heads, head_dim, page_tokens) || B > kMostRequests) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    const int64_t row = static_cast<int64_t>(kv_heads) * head_dim;
+    if (N < 1 || N > kMostTokens || B < 1 || (first_dev == nullptr && B != N) || pages < 1 || pages > INT32_MAX || table_pages < 1 || !stride_ok(table_stride, table_pages) ||
+        !stride_ok(ldk, row) || !stride_ok(ldv, row) || (vdt != SPDP_Y_F16 && vdt != SPDP_Y_F32))
+        return SPDP_ERR_INVALID_ARG;
+    if ((k_values_dev_out != nullptr && !stride_ok(ldk_values, row)) || (v_values_dev_out != nullptr && !stride_ok(ldv_values, row))) return SPDP_ERR_INVALID_ARG;
+    if (misaligned(k_dev, 1u) || misaligned(v_dev, vdt == SPDP_Y_F32 ? 3u : 1u) || misaligned(first_dev, 3u) || misaligned(table_dev, 3u) || misaligned(length_dev, 3u) ||
+        misaligned(cache_dev, 15u) || misaligned(k_values_dev_out, 1u) || misaligned(v_values_dev_out, 1u))
+        return SPDP_ERR_INVALID_ARG;
+    if (table_pages > kMostKeys / page_tokens) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    Kv8StoreCall c = {};
+    c.k = static_cast<const __half*>(k_dev), c.v = v_dev, c.first = static_cast<const int32_t*>(first_dev), c.table = static_cast<const int32_t*>(table_dev);
+    c.length = static_cast<const int32_t*>(length_dev), c.cache = static_cast<unsigned char*>(cache_dev);
+    c.k_values = static_cast<__half*>(k_values_dev_out), c.v_values = static_cast<__half*>(v_values_dev_out);
+    c.N = N, c.B = B, c.ldk = ldk, c.ldv = ldv, c.pages = pages, c.table_stride = table_stride, c.table_pages = table_pages;
+    c.ldk_values = k_values_dev_out != nullptr ? ldk_values : 0, c.ldv_values = v_values_dev_out != nullptr ? ldv_values : 0;
+    c.kv_heads = kv_heads, c.head_dim = head_dim, c.page_tokens = page_tokens, c.vdt = vdt;
+    return launch_kv8_store(c, static_cast<cudaStream_t>(stream));
+}
+
+spdp_status spdp_attn_kv8(const void* q_dev, int64_t ldq, int64_t N, int q_heads, int kv_heads, int head_dim, int64_t B, const void* first_dev, const void* cache_dev,
+                          int64_t pages, int page_tokens, const void* table_dev, int64_t table_stride, int64_t table_pages, const void* length_dev, float scale, float cap,
+                          int64_t window, int64_t sinks, float thr, void* y_dev, int64_t ldy, void* mask_dev_out, int64_t mask_stride, void* stream) {
+    if (q_dev == nullptr || cache_dev == nullptr || table_dev == nullptr || length_dev == nullptr || y_dev == nullptr) return SPDP_ERR_INVALID_ARG;
+    if (!kv4_shape_ok(kv_heads, head_dim, page_tokens) || q_heads < 1 || q_heads > 16 * kMostCacheHeads || q_heads % kv_heads != 0) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    if (B > kMostRequests) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    const int64_t row = static_cast<int64_t>(q_heads) * head_dim;
+    if (N < 1 || N > kMostTokens || B < 1 || (first_dev == nullptr && B != N) || pages < 1 || pages > INT32_MAX || table_pages < 1 || !stride_ok(table_stride, table_pages) ||
+        !stride_ok(ldq, row) || !stride_ok(ldy, row) || window < 0 || sinks < 0)
+        return SPDP_ERR_INVALID_ARG;
+    if (mask_dev_out != nullptr && !stride_ok(mask_stride, row / 32)) return SPDP_ERR_INVALID_ARG;
+    // products are below 2^41, so scores stay below the 10^30 that stands for "no score yet" in the kernel
+    if (!(scale >= -1.0e16f && scale <= 1.0e16f) || !(cap >= 0.0f && cap <= 1.0e38f)) return SPDP_ERR_INVALID_ARG;
+    if (misaligned(q_dev, 1u) || misaligned(first_dev, 3u) || misaligned(cache_dev, 15u) || misaligned(table_dev, 3u) || misaligned(length_dev, 3u) || misaligned(y_dev, 1u) ||
+        misaligned(mask_dev_out, 3u))
+        return SPDP_ERR_INVALID_ARG;
+    // the keys of a request, the rows of a key head and the 64-key units of all of them, with what the kernels add, are counted in 32 bits
+    if (table_pages > kMostKeys / page_tokens || N > INT32_MAX / q_heads) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    const int64_t tokens = first_dev == nullptr ? 1 : N, blocks = kv_heads * ((tokens * (q_heads / kv_heads) + 7) / 8);
+    if (blocks * (table_pages * page_tokens / 64 + 8) > INT32_MAX / B) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    Kv8AttnCall c = {};
+    c.q = static_cast<const __half*>(q_dev), c.cache = static_cast<const unsigned char*>(cache_dev), c.first = static_cast<const int32_t*>(first_dev);
+    c.table = static_cast<const int32_t*>(table_dev), c.length = static_cast<const int32_t*>(length_dev), c.y = static_cast<__half*>(y_dev), c.mask = static_cast<uint32_t*>(mask_dev_out);
+    c.N = N, c.B = B, c.ldq = ldq, c.ldy = ldy, c.table_stride = table_stride, c.table_pages = table_pages, c.mask_stride = mask_stride, c.pages = pages;
+    c.window = window, c.sinks = sinks, c.q_heads = q_heads, c.kv_heads = kv_heads, c.head_dim = head_dim, c.page_tokens = page_tokens;
+    c.scale = scale, c.cap = cap, c.thr = thr;
+    return launch_attn_kv8(c, static_cast<cudaStream_t>(stream));
+}
+
+spdp_status spdp_kv_pages_take(void* ref_dev, int64_t pages, void* table_dev, int64_t rows, int64_t table_stride, int64_t table_pages, const void* row_dev,
+                               const void* from_dev, const void* to_dev, int64_t n, void* short_dev_out, void* stream) {
+    KvPagesCall c = {};
+    const spdp_status st = pages_call(&c, ref_dev, pages, table_dev, rows, table_stride, table_pages, row_dev, from_dev, to_dev, n, short_dev_out);
+    return st != SPDP_OK ? st : launch_kv_pages_take(c, static_cast<cudaStream_t>(stream));
+}
+
+spdp_status spdp_kv_pages_free(void* ref_dev, int64_t pages, void* table_dev, int64_t rows, int64_t table_stride, int64_t table_pages, const void* row_dev,
+                               const void* from_dev, const void* to_dev, int64_t n, void* stream) {
+    KvPagesCall c = {};
+    const spdp_status st = pages_call(&c, ref_dev, pages, table_dev, rows, table_stride, table_pages, row_dev, from_dev, to_dev, n, nullptr);
+    return st != SPDP_OK ? st : launch_kv_pages_free(c, static_cast<cudaStream_t>(stream));
+}
+
+spdp_status spdp_kv_pages_fork(void* cache_dev, int layers, int64_t layer_stride, int64_t page_bytes, void* ref_dev, int64_t pages, void* table_dev, int64_t rows,
+                               int64_t table_stride, int64_t table_pages, int page_tokens, const void* parent_dev, const void* child_dev, const void* length_dev, int64_t n,
+                               void* short_dev_out, void* stream) {
+    KvPagesCall c = {};
+    spdp_status st = pages_call(&c, ref_dev, pages, table_dev, rows, table_stride, table_pages, parent_dev, child_dev, length_dev, n, short_dev_out);
+    if (st == SPDP_OK) st = pages_cache(&c, cache_dev, layers, layer_stride, page_bytes, pages);
+    if (st != SPDP_OK) return st;
+    if (page_tokens < 1 || page_tokens > 1 << 16 || (page_tokens & (page_tokens - 1)) != 0) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    c.page_tokens = page_tokens;
+    return launch_kv_pages_fork(c, static_cast<cudaStream_t>(stream));
+}
+
+spdp_status spdp_kv_pages_copy(void* cache_dev, int layers, int64_t layer_stride, int64_t page_bytes, int64_t pages, const void* src_dev, const void* dst_dev, int64_t n,
+                               void* stream) {
+    KvPagesCall c = {};
+    const spdp_status st = pages_cache(&c, cache_dev, layers, layer_stride, page_bytes, pages);
+    if (st != SPDP_OK) return st;
+    if (n < 0 || n > kMostRequests || (n > 0 && (src_dev == nullptr || dst_dev == nullptr)) || misaligned(src_dev, 3u) || misaligned(dst_dev, 3u)) return SPDP_ERR_INVALID_ARG;
+    c.row = static_cast<const int32_t*>(src_dev), c.to = static_cast<const int32_t*>(dst_dev), c.n = n;
+    return launch_kv_pages_copy(c, static_cast<cudaStream_t>(stream));
+}
+
+spdp_status spdp_kv_pages_compact(void* cache_dev, int layers, int64_t layer_stride, int64_t page_bytes, void* ref_dev, int64_t pages, void* table_dev, int64_t rows,
+                                  int64_t table_stride, int64_t table_pages, void* live_dev_out, void* stream) {
+    KvPagesCall c = {};
+    spdp_status st = pages_call(&c, ref_dev, pages, table_dev, rows, table_stride, table_pages, nullptr, nullptr, nullptr, 0, live_dev_out);
+    if (st == SPDP_OK) st = pages_cache(&c, cache_dev, layers, layer_stride, page_bytes, pages);
+    return st != SPDP_OK ? st : launch_kv_pages_compact(c, static_cast<cudaStream_t>(stream));
 }
 
 spdp_status spdp_row_shard(int64_t M, int world, int rank, int64_t* first_row_out, int64_t* rows_out) {

@@ -1,0 +1,402 @@
+// The pages of a key/value cache between steps: taken for growing requests, freed, forked, copied, brought together.  The state is the
+// caller's, on the device: a table of each request's pages and a count of the table's entries that name each page; a page that none names is
+// free.  What a call does follows from these alone, page by page in their order, so the same state gives the same pages; and all of it
+// may be captured together with the steps that use the pages.
+//
+// Counting and naming are integers; what takes time is moving pages (2 bytes of traffic to each byte of a page, in every layer).
+#include "kv8.cuh"
+
+namespace spdp {
+namespace {
+
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kMostRequests = 4096;
+constexpr unsigned kAll = 0xFFFFFFFFu;
+
+// A number for each thread -> the sum of those of the threads before it; the sum of all in *total.  (All threads; `sums`: a word to a
+// warp and one more.  Ends with a barrier.)
+__device__ __forceinline__ int64_t sum_before(int64_t mine, int64_t* sums, int64_t* total) {
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    int64_t up_to = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int64_t v = __shfl_up_sync(kAll, up_to, d);
+        if (lane >= d) up_to += v;
+    }
+    if (lane == 31) sums[w] = up_to;
+    __syncthreads();
+    if (w == 0) {
+        const int64_t all = sums[lane];
+        int64_t s = all;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int64_t v = __shfl_up_sync(kAll, s, d);
+            if (lane >= d) s += v;
+        }
+        __syncwarp();
+        sums[lane] = s - all;
+        if (lane == 31) sums[kWarps] = s;
+    }
+    __syncthreads();
+    const int64_t r = sums[w] + up_to - mine;
+    *total = sums[kWarps];
+    __syncthreads();
+    return r;
+}
+
+struct Table {
+    int32_t* entries;
+    int64_t stride;
+    int rows, pages;                    // entries of a row
+};
+__device__ __forceinline__ int within(int v, int most) { return v < 0 ? 0 : v < most ? v : most; }
+
+// Free pages, lowest first, to the places 0 .. wanted - 1: give(place, page) for each, page -1 where there are no more.  One CTA.
+constexpr int kAhead = 16;              // pages of a lane that are looked at at once
+template <typename Give>
+__device__ __forceinline__ int64_t give_pages(int32_t* ref, int pages, int64_t wanted, int64_t* sums, Give give) {
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    int64_t given = 0;
+    for (int64_t base = 0; base < pages && given < wanted; base += kThreads * kAhead) {
+        const int64_t mine = base + w * (32 * kAhead) + lane;
+        unsigned free[kAhead];
+        int count = 0;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) free[i] = mine + 32 * i < pages ? ref[mine + 32 * i] <= 0 : 0;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const unsigned all = __ballot_sync(kAll, free[i] != 0);
+            free[i] = all;
+            count += __popc(all);
+        }
+        int64_t total;
+        int64_t at = given + sum_before(lane == 0 ? count : 0, sums, &total);
+        at = __shfl_sync(kAll, at, 0);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int64_t place = at + __popc(free[i] & ((1u << lane) - 1));
+            if (free[i] >> lane & 1 && place < wanted) {
+                const int page = static_cast<int>(mine + 32 * i);
+                ref[page] = 1;
+                give(place, page);
+            }
+            at += __popc(free[i]);
+        }
+        given += total;
+    }
+    for (int64_t place = given + threadIdx.x; place < wanted; place += kThreads) give(place, -1);
+    return wanted > given ? wanted - given : 0;
+}
+
+// Which of n ascending starts place u lies behind: the last that is not above it (and not empty).
+__device__ __forceinline__ int owner_of(const int64_t* start, int n, int64_t u) {
+    int b = 0;
+    for (int lo = 0, hi = n - 1; lo <= hi;) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= u) b = mid, lo = mid + 1;
+        else hi = mid - 1;
+    }
+    return b;
+}
+
+// start[i]: the sum of count(0) .. count(i - 1); returns the sum of all n.
+template <typename Count>
+__device__ __forceinline__ int64_t starts_of(int n, int64_t* start, int64_t* sums, Count count) {
+    int64_t before = 0;
+    for (int base = 0; base < n; base += kThreads) {
+        const int i = base + threadIdx.x;
+        int64_t total;
+        const int64_t mine = i < n ? count(i) : 0, at = before + sum_before(mine, sums, &total);
+        if (i < n) start[i] = at;
+        before += total;
+    }
+    __syncthreads();
+    return before;
+}
+
+__global__ void __launch_bounds__(kThreads) take_kernel(int32_t* ref, int pages, Table t, const int32_t* row, const int32_t* from, const int32_t* to, int n, int32_t* short_out) {
+    __shared__ int64_t start[kMostRequests], sums[kWarps + 1];
+    dev::programmatic_start();
+    const int64_t wanted = starts_of(n, start, sums, [&](int i) -> int64_t {
+        return row[i] < 0 || row[i] >= t.rows ? 0 : max(0, within(to[i], t.pages) - within(from[i], t.pages));
+    });
+    const int64_t missing = give_pages(ref, pages, wanted, sums, [&](int64_t place, int page) {
+        const int i = owner_of(start, n, place);
+        t.entries[row[i] * t.stride + within(from[i], t.pages) + (place - start[i])] = page;
+    });
+    if (short_out != nullptr && threadIdx.x == 0) *short_out = static_cast<int>(missing < INT32_MAX ? missing : INT32_MAX);
+}
+
+__global__ void __launch_bounds__(256) free_kernel(int32_t* ref, int pages, Table t, const int32_t* row, const int32_t* from, const int32_t* to) {
+    dev::programmatic_start();
+    const int i = blockIdx.x, r = row[i];
+    if (r < 0 || r >= t.rows) return;
+    const int end = within(to[i], t.pages);
+    for (int e = within(from[i], t.pages) + threadIdx.x; e < end; e += blockDim.x) {
+        const int page = atomicExch(&t.entries[r * t.stride + e], -1);      // so that an entry that is named twice is freed once
+        if (page >= 0 && page < pages) atomicSub(&ref[page], 1);
+    }
+}
+
+// Block 0 takes pages for the children's last pages and writes down what is to be copied; the others share the full ones.
+__global__ void __launch_bounds__(kThreads) fork_kernel(int32_t* ref, int pages, Table t, const int32_t* parent, const int32_t* child, const int32_t* length, int n, int page_shift,
+                                                        int32_t* src, int32_t* dst, int32_t* short_out) {
+    __shared__ int64_t start[kMostRequests], sums[kWarps + 1];
+    dev::programmatic_start();
+    auto exists = [&](int i) { return parent[i] >= 0 && parent[i] < t.rows && child[i] >= 0 && child[i] < t.rows; };
+    const int64_t most = static_cast<int64_t>(t.pages) << page_shift;
+    auto tokens = [&](int i) { return static_cast<int>(length[i] < 0 ? 0 : length[i] < most ? length[i] : most); };
+    if (blockIdx.x > 0) {
+        for (int i = blockIdx.x - 1; i < n; i += gridDim.x - 1) {
+            if (!exists(i)) continue;
+            const int full = tokens(i) >> page_shift;
+            for (int e = threadIdx.x; e < full; e += kThreads) {
+                const int page = t.entries[parent[i] * t.stride + e];
+                const bool ok = page >= 0 && page < pages;
+                t.entries[child[i] * t.stride + e] = ok ? page : -1;
+                if (ok) atomicAdd(&ref[page], 1);
+            }
+        }
+        return;
+    }
+    auto last_page = [&](int i) {                               // the parent's partly filled page, or -1
+        if (!exists(i) || (tokens(i) & ((1 << page_shift) - 1)) == 0) return -1;
+        const int page = t.entries[parent[i] * t.stride + (tokens(i) >> page_shift)];
+        return page >= 0 && page < pages ? page : -1;
+    };
+    const int64_t wanted = starts_of(n, start, sums, [&](int i) -> int64_t {
+        const int page = last_page(i);
+        src[i] = page, dst[i] = -1;
+        if (page < 0 && exists(i) && (tokens(i) & ((1 << page_shift) - 1)) != 0) t.entries[child[i] * t.stride + (tokens(i) >> page_shift)] = -1;
+        return page >= 0 ? 1 : 0;
+    });
+    const int64_t missing = give_pages(ref, pages, wanted, sums, [&](int64_t place, int page) {
+        const int i = owner_of(start, n, place);
+        t.entries[child[i] * t.stride + (tokens(i) >> page_shift)] = page;
+        dst[i] = page;
+    });
+    if (short_out != nullptr && threadIdx.x == 0) *short_out = static_cast<int>(missing);
+}
+
+// ---- moving pages
+
+struct Pages {
+    unsigned char* cache;
+    int64_t layer_stride, page_bytes;   // bytes
+    int layers, pages;
+};
+constexpr int kMoveThreads = 256, kMoveLoads = 4;
+constexpr int kPiece = kMoveThreads * kMoveLoads * 16;          // bytes that a CTA moves at a time
+
+// Pages src[i] to dst[i], i < n, in all layers; pairs of which one is no page are left out.
+__device__ __forceinline__ void move_pages(const Pages& p, const int32_t* src, const int32_t* dst, int64_t n, int64_t cta, int64_t ctas) {
+    const int64_t pieces = (p.page_bytes + kPiece - 1) / kPiece, of_pair = pieces * p.layers;
+    for (int64_t u = cta; u < n * of_pair; u += ctas) {
+        const int64_t i = u / of_pair, layer = u % of_pair / pieces, at = u % pieces * kPiece + 16 * threadIdx.x;
+        const int a = src[i], b = dst[i];
+        if (a < 0 || a >= p.pages || b < 0 || b >= p.pages || a == b) continue;
+        const unsigned char* from = p.cache + layer * p.layer_stride + a * p.page_bytes;
+        unsigned char* to = p.cache + layer * p.layer_stride + b * p.page_bytes;
+        uint4 v[kMoveLoads];
+#pragma unroll
+        for (int j = 0; j < kMoveLoads; ++j)
+            if (at + j * kMoveThreads * 16 < p.page_bytes) v[j] = *reinterpret_cast<const uint4*>(from + at + j * kMoveThreads * 16);
+#pragma unroll
+        for (int j = 0; j < kMoveLoads; ++j)
+            if (at + j * kMoveThreads * 16 < p.page_bytes) *reinterpret_cast<uint4*>(to + at + j * kMoveThreads * 16) = v[j];
+    }
+}
+__global__ void __launch_bounds__(kMoveThreads) copy_kernel(const Pages p, const int32_t* src, const int32_t* dst, int64_t n) {
+    dev::programmatic_start();
+    move_pages(p, src, dst, n, blockIdx.x, gridDim.x);
+}
+unsigned move_ctas(const Pages& p, int64_t pairs, int sms) {
+    const int64_t all = pairs * p.layers * ((p.page_bytes + kPiece - 1) / kPiece);
+    return static_cast<unsigned>(all < 8 * sms ? (all > 0 ? all : 1) : 8 * sms);
+}
+
+// ---- bringing together
+//
+// With `live` pages in use, the i-th free page below `live` gets the i-th page in use from there on.  The pages are cut into kSegments
+// runs: a first kernel counts each run's pages in use, a second has every run's place from these counts and writes the two lists, a third
+// moves and renames.
+
+constexpr int kSegments = 1024;
+constexpr int kListThreads = 256;
+struct Lists {
+    int32_t* counts;                    // [kSegments] pages in use
+    int32_t* place;                     // [pages] of the pages from `live` on: the one's place in the lists, or -1
+    int32_t* src;                       // [pages / 2] pages to move
+    int32_t* dst;                       // [pages / 2] and where to
+    int32_t* moved;                     // how many
+};
+__device__ __forceinline__ int segment_length(int pages) { return (pages + kSegments - 1) / kSegments; }
+
+__global__ void __launch_bounds__(kListThreads) count_kernel(const int32_t* ref, int pages, Lists l) {
+    __shared__ int count;
+    dev::programmatic_start();
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    const int64_t begin = static_cast<int64_t>(blockIdx.x) * segment_length(pages), end = min(begin + segment_length(pages), static_cast<int64_t>(pages));
+    int mine = 0;
+    for (int64_t i = begin + threadIdx.x; i < end; i += kListThreads) mine += ref[i] > 0 ? 1 : 0;
+    mine = __reduce_add_sync(kAll, mine);
+    if ((threadIdx.x & 31) == 0) atomicAdd(&count, mine);
+    __syncthreads();
+    if (threadIdx.x == 0) l.counts[blockIdx.x] = count;
+}
+
+__device__ __forceinline__ int block_sum(int mine, int* word) {
+    mine = __reduce_add_sync(kAll, mine);
+    if (threadIdx.x == 0) *word = 0;
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) atomicAdd(word, mine);
+    __syncthreads();
+    const int r = *word;
+    __syncthreads();
+    return r;
+}
+
+__global__ void __launch_bounds__(kListThreads) list_kernel(const int32_t* ref, int pages, Lists l, int32_t* live_out) {
+    __shared__ int word, warp_counts[kListThreads / 32];
+    dev::programmatic_start();
+    const int length = segment_length(pages);
+    const int64_t begin = static_cast<int64_t>(blockIdx.x) * length, end = min(begin + length, static_cast<int64_t>(pages));
+    int all = 0, before = 0;
+    for (int i = threadIdx.x; i < kSegments; i += kListThreads) {
+        all += l.counts[i];
+        if (i < blockIdx.x) before += l.counts[i];
+    }
+    const int live = block_sum(all, &word);
+    before = block_sum(before, &word);                          // pages in use before this run
+    int below = 0;                                              // and below `live`
+    const int cut = live / length;
+    for (int i = threadIdx.x; i < cut; i += kListThreads) below += l.counts[i];
+    for (int64_t i = static_cast<int64_t>(cut) * length + threadIdx.x; i < live; i += kListThreads) below += ref[i] > 0 ? 1 : 0;
+    below = block_sum(below, &word);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        *l.moved = live - below;
+        if (live_out != nullptr) *live_out = live;
+    }
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    for (int64_t base = begin; base < end; base += kListThreads) {
+        const int64_t i = base + threadIdx.x;
+        const bool used = i < end && ref[i] > 0;
+        const unsigned bits = __ballot_sync(kAll, used);
+        if (lane == 0) warp_counts[w] = __popc(bits);
+        __syncthreads();
+        int at = before + __popc(bits & ((1u << lane) - 1));    // pages in use before page i
+        for (int j = 0; j < kListThreads / 32; ++j) {
+            if (j < w) at += warp_counts[j];
+            before += warp_counts[j];
+        }
+        if (i < end) {
+            if (i < live) {
+                if (!used) l.dst[i - at] = static_cast<int>(i);
+            } else {
+                l.place[i] = used ? at - below : -1;
+                if (used) l.src[at - below] = static_cast<int>(i);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// The last `renamers` CTAs rename the table's entries and hand over the counts, the others move.
+__global__ void __launch_bounds__(kMoveThreads) compact_kernel(const Pages p, int32_t* ref, Table t, Lists l, int renamers) {
+    dev::programmatic_start();
+    const int moved = *l.moved, movers = static_cast<int>(gridDim.x) - renamers;
+    if (static_cast<int>(blockIdx.x) < movers) {
+        move_pages(p, l.src, l.dst, moved, blockIdx.x, movers);
+        return;
+    }
+    __shared__ int word;
+    int all = 0;
+    for (int i = threadIdx.x; i < kSegments; i += kMoveThreads) all += l.counts[i];
+    const int live = block_sum(all, &word);
+    const int64_t at = static_cast<int64_t>(blockIdx.x - movers) * kMoveThreads + threadIdx.x, step = static_cast<int64_t>(renamers) * kMoveThreads;
+    for (int64_t i = at; i < moved; i += step) {
+        ref[l.dst[i]] = ref[l.src[i]];
+        ref[l.src[i]] = 0;
+    }
+    for (int64_t i = at; i < static_cast<int64_t>(t.rows) * t.pages; i += step) {
+        int32_t* entry = t.entries + i / t.pages * t.stride + i % t.pages;
+        const int page = *entry;
+        if (page < live || page >= p.pages) continue;
+        const int place = l.place[page];
+        if (place >= 0) *entry = l.dst[place];
+    }
+}
+
+Table table_of(const KvPagesCall& c) { return Table{c.table, c.table_stride, static_cast<int>(c.rows), static_cast<int>(c.table_pages)}; }
+Pages pages_of(const KvPagesCall& c) { return Pages{c.cache, c.layer_stride, c.page_bytes, c.layers, static_cast<int>(c.pages)}; }
+
+}  // namespace
+
+spdp_status launch_kv_pages_take(const KvPagesCall& c, cudaStream_t s) {
+    SPDP_CUDA_TRY(launch_programmatic(take_kernel, dim3(1), kThreads, 0, s, c.ref, static_cast<int>(c.pages), table_of(c), c.row, c.from, c.to, static_cast<int>(c.n), c.short_out));
+    return SPDP_OK;
+}
+
+spdp_status launch_kv_pages_free(const KvPagesCall& c, cudaStream_t s) {
+    if (c.n == 0) return SPDP_OK;
+    SPDP_CUDA_TRY(launch_programmatic(free_kernel, dim3(static_cast<unsigned>(c.n)), 256, 0, s, c.ref, static_cast<int>(c.pages), table_of(c), c.row, c.from, c.to));
+    return SPDP_OK;
+}
+
+spdp_status launch_kv_pages_copy(const KvPagesCall& c, cudaStream_t s) {
+    int device = 0, sms = 0;
+    const spdp_status st = current_device(&device, &sms);
+    if (st != SPDP_OK || c.n == 0) return st;
+    const Pages p = pages_of(c);
+    SPDP_CUDA_TRY(launch_programmatic(copy_kernel, dim3(move_ctas(p, c.n, sms)), kMoveThreads, 0, s, p, c.row, c.to, c.n));
+    return SPDP_OK;
+}
+
+spdp_status launch_kv_pages_fork(const KvPagesCall& c, cudaStream_t s) {
+    int device = 0, sms = 0;
+    spdp_status st = current_device(&device, &sms);
+    if (st != SPDP_OK) return st;
+    void* scratch = nullptr;
+    st = scratch_alloc(device, (2 * c.n + 1) * sizeof(int32_t), s, &scratch);
+    if (st != SPDP_OK) return st;
+    int32_t *src = static_cast<int32_t*>(scratch), *dst = src + c.n;
+    const Pages p = pages_of(c);
+    int shift = 0;
+    while ((1 << shift) < c.page_tokens) ++shift;
+    const unsigned sharers = static_cast<unsigned>(c.n < sms ? c.n : sms);
+    cudaError_t e = launch_programmatic(fork_kernel, dim3(1 + sharers), kThreads, 0, s, c.ref, static_cast<int>(c.pages), table_of(c), c.row, c.from, c.to, static_cast<int>(c.n), shift, src, dst,
+                                        c.short_out);
+    if (e == cudaSuccess && c.n > 0) e = launch_programmatic(copy_kernel, dim3(move_ctas(p, c.n, sms)), kMoveThreads, 0, s, p, static_cast<const int32_t*>(src), static_cast<const int32_t*>(dst), c.n);
+    const cudaError_t freed = cudaFreeAsync(scratch, s);
+    SPDP_CUDA_TRY(e);
+    SPDP_CUDA_TRY(freed);
+    return SPDP_OK;
+}
+
+spdp_status launch_kv_pages_compact(const KvPagesCall& c, cudaStream_t s) {
+    int device = 0, sms = 0;
+    spdp_status st = current_device(&device, &sms);
+    if (st != SPDP_OK) return st;
+    const int pages = static_cast<int>(c.pages);
+    void* scratch = nullptr;
+    st = scratch_alloc(device, (kSegments + 1 + 2ll * pages + 2) * sizeof(int32_t), s, &scratch);
+    if (st != SPDP_OK) return st;
+    Lists l;
+    l.counts = static_cast<int32_t*>(scratch);
+    l.moved = l.counts + kSegments;
+    l.place = l.moved + 1;
+    l.src = l.place + pages;
+    l.dst = l.src + pages / 2 + 1;
+    const Pages p = pages_of(c);
+    const int renamers = 16;
+    cudaError_t e = launch_programmatic(count_kernel, dim3(kSegments), kListThreads, 0, s, static_cast<const int32_t*>(c.ref), pages, l);
+    if (e == cudaSuccess) e = launch_programmatic(list_kernel, dim3(kSegments), kListThreads, 0, s, static_cast<const int32_t*>(c.ref), pages, l, c.short_out);
+    if (e == cudaSuccess) e = launch_programmatic(compact_kernel, dim3(move_ctas(p, pages / 2 + 1, sms) + renamers), kMoveThreads, 0, s, p, c.ref, table_of(c), l, renamers);
+    const cudaError_t freed = cudaFreeAsync(scratch, s);
+    SPDP_CUDA_TRY(e);
+    SPDP_CUDA_TRY(freed);
+    return SPDP_OK;
+}
+
+}  // namespace spdp

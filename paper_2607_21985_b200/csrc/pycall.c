@@ -485,6 +485,207 @@ static PyObject* call_attn_kv4(PyObject* self, PyObject* const* a, Py_ssize_t n)
     return PyLong_FromLong(st);
 }
 
+/* The pages of an 8-bit cache. */
+static int cache8_of(PyObject* o, int64_t kv_heads, int64_t dim, int page_tokens, int here, tensor* t) {
+    if (!look(o, "cache", t)) return 0;
+    if (t->ndim != 2 || t->kind != U8 || t->device != here || !contiguous(t) || t->size[1] != kv_heads * page_tokens * (2 * dim + 1))
+        return refuse("cache must be a contiguous CUDA uint8 [pages][spdp_kv8_page_bytes(kv_heads, head_dim, page_tokens)] on the current device");
+    return 1;
+}
+
+/* The requests of N tokens: first [B + 1] or None (a token each), table [B][pages], length [B]. */
+typedef struct { void *first, *length; tensor table; int64_t B, stride; } requests;
+static int requests_of(PyObject* first, PyObject* table, PyObject* length, int64_t N, int here, requests* r) {
+    if (!look(table, "table", &r->table)) return 0;
+    if (r->table.kind != I32 || r->table.ndim != 2 || length == Py_None) return refuse("table must be int32 [B][pages] and length int32 [B]");
+    r->B = r->table.size[0];
+    if (first == Py_None && r->B != N) return refuse("table must have a row for each token where first is None");
+    return rows(&r->table, r->B, r->table.size[1], "table", here, &r->stride) && vector(length, I32, "int32", r->B, NULL, "length", here, &r->length) &&
+           vector(first, I32, "int32", r->B + 1, NULL, "first", here, &r->first);
+}
+
+typedef int (*store8_fn)(const void*, int64_t, const void*, int64_t, int, int64_t, int, int, int64_t, const void*, const void*, int64_t, int64_t, const void*, void*, int64_t,
+                         int, void*, int64_t, void*, int64_t, void*);
+/* the device, k, v, cache, page_tokens, table, length, first, k_values, v_values, stream */
+static PyObject* call_kv8_store(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *f, *stream;
+    int64_t ldk, ldv, ldk_values = 0, ldv_values = 0;
+    int here, page, st;
+    tensor k, v, cache, k_values = {0}, v_values = {0};
+    requests r;
+    if (!count(n, 12) || !as_ptr(a[0], &f) || !as_int(a[1], &here) || !as_int(a[5], &page) || !look(a[2], "k", &k) || !look(a[3], "v", &v) ||
+        (a[9] != Py_None && !look(a[9], "k_values", &k_values)) || (a[10] != Py_None && !look(a[10], "v_values", &v_values)))
+        return NULL;
+    if (k.ndim != 3 || k.kind != F16 || (v.kind != F16 && v.kind != F32) || (a[9] != Py_None && k_values.kind != F16) || (a[10] != Py_None && v_values.kind != F16)) {
+        refuse("k must be fp16 [N][kv_heads][D], v fp16 or fp32, k_values and v_values fp16");
+        return NULL;
+    }
+    const int64_t N = k.size[0], kv_heads = k.size[1], D = k.size[2];
+    if (!heads(&k, N, kv_heads, D, "k", here, &ldk) || !heads(&v, N, kv_heads, D, "v", here, &ldv) || !cache8_of(a[4], kv_heads, D, page, here, &cache) ||
+        (a[9] != Py_None && !heads(&k_values, N, kv_heads, D, "k_values", here, &ldk_values)) ||
+        (a[10] != Py_None && !heads(&v_values, N, kv_heads, D, "v_values", here, &ldv_values)) || !requests_of(a[8], a[6], a[7], N, here, &r) ||
+        !stream_of(a[11], a[2], here, &stream))
+        return NULL;
+    if (kv_heads > INT32_MAX || D > INT32_MAX) { refuse("heads and their size must fit 32 bits"); return NULL; }
+    Py_BEGIN_ALLOW_THREADS
+    st = ((store8_fn)f)(k.p, ldk, v.p, ldv, v.kind == F32, N, (int)kv_heads, (int)D, r.B, r.first, r.table.p, r.stride, r.table.size[1], r.length, cache.p, cache.size[0], page,
+                        k_values.p, ldk_values, v_values.p, ldv_values, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
+typedef int (*attn8_fn)(const void*, int64_t, int64_t, int, int, int, int64_t, const void*, const void*, int64_t, int, const void*, int64_t, int64_t, const void*, float, float,
+                        int64_t, int64_t, float, void*, int64_t, void*, int64_t, void*);
+/* the device, q, cache, page_tokens, kv_heads, table, length, y, scale, first, cap, window, sinks, thr, mask, stream */
+static PyObject* call_attn_kv8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *f, *stream;
+    int64_t ldq, ldy, mask_stride = 0, window, sinks;
+    int here, page, kv_heads, st;
+    float scale, cap, thr;
+    tensor q, cache, y, mask = {0};
+    requests r;
+    if (!count(n, 17) || !as_ptr(a[0], &f) || !as_int(a[1], &here) || !as_int(a[4], &page) || !as_int(a[5], &kv_heads) || !as_float(a[9], &scale) ||
+        !as_float(a[11], &cap) || !as_i64(a[12], &window) || !as_i64(a[13], &sinks) || !as_float(a[14], &thr) || !look(a[2], "q", &q) || !look(a[8], "y", &y))
+        return NULL;
+    if (q.ndim != 3 || q.kind != F16 || y.kind != F16) {
+        refuse("q must be fp16 [N][q_heads][D] and y fp16");
+        return NULL;
+    }
+    const int64_t N = q.size[0], q_heads = q.size[1], D = q.size[2];
+    if (!heads(&q, N, q_heads, D, "q", here, &ldq) || !rows(&y, N, q_heads * D, "y", here, &ldy) || !cache8_of(a[3], kv_heads, D, page, here, &cache) ||
+        !requests_of(a[10], a[6], a[7], N, here, &r))
+        return NULL;
+    if (a[15] != Py_None) {
+        if (!look(a[15], "mask", &mask)) return NULL;
+        if (mask.ndim != 2 || (mask.kind != I32 && mask.kind != U32)) {
+            refuse("mask must be 32-bit integers, int32 or uint32 [N][words]");
+            return NULL;
+        }
+        if (!rows(&mask, N, mask.size[1], "mask", here, &mask_stride)) return NULL;
+        if (mask.size[1] < q_heads * D / 32) {
+            refuse("mask must hold a bit for each column of y");
+            return NULL;
+        }
+    }
+    if (!stream_of(a[16], a[2], here, &stream)) return NULL;
+    if (q_heads > INT32_MAX || D > INT32_MAX) { refuse("heads and their size must fit 32 bits"); return NULL; }
+    Py_BEGIN_ALLOW_THREADS
+    st = ((attn8_fn)f)(q.p, ldq, N, (int)q_heads, kv_heads, (int)D, r.B, r.first, cache.p, cache.size[0], page, r.table.p, r.stride, r.table.size[1], r.length, scale, cap, window,
+                       sinks, thr, y.p, ldy, mask.p, mask_stride, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
+/* [pages][bytes] or [layers][pages][bytes], layers apart as they may be. */
+static int pages_of(PyObject* o, int here, tensor* t, int* layers, int64_t* stride) {
+    if (!look(o, "cache", t)) return 0;
+    if (t->ndim == 2) {
+        t->size[2] = t->size[1], t->step[2] = t->step[1], t->size[1] = t->size[0], t->step[1] = t->step[0];
+        t->size[0] = 1, t->step[0] = t->size[1] * t->size[2], t->ndim = 3;
+    }
+    if (t->ndim != 3 || t->kind != U8 || t->device != here || (t->size[2] > 1 && t->step[2] != 1) || (t->size[1] > 1 && t->step[1] != t->size[2]) || t->size[0] > INT32_MAX)
+        return refuse("cache must be CUDA uint8 [pages][bytes] or [layers][pages][bytes] on the current device, contiguous within a layer");
+    *layers = (int)t->size[0], *stride = t->step[0];
+    return 1;
+}
+
+typedef struct { void *ref, *a, *b, *c, *number; tensor table; int64_t pages, stride, n; } page_lists;
+/* ref int32 [pages], table int32 [rows][entries], three int32 [n], an int32 [1] or None */
+static int page_lists_of(PyObject* ref, PyObject* table, PyObject* a, PyObject* b, PyObject* c, const char* na, const char* nb, const char* nc, PyObject* number, const char* nn,
+                         int here, page_lists* l) {
+    l->a = l->b = l->c = NULL, l->n = 0;
+    if (ref == Py_None || (a != NULL && (a == Py_None || b == Py_None || c == Py_None))) return refuse("ref and the lists are required");
+    if (!look(table, "table", &l->table)) return 0;
+    if (l->table.kind != I32 || l->table.ndim != 2) return refuse("table must be int32 [rows][pages of a request]");
+    return rows(&l->table, l->table.size[0], l->table.size[1], "table", here, &l->stride) && vector(ref, I32, "int32", -1, &l->pages, "ref", here, &l->ref) &&
+           (a == NULL || (vector(a, I32, "int32", -1, &l->n, na, here, &l->a) && vector(b, I32, "int32", l->n, NULL, nb, here, &l->b) &&
+                          vector(c, I32, "int32", l->n, NULL, nc, here, &l->c))) &&
+           vector(number, I32, "int32", 1, NULL, nn, here, &l->number);
+}
+
+typedef int (*take_fn)(void*, int64_t, void*, int64_t, int64_t, int64_t, const void*, const void*, const void*, int64_t, void*, void*);
+/* the device, ref, table, row, start, stop, short, stream */
+static PyObject* call_kv_pages_take(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *f, *stream;
+    int here, st;
+    page_lists l;
+    if (!count(n, 9) || !as_ptr(a[0], &f) || !as_int(a[1], &here) || !page_lists_of(a[2], a[3], a[4], a[5], a[6], "row", "start", "stop", a[7], "short", here, &l) ||
+        !stream_of(a[8], a[2], here, &stream))
+        return NULL;
+    Py_BEGIN_ALLOW_THREADS
+    st = ((take_fn)f)(l.ref, l.pages, l.table.p, l.table.size[0], l.stride, l.table.size[1], l.a, l.b, l.c, l.n, l.number, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
+typedef int (*free_fn)(void*, int64_t, void*, int64_t, int64_t, int64_t, const void*, const void*, const void*, int64_t, void*);
+/* the device, ref, table, row, start, stop, stream */
+static PyObject* call_kv_pages_free(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *f, *stream;
+    int here, st;
+    page_lists l;
+    if (!count(n, 8) || !as_ptr(a[0], &f) || !as_int(a[1], &here) || !page_lists_of(a[2], a[3], a[4], a[5], a[6], "row", "start", "stop", Py_None, "", here, &l) ||
+        !stream_of(a[7], a[2], here, &stream))
+        return NULL;
+    Py_BEGIN_ALLOW_THREADS
+    st = ((free_fn)f)(l.ref, l.pages, l.table.p, l.table.size[0], l.stride, l.table.size[1], l.a, l.b, l.c, l.n, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
+/* ref has a count for each of the cache's pages */
+static int same_pages(const page_lists* l, const tensor* cache) { return l->pages == cache->size[1] || refuse("ref must have a count for each page of the cache"); }
+
+typedef int (*fork_fn)(void*, int, int64_t, int64_t, void*, int64_t, void*, int64_t, int64_t, int64_t, int, const void*, const void*, const void*, int64_t, void*, void*);
+/* the device, cache, ref, table, page_tokens, parent, child, length, short, stream */
+static PyObject* call_kv_pages_fork(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *f, *stream;
+    int here, st, layers, page;
+    int64_t layer_stride;
+    tensor cache;
+    page_lists l;
+    if (!count(n, 11) || !as_ptr(a[0], &f) || !as_int(a[1], &here) || !as_int(a[5], &page) || !pages_of(a[2], here, &cache, &layers, &layer_stride) ||
+        !page_lists_of(a[3], a[4], a[6], a[7], a[8], "parent", "child", "length", a[9], "short", here, &l) || !same_pages(&l, &cache) || !stream_of(a[10], a[2], here, &stream))
+        return NULL;
+    Py_BEGIN_ALLOW_THREADS
+    st = ((fork_fn)f)(cache.p, layers, layer_stride, cache.size[2], l.ref, l.pages, l.table.p, l.table.size[0], l.stride, l.table.size[1], page, l.a, l.b, l.c, l.n, l.number, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
+typedef int (*copy_fn)(void*, int, int64_t, int64_t, int64_t, const void*, const void*, int64_t, void*);
+/* the device, cache, src, dst, stream */
+static PyObject* call_kv_pages_copy(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *f, *stream, *src, *dst;
+    int here, st, layers;
+    int64_t layer_stride, pairs = 0;
+    tensor cache;
+    if (!count(n, 6) || !as_ptr(a[0], &f) || !as_int(a[1], &here) || !pages_of(a[2], here, &cache, &layers, &layer_stride)) return NULL;
+    if (a[3] == Py_None || a[4] == Py_None) { refuse("src and dst are required"); return NULL; }
+    if (!vector(a[3], I32, "int32", -1, &pairs, "src", here, &src) || !vector(a[4], I32, "int32", pairs, NULL, "dst", here, &dst) || !stream_of(a[5], a[2], here, &stream)) return NULL;
+    Py_BEGIN_ALLOW_THREADS
+    st = ((copy_fn)f)(cache.p, layers, layer_stride, cache.size[2], cache.size[1], src, dst, pairs, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
+typedef int (*compact_fn)(void*, int, int64_t, int64_t, void*, int64_t, void*, int64_t, int64_t, int64_t, void*, void*);
+/* the device, cache, ref, table, live, stream */
+static PyObject* call_kv_pages_compact(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+    void *f, *stream;
+    int here, st, layers;
+    int64_t layer_stride;
+    tensor cache;
+    page_lists l;
+    if (!count(n, 7) || !as_ptr(a[0], &f) || !as_int(a[1], &here) || !pages_of(a[2], here, &cache, &layers, &layer_stride) ||
+        !page_lists_of(a[3], a[4], NULL, NULL, NULL, "", "", "", a[5], "live", here, &l) || !same_pages(&l, &cache) || !stream_of(a[6], a[2], here, &stream))
+        return NULL;
+    Py_BEGIN_ALLOW_THREADS
+    st = ((compact_fn)f)(cache.p, layers, layer_stride, cache.size[2], l.ref, l.pages, l.table.p, l.table.size[0], l.stride, l.table.size[1], l.number, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
 static PyMethodDef methods[] = {
     {"spmspv", (PyCFunction)(void (*)(void))call_spmspv, METH_FASTCALL, "spdp_spmspv"},
     {"spmspv_batch", (PyCFunction)(void (*)(void))call_spmspv_batch, METH_FASTCALL, "spdp_spmspv_batch"},
@@ -494,6 +695,13 @@ static PyMethodDef methods[] = {
     {"qk_norm_rope", (PyCFunction)(void (*)(void))call_qk_norm_rope, METH_FASTCALL, "spdp_qk_norm_rope"},
     {"kv4_store", (PyCFunction)(void (*)(void))call_kv4_store, METH_FASTCALL, "spdp_kv4_store"},
     {"attn_kv4", (PyCFunction)(void (*)(void))call_attn_kv4, METH_FASTCALL, "spdp_attn_kv4"},
+    {"kv8_store", (PyCFunction)(void (*)(void))call_kv8_store, METH_FASTCALL, "spdp_kv8_store"},
+    {"attn_kv8", (PyCFunction)(void (*)(void))call_attn_kv8, METH_FASTCALL, "spdp_attn_kv8"},
+    {"kv_pages_take", (PyCFunction)(void (*)(void))call_kv_pages_take, METH_FASTCALL, "spdp_kv_pages_take"},
+    {"kv_pages_free", (PyCFunction)(void (*)(void))call_kv_pages_free, METH_FASTCALL, "spdp_kv_pages_free"},
+    {"kv_pages_fork", (PyCFunction)(void (*)(void))call_kv_pages_fork, METH_FASTCALL, "spdp_kv_pages_fork"},
+    {"kv_pages_copy", (PyCFunction)(void (*)(void))call_kv_pages_copy, METH_FASTCALL, "spdp_kv_pages_copy"},
+    {"kv_pages_compact", (PyCFunction)(void (*)(void))call_kv_pages_compact, METH_FASTCALL, "spdp_kv_pages_compact"},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", "Per-token entry points of libspdp.", -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__pycall(void) { return PyModule_Create(&module); }

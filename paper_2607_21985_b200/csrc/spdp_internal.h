@@ -216,6 +216,52 @@ struct Kv4AttnCall {
 };
 spdp_status launch_attn_kv4(const Kv4AttnCall& call, cudaStream_t s);
 
+// kv8.cu, kv8_prompt.cu
+struct Kv8StoreCall {
+    const __half* k;
+    const void* v;
+    const int32_t* first;       // null: one token to a request
+    const int32_t* table;
+    const int32_t* length;
+    unsigned char* cache;
+    __half* k_values;           // may be null
+    __half* v_values;           // may be null
+    int64_t N, B, ldk, ldv, ldk_values, ldv_values, pages, table_stride, table_pages;
+    int kv_heads, head_dim, page_tokens, vdt;
+};
+spdp_status launch_kv8_store(const Kv8StoreCall& call, cudaStream_t s);
+struct Kv8AttnCall {
+    const __half* q;
+    const unsigned char* cache;
+    const int32_t* first;       // null: one token to a request
+    const int32_t* table;
+    const int32_t* length;
+    __half* y;
+    uint32_t* mask;             // may be null
+    int64_t N, B, ldq, ldy, table_stride, table_pages, mask_stride, pages, window, sinks;
+    int q_heads, kv_heads, head_dim, page_tokens;
+    float scale, cap, thr;
+};
+spdp_status launch_attn_kv8(const Kv8AttnCall& call, cudaStream_t s);
+
+// kv_pages.cu
+struct KvPagesCall {
+    unsigned char* cache;
+    int32_t* ref;
+    int32_t* table;
+    const int32_t* row;         // of a table, or of the parents; pages to copy
+    const int32_t* from;        // entries; or rows of the children
+    const int32_t* to;          // entries; or tokens of the parents, or pages to copy to
+    int32_t* short_out;         // may be null; or pages in use
+    int64_t layer_stride, page_bytes, pages, rows, table_stride, table_pages, n;
+    int layers, page_tokens;
+};
+spdp_status launch_kv_pages_take(const KvPagesCall& call, cudaStream_t s);
+spdp_status launch_kv_pages_free(const KvPagesCall& call, cudaStream_t s);
+spdp_status launch_kv_pages_copy(const KvPagesCall& call, cudaStream_t s);
+spdp_status launch_kv_pages_fork(const KvPagesCall& call, cudaStream_t s);
+spdp_status launch_kv_pages_compact(const KvPagesCall& call, cudaStream_t s);
+
 // spmm.cu
 spdp_status configure_spmm_kernel();            // per-device kernel attributes; idempotent
 spdp_status launch_spmm(const spdp_matrix* h, const __half* X, int64_t N, int64_t ldx, void* Y, int64_t ldy, int ydt,

@@ -32,6 +32,8 @@ EXPORTS = (
     "spdp_active_columns", "spdp_last_device_status", "spdp_set_num_ctas", "spdp_last_cuda_error",
     "spdp_status_string", "spdp_probe_stream_read", "spdp_probe_gather", "spdp_spmm", "spdp_pack_tiled_cbc_q4", "spdp_export_q4", "spdp_row_shard", "spdp_swiglu_dp",
     "spdp_lora", "spdp_qk_norm_rope", "spdp_kv4_page_bytes", "spdp_kv4_store", "spdp_attn_kv4",
+    "spdp_kv8_page_bytes", "spdp_kv8_store", "spdp_attn_kv8",
+    "spdp_kv_pages_take", "spdp_kv_pages_free", "spdp_kv_pages_fork", "spdp_kv_pages_copy", "spdp_kv_pages_compact",
 )
 
 
@@ -85,6 +87,14 @@ def lib():
         L.spdp_kv4_page_bytes.argtypes = [ci, ci, ci, ctypes.POINTER(i64)]
         L.spdp_kv4_store.argtypes = [vp, i64, vp, i64, ci, i64, ci, ci, vp, vp, i64, ci, vp, i64, vp, i64, vp]
         L.spdp_attn_kv4.argtypes = [vp, i64, i64, ci, ci, ci, vp, i64, ci, vp, i64, i64, vp, cf, cf, i64, cf, vp, i64, vp, i64, vp]
+        L.spdp_kv8_page_bytes.argtypes = [ci, ci, ci, ctypes.POINTER(i64)]
+        L.spdp_kv8_store.argtypes = [vp, i64, vp, i64, ci, i64, ci, ci, i64, vp, vp, i64, i64, vp, vp, i64, ci, vp, i64, vp, i64, vp]
+        L.spdp_attn_kv8.argtypes = [vp, i64, i64, ci, ci, ci, i64, vp, vp, i64, ci, vp, i64, i64, vp, cf, cf, i64, i64, cf, vp, i64, vp, i64, vp]
+        L.spdp_kv_pages_take.argtypes = [vp, i64, vp, i64, i64, i64, vp, vp, vp, i64, vp, vp]
+        L.spdp_kv_pages_free.argtypes = [vp, i64, vp, i64, i64, i64, vp, vp, vp, i64, vp]
+        L.spdp_kv_pages_fork.argtypes = [vp, ci, i64, i64, vp, i64, vp, i64, i64, i64, ci, vp, vp, vp, i64, vp, vp]
+        L.spdp_kv_pages_copy.argtypes = [vp, ci, i64, i64, i64, vp, vp, i64, vp]
+        L.spdp_kv_pages_compact.argtypes = [vp, ci, i64, i64, vp, i64, vp, i64, i64, i64, vp, vp]
         L.spdp_row_shard.argtypes = [i64, ci, ci, ctypes.POINTER(i64), ctypes.POINTER(i64)]
         L.spdp_probe_stream_read.argtypes = [vp, vp]
         L.spdp_probe_gather.argtypes = [vp, vp, ci, cf, vp, vp]
@@ -99,7 +109,8 @@ def lib():
         except ImportError as e:
             raise RuntimeError("the _pycall module is missing: build it with `python -m paper_2607_21985_b200.build`") from e
         # the per-token calls: same entry points, arguments converted in C (csrc/pycall.c)
-        for name in ("spmspv", "spmspv_batch", "spmm", "swiglu_dp", "lora", "qk_norm_rope", "kv4_store", "attn_kv4"):
+        for name in ("spmspv", "spmspv_batch", "spmm", "swiglu_dp", "lora", "qk_norm_rope", "kv4_store", "attn_kv4", "kv8_store",
+                     "attn_kv8", "kv_pages_take", "kv_pages_free", "kv_pages_fork", "kv_pages_copy", "kv_pages_compact"):
             address = ctypes.cast(getattr(L, "spdp_" + name), ctypes.c_void_p).value
             setattr(L, "call_" + name, functools.partial(getattr(_pycall, name), address))
         _lib = L
@@ -378,6 +389,71 @@ def spdp_attn_kv4(q, cache, page_tokens: int, kv_heads: int, table, length, y, s
     st = (_lib or lib()).call_attn_kv4(_here(), q, cache, page_tokens, kv_heads, table, length, y, scale, cap, window, thr, mask, stream)
     if st:
         _check(st, "spdp_attn_kv4")
+
+
+def spdp_kv8_page_bytes(kv_heads: int, head_dim: int, page_tokens: int) -> int:
+    """Bytes of one page of an 8-bit key/value cache; the cache is a uint8 CUDA tensor [pages][that]."""
+    out = ctypes.c_int64(0)
+    _check(lib().spdp_kv8_page_bytes(kv_heads, head_dim, page_tokens, ctypes.byref(out)), "spdp_kv8_page_bytes")
+    return out.value
+
+
+def spdp_kv8_store(k, v, cache, page_tokens: int, table, length, first=None, k_values=None, v_values=None, stream=None) -> None:
+    """Keys k (fp16 CUDA [N][kv_heads][D]) and values v (fp16 or fp32) of new tokens into an 8-bit cache: request b's are the tokens
+    first[b] .. first[b + 1] - 1 (int32 [B + 1]; None: one token to each request) and become the last of its length[b] (int32 [B]) tokens in
+    the pages table[b] (int32 [B][pages of a request]); k_values and v_values (fp16, optional) get what the codes stand for."""
+    st = (_lib or lib()).call_kv8_store(_here(), k, v, cache, page_tokens, table, length, first, k_values, v_values, stream)
+    if st:
+        _check(st, "spdp_kv8_store")
+
+
+def spdp_attn_kv8(q, cache, page_tokens: int, kv_heads: int, table, length, y, scale: float, first=None, cap: float = 0.0, window: int = 0, sinks: int = 0,
+                  thr: float = 0.0, mask=None, stream=None) -> None:
+    """Attention of new tokens q (fp16 CUDA [N][q_heads][D]; first, table and length as for spdp_kv8_store, which has stored them) over the keys
+    up to each token in an 8-bit cache, or the last `window` of them and the request's first `sinks`; y fp16 [N][q_heads * D] and, where
+    mask (int32/uint32 [N][>= q_heads * D / 32]) is given, the bits of the columns with |y| above thr."""
+    st = (_lib or lib()).call_attn_kv8(_here(), q, cache, page_tokens, kv_heads, table, length, y, scale, first, cap, window, sinks, thr, mask, stream)
+    if st:
+        _check(st, "spdp_attn_kv8")
+
+
+def spdp_kv_pages_take(ref, table, row, start, stop, short=None, stream=None) -> None:
+    """Entries start[i] .. stop[i] - 1 of table[row[i]] (int32 CUDA [n] each) get free pages, the lowest first; ref int32 [pages] counts the entries
+    that name a page (0: free), table int32 [rows][pages of a request].  short (int32 [1], optional) gets the number of entries that got none (-1)."""
+    st = (_lib or lib()).call_kv_pages_take(_here(), ref, table, row, start, stop, short, stream)
+    if st:
+        _check(st, "spdp_kv_pages_take")
+
+
+def spdp_kv_pages_free(ref, table, row, start, stop, stream=None) -> None:
+    """Entries start[i] .. stop[i] - 1 of table[row[i]] give their pages back and become -1."""
+    st = (_lib or lib()).call_kv_pages_free(_here(), ref, table, row, start, stop, stream)
+    if st:
+        _check(st, "spdp_kv_pages_free")
+
+
+def spdp_kv_pages_fork(cache, ref, table, page_tokens: int, parent, child, length, short=None, stream=None) -> None:
+    """table[child[i]] becomes a request with the first length[i] tokens of table[parent[i]] (int32 CUDA [n] each): full pages are shared, a last, partly
+    filled one is copied to a free page in all layers of cache (uint8 [pages][bytes] or [layers][pages][bytes]).  short (int32 [1],
+    optional) gets the number of children for whose copy there was no page."""
+    st = (_lib or lib()).call_kv_pages_fork(_here(), cache, ref, table, page_tokens, parent, child, length, short, stream)
+    if st:
+        _check(st, "spdp_kv_pages_fork")
+
+
+def spdp_kv_pages_copy(cache, src, dst, stream=None) -> None:
+    """Pages src[i] of cache (as for spdp_kv_pages_fork) to pages dst[i] (int32 CUDA [n]) in all layers."""
+    st = (_lib or lib()).call_kv_pages_copy(_here(), cache, src, dst, stream)
+    if st:
+        _check(st, "spdp_kv_pages_copy")
+
+
+def spdp_kv_pages_compact(cache, ref, table, live=None, stream=None) -> None:
+    """Brings the pages in use to the cache's start, in all layers, with their counts in ref and their entries in table; live (int32 [1],
+    optional) gets their number."""
+    st = (_lib or lib()).call_kv_pages_compact(_here(), cache, ref, table, live, stream)
+    if st:
+        _check(st, "spdp_kv_pages_compact")
 
 
 def spdp_row_shard(M: int, world: int, rank: int):
