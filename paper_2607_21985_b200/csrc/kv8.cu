@@ -302,6 +302,7 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kUnitCells = 4;
 constexpr int kMostRequests = 4096;
+constexpr int kFewRows = 64;            // of a request and key head, up to which this form is taken
 constexpr float kHeadroom = 12.0f;      // weights are below 2^(kHeadroom + kSlack)
 constexpr float kSlack = 2.5f;
 
@@ -799,11 +800,16 @@ spdp_status launch_attn_kv8(const Kv8AttnCall& call, cudaStream_t s) {
     p.cap_near = 0.25f * p.cap;
     p.thr = call.thr;
     p.wide_q = rows_aligned16(p.q, p.ldq, 2), p.wide_y = rows_alignment(p.y, p.ldy, 2) >= 8;
-    switch (call.head_dim) {
-        case 64: return launch_dim<1>(p, device, sms, s);
-        case 128: return launch_dim<2>(p, device, sms, s);
-        default: return launch_dim<4>(p, device, sms, s);
+    // requests of more rows than kFewRows are the other kernel's; where no request can have as few, or as many, one of the two is not launched
+    const int64_t rows = static_cast<int64_t>(p.N) * p.group;
+    const bool prompts = p.first != nullptr && rows > kFewRows;
+    if (prompts) p.most_rows = kFewRows;
+    if (!prompts || p.B > 1) {
+        const spdp_status few = call.head_dim == 64 ? launch_dim<1>(p, device, sms, s) : call.head_dim == 128 ? launch_dim<2>(p, device, sms, s) : launch_dim<4>(p, device, sms, s);
+        if (few != SPDP_OK || !prompts) return few;
     }
+    p.low_rows = p.B > 1 ? kFewRows + 1 : 0, p.most_rows = INT32_MAX;
+    return launch_kv8_prompt(p, call.head_dim, device, sms, s);
 }
 
 }  // namespace spdp

@@ -227,4 +227,8 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParam
 }
 
 }  // namespace kv8
+
+// kv8_prompt.cu: the requests with a.low_rows rows and more.
+spdp_status launch_kv8_prompt(const kv8::AttnParams& a, int head_dim, int device, int sms, cudaStream_t s);
+
 }  // namespace spdp

@@ -1,0 +1,763 @@
+// Attention over the 8-bit cache for requests with many new tokens: prompts and pieces of them, on the 5th-generation tensor cores.
+//
+// The rows of a key head, token by token its query heads, are cut into blocks of kTiles tiles of 128 rows; a block's keys, 128 to
+// a unit, are those that any of its tokens sees.  The units of all blocks and heads stand in one line that is cut into equal
+// runs, one to a CTA (kv8.cuh); a first small kernel writes down where each block begins.
+//
+// Inside a CTA: a warpgroup turns codes into fp16 operand tiles in shared memory, a thread issues the products, and a warpgroup to each
+// tile has the softmax, a row to a thread.  Scores are Q K^T into tensor memory; weights go back there, over the scores, as the
+// first operand of the product with the values, whose sums stay in tensor memory through the block.  While one tile's scores become
+// weights the tensor cores work on the other's.  Codes times their scale are fp16 numbers, so both operands of the first product and
+// the values of the second are exact; the weights are rounded to fp16 (2^-11, the one rounding besides the result's).
+//
+// The order of a unit's keys is what suits the operand tiles, and the same in both: row n of the keys' tile is token 2 (n % 64 / 16) + n % 2 +
+// 8 (n % 4 / 2) of cell 4 (n / 64) + 2 (n / 8 % 2) + n / 4 % 2.  So the 8 keys of a 16-byte piece of a dimension's row of the values' tile are
+// words of two cells that one lane has, and the lanes' pieces of either tile fall into different banks.
+#include <mutex>
+
+#include "kv8.cuh"
+
+namespace spdp {
+namespace {
+
+using namespace kv8;
+
+constexpr int kUnitCells = 8, kUnitKeys = kUnitCells * kCell;
+constexpr int kTileRows = 128;
+constexpr int kThreads = 512;           // warps 0-3 and 4-7: softmax; 8-11: codes to operands; 12: products; 13-15: tokens without keys
+constexpr int kRowBytes = 128;          // of an operand tile: 64 fp16 numbers, in the 128-byte swizzle
+constexpr int kAtomBytes = 8 * kRowBytes;
+constexpr int kFlags = 8;               // units whose cells' existence is kept
+constexpr float kHeadroom = 12.0f, kSlack = 2.5f;       // weights are below 2^(kHeadroom + kSlack)
+// Registers of a thread by its warpgroup; with the 128 of the launch the four come to the same sum.
+constexpr int kSoftmaxRegs = 176, kDecodeRegs = 112, kOtherRegs = 48;
+static_assert(2 * kSoftmaxRegs + kDecodeRegs + kOtherRegs == 4 * 128, "the launch's registers");
+
+template <int kDim>
+struct Form {
+    static constexpr int kTiles = kDim == 256 ? 1 : 2;
+    static constexpr int kStages = kDim == 256 ? 1 : 2;                 // of the keys' and of the values' tiles
+    static constexpr int kRows = kTiles * kTileRows;
+    static constexpr int kKeyBytes = kUnitKeys * kDim * 2, kQueryBytes = kTileRows * kDim * 2;
+    static constexpr int kSums = 256;                                   // first tensor-memory column of the sums; scores of tile t at 128 t
+    static constexpr int kOperands = kTiles * kQueryBytes + 2 * kStages * kKeyBytes;
+};
+
+struct Block {                          // of rows
+    int start;                          // in the line of one head
+    int request, row0, pad;
+};
+struct PromptParams {
+    AttnParams a;
+    Block* blocks;
+    int* totals;                        // blocks; length of the line of one head
+    int most_list;                      // blocks that there can be
+    bool negative;                      // the scale; a.scale is its size
+    bool wide16;                        // rows of y on 16-byte boundaries
+};
+
+// The cells with keys that any token of a block of rows sees.
+struct Span {
+    Request r;                          // with sink_cells, low_cell and cells those of the block
+    int rows, earliest, latest;         // positions of the block's tokens
+};
+template <int kRows>
+__device__ __forceinline__ Span span_of(const AttnParams& p, const Request& rq, int row0) {
+    Span s;
+    s.r = rq;
+    s.rows = min(kRows, rq.n * p.group - row0);
+    const int before = rq.length - rq.n;
+    s.earliest = before + row0 / p.group, s.latest = before + (row0 + s.rows - 1) / p.group;
+    const int end = max(s.latest, 0) / kCell + 1;
+    s.r.low_cell = s.r.sink_cells = 0;
+    if (p.window > 0) {
+        s.r.low_cell = max(max(s.earliest, 0) + 1 - p.window, 0) / kCell;
+        s.r.sink_cells = min((p.sinks + kCell - 1) / kCell, s.r.low_cell);
+    }
+    s.r.cells = s.r.sink_cells + end - s.r.low_cell;            // one at least
+    return s;
+}
+
+// ---- where each block begins
+
+constexpr int kListThreads = 1024;
+
+__device__ __forceinline__ int scan_add(int mine, int* sums, int* total) {       // the sum of the threads before this one; all threads, ends with a barrier
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    int up_to = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int v = __shfl_up_sync(0xFFFFFFFFu, up_to, d);
+        if (lane >= d) up_to += v;
+    }
+    if (lane == 31) sums[w] = up_to;
+    __syncthreads();
+    if (w == 0) {
+        const int all = sums[lane];
+        int s = all;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int v = __shfl_up_sync(0xFFFFFFFFu, s, d);
+            if (lane >= d) s += v;
+        }
+        __syncwarp();
+        sums[lane] = s - all;
+        if (lane == 31) sums[32] = s;
+    }
+    __syncthreads();
+    const int r = sums[w] + up_to - mine;
+    *total = sums[32];
+    __syncthreads();
+    return r;
+}
+
+template <int kRows>
+__global__ void __launch_bounds__(kListThreads) kv8_blocks_kernel(const PromptParams p) {
+    __shared__ int first[4096 + 1], sums[33];
+    dev::programmatic_start();
+    int total = 0;
+    for (int base = 0; base < p.a.B; base += kListThreads) {    // the first block of each request
+        const int b = base + threadIdx.x;
+        int mine = 0, all;
+        if (b < p.a.B) {
+            const Request rq = request_of(p.a, b);
+            mine = rq.cells > 0 ? (rq.n * p.a.group + kRows - 1) / kRows : 0;
+        }
+        const int at = total + scan_add(mine, sums, &all);
+        if (b < p.a.B) first[b] = at;
+        total += all;
+    }
+    __syncthreads();
+    total = min(total, p.most_list);
+    int length = 0;
+    for (int base = 0; base < total; base += kListThreads) {
+        const int i = base + threadIdx.x;
+        int mine = 0, all, b = 0, row0 = 0;
+        if (i < total) {
+            b = request_at(first, p.a.B, i);
+            row0 = (i - first[b]) * kRows;
+            mine = triple_length((span_of<kRows>(p.a, request_of(p.a, b), row0).r.cells + kUnitCells - 1) / kUnitCells);
+        }
+        const int at = length + scan_add(mine, sums, &all);
+        if (i < total) p.blocks[i] = Block{at, b, row0, 0};
+        length += all;
+    }
+    if (threadIdx.x == 0) p.totals[0] = total, p.totals[1] = length;
+}
+
+// ---- a CTA's pieces of blocks, in order: every role goes through the same list
+
+struct Piece {
+    int block, h, request, row0, off, count, units, slot, last_cta;
+    bool whole;
+};
+struct Pieces {
+    int n, length, total, ctas, u, stop, block, h;
+    int done;
+    __device__ __forceinline__ explicit Pieces(const PromptParams& p) {
+        n = p.totals[0], length = p.totals[1];
+        total = length * p.a.heads, ctas = min(static_cast<int>(gridDim.x), total);
+        u = stop = done = block = h = 0;
+        if (static_cast<int>(blockIdx.x) >= ctas) return;
+        u = run_start(total, ctas, blockIdx.x), stop = run_start(total, ctas, blockIdx.x + 1);
+        h = u / length;
+        const int v = u % length;
+        for (int lo = 0, hi = n - 1; lo <= hi;) {
+            const int mid = (lo + hi) >> 1;
+            if (p.blocks[mid].start <= v) block = mid, lo = mid + 1;
+            else hi = mid - 1;
+        }
+    }
+    __device__ __forceinline__ bool next(const PromptParams& p, Piece& s) {
+        while (u < stop) {
+            const Block b = p.blocks[block];
+            const int end = block + 1 < n ? p.blocks[block + 1].start : length, len = end - b.start, start = h * length + b.start;
+            const int off = max(0, u - start - kStart), count = max(0, min(len, stop - start) - kStart) - off;
+            s.block = block, s.h = h;
+            u = min(start + len, stop);
+            if (++block == n) block = 0, ++h;
+            if (count <= 0) continue;                           // the run ends before the block's first unit
+            s.request = b.request, s.row0 = b.row0, s.off = off, s.count = count, s.units = len - kStart;
+            s.whole = count == s.units;
+            s.slot = 2 * blockIdx.x + (done > 0 ? 1 : 0);       // what is not whole is the first piece of a run or the last
+            s.last_cta = static_cast<int>(((static_cast<int64_t>(start) + len) * ctas - 1) / total);
+            ++done;
+            return true;
+        }
+        return false;
+    }
+};
+
+// ---- tensor cores, barriers
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+// Shared-memory operand descriptor of tcgen05.mma, K-major rows of 128 bytes in the 128-byte swizzle: start address (in 16 bytes) in the lower
+// half; in the upper the distance of 8 rows, the descriptor's version, the layout.
+constexpr uint32_t kDescHigh = (kAtomBytes >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr) { return ((addr & 0x3FFFFu) >> 4) | (1u << 16); }
+// fp16 x fp16 -> fp32, both K-major, 128 rows, n columns
+__device__ __forceinline__ constexpr uint32_t instr_desc(int n) { return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(kTileRows >> 4) << 24); }
+__device__ __forceinline__ void mma_smem(uint32_t d, uint32_t a_low, uint32_t b_low, uint32_t id, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n"
+                 " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}" ::"r"(d), "r"(a_low), "r"(b_low), "r"(id), "r"(accumulate), "n"(kDescHigh) : "memory");
+}
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint32_t b_low, uint32_t id, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p;\n .reg .b64 b;\n setp.ne.b32 p, %4, 0;\n mov.b64 b, {%2, %5};\n"
+                 " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}" ::"r"(d), "r"(a), "r"(b_low), "r"(id), "r"(accumulate), "n"(kDescHigh) : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+    unsigned e;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(e));
+    return e != 0u;
+}
+__device__ __forceinline__ void barrier_init(uint64_t* bar, uint32_t arrivals) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(arrivals) : "memory");
+}
+__device__ __forceinline__ void arrive(uint64_t* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory"); }
+constexpr int kWaitTries = 1 << 22;     // a wait that runs out (none should) ends its role; what the CTA would have written becomes NaN
+constexpr int kDrainTries = 1 << 18;
+__device__ __forceinline__ bool wait_parity(uint64_t* bar, unsigned parity, int limit = kWaitTries) {
+    const uint32_t a = smem_u32(bar);
+    for (int tries = 0; tries < limit; ++tries) {
+        unsigned done;
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(a), "r"(parity) : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_operands() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+#define SPDP_R8(a, i) "=f"((a)[i]), "=f"((a)[i + 1]), "=f"((a)[i + 2]), "=f"((a)[i + 3]), "=f"((a)[i + 4]), "=f"((a)[i + 5]), "=f"((a)[i + 6]), "=f"((a)[i + 7])
+#define SPDP_W8(a, i) "r"((a)[i]), "r"((a)[i + 1]), "r"((a)[i + 2]), "r"((a)[i + 3]), "r"((a)[i + 4]), "r"((a)[i + 5]), "r"((a)[i + 6]), "r"((a)[i + 7])
+// 32 columns of tensor memory, the thread's lane.
+__device__ __forceinline__ void tmem_load(uint32_t at, float* v) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, "
+                 "%28, %29, %30, %31}, [%32];"
+                 : SPDP_R8(v, 0), SPDP_R8(v, 8), SPDP_R8(v, 16), SPDP_R8(v, 24) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t* v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, "
+                 "%28, %29, %30, %31, %32};" ::"r"(at), SPDP_W8(v, 0), SPDP_W8(v, 8), SPDP_W8(v, 16), SPDP_W8(v, 24) : "memory");
+}
+__device__ __forceinline__ void tmem_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Pairs of 32-bit numbers in one operation.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mov.b64 z, {%6, %7};\n fma.rn.f32x2 x, x, y, z;\n mov.b64 {%0, %1}, x;\n}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+
+struct Barriers {
+    uint64_t q_full[2], s_full[2], p_full[2], o_full[2], k_full[2], k_free[2], v_full[2], v_free[2], drained;
+    uint32_t tmem;
+    alignas(16) int there[kFlags][4];   // of the units' cells, two bits to a decoding warp
+};
+
+// Key of column n of a unit, from the first key of its cell
+__host__ __device__ constexpr int cell_of(int n) { return 4 * (n / 64) + 2 * (n / 8 % 2) + n / 4 % 2; }
+__host__ __device__ constexpr int token_of(int n) { return 2 * (n % 64 / 16) + n % 2 + 8 * (n % 4 / 2); }
+
+// ---- codes to operands
+
+template <int kDim>
+__device__ __forceinline__ void decode_role(const PromptParams& p, Barriers* bars, uint32_t keys, uint32_t values) {
+    using F = Form<kDim>;
+    constexpr int kLoads = kDim / 32;   // 16-byte loads of a side of a cell
+    const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) & 3, g = lane >> 2, c = lane & 3;
+    const AttnParams& a = p.a;
+    const int in_page = (1 << a.cells_shift) - 1;
+    const int64_t page_bytes = (static_cast<int64_t>(a.heads) << a.cells_shift) * cell_bytes(kDim);
+    // places in the tiles: the lane's key g of a cell (the other one, g + 8, two rows on), 16 dimensions from 16 c; dimension g, 8 keys
+    const uint32_t key_row = 16 * (g >> 1) + 8 * (w & 1) + 64 * (w >> 1) + (g & 1);
+    const uint32_t value_at = g * kRowBytes + (((2 * c + (w & 1)) ^ g) << 4) + (w >> 1) * (kDim * kRowBytes);
+    unsigned unit = 0;
+    Pieces list(p);
+    Piece s;
+    while (list.next(p, s)) {
+        const Span span = span_of<F::kRows>(a, request_of(a, s.request), s.row0);
+        const Request& rq = span.r;
+        const int32_t* table = a.table + s.request * a.table_stride;
+        const unsigned char* head = a.cache + (static_cast<int64_t>(s.h) << a.cells_shift) * cell_bytes(kDim) + 16 * lane;
+        auto place = [&](int i, int j) { return (s.off + i) * kUnitCells + 2 * w + j; };        // in the block's line, of cell j of the warp's in unit i
+        auto pages_of = [&](int i) {                            // of the units i .. i + 15
+            const int at = place(i + (lane >> 1), lane & 1);
+            return i + (lane >> 1) < s.count && at < rq.cells ? table[rq.cell_at(at) >> a.cells_shift] : -1;
+        };
+        int pages = pages_of(0), pages_after = pages_of(16);
+        uint4 k[2][kLoads], v[2][kLoads];
+        float2 scale[2], scale_next[2];
+        bool ok[2], ok_next[2];
+        const unsigned char* from[2];
+        auto locate = [&](int i) {
+            if (i > 0 && (i & 15) == 0) pages = pages_after, pages_after = pages_of(i + 16);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const unsigned page = __shfl_sync(0xFFFFFFFFu, pages, (2 * i + j) & 31);
+                ok_next[j] = i < s.count && page < a.pages;
+                from[j] = head + static_cast<int64_t>(ok_next[j] ? page : 0u) * page_bytes + (rq.cell_at(place(i, j)) & in_page) * cell_bytes(kDim);
+            }
+        };
+        auto load_keys = [&]() {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                scale_next[j] = make_float2(0.0f, 0.0f);
+                if (ok_next[j]) scale_next[j] = *reinterpret_cast<const float2*>(from[j] + 2 * kCell * kDim - 16 * lane);
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    k[j][i] = make_uint4(0, 0, 0, 0);
+                    if (ok_next[j]) k[j][i] = *reinterpret_cast<const uint4*>(from[j] + 512 * i);
+                }
+            }
+        };
+        auto load_values = [&]() {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    v[j][i] = make_uint4(0, 0, 0, 0);
+                    if (ok_next[j]) v[j][i] = *reinterpret_cast<const uint4*>(from[j] + kCell * kDim + 512 * i);
+                }
+            }
+        };
+        auto scaled = [](uint32_t codes, __half2 f) {
+            const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&codes), f);
+            return *reinterpret_cast<const uint32_t*>(&r);
+        };
+        auto put = [](uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t t) { asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(t) : "memory"); };
+        locate(0);
+        load_keys();
+        load_values();
+        for (int i = 0; i < s.count; ++i, ++unit) {
+            const unsigned stage = unit % F::kStages, parity = (unit / F::kStages - 1u) & 1u;
+            int key[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) scale[j] = scale_next[j], ok[j] = ok_next[j], key[j] = rq.cell_at(place(i, j)) * kCell;
+            if (unit >= F::kStages && !__all_sync(0xFFFFFFFFu, wait_parity(&bars->k_free[stage], parity))) return;
+            if (lane == 0) bars->there[unit % kFlags][w] = (ok[0] ? 1 : 0) | (ok[1] ? 2 : 0);
+            const uint32_t k_tile = keys + stage * F::kKeyBytes;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const __half2 f = __float2half2_rn(scale[j].x);
+#pragma unroll
+                for (int t = 0; t < kLoads; ++t) {              // 64 dimensions t / 2, key g + 8 (t % 2)
+                    const uint32_t row = key_row + 4 * j + 2 * (t & 1), at = k_tile + (t >> 1) * (kUnitKeys * kRowBytes) + row * kRowBytes;
+                    const uint4& x = k[j][t];
+                    put(at + (((2 * c) ^ (row & 7)) << 4), scaled(low_codes(x.x), f), scaled(high_codes(x.x), f), scaled(low_codes(x.y), f), scaled(high_codes(x.y), f));
+                    put(at + (((2 * c + 1) ^ (row & 7)) << 4), scaled(low_codes(x.z), f), scaled(high_codes(x.z), f), scaled(low_codes(x.w), f), scaled(high_codes(x.w), f));
+                }
+            }
+            fence_operands();
+            __syncwarp();
+            if (lane == 0) arrive(&bars->k_full[stage]);
+            locate(i + 1);
+            load_keys();
+            if (unit >= F::kStages && !__all_sync(0xFFFFFFFFu, wait_parity(&bars->v_free[stage], parity))) return;
+            if (key[0] + 2 * kCell > rq.length || key[1] + kCell > rq.length) {     // behind the last key: whatever the cell holds there
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    uint32_t keep = 0;
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) keep |= key[j] + 2 * c + (m & 1) + 8 * (m >> 1) < rq.length ? 0xFFu << 8 * m : 0u;
+#pragma unroll
+                    for (int t = 0; t < kLoads; ++t) v[j][t].x &= keep, v[j][t].y &= keep, v[j][t].z &= keep, v[j][t].w &= keep;
+                }
+            }
+            const uint32_t v_tile = values + stage * F::kKeyBytes + value_at;
+            const __half2 f0 = __float2half2_rn(scale[0].y), f1 = __float2half2_rn(scale[1].y);
+#pragma unroll
+            for (int t = 0; t < kLoads; ++t) {                  // dimensions 32 t + 8 m + g
+                const uint32_t x[4] = {v[0][t].x, v[0][t].y, v[0][t].z, v[0][t].w}, y[4] = {v[1][t].x, v[1][t].y, v[1][t].z, v[1][t].w};
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+                    put(v_tile + (32 * t + 8 * m) * kRowBytes, scaled(low_codes(x[m]), f0), scaled(high_codes(x[m]), f0), scaled(low_codes(y[m]), f1), scaled(high_codes(y[m]), f1));
+            }
+            fence_operands();
+            __syncwarp();
+            if (lane == 0) arrive(&bars->v_full[stage]);
+            load_values();
+        }
+    }
+}
+
+// ---- products (one thread)
+
+template <int kDim>
+__device__ __forceinline__ void product_role(const PromptParams& p, Barriers* bars, uint32_t queries, uint32_t keys, uint32_t values, uint32_t tmem) {
+    using F = Form<kDim>;
+    const uint32_t q_low = desc_low(queries), k_low = desc_low(keys), v_low = desc_low(values);
+    constexpr uint32_t kIdScores = instr_desc(kUnitKeys), kIdSums = instr_desc(kDim);
+    unsigned piece_of[2] = {0, 0}, unit = 0, weights_of[2] = {0, 0};    // pieces and units so far, of each tile
+    bool ok = true, issued = false;
+    Pieces list(p);
+    Piece s;
+    auto scores = [&](int t, unsigned u) {
+        const uint32_t stage = u % F::kStages;
+#pragma unroll
+        for (int kk = 0; kk < kDim / 16; ++kk)
+            mma_smem(tmem + 128 * t, q_low + ((t * F::kQueryBytes + kk / 4 * (kTileRows * kRowBytes) + kk % 4 * 32) >> 4),
+                     k_low + ((stage * F::kKeyBytes + kk / 4 * (kUnitKeys * kRowBytes) + kk % 4 * 32) >> 4), kIdScores, kk > 0);
+        issued = true;
+        commit(&bars->s_full[t]);
+    };
+    while (ok && list.next(p, s)) {
+        const int tiles = F::kTiles == 2 && span_of<F::kRows>(p.a, request_of(p.a, s.request), s.row0).rows > kTileRows ? 2 : 1;
+        ok = wait_parity(&bars->k_full[unit % F::kStages], (unit / F::kStages) & 1u);
+        for (int t = 0; ok && t < tiles; ++t) {
+            ok = wait_parity(&bars->q_full[t], piece_of[t]++ & 1u);
+            if (!ok) break;
+            fence_after();
+            scores(t, unit);
+        }
+        if (ok) commit(&bars->k_free[unit % F::kStages]);
+        for (int i = 0; ok && i < s.count; ++i, ++unit) {
+            const uint32_t stage = unit % F::kStages;
+            ok = wait_parity(&bars->v_full[stage], (unit / F::kStages) & 1u);
+            for (int t = 0; ok && t < tiles; ++t) {
+                ok = wait_parity(&bars->p_full[t], weights_of[t]++ & 1u);
+                if (!ok) break;
+                fence_after();
+#pragma unroll
+                for (int kk = 0; kk < kUnitKeys / 16; ++kk)
+                    mma_tmem(tmem + F::kSums + t * kDim, tmem + 128 * t + 8 * kk, v_low + ((stage * F::kKeyBytes + kk / 4 * (kDim * kRowBytes) + kk % 4 * 32) >> 4), kIdSums,
+                             i > 0 || kk > 0);
+                if (i + 1 < s.count) {
+                    if (t == 0) ok = wait_parity(&bars->k_full[(unit + 1) % F::kStages], ((unit + 1) / F::kStages) & 1u);
+                    if (!ok) break;
+                    scores(t, unit + 1);
+                } else commit(&bars->o_full[t]);
+            }
+            if (!ok) break;
+            commit(&bars->v_free[stage]);
+            if (i + 1 < s.count) commit(&bars->k_free[(unit + 1) % F::kStages]);
+        }
+    }
+    if (issued) {                       // tensor memory is not freed under running products
+        commit(&bars->drained);
+        wait_parity(&bars->drained, 0u, kDrainTries);
+    }
+}
+
+// ---- softmax of a tile's rows, a row to a thread
+
+template <int kDim>
+__device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* bars, unsigned char* queries, uint32_t tmem, int tile) {
+    using F = Form<kDim>;
+    const AttnParams& a = p.a;
+    const int t = threadIdx.x & 127, lane = t & 31, w = t >> 5;
+    const uint32_t lanes = static_cast<uint32_t>(32 * w) << 16, at_scores = tmem + 128 * tile + lanes, at_sums = tmem + F::kSums + tile * kDim + lanes;
+    unsigned char* my_queries = queries + tile * F::kQueryBytes;
+    unsigned unit = 0, units = 0, pieces = 0;                   // of the CTA; of this tile
+    bool ok = true;
+    Pieces list(p);
+    Piece s;
+    while (list.next(p, s)) {
+        const Span span = span_of<F::kRows>(a, request_of(a, s.request), s.row0);
+        const Request& rq = span.r;
+        const int rows = span.rows - tile * kTileRows, row0 = s.row0 + tile * kTileRows;
+        if (s.off == 0 && tile == 0 && t == 0 && !s.whole)      // the CTAs with the rest follow this one
+            a.open[blockIdx.x] = make_int4(s.block, s.h, s.slot, s.last_cta);
+        if (rows <= 0) {                                        // the block ends in the first tile
+            unit += s.count;
+            continue;
+        }
+        // the rows of q as an operand; all products with those before are done
+        for (int e = t; e < kTileRows * (kDim / 8); e += 128) {
+            const int r = e / (kDim / 8), piece = e % (kDim / 8);
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (r < rows) {
+                const __half* from = a.q + (rq.n0 + (row0 + r) / a.group) * a.ldq + static_cast<int64_t>(s.h * a.group + (row0 + r) % a.group) * kDim + 8 * piece;
+                if (a.wide_q) x = *reinterpret_cast<const uint4*>(from);
+                else {
+                    const unsigned short* h = reinterpret_cast<const unsigned short*>(from);
+                    x = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+                }
+                if (p.negative) x.x ^= 0x80008000u, x.y ^= 0x80008000u, x.z ^= 0x80008000u, x.w ^= 0x80008000u;
+            }
+            *reinterpret_cast<uint4*>(my_queries + piece / 8 * (kTileRows * kRowBytes) + r * kRowBytes + ((piece % 8) ^ (r & 7)) * 16) = x;
+        }
+        fence_operands();
+        __syncwarp();
+        if (lane == 0) arrive(&bars->q_full[tile]);
+        const int position = rq.length - rq.n + (row0 + min(t, rows - 1)) / a.group;
+        float top = kLowest, weight = 0.0f;
+        for (int i = 0; i < s.count; ++i, ++unit, ++units) {
+            ok = ok && __all_sync(0xFFFFFFFFu, wait_parity(&bars->s_full[tile], units & 1u));
+            if (!ok) break;
+            fence_after();
+            float x[128];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) tmem_load(at_scores + 32 * j, x + 32 * j);
+            const int first = (s.off + i) * kUnitCells;         // cell, in the block's line
+            const int low = rq.cell_at(first) * kCell, high = rq.cell_at(first + kUnitCells - 1) * kCell + kCell - 1;
+            const int4 there = *reinterpret_cast<const int4*>(bars->there[unit % kFlags]);
+            const bool whole = (there.x & there.y & there.z & there.w) == 3 && high <= span.earliest && (a.window == 0 || low > span.latest - a.window || high < a.sinks);
+            tmem_loaded();
+            if (a.cap > 0.0f) {
+#pragma unroll
+                for (int n = 0; n < 128; ++n) x[n] = capped(a, x[n] * a.scale);
+            }
+            if (!whole) {
+                const int bits = there.x | there.y << 2 | there.z << 4 | there.w << 6;
+                int from[kUnitCells];                           // first key of each cell; none that a token sees where it does not exist
+#pragma unroll
+                for (int j = 0; j < kUnitCells; ++j) from[j] = bits >> j & 1 ? rq.cell_at(first + j) * kCell : INT32_MAX - kCell;
+#pragma unroll
+                for (int n = 0; n < 128; ++n) {
+                    if (!sees(a, position, from[cell_of(n)] + token_of(n))) x[n] = -INFINITY;
+                }
+            }
+            float most = x[0];
+#pragma unroll
+            for (int n = 1; n < 128; ++n) most = fmaxf(most, x[n]);
+            const float factor = a.cap > 0.0f ? 1.0f : a.scale;
+            most *= factor;
+            // weights as in kv8.cu: 2^(score - top), top the largest score so far less kHeadroom, or up to kSlack less
+            if (__any_sync(0xFFFFFFFFu, most > top + (kHeadroom + kSlack))) {
+                const float next = fmaxf(top, most - kHeadroom), f = exp2_of(top - next);
+                top = next;
+                weight *= f;
+                if (i > 0) {
+#pragma unroll 1
+                    for (int d = 0; d < kDim; d += 32) {
+                        float o[32];
+                        tmem_load(at_sums + d, o);
+                        tmem_loaded();
+#pragma unroll
+                        for (int n = 0; n < 32; ++n) o[n] *= f;
+                        tmem_store(at_sums + d, reinterpret_cast<const uint32_t*>(o));
+                    }
+                    tmem_stored();
+                }
+            }
+            const float2 factors = make_float2(factor, factor), tops = make_float2(-top, -top);
+            float2 sums[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint32_t out[32];
+#pragma unroll
+                for (int n = 0; n < 32; ++n) {
+                    float2 z = fma2(make_float2(x[64 * half + 2 * n], x[64 * half + 2 * n + 1]), factors, tops);
+                    z.x = exp2_of(z.x), z.y = exp2_of(z.y);
+                    sums[n & 1] = add2(sums[n & 1], z);
+                    const __half2 h = __floats2half2_rn(z.x, z.y);
+                    out[n] = *reinterpret_cast<const uint32_t*>(&h);
+                }
+                tmem_store(at_scores + 32 * half, out);
+            }
+            weight += (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);
+            tmem_stored();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) arrive(&bars->p_full[tile]);
+        }
+        // ---- the piece's sums
+        ok = ok && __all_sync(0xFFFFFFFFu, wait_parity(&bars->o_full[tile], pieces & 1u));
+        ++pieces;
+        fence_after();
+        if (!ok) weight = __int_as_float(0x7FC00000);           // NaN
+        const int token = rq.n0 + (row0 + t) / a.group;
+        const int64_t column = static_cast<int64_t>(s.h * a.group + (row0 + t) % a.group) * kDim;
+        const bool mine = t < rows;
+        if (!s.whole && mine) a.stats[static_cast<int64_t>(s.slot) * F::kRows + tile * kTileRows + t] = make_float2(top, weight);
+        const bool some = weight > 0.0f || weight != weight;
+#pragma unroll 1
+        for (int d = 0; d < kDim; d += 32) {
+            float o[32];
+            __syncwarp();
+            tmem_load(at_sums + d, o);
+            tmem_loaded();
+            if (!mine) continue;
+            if (!ok) {
+#pragma unroll
+                for (int n = 0; n < 32; ++n) o[n] = weight;
+            }
+            if (!s.whole) {
+                float4* to = reinterpret_cast<float4*>(a.sums + (static_cast<int64_t>(s.slot) * F::kRows + tile * kTileRows + t) * kDim + d);
+#pragma unroll
+                for (int n = 0; n < 8; ++n) to[n] = make_float4(o[4 * n], o[4 * n + 1], o[4 * n + 2], o[4 * n + 3]);
+                continue;
+            }
+            uint32_t words[16], keep = 0;
+#pragma unroll
+            for (int n = 0; n < 16; ++n) {
+                const __half2 h = __floats2half2_rn(some ? o[2 * n] / weight : 0.0f, some ? o[2 * n + 1] / weight : 0.0f);
+                words[n] = *reinterpret_cast<const uint32_t*>(&h);
+                const float2 f = __half22float2(h);
+                keep |= (fabsf(f.x) <= a.thr ? 0u : 1u) << (2 * n) | (fabsf(f.y) <= a.thr ? 0u : 2u) << (2 * n);
+            }
+            __half* to = a.y + token * a.ldy + column + d;
+            if (p.wide16) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) reinterpret_cast<uint4*>(to)[n] = make_uint4(words[4 * n], words[4 * n + 1], words[4 * n + 2], words[4 * n + 3]);
+            } else {
+                unsigned short* h = reinterpret_cast<unsigned short*>(to);
+#pragma unroll
+                for (int n = 0; n < 16; ++n) h[2 * n] = static_cast<unsigned short>(words[n]), h[2 * n + 1] = static_cast<unsigned short>(words[n] >> 16);
+            }
+            if (a.mask != nullptr) a.mask[token * a.mask_stride + (column + d) / 32] = keep;
+        }
+        fence_before();
+    }
+}
+
+template <int kDim>
+__global__ void __launch_bounds__(kThreads, 1) kv8_prompt_kernel(const __grid_constant__ PromptParams p) {
+    using F = Form<kDim>;
+    extern __shared__ unsigned char raw[];
+    unsigned char* operands = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+    Barriers* bars = reinterpret_cast<Barriers*>(operands + F::kOperands);
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0);
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            barrier_init(&bars->q_full[i], 4);
+            barrier_init(&bars->s_full[i], 1);
+            barrier_init(&bars->p_full[i], 4);
+            barrier_init(&bars->o_full[i], 1);
+            barrier_init(&bars->k_full[i], 4);
+            barrier_init(&bars->k_free[i], 1);
+            barrier_init(&bars->v_full[i], 4);
+            barrier_init(&bars->v_free[i], 1);
+        }
+        barrier_init(&bars->drained, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem)), "n"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    dev::programmatic_start();
+    const uint32_t tmem = bars->tmem, queries = smem_u32(operands), keys = queries + F::kTiles * F::kQueryBytes, values = keys + F::kStages * F::kKeyBytes;
+    if (threadIdx.x == 0) p.a.open[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    __syncthreads();
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        if (warp < 4 * F::kTiles) softmax_role<kDim>(p, bars, operands, tmem, warp >> 2);
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
+        decode_role<kDim>(p, bars, keys, values);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (warp == 12) {
+            if (elect_one()) product_role<kDim>(p, bars, queries, keys, values, tmem);
+            __syncwarp();
+        } else {
+            const int t = threadIdx.x - 13 * 32, columns = p.a.heads * p.a.group * kDim;
+            for (int b = blockIdx.x; b < p.a.B; b += gridDim.x) {       // tokens of requests without keys
+                const Request rq = request_of(p.a, b);
+                if (rq.cells > 0) continue;
+                for (int n = rq.n0; n < rq.n0 + rq.n; ++n) {
+                    for (int i = t; i < columns; i += 96) p.a.y[n * p.a.ldy + i] = __ushort_as_half(0);
+                    if (p.a.mask != nullptr)
+                        for (int i = t; i < columns / 32; i += 96) p.a.mask[n * p.a.mask_stride + i] = 0.0f <= p.a.thr ? 0u : 0xFFFFFFFFu;
+                }
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
+}
+
+// Joins the partial sums of a block that several CTAs have, in the order of its keys: a row to a warp.
+constexpr int kJoinWarps = 8;
+
+template <int kDim>
+__global__ void __launch_bounds__(32 * kJoinWarps) kv8_prompt_join_kernel(const __grid_constant__ PromptParams p) {
+    constexpr int kRows = Form<kDim>::kRows, kLanes = kDim / 4, kFours = kDim > 128 ? kDim / 128 : 1;
+    dev::programmatic_start();
+    const AttnParams& a = p.a;
+    const int4 open = a.open[blockIdx.x];
+    if (open.x < 0) return;
+    const Block block = p.blocks[open.x];
+    const Request rq = request_of(a, block.request);
+    const int row = blockIdx.y * kJoinWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31, mine = block.row0 + row;
+    if (mine >= rq.n * a.group) return;
+    const int count = open.w - open.z / 2 + 1;
+    float m = kLowest, wt = 0.0f;
+    float4 sum[kFours] = {};
+#pragma unroll 2
+    for (int i = 0; i < count; ++i) {
+        const int64_t from = (i == 0 ? open.z : 2 * (open.z / 2 + static_cast<int64_t>(i))) * kRows + row;
+        const float2 st = a.stats[from];
+        const float top = fmaxf(m, st.x), f = exp2_of(m - top), fs = exp2_of(st.x - top);
+#pragma unroll
+        for (int j = 0; j < kFours; ++j) {
+            if (lane >= kLanes) continue;
+            const float4 v = *reinterpret_cast<const float4*>(a.sums + from * kDim + 128 * j + 4 * lane);
+            sum[j].x = sum[j].x * f + v.x * fs, sum[j].y = sum[j].y * f + v.y * fs, sum[j].z = sum[j].z * f + v.z * fs, sum[j].w = sum[j].w * f + v.w * fs;
+        }
+        wt = wt * f + st.y * fs;
+        m = top;
+    }
+#pragma unroll
+    for (int j = 0; j < kFours; ++j)
+        if (lane < kLanes) store_result(a, rq.n0 + mine / a.group, static_cast<int64_t>(open.y * a.group + mine % a.group) * kDim + 128 * j + 4 * lane, sum[j], wt);
+}
+
+template <int kDim>
+spdp_status launch_form(PromptParams p, int device, int sms, cudaStream_t s) {
+    using F = Form<kDim>;
+    constexpr size_t kShared = 1024 + F::kOperands + sizeof(Barriers);
+    static_assert(kShared <= 227 * 1024, "shared memory of a CTA");
+    static std::mutex mu;
+    static bool configured[64] = {};
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!configured[device]) {
+            SPDP_CUDA_TRY(cudaFuncSetAttribute(kv8_prompt_kernel<kDim>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kShared)));
+            configured[device] = true;
+        }
+    }
+    const int64_t rows = static_cast<int64_t>(p.a.N) * p.a.group;
+    p.most_list = static_cast<int>(rows / F::kRows + p.a.B);
+    const size_t sums = 2ull * sms * F::kRows * kDim * sizeof(float), stats = 2ull * sms * F::kRows * sizeof(float2), open = sms * sizeof(int4);
+    void* scratch = nullptr;
+    const spdp_status st = scratch_alloc(device, sums + stats + open + p.most_list * sizeof(Block) + 2 * sizeof(int), s, &scratch);
+    if (st != SPDP_OK) return st;
+    char* at = static_cast<char*>(scratch);
+    p.a.sums = reinterpret_cast<float*>(at), p.a.stats = reinterpret_cast<float2*>(at + sums), p.a.open = reinterpret_cast<int4*>(at + sums + stats);
+    p.blocks = reinterpret_cast<Block*>(at + sums + stats + open), p.totals = reinterpret_cast<int*>(p.blocks + p.most_list);
+    cudaError_t e = launch_programmatic(kv8_blocks_kernel<F::kRows>, dim3(1), kListThreads, 0, s, p);
+    if (e == cudaSuccess) e = launch_programmatic(kv8_prompt_kernel<kDim>, dim3(static_cast<unsigned>(sms)), kThreads, kShared, s, p);
+    if (e == cudaSuccess) e = launch_programmatic(kv8_prompt_join_kernel<kDim>, dim3(static_cast<unsigned>(sms), F::kRows / kJoinWarps), 32 * kJoinWarps, 0, s, p);
+    const cudaError_t freed = cudaFreeAsync(scratch, s);
+    SPDP_CUDA_TRY(e);
+    SPDP_CUDA_TRY(freed);
+    return SPDP_OK;
+}
+
+}  // namespace
+
+spdp_status launch_kv8_prompt(const AttnParams& a, int head_dim, int device, int sms, cudaStream_t s) {
+    PromptParams p = {};
+    p.a = a;
+    p.negative = a.scale < 0.0f;
+    p.a.scale = fmaxf(fabsf(a.scale), 1.0e-30f);                // never 0: a masked score is -Inf, and stays it
+    p.wide16 = rows_aligned16(a.y, a.ldy, 2);
+    switch (head_dim) {
+        case 64: return launch_form<64>(p, device, sms, s);
+        case 128: return launch_form<128>(p, device, sms, s);
+        default: return launch_form<256>(p, device, sms, s);
+    }
+}
+
+}  // namespace spdp
