@@ -4,8 +4,9 @@
 // a unit, are those that any of its tokens sees.  The units of all blocks and heads stand in one line that is cut into equal
 // runs, one to a CTA (kv8.cuh); a first small kernel writes down where each block begins.
 //
-// Inside a CTA: a warpgroup turns codes into fp16 operand tiles in shared memory, a thread issues the products, and a warpgroup to each
-// tile has the softmax, a row to a thread.  Scores are Q K^T into tensor memory; weights go back there, over the scores, as the
+// Inside a CTA: a warp goes through the run and tells the others its pieces of blocks, two bring rows of q to shared memory, a warpgroup
+// turns codes into fp16 operand tiles there, a thread issues the products, and a warpgroup to each tile has the softmax, a row to a
+// thread.  Scores are Q K^T into tensor memory; weights go back there, over the scores, as the
 // first operand of the product with the values, whose sums stay in tensor memory through the block.  While one tile's scores become
 // weights the tensor cores work on the other's.  Codes times their scale are fp16 numbers, so both operands of the first product and
 // the values of the second are exact; the weights are rounded to fp16 (2^-11, the one rounding besides the result's).
@@ -24,7 +25,7 @@ using namespace kv8;
 
 constexpr int kUnitCells = 8, kUnitKeys = kUnitCells * kCell;
 constexpr int kTileRows = 128;
-constexpr int kThreads = 512;           // warps 0-3 and 4-7: softmax; 8-11: codes to operands; 12: products; 13-15: tokens without keys
+constexpr int kThreads = 512;           // warps 0-3 and 4-7: softmax; 8-11: codes to operands; 12: products; 13: pieces; 14, 15: rows of q
 constexpr int kRowBytes = 128;          // of an operand tile: 64 fp16 numbers, in the 128-byte swizzle
 constexpr int kAtomBytes = 8 * kRowBytes;
 constexpr int kFlags = 8;               // units whose cells' existence is kept
@@ -43,9 +44,14 @@ struct Form {
     static constexpr int kOperands = kTiles * kQueryBytes + 2 * kStages * kKeyBytes;
 };
 
-struct Block {                          // of rows
-    int start;                          // in the line of one head
-    int request, row0, pad;
+struct alignas(16) Block {              // of rows, and the cells with keys that any of its tokens sees, as one line (kv8.cuh, Request)
+    int start, length;                  // in the line of one head
+    int request, row0, rows;
+    int n0, before, keys;               // the request's first token, its keys before that, all its keys
+    int sink_cells, low_cell, cells;
+    int earliest, latest;               // positions of the block's tokens
+    int pad[3];
+    __device__ __forceinline__ int cell_at(int i) const { return i < sink_cells ? i : i - sink_cells + low_cell; }
 };
 struct PromptParams {
     AttnParams a;
@@ -54,27 +60,23 @@ struct PromptParams {
     int most_list;                      // blocks that there can be
     bool negative;                      // the scale; a.scale is its size
     bool wide16;                        // rows of y on 16-byte boundaries
+    uint32_t magic, shift;              // of a division by the group
+    // n / group for 0 <= n < 2^31: with 2^shift >= group, magic = (2^shift - group) 2^32 / group, rounded down, plus 1 (Granlund and Montgomery)
+    __device__ __forceinline__ int by_group(int n) const { return static_cast<int>((__umulhi(magic, static_cast<uint32_t>(n)) + static_cast<uint32_t>(n)) >> shift); }
 };
 
-// The cells with keys that any token of a block of rows sees.
-struct Span {
-    Request r;                          // with sink_cells, low_cell and cells those of the block
-    int rows, earliest, latest;         // positions of the block's tokens
-};
 template <int kRows>
-__device__ __forceinline__ Span span_of(const AttnParams& p, const Request& rq, int row0) {
-    Span s;
-    s.r = rq;
-    s.rows = min(kRows, rq.n * p.group - row0);
-    const int before = rq.length - rq.n;
-    s.earliest = before + row0 / p.group, s.latest = before + (row0 + s.rows - 1) / p.group;
-    const int end = max(s.latest, 0) / kCell + 1;
-    s.r.low_cell = s.r.sink_cells = 0;
+__device__ __forceinline__ Block block_of(const AttnParams& p, int b, int row0) {
+    const Request rq = request_of(p, b);
+    Block s = {};
+    s.request = b, s.row0 = row0, s.rows = min(kRows, rq.n * p.group - row0), s.n0 = rq.n0, s.before = rq.length - rq.n, s.keys = rq.length;
+    s.earliest = s.before + row0 / p.group, s.latest = s.before + (row0 + s.rows - 1) / p.group;
     if (p.window > 0) {
-        s.r.low_cell = max(max(s.earliest, 0) + 1 - p.window, 0) / kCell;
-        s.r.sink_cells = min((p.sinks + kCell - 1) / kCell, s.r.low_cell);
+        s.low_cell = max(max(s.earliest, 0) + 1 - p.window, 0) / kCell;
+        s.sink_cells = min((p.sinks + kCell - 1) / kCell, s.low_cell);
     }
-    s.r.cells = s.r.sink_cells + end - s.r.low_cell;            // one at least
+    s.cells = s.sink_cells + max(s.latest, 0) / kCell + 1 - s.low_cell;         // one at least
+    s.length = triple_length((s.cells + kUnitCells - 1) / kUnitCells);
     return s;
 }
 
@@ -132,61 +134,29 @@ __global__ void __launch_bounds__(kListThreads) kv8_blocks_kernel(const PromptPa
     int length = 0;
     for (int base = 0; base < total; base += kListThreads) {
         const int i = base + threadIdx.x;
-        int mine = 0, all, b = 0, row0 = 0;
+        int all;
+        Block block = {};
         if (i < total) {
-            b = request_at(first, p.a.B, i);
-            row0 = (i - first[b]) * kRows;
-            mine = triple_length((span_of<kRows>(p.a, request_of(p.a, b), row0).r.cells + kUnitCells - 1) / kUnitCells);
+            const int b = request_at(first, p.a.B, i);
+            block = block_of<kRows>(p.a, b, (i - first[b]) * kRows);
         }
-        const int at = length + scan_add(mine, sums, &all);
-        if (i < total) p.blocks[i] = Block{at, b, row0, 0};
+        block.start = length + scan_add(block.length, sums, &all);
+        if (i < total) p.blocks[i] = block;
         length += all;
     }
     if (threadIdx.x == 0) p.totals[0] = total, p.totals[1] = length;
 }
 
-// ---- a CTA's pieces of blocks, in order: every role goes through the same list
+// ---- a CTA's pieces of blocks, in order
 
-struct Piece {
-    int block, h, request, row0, off, count, units, slot, last_cta;
-    bool whole;
+struct alignas(16) Piece {
+    Block block;
+    int index, h;                       // the block's number, the key head
+    int off, count;                     // units; count 0: no piece any more
+    int whole, slot, last_cta;
+    unsigned unit0;                     // units of the CTA before it
 };
-struct Pieces {
-    int n, length, total, ctas, u, stop, block, h;
-    int done;
-    __device__ __forceinline__ explicit Pieces(const PromptParams& p) {
-        n = p.totals[0], length = p.totals[1];
-        total = length * p.a.heads, ctas = min(static_cast<int>(gridDim.x), total);
-        u = stop = done = block = h = 0;
-        if (static_cast<int>(blockIdx.x) >= ctas) return;
-        u = run_start(total, ctas, blockIdx.x), stop = run_start(total, ctas, blockIdx.x + 1);
-        h = u / length;
-        const int v = u % length;
-        for (int lo = 0, hi = n - 1; lo <= hi;) {
-            const int mid = (lo + hi) >> 1;
-            if (p.blocks[mid].start <= v) block = mid, lo = mid + 1;
-            else hi = mid - 1;
-        }
-    }
-    __device__ __forceinline__ bool next(const PromptParams& p, Piece& s) {
-        while (u < stop) {
-            const Block b = p.blocks[block];
-            const int end = block + 1 < n ? p.blocks[block + 1].start : length, len = end - b.start, start = h * length + b.start;
-            const int off = max(0, u - start - kStart), count = max(0, min(len, stop - start) - kStart) - off;
-            s.block = block, s.h = h;
-            u = min(start + len, stop);
-            if (++block == n) block = 0, ++h;
-            if (count <= 0) continue;                           // the run ends before the block's first unit
-            s.request = b.request, s.row0 = b.row0, s.off = off, s.count = count, s.units = len - kStart;
-            s.whole = count == s.units;
-            s.slot = 2 * blockIdx.x + (done > 0 ? 1 : 0);       // what is not whole is the first piece of a run or the last
-            s.last_cta = static_cast<int>(((static_cast<int64_t>(start) + len) * ctas - 1) / total);
-            ++done;
-            return true;
-        }
-        return false;
-    }
-};
+constexpr int kPieces = 4;              // that are known at a time
 
 // ---- tensor cores, barriers
 
@@ -217,7 +187,7 @@ __device__ __forceinline__ void barrier_init(uint64_t* bar, uint32_t arrivals) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(arrivals) : "memory");
 }
 __device__ __forceinline__ void arrive(uint64_t* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory"); }
-constexpr int kWaitTries = 1 << 22;     // a wait that runs out (none should) ends its role; what the CTA would have written becomes NaN
+constexpr int kWaitTries = 1 << 22;     // a wait that runs out (none should) ends its role: the rows of the piece that is worked on become NaN, later ones stay unwritten
 constexpr int kDrainTries = 1 << 18;
 __device__ __forceinline__ bool wait_parity(uint64_t* bar, unsigned parity, int limit = kWaitTries) {
     const uint32_t a = smem_u32(bar);
@@ -262,14 +232,106 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 }
 
 struct Barriers {
-    uint64_t q_full[2], s_full[2], p_full[2], o_full[2], k_full[2], k_free[2], v_full[2], v_free[2], drained;
+    uint64_t q_full[2], q_free[2], s_full[2], p_full[2], o_full[2], k_full[2], k_free[2], v_full[2], v_free[2], piece_full[kPieces], piece_free[kPieces], drained;
     uint32_t tmem;
+    Piece pieces[kPieces];
     alignas(16) int there[kFlags][4];   // of the units' cells, two bits to a decoding warp
 };
 
 // Key of column n of a unit, from the first key of its cell
 __host__ __device__ constexpr int cell_of(int n) { return 4 * (n / 64) + 2 * (n / 8 % 2) + n / 4 % 2; }
 __host__ __device__ constexpr int token_of(int n) { return 2 * (n % 64 / 16) + n % 2 + 8 * (n % 4 / 2); }
+
+// The next piece for a role (whole warps, or one thread): null at the end, or where it does not come.
+__device__ __forceinline__ const Piece* piece_at(Barriers* bars, unsigned i) {
+    if (!wait_parity(&bars->piece_full[i % kPieces], (i / kPieces) & 1u)) return nullptr;
+    const Piece* s = &bars->pieces[i % kPieces];
+    return s->count > 0 ? s : nullptr;
+}
+
+// ---- pieces (a warp)
+
+__device__ __forceinline__ void piece_role(const PromptParams& p, Barriers* bars) {
+    const int lane = threadIdx.x & 31, n = p.totals[0], length = p.totals[1], total = length * p.a.heads, ctas = min(static_cast<int>(gridDim.x), total);
+    int u = 0, stop = 0, index = 0, h = 0;
+    if (static_cast<int>(blockIdx.x) < ctas) {
+        u = run_start(total, ctas, blockIdx.x), stop = run_start(total, ctas, blockIdx.x + 1);
+        h = u / length;
+        const int v = u % length;
+        for (int count = n; count > 1;) {                       // the last of the blocks index .. index + count - 1 that does not begin behind v
+            const int step = (count + 31) / 32, last = 31 - __clz(__ballot_sync(0xFFFFFFFFu, lane * step < count && p.blocks[index + lane * step].start <= v));
+            const int end = index + count;
+            index += last * step, count = min(step, end - index);
+        }
+    }
+    unsigned i = 0, units = 0;
+    for (bool more = true; more;) {
+        Piece s;
+        s.count = 0;
+        while (u < stop && s.count <= 0) {
+            s.block = p.blocks[index];
+            const int start = h * length + s.block.start;
+            s.off = max(0, u - start - kStart), s.count = max(0, min(s.block.length, stop - start) - kStart) - s.off;
+            s.index = index, s.h = h, s.whole = s.count == s.block.length - kStart;
+            s.slot = 2 * blockIdx.x + (i > 0 ? 1 : 0);          // what is not whole is the first piece of a run or the last
+            s.last_cta = static_cast<int>(((static_cast<int64_t>(start) + s.block.length) * ctas - 1) / total);
+            u = min(start + s.block.length, stop);
+            if (++index == n) index = 0, ++h;                   // count <= 0: the run ends before the block's first unit
+        }
+        s.count = max(s.count, 0);
+        s.unit0 = units, units += s.count;
+        more = s.count > 0;
+        if (i >= kPieces && !__all_sync(0xFFFFFFFFu, wait_parity(&bars->piece_free[i % kPieces], (i / kPieces - 1u) & 1u))) return;
+        if (lane == 0) {
+            if (more && s.off == 0 && !s.whole) p.a.open[blockIdx.x] = make_int4(s.index, s.h, s.slot, s.last_cta);     // the CTAs with the rest follow this one
+            bars->pieces[i % kPieces] = s;
+            arrive(&bars->piece_full[i % kPieces]);
+        }
+        __syncwarp();
+        ++i;
+    }
+}
+
+// ---- rows of q (a warp to each tile, or two to one)
+
+template <int kDim>
+__device__ __forceinline__ void query_role(const PromptParams& p, Barriers* bars, uint32_t queries, int warp) {
+    using F = Form<kDim>;
+    constexpr int kOfRow = kDim / 8;    // 16-byte pieces of a row
+    const int lane = threadIdx.x & 31, tile = F::kTiles == 2 ? warp : 0, first = F::kTiles == 2 ? 0 : 64 * warp, count = F::kTiles == 2 ? 128 : 64;
+    const AttnParams& a = p.a;
+    const uint32_t my_queries = queries + tile * F::kQueryBytes;
+    unsigned mine = 0;
+    for (unsigned i = 0;; ++i) {
+        const Piece* s = piece_at(bars, i);
+        if (__any_sync(0xFFFFFFFFu, s == nullptr)) return;
+        const int rows = s->block.rows - tile * kTileRows, row0 = s->block.row0 + tile * kTileRows, n0 = s->block.n0, h = s->h;
+        if (rows > 0) {
+            if (mine > 0 && !__all_sync(0xFFFFFFFFu, wait_parity(&bars->q_free[tile], (mine - 1u) & 1u))) return;
+            ++mine;
+#pragma unroll 4
+            for (int e = lane; e < count * kOfRow; e += 32) {
+                const int r = first + e / kOfRow, piece = e % kOfRow, row = row0 + min(r, rows - 1), token = p.by_group(row);
+                const __half* from = a.q + (n0 + token) * a.ldq + static_cast<int64_t>(h * a.group + row - token * a.group) * kDim + 8 * piece;
+                const uint32_t to = my_queries + piece / 8 * (kTileRows * kRowBytes) + r * kRowBytes + ((piece % 8) ^ (r & 7)) * 16;
+                if (a.wide_q) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(r < rows ? 16 : 0) : "memory");   // zeros behind the last row
+                else {
+                    const unsigned short* x = reinterpret_cast<const unsigned short*>(from);
+                    uint32_t v[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = r < rows ? x[2 * j] | static_cast<uint32_t>(x[2 * j + 1]) << 16 : 0u;
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_operands();
+            __syncwarp();
+            if (lane == 0) arrive(&bars->q_full[tile]);
+        }
+        __syncwarp();
+        if (lane == 0) arrive(&bars->piece_free[i % kPieces]);
+    }
+}
 
 // ---- codes to operands
 
@@ -285,17 +347,17 @@ __device__ __forceinline__ void decode_role(const PromptParams& p, Barriers* bar
     const uint32_t key_row = 16 * (g >> 1) + 8 * (w & 1) + 64 * (w >> 1) + (g & 1);
     const uint32_t value_at = g * kRowBytes + (((2 * c + (w & 1)) ^ g) << 4) + (w >> 1) * (kDim * kRowBytes);
     unsigned unit = 0;
-    Pieces list(p);
-    Piece s;
-    while (list.next(p, s)) {
-        const Span span = span_of<F::kRows>(a, request_of(a, s.request), s.row0);
-        const Request& rq = span.r;
-        const int32_t* table = a.table + s.request * a.table_stride;
-        const unsigned char* head = a.cache + (static_cast<int64_t>(s.h) << a.cells_shift) * cell_bytes(kDim) + 16 * lane;
-        auto place = [&](int i, int j) { return (s.off + i) * kUnitCells + 2 * w + j; };        // in the block's line, of cell j of the warp's in unit i
+    for (unsigned number = 0;; ++number) {
+        const Piece* s = piece_at(bars, number);
+        if (__any_sync(0xFFFFFFFFu, s == nullptr)) return;
+        const Block& rq = s->block;
+        const int count = s->count, line0 = s->off * kUnitCells + 2 * w;
+        const int32_t* table = a.table + rq.request * a.table_stride;
+        const unsigned char* head = a.cache + (static_cast<int64_t>(s->h) << a.cells_shift) * cell_bytes(kDim) + 16 * lane;
+        auto place = [&](int i, int j) { return line0 + i * kUnitCells + j; };  // in the block's line, of cell j of the warp's in unit i
         auto pages_of = [&](int i) {                            // of the units i .. i + 15
             const int at = place(i + (lane >> 1), lane & 1);
-            return i + (lane >> 1) < s.count && at < rq.cells ? table[rq.cell_at(at) >> a.cells_shift] : -1;
+            return i + (lane >> 1) < count && at < rq.cells ? table[rq.cell_at(at) >> a.cells_shift] : -1;
         };
         int pages = pages_of(0), pages_after = pages_of(16);
         uint4 k[2][kLoads], v[2][kLoads];
@@ -307,7 +369,7 @@ __device__ __forceinline__ void decode_role(const PromptParams& p, Barriers* bar
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const unsigned page = __shfl_sync(0xFFFFFFFFu, pages, (2 * i + j) & 31);
-                ok_next[j] = i < s.count && page < a.pages;
+                ok_next[j] = i < count && page < a.pages;
                 from[j] = head + static_cast<int64_t>(ok_next[j] ? page : 0u) * page_bytes + (rq.cell_at(place(i, j)) & in_page) * cell_bytes(kDim);
             }
         };
@@ -341,7 +403,7 @@ __device__ __forceinline__ void decode_role(const PromptParams& p, Barriers* bar
         locate(0);
         load_keys();
         load_values();
-        for (int i = 0; i < s.count; ++i, ++unit) {
+        for (int i = 0; i < count; ++i, ++unit) {
             const unsigned stage = unit % F::kStages, parity = (unit / F::kStages - 1u) & 1u;
             int key[2];
 #pragma unroll
@@ -366,12 +428,12 @@ __device__ __forceinline__ void decode_role(const PromptParams& p, Barriers* bar
             locate(i + 1);
             load_keys();
             if (unit >= F::kStages && !__all_sync(0xFFFFFFFFu, wait_parity(&bars->v_free[stage], parity))) return;
-            if (key[0] + 2 * kCell > rq.length || key[1] + kCell > rq.length) {     // behind the last key: whatever the cell holds there
+            if (max(key[0], key[1]) + kCell > rq.keys) {     // behind the last key: whatever the cell holds there
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     uint32_t keep = 0;
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) keep |= key[j] + 2 * c + (m & 1) + 8 * (m >> 1) < rq.length ? 0xFFu << 8 * m : 0u;
+                    for (int m = 0; m < 4; ++m) keep |= key[j] + 2 * c + (m & 1) + 8 * (m >> 1) < rq.keys ? 0xFFu << 8 * m : 0u;
 #pragma unroll
                     for (int t = 0; t < kLoads; ++t) v[j][t].x &= keep, v[j][t].y &= keep, v[j][t].z &= keep, v[j][t].w &= keep;
                 }
@@ -390,6 +452,8 @@ __device__ __forceinline__ void decode_role(const PromptParams& p, Barriers* bar
             if (lane == 0) arrive(&bars->v_full[stage]);
             load_values();
         }
+        __syncwarp();
+        if (lane == 0) arrive(&bars->piece_free[number % kPieces]);
     }
 }
 
@@ -399,31 +463,34 @@ template <int kDim>
 __device__ __forceinline__ void product_role(const PromptParams& p, Barriers* bars, uint32_t queries, uint32_t keys, uint32_t values, uint32_t tmem) {
     using F = Form<kDim>;
     const uint32_t q_low = desc_low(queries), k_low = desc_low(keys), v_low = desc_low(values);
-    constexpr uint32_t kIdScores = instr_desc(kUnitKeys), kIdSums = instr_desc(kDim);
+    const uint32_t id_scores = instr_desc(kUnitKeys) | (p.negative ? 1u << 13 : 0u);    // the first operand times -1
+    constexpr uint32_t kIdSums = instr_desc(kDim);
     unsigned piece_of[2] = {0, 0}, unit = 0, weights_of[2] = {0, 0};    // pieces and units so far, of each tile
     bool ok = true, issued = false;
-    Pieces list(p);
-    Piece s;
     auto scores = [&](int t, unsigned u) {
         const uint32_t stage = u % F::kStages;
 #pragma unroll
         for (int kk = 0; kk < kDim / 16; ++kk)
             mma_smem(tmem + 128 * t, q_low + ((t * F::kQueryBytes + kk / 4 * (kTileRows * kRowBytes) + kk % 4 * 32) >> 4),
-                     k_low + ((stage * F::kKeyBytes + kk / 4 * (kUnitKeys * kRowBytes) + kk % 4 * 32) >> 4), kIdScores, kk > 0);
+                     k_low + ((stage * F::kKeyBytes + kk / 4 * (kUnitKeys * kRowBytes) + kk % 4 * 32) >> 4), id_scores, kk > 0);
         issued = true;
         commit(&bars->s_full[t]);
     };
-    while (ok && list.next(p, s)) {
-        const int tiles = F::kTiles == 2 && span_of<F::kRows>(p.a, request_of(p.a, s.request), s.row0).rows > kTileRows ? 2 : 1;
+    for (unsigned number = 0; ok; ++number) {
+        const Piece* s = piece_at(bars, number);
+        if (s == nullptr) break;
+        const int tiles = F::kTiles == 2 && s->block.rows > kTileRows ? 2 : 1, count = s->count;
+        arrive(&bars->piece_free[number % kPieces]);
         ok = wait_parity(&bars->k_full[unit % F::kStages], (unit / F::kStages) & 1u);
         for (int t = 0; ok && t < tiles; ++t) {
             ok = wait_parity(&bars->q_full[t], piece_of[t]++ & 1u);
             if (!ok) break;
             fence_after();
             scores(t, unit);
+            if (count == 1) commit(&bars->q_free[t]);
         }
         if (ok) commit(&bars->k_free[unit % F::kStages]);
-        for (int i = 0; ok && i < s.count; ++i, ++unit) {
+        for (int i = 0; ok && i < count; ++i, ++unit) {
             const uint32_t stage = unit % F::kStages;
             ok = wait_parity(&bars->v_full[stage], (unit / F::kStages) & 1u);
             for (int t = 0; ok && t < tiles; ++t) {
@@ -434,15 +501,16 @@ __device__ __forceinline__ void product_role(const PromptParams& p, Barriers* ba
                 for (int kk = 0; kk < kUnitKeys / 16; ++kk)
                     mma_tmem(tmem + F::kSums + t * kDim, tmem + 128 * t + 8 * kk, v_low + ((stage * F::kKeyBytes + kk / 4 * (kDim * kRowBytes) + kk % 4 * 32) >> 4), kIdSums,
                              i > 0 || kk > 0);
-                if (i + 1 < s.count) {
+                if (i + 1 < count) {
                     if (t == 0) ok = wait_parity(&bars->k_full[(unit + 1) % F::kStages], ((unit + 1) / F::kStages) & 1u);
                     if (!ok) break;
                     scores(t, unit + 1);
+                    if (i + 2 == count) commit(&bars->q_free[t]);
                 } else commit(&bars->o_full[t]);
             }
             if (!ok) break;
             commit(&bars->v_free[stage]);
-            if (i + 1 < s.count) commit(&bars->k_free[(unit + 1) % F::kStages]);
+            if (i + 1 < count) commit(&bars->k_free[(unit + 1) % F::kStages]);
         }
     }
     if (issued) {                       // tensor memory is not freed under running products
@@ -454,57 +522,36 @@ __device__ __forceinline__ void product_role(const PromptParams& p, Barriers* ba
 // ---- softmax of a tile's rows, a row to a thread
 
 template <int kDim>
-__device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* bars, unsigned char* queries, uint32_t tmem, int tile) {
+__device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* bars, uint32_t tmem, int tile) {
     using F = Form<kDim>;
     const AttnParams& a = p.a;
     const int t = threadIdx.x & 127, lane = t & 31, w = t >> 5;
     const uint32_t lanes = static_cast<uint32_t>(32 * w) << 16, at_scores = tmem + 128 * tile + lanes, at_sums = tmem + F::kSums + tile * kDim + lanes;
-    unsigned char* my_queries = queries + tile * F::kQueryBytes;
-    unsigned unit = 0, units = 0, pieces = 0;                   // of the CTA; of this tile
+    unsigned units = 0, pieces = 0;                             // of this tile
     bool ok = true;
-    Pieces list(p);
-    Piece s;
-    while (list.next(p, s)) {
-        const Span span = span_of<F::kRows>(a, request_of(a, s.request), s.row0);
-        const Request& rq = span.r;
-        const int rows = span.rows - tile * kTileRows, row0 = s.row0 + tile * kTileRows;
-        if (s.off == 0 && tile == 0 && t == 0 && !s.whole)      // the CTAs with the rest follow this one
-            a.open[blockIdx.x] = make_int4(s.block, s.h, s.slot, s.last_cta);
+    for (unsigned number = 0;; ++number) {
+        const Piece* const s = piece_at(bars, number);
+        if (__any_sync(0xFFFFFFFFu, s == nullptr)) return;
+        const Block& block = s->block;
+        const int rows = block.rows - tile * kTileRows;
         if (rows <= 0) {                                        // the block ends in the first tile
-            unit += s.count;
+            __syncwarp();
+            if (lane == 0) arrive(&bars->piece_free[number % kPieces]);
             continue;
         }
-        // the rows of q as an operand; all products with those before are done
-        for (int e = t; e < kTileRows * (kDim / 8); e += 128) {
-            const int r = e / (kDim / 8), piece = e % (kDim / 8);
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (r < rows) {
-                const __half* from = a.q + (rq.n0 + (row0 + r) / a.group) * a.ldq + static_cast<int64_t>(s.h * a.group + (row0 + r) % a.group) * kDim + 8 * piece;
-                if (a.wide_q) x = *reinterpret_cast<const uint4*>(from);
-                else {
-                    const unsigned short* h = reinterpret_cast<const unsigned short*>(from);
-                    x = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
-                }
-                if (p.negative) x.x ^= 0x80008000u, x.y ^= 0x80008000u, x.z ^= 0x80008000u, x.w ^= 0x80008000u;
-            }
-            *reinterpret_cast<uint4*>(my_queries + piece / 8 * (kTileRows * kRowBytes) + r * kRowBytes + ((piece % 8) ^ (r & 7)) * 16) = x;
-        }
-        fence_operands();
-        __syncwarp();
-        if (lane == 0) arrive(&bars->q_full[tile]);
-        const int position = rq.length - rq.n + (row0 + min(t, rows - 1)) / a.group;
+        const int row = block.row0 + tile * kTileRows + min(t, rows - 1), token = p.by_group(row), position = block.before + token, count = s->count;
         float top = kLowest, weight = 0.0f;
-        for (int i = 0; i < s.count; ++i, ++unit, ++units) {
+        for (int i = 0; i < count; ++i, ++units) {
             ok = ok && __all_sync(0xFFFFFFFFu, wait_parity(&bars->s_full[tile], units & 1u));
             if (!ok) break;
             fence_after();
             float x[128];
 #pragma unroll
             for (int j = 0; j < 4; ++j) tmem_load(at_scores + 32 * j, x + 32 * j);
-            const int first = (s.off + i) * kUnitCells;         // cell, in the block's line
-            const int low = rq.cell_at(first) * kCell, high = rq.cell_at(first + kUnitCells - 1) * kCell + kCell - 1;
-            const int4 there = *reinterpret_cast<const int4*>(bars->there[unit % kFlags]);
-            const bool whole = (there.x & there.y & there.z & there.w) == 3 && high <= span.earliest && (a.window == 0 || low > span.latest - a.window || high < a.sinks);
+            const int first = (s->off + i) * kUnitCells;        // cell, in the block's line
+            const int low = block.cell_at(first) * kCell, high = block.cell_at(first + kUnitCells - 1) * kCell + kCell - 1;
+            const int4 there = *reinterpret_cast<const int4*>(bars->there[(s->unit0 + i) % kFlags]);
+            const bool whole = (there.x & there.y & there.z & there.w) == 3 && high <= block.earliest && (a.window == 0 || low > block.latest - a.window || high < a.sinks);
             tmem_loaded();
             if (a.cap > 0.0f) {
 #pragma unroll
@@ -514,15 +561,21 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
                 const int bits = there.x | there.y << 2 | there.z << 4 | there.w << 6;
                 int from[kUnitCells];                           // first key of each cell; none that a token sees where it does not exist
 #pragma unroll
-                for (int j = 0; j < kUnitCells; ++j) from[j] = bits >> j & 1 ? rq.cell_at(first + j) * kCell : INT32_MAX - kCell;
+                for (int j = 0; j < kUnitCells; ++j) from[j] = bits >> j & 1 ? block.cell_at(first + j) * kCell : INT32_MAX - kCell;
 #pragma unroll
                 for (int n = 0; n < 128; ++n) {
                     if (!sees(a, position, from[cell_of(n)] + token_of(n))) x[n] = -INFINITY;
                 }
             }
-            float most = x[0];
+            float mosts[8];                                     // in chains side by side
 #pragma unroll
-            for (int n = 1; n < 128; ++n) most = fmaxf(most, x[n]);
+            for (int n = 0; n < 8; ++n) mosts[n] = fmaxf(x[n], x[n + 8]);
+#pragma unroll
+            for (int n = 16; n < 128; n += 16) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) mosts[j] = fmaxf(mosts[j], fmaxf(x[n + j], x[n + j + 8]));
+            }
+            float most = fmaxf(fmaxf(fmaxf(mosts[0], mosts[1]), fmaxf(mosts[2], mosts[3])), fmaxf(fmaxf(mosts[4], mosts[5]), fmaxf(mosts[6], mosts[7])));
             const float factor = a.cap > 0.0f ? 1.0f : a.scale;
             most *= factor;
             // weights as in kv8.cu: 2^(score - top), top the largest score so far less kHeadroom, or up to kSlack less
@@ -544,7 +597,7 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
                 }
             }
             const float2 factors = make_float2(factor, factor), tops = make_float2(-top, -top);
-            float2 sums[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+            float2 sums[4] = {};
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 uint32_t out[32];
@@ -552,13 +605,14 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
                 for (int n = 0; n < 32; ++n) {
                     float2 z = fma2(make_float2(x[64 * half + 2 * n], x[64 * half + 2 * n + 1]), factors, tops);
                     z.x = exp2_of(z.x), z.y = exp2_of(z.y);
-                    sums[n & 1] = add2(sums[n & 1], z);
+                    sums[n & 3] = add2(sums[n & 3], z);
                     const __half2 h = __floats2half2_rn(z.x, z.y);
                     out[n] = *reinterpret_cast<const uint32_t*>(&h);
                 }
                 tmem_store(at_scores + 32 * half, out);
             }
-            weight += (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);
+            const float2 sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
+            weight += sum.x + sum.y;
             tmem_stored();
             fence_before();
             __syncwarp();
@@ -569,48 +623,56 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
         ++pieces;
         fence_after();
         if (!ok) weight = __int_as_float(0x7FC00000);           // NaN
-        const int token = rq.n0 + (row0 + t) / a.group;
-        const int64_t column = static_cast<int64_t>(s.h * a.group + (row0 + t) % a.group) * kDim;
+        const int64_t column = static_cast<int64_t>(s->h * a.group + row - token * a.group) * kDim;
         const bool mine = t < rows;
-        if (!s.whole && mine) a.stats[static_cast<int64_t>(s.slot) * F::kRows + tile * kTileRows + t] = make_float2(top, weight);
-        const bool some = weight > 0.0f || weight != weight;
+        if (!s->whole && mine) a.stats[static_cast<int64_t>(s->slot) * F::kRows + tile * kTileRows + t] = make_float2(top, weight);
+        const float inverse = weight > 0.0f || weight != weight ? 1.0f / weight : 0.0f;
 #pragma unroll 1
-        for (int d = 0; d < kDim; d += 32) {
-            float o[32];
+        for (int d0 = 0; d0 < kDim; d0 += 64) {
+            float o[64];
             __syncwarp();
-            tmem_load(at_sums + d, o);
+            tmem_load(at_sums + d0, o);
+            tmem_load(at_sums + d0 + 32, o + 32);
             tmem_loaded();
             if (!mine) continue;
             if (!ok) {
 #pragma unroll
-                for (int n = 0; n < 32; ++n) o[n] = weight;
+                for (int n = 0; n < 64; ++n) o[n] = weight;
             }
-            if (!s.whole) {
-                float4* to = reinterpret_cast<float4*>(a.sums + (static_cast<int64_t>(s.slot) * F::kRows + tile * kTileRows + t) * kDim + d);
+            if (!s->whole) {
+                float4* to = reinterpret_cast<float4*>(a.sums + (static_cast<int64_t>(s->slot) * F::kRows + tile * kTileRows + t) * kDim + d0);
 #pragma unroll
-                for (int n = 0; n < 8; ++n) to[n] = make_float4(o[4 * n], o[4 * n + 1], o[4 * n + 2], o[4 * n + 3]);
+                for (int n = 0; n < 16; ++n) to[n] = make_float4(o[4 * n], o[4 * n + 1], o[4 * n + 2], o[4 * n + 3]);
                 continue;
             }
-            uint32_t words[16], keep = 0;
+            uint32_t words[32], keep[2] = {0, 0};
 #pragma unroll
-            for (int n = 0; n < 16; ++n) {
-                const __half2 h = __floats2half2_rn(some ? o[2 * n] / weight : 0.0f, some ? o[2 * n + 1] / weight : 0.0f);
+            for (int n = 0; n < 32; ++n) {
+                const __half2 h = __floats2half2_rn(o[2 * n] * inverse, o[2 * n + 1] * inverse);
                 words[n] = *reinterpret_cast<const uint32_t*>(&h);
-                const float2 f = __half22float2(h);
-                keep |= (fabsf(f.x) <= a.thr ? 0u : 1u) << (2 * n) | (fabsf(f.y) <= a.thr ? 0u : 2u) << (2 * n);
             }
-            __half* to = a.y + token * a.ldy + column + d;
+            __half* to = a.y + (block.n0 + token) * a.ldy + column + d0;
             if (p.wide16) {
 #pragma unroll
-                for (int n = 0; n < 4; ++n) reinterpret_cast<uint4*>(to)[n] = make_uint4(words[4 * n], words[4 * n + 1], words[4 * n + 2], words[4 * n + 3]);
+                for (int n = 0; n < 8; ++n) reinterpret_cast<uint4*>(to)[n] = make_uint4(words[4 * n], words[4 * n + 1], words[4 * n + 2], words[4 * n + 3]);
             } else {
                 unsigned short* h = reinterpret_cast<unsigned short*>(to);
 #pragma unroll
-                for (int n = 0; n < 16; ++n) h[2 * n] = static_cast<unsigned short>(words[n]), h[2 * n + 1] = static_cast<unsigned short>(words[n] >> 16);
+                for (int n = 0; n < 32; ++n) h[2 * n] = static_cast<unsigned short>(words[n]), h[2 * n + 1] = static_cast<unsigned short>(words[n] >> 16);
             }
-            if (a.mask != nullptr) a.mask[token * a.mask_stride + (column + d) / 32] = keep;
+            if (a.mask != nullptr) {
+#pragma unroll
+                for (int n = 0; n < 32; ++n) {
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&words[n]));
+                    keep[n / 16] |= (fabsf(f.x) <= a.thr ? 0u : 1u) << (2 * n & 31) | (fabsf(f.y) <= a.thr ? 0u : 2u) << (2 * n & 31);
+                }
+                uint32_t* to_mask = a.mask + (block.n0 + token) * a.mask_stride + (column + d0) / 32;
+                to_mask[0] = keep[0], to_mask[1] = keep[1];
+            }
         }
         fence_before();
+        __syncwarp();
+        if (lane == 0) arrive(&bars->piece_free[number % kPieces]);
     }
 }
 
@@ -624,7 +686,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_prompt_kernel(const __grid_co
     if (threadIdx.x == 0) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            barrier_init(&bars->q_full[i], 4);
+            barrier_init(&bars->q_full[i], F::kTiles == 2 ? 1 : 2);
+            barrier_init(&bars->q_free[i], 1);
             barrier_init(&bars->s_full[i], 1);
             barrier_init(&bars->p_full[i], 4);
             barrier_init(&bars->o_full[i], 1);
@@ -632,6 +695,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_prompt_kernel(const __grid_co
             barrier_init(&bars->k_free[i], 1);
             barrier_init(&bars->v_full[i], 4);
             barrier_init(&bars->v_free[i], 1);
+        }
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            barrier_init(&bars->piece_full[i], 1);
+            barrier_init(&bars->piece_free[i], 4 * F::kTiles + 4 + 1 + 2);      // softmax, codes, products, rows of q
         }
         barrier_init(&bars->drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -650,7 +718,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_prompt_kernel(const __grid_co
     __syncthreads();
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        if (warp < 4 * F::kTiles) softmax_role<kDim>(p, bars, operands, tmem, warp >> 2);
+        if (warp < 4 * F::kTiles) softmax_role<kDim>(p, bars, tmem, warp >> 2);
     } else if (warp < 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
         decode_role<kDim>(p, bars, keys, values);
@@ -659,18 +727,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_prompt_kernel(const __grid_co
         if (warp == 12) {
             if (elect_one()) product_role<kDim>(p, bars, queries, keys, values, tmem);
             __syncwarp();
-        } else {
-            const int t = threadIdx.x - 13 * 32, columns = p.a.heads * p.a.group * kDim;
+        } else if (warp == 13) {
+            piece_role(p, bars);
+            const int columns = p.a.heads * p.a.group * kDim;
             for (int b = blockIdx.x; b < p.a.B; b += gridDim.x) {       // tokens of requests without keys
                 const Request rq = request_of(p.a, b);
                 if (rq.cells > 0) continue;
                 for (int n = rq.n0; n < rq.n0 + rq.n; ++n) {
-                    for (int i = t; i < columns; i += 96) p.a.y[n * p.a.ldy + i] = __ushort_as_half(0);
+                    for (int i = threadIdx.x & 31; i < columns; i += 32) p.a.y[n * p.a.ldy + i] = __ushort_as_half(0);
                     if (p.a.mask != nullptr)
-                        for (int i = t; i < columns / 32; i += 96) p.a.mask[n * p.a.mask_stride + i] = 0.0f <= p.a.thr ? 0u : 0xFFFFFFFFu;
+                        for (int i = threadIdx.x & 31; i < columns / 32; i += 32) p.a.mask[n * p.a.mask_stride + i] = 0.0f <= p.a.thr ? 0u : 0xFFFFFFFFu;
                 }
             }
-        }
+        } else query_role<kDim>(p, bars, queries, warp - 14);
     }
     fence_before();
     __syncthreads();
@@ -687,10 +756,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv8_prompt_join_kernel(const 
     const AttnParams& a = p.a;
     const int4 open = a.open[blockIdx.x];
     if (open.x < 0) return;
-    const Block block = p.blocks[open.x];
-    const Request rq = request_of(a, block.request);
+    const Block& block = p.blocks[open.x];
     const int row = blockIdx.y * kJoinWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31, mine = block.row0 + row;
-    if (mine >= rq.n * a.group) return;
+    if (row >= block.rows) return;
     const int count = open.w - open.z / 2 + 1;
     float m = kLowest, wt = 0.0f;
     float4 sum[kFours] = {};
@@ -710,7 +778,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv8_prompt_join_kernel(const 
     }
 #pragma unroll
     for (int j = 0; j < kFours; ++j)
-        if (lane < kLanes) store_result(a, rq.n0 + mine / a.group, static_cast<int64_t>(open.y * a.group + mine % a.group) * kDim + 128 * j + 4 * lane, sum[j], wt);
+        if (lane < kLanes) store_result(a, block.n0 + mine / a.group, static_cast<int64_t>(open.y * a.group + mine % a.group) * kDim + 128 * j + 4 * lane, sum[j], wt);
 }
 
 template <int kDim>
@@ -753,6 +821,8 @@ spdp_status launch_kv8_prompt(const AttnParams& a, int head_dim, int device, int
     p.negative = a.scale < 0.0f;
     p.a.scale = fmaxf(fabsf(a.scale), 1.0e-30f);                // never 0: a masked score is -Inf, and stays it
     p.wide16 = rows_aligned16(a.y, a.ldy, 2);
+    while ((1u << p.shift) < static_cast<unsigned>(a.group)) ++p.shift;
+    p.magic = static_cast<uint32_t>((((1ull << p.shift) - a.group) << 32) / a.group + 1);
     switch (head_dim) {
         case 64: return launch_form<64>(p, device, sms, s);
         case 128: return launch_form<128>(p, device, sms, s);
