@@ -231,8 +231,18 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     return r;
 }
 
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mul.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 twice(float a) { return make_float2(a, a); }
+// The lowest n bits of 16: none below 0, all from 16 on.
+__device__ __forceinline__ uint32_t low_bits(int n) { return (1u << min(max(n, 0), kCell)) - 1u; }
+
 struct Barriers {
-    uint64_t q_full[2], q_free[2], s_full[2], p_full[2], o_full[2], k_full[2], k_free[2], v_full[2], v_free[2], piece_full[kPieces], piece_free[kPieces], drained;
+    uint64_t q_full[2], q_free[2], s_full[2], p_full[2][2], o_full[2], k_full[2], k_free[2], v_full[2], v_free[2], piece_full[kPieces], piece_free[kPieces], drained;
     uint32_t tmem;
     Piece pieces[kPieces];
     alignas(16) int there[kFlags][4];   // of the units' cells, two bits to a decoding warp
@@ -494,13 +504,18 @@ __device__ __forceinline__ void product_role(const PromptParams& p, Barriers* ba
             const uint32_t stage = unit % F::kStages;
             ok = wait_parity(&bars->v_full[stage], (unit / F::kStages) & 1u);
             for (int t = 0; ok && t < tiles; ++t) {
-                ok = wait_parity(&bars->p_full[t], weights_of[t]++ & 1u);
-                if (!ok) break;
-                fence_after();
 #pragma unroll
-                for (int kk = 0; kk < kUnitKeys / 16; ++kk)
-                    mma_tmem(tmem + F::kSums + t * kDim, tmem + 128 * t + 8 * kk, v_low + ((stage * F::kKeyBytes + kk / 4 * (kDim * kRowBytes) + kk % 4 * 32) >> 4), kIdSums,
-                             i > 0 || kk > 0);
+                for (int half = 0; half < 2; ++half) {
+                    ok = ok && wait_parity(&bars->p_full[t][half], weights_of[t] & 1u);
+                    if (!ok) break;
+                    fence_after();
+#pragma unroll
+                    for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
+                        mma_tmem(tmem + F::kSums + t * kDim, tmem + 128 * t + 8 * kk, v_low + ((stage * F::kKeyBytes + half * (kDim * kRowBytes) + kk % 4 * 32) >> 4), kIdSums,
+                                 i > 0 || kk > 0);
+                }
+                if (!ok) break;
+                ++weights_of[t];
                 if (i + 1 < count) {
                     if (t == 0) ok = wait_parity(&bars->k_full[(unit + 1) % F::kStages], ((unit + 1) / F::kStages) & 1u);
                     if (!ok) break;
@@ -521,7 +536,7 @@ __device__ __forceinline__ void product_role(const PromptParams& p, Barriers* ba
 
 // ---- softmax of a tile's rows, a row to a thread
 
-template <int kDim>
+template <int kDim, bool kCap>
 __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* bars, uint32_t tmem, int tile) {
     using F = Form<kDim>;
     const AttnParams& a = p.a;
@@ -553,19 +568,36 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
             const int4 there = *reinterpret_cast<const int4*>(bars->there[(s->unit0 + i) % kFlags]);
             const bool whole = (there.x & there.y & there.z & there.w) == 3 && high <= block.earliest && (a.window == 0 || low > block.latest - a.window || high < a.sinks);
             tmem_loaded();
-            if (a.cap > 0.0f) {
+            if constexpr (kCap) {
+                float most = 0.0f;
 #pragma unroll
-                for (int n = 0; n < 128; ++n) x[n] = capped(a, x[n] * a.scale);
+                for (int n = 0; n < 128; n += 4) most = fmaxf(most, fmaxf(fmaxf(fabsf(x[n]), fabsf(x[n + 1])), fmaxf(fabsf(x[n + 2]), fabsf(x[n + 3]))));
+                if (__any_sync(0xFFFFFFFFu, !(most * a.scale <= a.cap_near))) {
+#pragma unroll
+                    for (int n = 0; n < 128; ++n) x[n] = capped(a, x[n] * a.scale);
+                } else {                                        // as capped_near, in pairs
+                    const float f = a.scale * a.cap_inv;
+#pragma unroll
+                    for (int n = 0; n < 128; n += 2) {
+                        const float2 z = mul2(make_float2(x[n], x[n + 1]), twice(a.scale)), y = mul2(make_float2(x[n], x[n + 1]), twice(f)), t = mul2(y, y);
+                        const float2 r = fma2(mul2(z, t), fma2(fma2(twice(-17.0f / 315.0f), t, twice(2.0f / 15.0f)), t, twice(-1.0f / 3.0f)), z);
+                        x[n] = r.x, x[n + 1] = r.y;
+                    }
+                }
             }
             if (!whole) {
+                // Bits of the keys that the row's token sees: of each cell, those up to its own place, and of these the window's and the first ones.
                 const int bits = there.x | there.y << 2 | there.z << 4 | there.w << 6;
-                int from[kUnitCells];                           // first key of each cell; none that a token sees where it does not exist
+                uint32_t seen[kUnitCells];
 #pragma unroll
-                for (int j = 0; j < kUnitCells; ++j) from[j] = bits >> j & 1 ? block.cell_at(first + j) * kCell : INT32_MAX - kCell;
-#pragma unroll
-                for (int n = 0; n < 128; ++n) {
-                    if (!sees(a, position, from[cell_of(n)] + token_of(n))) x[n] = -INFINITY;
+                for (int j = 0; j < kUnitCells; ++j) {
+                    const int from = block.cell_at(first + j) * kCell;
+                    uint32_t m = low_bits(position + 1 - from);
+                    if (a.window > 0) m &= ~low_bits(position + 1 - a.window - from) | low_bits(a.sinks - from);
+                    seen[j] = bits >> j & 1 ? m : 0u;
                 }
+#pragma unroll
+                for (int n = 0; n < 128; ++n) x[n] = seen[cell_of(n)] & 1u << token_of(n) ? x[n] : -INFINITY;
             }
             float mosts[8];                                     // in chains side by side
 #pragma unroll
@@ -576,7 +608,7 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
                 for (int j = 0; j < 8; ++j) mosts[j] = fmaxf(mosts[j], fmaxf(x[n + j], x[n + j + 8]));
             }
             float most = fmaxf(fmaxf(fmaxf(mosts[0], mosts[1]), fmaxf(mosts[2], mosts[3])), fmaxf(fmaxf(mosts[4], mosts[5]), fmaxf(mosts[6], mosts[7])));
-            const float factor = a.cap > 0.0f ? 1.0f : a.scale;
+            const float factor = kCap ? 1.0f : a.scale;
             most *= factor;
             // weights as in kv8.cu: 2^(score - top), top the largest score so far less kHeadroom, or up to kSlack less
             if (__any_sync(0xFFFFFFFFu, most > top + (kHeadroom + kSlack))) {
@@ -610,13 +642,13 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
                     out[n] = *reinterpret_cast<const uint32_t*>(&h);
                 }
                 tmem_store(at_scores + 32 * half, out);
+                tmem_stored();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) arrive(&bars->p_full[tile][half]);
             }
             const float2 sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
             weight += sum.x + sum.y;
-            tmem_stored();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) arrive(&bars->p_full[tile]);
         }
         // ---- the piece's sums
         ok = ok && __all_sync(0xFFFFFFFFu, wait_parity(&bars->o_full[tile], pieces & 1u));
@@ -676,7 +708,7 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
     }
 }
 
-template <int kDim>
+template <int kDim, bool kCap>
 __global__ void __launch_bounds__(kThreads, 1) kv8_prompt_kernel(const __grid_constant__ PromptParams p) {
     using F = Form<kDim>;
     extern __shared__ unsigned char raw[];
@@ -689,7 +721,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_prompt_kernel(const __grid_co
             barrier_init(&bars->q_full[i], F::kTiles == 2 ? 1 : 2);
             barrier_init(&bars->q_free[i], 1);
             barrier_init(&bars->s_full[i], 1);
-            barrier_init(&bars->p_full[i], 4);
+            barrier_init(&bars->p_full[i][0], 4);
+            barrier_init(&bars->p_full[i][1], 4);
             barrier_init(&bars->o_full[i], 1);
             barrier_init(&bars->k_full[i], 4);
             barrier_init(&bars->k_free[i], 1);
@@ -718,7 +751,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_prompt_kernel(const __grid_co
     __syncthreads();
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        if (warp < 4 * F::kTiles) softmax_role<kDim>(p, bars, tmem, warp >> 2);
+        if (warp < 4 * F::kTiles) softmax_role<kDim, kCap>(p, bars, tmem, warp >> 2);
     } else if (warp < 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
         decode_role<kDim>(p, bars, keys, values);
@@ -781,7 +814,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv8_prompt_join_kernel(const 
         if (lane < kLanes) store_result(a, block.n0 + mine / a.group, static_cast<int64_t>(open.y * a.group + mine % a.group) * kDim + 128 * j + 4 * lane, sum[j], wt);
 }
 
-template <int kDim>
+template <int kDim, bool kCap>
 spdp_status launch_form(PromptParams p, int device, int sms, cudaStream_t s) {
     using F = Form<kDim>;
     constexpr size_t kShared = 1024 + F::kOperands + sizeof(Barriers);
@@ -791,7 +824,7 @@ spdp_status launch_form(PromptParams p, int device, int sms, cudaStream_t s) {
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!configured[device]) {
-            SPDP_CUDA_TRY(cudaFuncSetAttribute(kv8_prompt_kernel<kDim>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kShared)));
+            SPDP_CUDA_TRY(cudaFuncSetAttribute(kv8_prompt_kernel<kDim, kCap>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kShared)));
             configured[device] = true;
         }
     }
@@ -805,7 +838,7 @@ spdp_status launch_form(PromptParams p, int device, int sms, cudaStream_t s) {
     p.a.sums = reinterpret_cast<float*>(at), p.a.stats = reinterpret_cast<float2*>(at + sums), p.a.open = reinterpret_cast<int4*>(at + sums + stats);
     p.blocks = reinterpret_cast<Block*>(at + sums + stats + open), p.totals = reinterpret_cast<int*>(p.blocks + p.most_list);
     cudaError_t e = launch_programmatic(kv8_blocks_kernel<F::kRows>, dim3(1), kListThreads, 0, s, p);
-    if (e == cudaSuccess) e = launch_programmatic(kv8_prompt_kernel<kDim>, dim3(static_cast<unsigned>(sms)), kThreads, kShared, s, p);
+    if (e == cudaSuccess) e = launch_programmatic(kv8_prompt_kernel<kDim, kCap>, dim3(static_cast<unsigned>(sms)), kThreads, kShared, s, p);
     if (e == cudaSuccess) e = launch_programmatic(kv8_prompt_join_kernel<kDim>, dim3(static_cast<unsigned>(sms), F::kRows / kJoinWarps), 32 * kJoinWarps, 0, s, p);
     const cudaError_t freed = cudaFreeAsync(scratch, s);
     SPDP_CUDA_TRY(e);
@@ -824,9 +857,9 @@ spdp_status launch_kv8_prompt(const AttnParams& a, int head_dim, int device, int
     while ((1u << p.shift) < static_cast<unsigned>(a.group)) ++p.shift;
     p.magic = static_cast<uint32_t>((((1ull << p.shift) - a.group) << 32) / a.group + 1);
     switch (head_dim) {
-        case 64: return launch_form<64>(p, device, sms, s);
-        case 128: return launch_form<128>(p, device, sms, s);
-        default: return launch_form<256>(p, device, sms, s);
+        case 64: return a.cap > 0.0f ? launch_form<64, true>(p, device, sms, s) : launch_form<64, false>(p, device, sms, s);
+        case 128: return a.cap > 0.0f ? launch_form<128, true>(p, device, sms, s) : launch_form<128, false>(p, device, sms, s);
+        default: return a.cap > 0.0f ? launch_form<256, true>(p, device, sms, s) : launch_form<256, false>(p, device, sms, s);
     }
 }
 
