@@ -29,7 +29,7 @@ constexpr int kThreads = 512;           // warps 0-3 and 4-7: softmax; 8-11: cod
 constexpr int kRowBytes = 128;          // of an operand tile: 64 fp16 numbers, in the 128-byte swizzle
 constexpr int kAtomBytes = 8 * kRowBytes;
 constexpr int kFlags = 8;               // units whose cells' existence is kept
-constexpr float kHeadroom = 12.0f, kSlack = 2.5f;       // weights are below 2^(kHeadroom + kSlack)
+constexpr float kHeadroom = 8.0f, kSlack = 6.5f;       // weights are below 2^(kHeadroom + kSlack); 12 and 2.5 scale the sums anew more often: 336 -> 342 us
 // Registers of a thread by its warpgroup; with the 128 of the launch the four come to the same sum.
 constexpr int kSoftmaxRegs = 176, kDecodeRegs = 112, kOtherRegs = 48;
 static_assert(2 * kSoftmaxRegs + kDecodeRegs + kOtherRegs == 4 * 128, "the launch's registers");
@@ -555,6 +555,15 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
             continue;
         }
         const int row = block.row0 + tile * kTileRows + min(t, rows - 1), token = p.by_group(row), position = block.before + token, count = s->count;
+        // The piece's units whose every key every token of the block sees (one run of them), if the pages exist.  (Found once, in registers: a load from
+        // shared memory waits behind the exponentials of the scheduler's other warps.)
+        int whole_begin = 0, whole_end = count;
+        {
+            const int off = s->off, sinks = block.sink_cells, past = a.window > 0 ? max(block.latest + 1 - a.window, 0) : 0;   // keys before `past` are behind some window
+            while (whole_begin < count && sinks + ((past + kCell - 1) / kCell - block.low_cell) > (off + whole_begin) * kUnitCells) ++whole_begin;
+            whole_end = min(count, (block.earliest + 1 < 0 ? 0 : sinks + (block.earliest + 1) / kCell - block.low_cell) / kUnitCells - off);
+        }
+        const unsigned unit0 = s->unit0;
         float top = kLowest, weight = 0.0f;
         for (int i = 0; i < count; ++i, ++units) {
             ok = ok && __all_sync(0xFFFFFFFFu, wait_parity(&bars->s_full[tile], units & 1u));
@@ -563,10 +572,8 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
             float x[128];
 #pragma unroll
             for (int j = 0; j < 4; ++j) tmem_load(at_scores + 32 * j, x + 32 * j);
-            const int first = (s->off + i) * kUnitCells;        // cell, in the block's line
-            const int low = block.cell_at(first) * kCell, high = block.cell_at(first + kUnitCells - 1) * kCell + kCell - 1;
-            const int4 there = *reinterpret_cast<const int4*>(bars->there[(s->unit0 + i) % kFlags]);
-            const bool whole = (there.x & there.y & there.z & there.w) == 3 && high <= block.earliest && (a.window == 0 || low > block.latest - a.window || high < a.sinks);
+            const int4 there = *reinterpret_cast<const int4*>(bars->there[(unit0 + i) % kFlags]);
+            const bool whole = i >= whole_begin && i < whole_end && (there.x & there.y & there.z & there.w) == 3;
             tmem_loaded();
             if constexpr (kCap) {
                 float most = 0.0f;
@@ -591,7 +598,7 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
                 uint32_t seen[kUnitCells];
 #pragma unroll
                 for (int j = 0; j < kUnitCells; ++j) {
-                    const int from = block.cell_at(first + j) * kCell;
+                    const int from = block.cell_at((s->off + i) * kUnitCells + j) * kCell;
                     uint32_t m = low_bits(position + 1 - from);
                     if (a.window > 0) m &= ~low_bits(position + 1 - a.window - from) | low_bits(a.sinks - from);
                     seen[j] = bits >> j & 1 ? m : 0u;

@@ -194,10 +194,10 @@ def filled(rng, heads, D, page, lengths, spare=2, sizes=(0.01, 1.0, 30.0)):
 
 def attn_bound(want, spread, reach, keys, cap, most):
     """Scores: D / 16 products of 17 additions at 2 v of the sizes, 8 sums and roundings more; a cap adds 8 v of itself; the values' exponent, -15 .. 8, and the exponential 2^-20.
-    Weights: twice the scores' error, one rounding u and, where small, half of fp16's smallest step, 2^-25, against a largest weight of 2^12 at least: 2^-37 of the values, whose largest is at
-    most twice that of its cell or 448 * 2^-15; the result's rounding."""
+    Weights: twice the scores' error, one rounding u and, where small, half of fp16's smallest step, 2^-25, against a largest weight of 2^8 at least (2^12 of few tokens, whose values count by their
+    cell's scale: at most twice its largest, or 448 * 2^-15): 2^-33 of the largest value; the result's rounding."""
     ds = (2 * 2 * V * (17 * 16 + 8) * reach + 8 * V * cap + 2.0 ** -20)[..., None]
-    return U * np.abs(want) * 1.01 + (U + 2 * ds) * 1.01 * spread + (keys * 2.0 ** -36 * (most + 0.014))[:, None, None] + TINY
+    return U * np.abs(want) * 1.01 + (U + 2 * ds) * 1.01 * spread + (keys * 2.0 ** -33 * (most + 0.014))[:, None, None] + TINY
 
 
 def attn_check(y, q, cache, table, first, length, scale, cap=0.0, window=0, sinks=0, most=200.0):
@@ -348,7 +348,7 @@ def device_check(y, q, k, v, seen, scale, kmost, vmost):
     """As attn_bound, with the scores' reach from the largest key."""
     want, spread = exact_on_device(q, k, v, seen, scale)
     reach = scale * (q.double().abs().sum(-1) * kmost)[..., None]
-    bound = U * want.abs() * 1.01 + (U + 2 * (reach * 1120 * V + 2.0 ** -20)) * 1.02 * spread + k.shape[1] * 2.0 ** -36 * (vmost + 0.014) + TINY
+    bound = U * want.abs() * 1.01 + (U + 2 * (reach * 1120 * V + 2.0 ** -20)) * 1.02 * spread + k.shape[1] * 2.0 ** -33 * (vmost + 0.014) + TINY
     err = (y.double().view_as(want) - want).abs()
     assert bool((err <= bound).all()), float((err - bound).max())
 
@@ -642,7 +642,7 @@ def test_serving_with_forks_and_windows(S):
                 # most) and values
                 reach = scale * (q[part].double().abs().sum(-1) * 7.0)[..., None]
                 moved = 2.0 ** -15
-                bound = U * want.abs() * 1.01 + (U + 2 * (reach * 1120 * V + scale * q[part].double().abs().sum(-1)[..., None] * moved + 2.0 ** -20)) * 1.02 * spread + T * 2.0 ** -36 * 7.1 + moved + TINY
+                bound = U * want.abs() * 1.01 + (U + 2 * (reach * 1120 * V + scale * q[part].double().abs().sum(-1)[..., None] * moved + 2.0 ** -20)) * 1.02 * spread + T * 2.0 ** -33 * 7.1 + moved + TINY
                 err = (y[part].double().view_as(want) - want).abs()
                 assert bool((err <= bound).all()), (layer, r, float((err - bound).max()))
 
