@@ -96,25 +96,34 @@ __device__ __forceinline__ uint4 transpose_words(uint32_t a, uint32_t b, uint32_
     return make_uint4(a, b, c, d);
 }
 
-// Four values of a row as fp16 numbers within the cache's range.
+// Four values of a row, as they are.
+template <typename T> struct Four { uint2 v; };
+template <> struct Four<float> { uint4 v; };
 template <typename T, bool kWide>
-__device__ __forceinline__ uint2 load_four(const T* at) {
-    uint2 r;
+__device__ __forceinline__ Four<T> load_four(const T* at) {
+    Four<T> r;
     if constexpr (sizeof(T) == 2) {
-        if constexpr (kWide) r = *reinterpret_cast<const uint2*>(at);
-        else {
-            const unsigned short* u = reinterpret_cast<const unsigned short*>(at);
-            r = make_uint2(u[0] | static_cast<uint32_t>(u[1]) << 16, u[2] | static_cast<uint32_t>(u[3]) << 16);
-        }
+        const unsigned short* u = reinterpret_cast<const unsigned short*>(at);
+        if constexpr (kWide) r.v = *reinterpret_cast<const uint2*>(at);
+        else r.v = make_uint2(u[0] | static_cast<uint32_t>(u[1]) << 16, u[2] | static_cast<uint32_t>(u[3]) << 16);
     } else {
-        float4 f;
-        if constexpr (kWide) f = *reinterpret_cast<const float4*>(at);
-        else f = make_float4(at[0], at[1], at[2], at[3]);
-        const __half2 a = __floats2half2_rn(f.x, f.y), b = __floats2half2_rn(f.z, f.w);
-        r = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+        const uint32_t* u = reinterpret_cast<const uint32_t*>(at);
+        if constexpr (kWide) r.v = *reinterpret_cast<const uint4*>(at);
+        else r.v = make_uint4(u[0], u[1], u[2], u[3]);
+    }
+    return r;
+}
+// The same as fp16 numbers within the cache's range.
+template <typename T>
+__device__ __forceinline__ uint2 limited(const Four<T>& x) {
+    __half2 a, b;
+    if constexpr (sizeof(T) == 2) a = *reinterpret_cast<const __half2*>(&x.v.x), b = *reinterpret_cast<const __half2*>(&x.v.y);
+    else {
+        a = __floats2half2_rn(__uint_as_float(x.v.x), __uint_as_float(x.v.y));
+        b = __floats2half2_rn(__uint_as_float(x.v.z), __uint_as_float(x.v.w));
     }
     const __half2 top = __float2half2_rn(kMost), bottom = __float2half2_rn(-kMost);
-    const __half2 a = __hmax2(__hmin2(*reinterpret_cast<const __half2*>(&r.x), top), bottom), b = __hmax2(__hmin2(*reinterpret_cast<const __half2*>(&r.y), top), bottom);
+    a = __hmax2(__hmin2(a, top), bottom), b = __hmax2(__hmin2(b, top), bottom);
     return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
@@ -132,14 +141,20 @@ __device__ __forceinline__ void store_side(const T* x, int64_t ld, __half* value
     if (old > 0 && cell != nullptr) scale_old = *reinterpret_cast<const float*>(cell + 2 * kCell * kDim + (is_v ? 4 : 0));
 #pragma unroll
     for (int l = 0; l < kLoops; ++l) {
+        Four<T> raw[kTs][4];                                    // all on their way before the first is looked at
 #pragma unroll
         for (int t = 0; t < kTs; ++t) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = token(t, i);
-                f[l][t][i] = make_uint2(0, 0);
-                if (r >= old && r < end) f[l][t][i] = load_four<T, kWide>(x + (row0 + r) * ld + 128 * l + d0);
+                raw[t][i] = {};
+                if (r >= old && r < end) raw[t][i] = load_four<T, kWide>(x + (row0 + r) * ld + 128 * l + d0);
             }
+        }
+#pragma unroll
+        for (int t = 0; t < kTs; ++t) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[l][t][i] = limited<T>(raw[t][i]);
         }
     }
 #pragma unroll
@@ -246,18 +261,29 @@ __global__ void __launch_bounds__(32 * kStoreWarps) kv8_store_kernel(const Store
     const int h = static_cast<int>(item % p.heads);
     const bool is_v = item / p.heads % 2 != 0;
     const int64_t begin = item / p.heads / 2 * p.chunk;
-    const int stop = static_cast<int>(begin + p.chunk < p.N ? begin + p.chunk : p.N);
+    const int stop = static_cast<int>(begin + p.chunk < p.N ? begin + p.chunk : p.N), lane = threadIdx.x & 31;
+    // up to 31 requests, a lane knows where one begins and how long it is: what a warp waits for one load after another, not the requests'
+    // number of them, is most of its time
+    const bool few = p.first != nullptr && p.B < 32;
+    int lane_first = 0, lane_length = 0;
+    if (few) lane_first = clamped(p.first[min(lane, p.B)], p.N), lane_length = p.length[min(lane, p.B - 1)];
     for (int n = static_cast<int>(begin); n < stop;) {
-        int b = n, first = n, last = n + 1;                     // the request's tokens: first .. last - 1
-        if (p.first != nullptr) {
-            b = request_of_token(p.first, p.B, n);
-            first = clamped(p.first[b], p.N), last = clamped(p.first[b + 1], p.N);
-            if (first > n || last <= n) {                       // a token of no request
-                ++n;
-                continue;
+        int b = n, first = n, last = n + 1, length;             // the request's tokens: first .. last - 1
+        if (few) {
+            b = max(31 - __clz(__ballot_sync(0xFFFFFFFFu, lane < p.B && lane_first <= n)), 0);
+            first = __shfl_sync(0xFFFFFFFFu, lane_first, b), last = __shfl_sync(0xFFFFFFFFu, lane_first, b + 1), length = __shfl_sync(0xFFFFFFFFu, lane_length, b);
+        } else {
+            if (p.first != nullptr) {
+                b = request_of_token(p.first, p.B, n);
+                first = clamped(p.first[b], p.N), last = clamped(p.first[b + 1], p.N);
             }
+            length = p.length[b];
         }
-        const int place = clamped(p.length[b], p.most_cells * kCell) - (last - n);     // the token's among its request's keys
+        if (first > n || last <= n) {                           // a token of no request
+            ++n;
+            continue;
+        }
+        const int place = clamped(length, p.most_cells * kCell) - (last - n);          // the token's among its request's keys
         const int old = place < 0 ? place : place % kCell;
         if (old < 0 || (old > 0 && n != first)) {               // nowhere to store it, or the warp of its cell's first new token does
             n += old < 0 ? min(-old, last - n) : min(kCell - old, last - n);
