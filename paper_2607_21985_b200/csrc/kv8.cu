@@ -113,6 +113,14 @@ __device__ __forceinline__ Four<T> load_four(const T* at) {
     }
     return r;
 }
+template <bool kWide>
+__device__ __forceinline__ void store_four(__half* at, uint2 h) {
+    if constexpr (kWide) *reinterpret_cast<uint2*>(at) = h;
+    else {
+        unsigned short* u = reinterpret_cast<unsigned short*>(at);
+        u[0] = static_cast<unsigned short>(h.x), u[1] = static_cast<unsigned short>(h.x >> 16), u[2] = static_cast<unsigned short>(h.y), u[3] = static_cast<unsigned short>(h.y >> 16);
+    }
+}
 // The same as fp16 numbers within the cache's range.
 template <typename T>
 __device__ __forceinline__ uint2 limited(const Four<T>& x) {
@@ -135,6 +143,32 @@ __device__ __forceinline__ void store_side(const T* x, int64_t ld, __half* value
     constexpr int kLanes = kDim == 64 ? 16 : 32, kTs = 4 * kLanes / 32, kLoops = kDim > 128 ? kDim / 128 : 1;
     const int lane = threadIdx.x & 31, part = lane / kLanes, d0 = 4 * (lane % kLanes);
     auto token = [&](int t, int i) { return 2 * (part * kTs + t) + (i & 1) + 8 * (i >> 1); };
+    if (end == old + 1 && old > 0 && cell != nullptr) {         // one token behind others, whose scale is usually large enough: only its own bytes
+        const float scale = *reinterpret_cast<const float*>(cell + 2 * kCell * kDim + (is_v ? 4 : 0));
+        uint2 f[kLoops];
+        __half2 most = __float2half2_rn(0.0f);
+#pragma unroll
+        for (int l = 0; l < kLoops; ++l) {
+            f[l] = limited<T>(load_four<T, kWide>(x + (row0 + old) * ld + 128 * l + d0));
+            most = __hmax2(most, __hmax2(__habs2(*reinterpret_cast<const __half2*>(&f[l].x)), __habs2(*reinterpret_cast<const __half2*>(&f[l].y))));
+        }
+        const uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, max(static_cast<uint32_t>(__half_as_ushort(__low2half(most))), static_cast<uint32_t>(__half_as_ushort(__high2half(most)))));
+        if (scale_for(__half2float(__ushort_as_half(static_cast<unsigned short>(bits)))) <= scale) {
+            if (part > 0) return;                               // the other half of the warp has the same dimensions
+#pragma unroll
+            for (int l = 0; l < kLoops; ++l) {
+                const int d = 128 * l + d0;
+                const uint32_t c = codes_of(f[l], __float2half2_rn(1.0f / scale));
+                if (!is_v) *reinterpret_cast<uint32_t*>(cell + d / 64 * 1024 + old * 64 + d % 64) = c;
+                else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) cell[kCell * kDim + value_place(old, d + j)] = static_cast<unsigned char>(c >> 8 * j);
+                }
+                if (values != nullptr) store_four<kWide>(values + (row0 + old) * ld_values + d, halves_of(c, __float2half2_rn(scale)));
+            }
+            return;
+        }
+    }
     uint2 f[kLoops][kTs][4];
     __half2 most = __float2half2_rn(0.0f);
     float scale_old = 0.0f;
@@ -185,13 +219,7 @@ __device__ __forceinline__ void store_side(const T* x, int64_t ld, __half* value
                 const int r = token(t, i);
                 c[t][i] = codes_of(f[l][t][i], down);
                 if (values != nullptr && r >= old && r < end) {
-                    const uint2 h = halves_of(c[t][i], up);
-                    __half* to = values + (row0 + r) * ld_values + 128 * l + d0;
-                    if constexpr (kWide) *reinterpret_cast<uint2*>(to) = h;
-                    else {
-                        unsigned short* u = reinterpret_cast<unsigned short*>(to);
-                        u[0] = static_cast<unsigned short>(h.x), u[1] = static_cast<unsigned short>(h.x >> 16), u[2] = static_cast<unsigned short>(h.y), u[3] = static_cast<unsigned short>(h.y >> 16);
-                    }
+                    store_four<kWide>(values + (row0 + r) * ld_values + 128 * l + d0, halves_of(c[t][i], up));
                 }
             }
         }
