@@ -790,7 +790,7 @@ spdp_status launch_form(AttnParams p, int device, int sms, cudaStream_t s) {
     p.open = reinterpret_cast<int4*>(static_cast<char*>(scratch) + sums + stats);
     cudaError_t e = launch_programmatic(kv8_attn_kernel<kChunks, kCols>, dim3(static_cast<unsigned>(ctas)), kThreads, line_bytes<kChunks, kCols>(p.B), s, p);
     if (e == cudaSuccess)
-        e = launch_programmatic(attn_join_kernel<kDim, kRows>, dim3(static_cast<unsigned>(places), static_cast<unsigned>(most_rows < kRows ? most_rows : kRows)), kJoinThreads, 0, s, p);
+        e = launch_programmatic(ctas >= kJoinFew * places ? attn_join_few_kernel<kDim, kRows> : attn_join_kernel<kDim, kRows>, dim3(static_cast<unsigned>(places), static_cast<unsigned>(most_rows < kRows ? most_rows : kRows)), kJoinThreads, 0, s, p);
     const cudaError_t freed = cudaFreeAsync(scratch, s);
     SPDP_CUDA_TRY(e);
     SPDP_CUDA_TRY(freed);

@@ -226,6 +226,78 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParam
     store_result(p, r.n0 + mine_row / p.group, static_cast<int64_t>(h * p.group + mine_row % p.group) * kDim + d, sum, wt);
 }
 
+// The same for few triples of many sums each, where it is all latency: the first kAhead sums of a group are asked for together with
+// all maxima.  Taken from kJoinFew CTAs to a triple on (measured on the like of it in kv4.cu).
+constexpr int kJoinFew = 16;
+constexpr int kJoinChunk = kJoinThreads;                        // sums whose maxima and weights are in shared memory at a time
+
+template <int kDim, int kRows>
+__global__ void __launch_bounds__(kJoinThreads) attn_join_few_kernel(const AttnParams p) {
+    constexpr int kLanes = kDim / 4, kParts = kJoinThreads / kLanes, kAhead = 12;
+    __shared__ __align__(16) float part[kParts][kDim];
+    __shared__ float2 stats[kJoinChunk];
+    __shared__ float warp_tops[kJoinThreads / 32], weights[kParts];
+    dev::programmatic_start();
+    const int4 open = p.open[blockIdx.x];
+    if (open.x < 0) return;
+    const Request r = request_of(p, open.x);
+    const int h = open.y / p.most_blocks, row = blockIdx.y, mine_row = open.y % p.most_blocks * kRows + row;
+    if (mine_row >= r.n * p.group) return;
+    const int at = threadIdx.x % kLanes, mine = threadIdx.x / kLanes, count = open.w - open.z / 2 + 1;
+    auto place = [&](int i) { return (i == 0 ? open.z : 2 * (open.z / 2 + static_cast<int64_t>(i))) * kRows + row; };
+    auto sum_at = [&](int i) { return *reinterpret_cast<const float4*>(p.sums + place(i) * kDim + 4 * at); };
+    float4 ahead[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+        if (mine + j * kParts < count) ahead[j] = sum_at(mine + j * kParts);
+    float m = kLowest, wt = 0.0f;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto add = [&](float4 v, float2 st) {
+        const float f = exp2_of(st.x - m);
+        sum.x += v.x * f, sum.y += v.y * f, sum.z += v.z * f, sum.w += v.w * f;
+        wt += st.y * f;
+    };
+    for (int i0 = 0; i0 < count; i0 += kJoinChunk) {
+        const int n = min(kJoinChunk, count - i0);
+        float top = m;
+        for (int i = threadIdx.x; i < n; i += kJoinThreads) {
+            stats[i] = p.stats[place(i0 + i)];
+            top = fmaxf(top, stats[i].x);
+        }
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+        if (threadIdx.x % 32 == 0) warp_tops[threadIdx.x / 32] = top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kJoinThreads / 32; ++i) top = fmaxf(top, warp_tops[i]);
+        const float f = exp2_of(m - top);
+        sum.x *= f, sum.y *= f, sum.z *= f, sum.w *= f, wt *= f, m = top;
+        int i = mine;
+        if (i0 == 0) {
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j, i += kParts)
+                if (i < n) add(ahead[j], stats[i]);
+        }
+#pragma unroll 4
+        for (; i < n; i += kParts) add(sum_at(i0 + i), stats[i]);
+        __syncthreads();                                        // before the next maxima take their place
+    }
+    *reinterpret_cast<float4*>(&part[mine][4 * at]) = sum;
+    if (at == 0) weights[mine] = wt;
+    __syncthreads();
+    const int d = 4 * threadIdx.x;
+    if (d >= kDim) return;
+    wt = 0.0f;
+    sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+        const float4 v = *reinterpret_cast<const float4*>(&part[i][d]);
+        wt += weights[i];
+        sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+    }
+    store_result(p, r.n0 + mine_row / p.group, static_cast<int64_t>(h * p.group + mine_row % p.group) * kDim + d, sum, wt);
+}
+
 }  // namespace kv8
 
 // kv8_prompt.cu: the requests with a.low_rows rows and more.
