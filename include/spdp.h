@@ -425,7 +425,7 @@ SPDP_API spdp_status spdp_kv_pages_free(void* ref_dev, int64_t pages, void* tabl
 /* Row child[i] becomes a request with the first length[i] tokens of row parent[i]: full pages (of page_tokens, a power of two, 1 .. 2^16) are shared, a last,
  * partly filled one is copied to a free page (the lowest to the first i) in all layers.  Entries behind these stay as they were.  Where the parent
  * has no page the child gets -1; so it does where there is no free page for a copy, and short_dev_out (int32 [1], or NULL) gets
- * the number of these.  Children are distinct rows that are no parents, whose first entries name no pages.  Two kernels, some KB of scratch memory. */
+ * the number of these.  Children are distinct rows that are no parents, whose first entries name no pages.  Two kernels. */
 SPDP_API spdp_status spdp_kv_pages_fork(void* cache_dev, int layers, int64_t layer_stride, int64_t page_bytes, void* ref_dev, int64_t pages, void* table_dev, int64_t rows,
                            int64_t table_stride, int64_t table_pages, int page_tokens, const void* parent_dev, const void* child_dev, const void* length_dev, int64_t n,
                            void* short_dev_out, void* stream);
@@ -436,8 +436,8 @@ SPDP_API spdp_status spdp_kv_pages_copy(void* cache_dev, int layers, int64_t lay
                            void* stream);
 
 /* Brings the pages in use together: with `live` of them, the i-th free page below `live` gets the i-th page in use from `live` on, in all layers, counts and table
- * entries (of all rows) with it.  live_dev_out (int32 [1], or NULL) gets their number: the pages from there on are free.  Three
- * kernels, 8 bytes of scratch memory to a page. */
+ * entries (of all rows) with it.  live_dev_out (int32 [1], or NULL) gets their number: the pages from there on are free.  Two
+ * or three kernels, 8 bytes of scratch memory to a page. */
 SPDP_API spdp_status spdp_kv_pages_compact(void* cache_dev, int layers, int64_t layer_stride, int64_t page_bytes, void* ref_dev, int64_t pages, void* table_dev, int64_t rows,
                            int64_t table_stride, int64_t table_pages, void* live_dev_out, void* stream);
 

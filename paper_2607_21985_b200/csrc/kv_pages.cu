@@ -148,44 +148,48 @@ __global__ void __launch_bounds__(256) free_kernel(int32_t* ref, int pages, Tabl
 
 constexpr size_t kGiveBytes = (kMostRequests + kWarps + 1) * sizeof(int64_t) + kRun * sizeof(int32_t);
 
-// Block 0 takes pages for the children's last pages and writes down what is to be copied; the others share the full ones.
-__global__ void __launch_bounds__(kThreads) fork_kernel(int32_t* ref, int pages, Table t, const int32_t* parent, const int32_t* child, const int32_t* length, int n, int page_shift,
-                                                        int32_t* src, int32_t* dst, int32_t* short_out) {
+struct Forks {
+    const int32_t* parent;
+    const int32_t* child;
+    const int32_t* length;
+    int n, page_shift;
+    __device__ __forceinline__ bool exists(const Table& t, int i) const { return parent[i] >= 0 && parent[i] < t.rows && child[i] >= 0 && child[i] < t.rows; }
+    __device__ __forceinline__ int tokens(const Table& t, int i) const {
+        const int64_t most = static_cast<int64_t>(t.pages) << page_shift;
+        return static_cast<int>(length[i] < 0 ? 0 : length[i] < most ? length[i] : most);
+    }
+    __device__ __forceinline__ bool partly(int tokens) const { return (tokens & ((1 << page_shift) - 1)) != 0; }
+};
+
+// Block 0 takes pages for the children's last pages; the others share the full ones.
+__global__ void __launch_bounds__(kThreads) fork_kernel(int32_t* ref, int pages, Table t, const Forks f, int32_t* short_out) {
     extern __shared__ int64_t start[];                          // [kMostRequests], then what give_pages() wants
     int64_t* sums = start + kMostRequests;
     int32_t* found = reinterpret_cast<int32_t*>(sums + kWarps + 1);
     dev::programmatic_start();
-    auto exists = [&](int i) { return parent[i] >= 0 && parent[i] < t.rows && child[i] >= 0 && child[i] < t.rows; };
-    const int64_t most = static_cast<int64_t>(t.pages) << page_shift;
-    auto tokens = [&](int i) { return static_cast<int>(length[i] < 0 ? 0 : length[i] < most ? length[i] : most); };
     if (blockIdx.x > 0) {
-        for (int i = blockIdx.x - 1; i < n; i += gridDim.x - 1) {
-            if (!exists(i)) continue;
-            const int full = tokens(i) >> page_shift;
+        for (int i = blockIdx.x - 1; i < f.n; i += gridDim.x - 1) {
+            if (!f.exists(t, i)) continue;
+            const int full = f.tokens(t, i) >> f.page_shift;
             for (int e = threadIdx.x; e < full; e += kThreads) {
-                const int page = t.entries[parent[i] * t.stride + e];
+                const int page = t.entries[f.parent[i] * t.stride + e];
                 const bool ok = page >= 0 && page < pages;
-                t.entries[child[i] * t.stride + e] = ok ? page : -1;
+                t.entries[f.child[i] * t.stride + e] = ok ? page : -1;
                 if (ok) atomicAdd(&ref[page], 1);
             }
         }
         return;
     }
-    auto last_page = [&](int i) {                               // the parent's partly filled page, or -1
-        if (!exists(i) || (tokens(i) & ((1 << page_shift) - 1)) == 0) return -1;
-        const int page = t.entries[parent[i] * t.stride + (tokens(i) >> page_shift)];
-        return page >= 0 && page < pages ? page : -1;
-    };
-    const int64_t wanted = starts_of(n, start, sums, [&](int i) -> int64_t {
-        const int page = last_page(i);
-        src[i] = page, dst[i] = -1;
-        if (page < 0 && exists(i) && (tokens(i) & ((1 << page_shift) - 1)) != 0) t.entries[child[i] * t.stride + (tokens(i) >> page_shift)] = -1;
-        return page >= 0 ? 1 : 0;
+    const int64_t wanted = starts_of(f.n, start, sums, [&](int i) -> int64_t {
+        if (!f.exists(t, i) || !f.partly(f.tokens(t, i))) return 0;
+        const int e = f.tokens(t, i) >> f.page_shift, page = t.entries[f.parent[i] * t.stride + e];
+        if (page >= 0 && page < pages) return 1;
+        t.entries[f.child[i] * t.stride + e] = -1;
+        return 0;
     });
     const int64_t missing = give_pages(ref, pages, wanted, sums, found, [&](int64_t place, int page) {
-        const int i = owner_of(start, n, place);
-        t.entries[child[i] * t.stride + (tokens(i) >> page_shift)] = page;
-        dst[i] = page;
+        const int i = owner_of(start, f.n, place);
+        t.entries[f.child[i] * t.stride + (f.tokens(t, i) >> f.page_shift)] = page;
     });
     if (short_out != nullptr && threadIdx.x == 0) *short_out = static_cast<int>(missing);
 }
@@ -200,14 +204,15 @@ struct Pages {
 constexpr int kMoveThreads = 256, kMoveLoads = 4;
 constexpr int kPiece = 32 * kMoveLoads * 16;                    // bytes that a warp moves at a time
 
-// Pages src[i] to dst[i], i < n, in all layers; pairs of which one is no page are left out.  Every `warps`-th piece of a page is the warp's: the place of the
+// Pages from_page(i) to to_page(i), i < n, in all layers; pairs of which one is no page are left out.  Every `warps`-th piece of a page is the warp's: the place of the
 // next one by additions with carries, not by divisions.
-__device__ __forceinline__ void move_pages(const Pages& p, const int32_t* src, const int32_t* dst, int64_t n, int64_t warp, int64_t warps) {
+template <typename From, typename To>
+__device__ __forceinline__ void move_pages(const Pages& p, From from_page, To to_page, int64_t n, int64_t warp, int64_t warps) {
     const int64_t pieces = (p.page_bytes + kPiece - 1) / kPiece, of_pair = pieces * p.layers;
     int64_t i = warp / of_pair, layer = warp % of_pair / pieces, piece = warp % pieces;
     const int64_t step_i = warps / of_pair, step_layer = warps % of_pair / pieces, step_piece = warps % pieces;
     for (; i < n;) {
-        const int a = src[i], b = dst[i];
+        const int a = from_page(i), b = to_page(i);
         if (a >= 0 && a < p.pages && b >= 0 && b < p.pages && a != b) {
             const int64_t at = piece * kPiece + 16 * (threadIdx.x & 31);
             const unsigned char* from = p.cache + layer * p.layer_stride + a * p.page_bytes + at;
@@ -225,10 +230,20 @@ __device__ __forceinline__ void move_pages(const Pages& p, const int32_t* src, c
         if (layer >= p.layers) layer -= p.layers, ++i;
     }
 }
+constexpr int kMoveWarps = kMoveThreads / 32;
+__device__ __forceinline__ int64_t my_warp() { return static_cast<int64_t>(blockIdx.x) * kMoveWarps + (threadIdx.x >> 5); }
 __global__ void __launch_bounds__(kMoveThreads) copy_kernel(const Pages p, const int32_t* src, const int32_t* dst, int64_t n) {
     dev::programmatic_start();
-    constexpr int kWarpsOf = kMoveThreads / 32;
-    move_pages(p, src, dst, n, static_cast<int64_t>(blockIdx.x) * kWarpsOf + (threadIdx.x >> 5), static_cast<int64_t>(gridDim.x) * kWarpsOf);
+    move_pages(p, [&](int64_t i) { return src[i]; }, [&](int64_t i) { return dst[i]; }, n, my_warp(), static_cast<int64_t>(gridDim.x) * kMoveWarps);
+}
+// The partly filled pages of forks: where they come from and go to stands in the table.
+__global__ void __launch_bounds__(kMoveThreads) copy_forks_kernel(const Pages p, const Table t, const Forks f) {
+    dev::programmatic_start();
+    auto entry = [&](const int32_t* row, int64_t i64) {
+        const int i = static_cast<int>(i64), n = f.exists(t, i) ? f.tokens(t, i) : 0;
+        return f.partly(n) ? t.entries[row[i] * t.stride + (n >> f.page_shift)] : -1;
+    };
+    move_pages(p, [&](int64_t i) { return entry(f.parent, i); }, [&](int64_t i) { return entry(f.child, i); }, f.n, my_warp(), static_cast<int64_t>(gridDim.x) * kMoveWarps);
 }
 unsigned move_ctas(const Pages& p, int64_t pairs, int sms) {
     const int64_t all = (pairs * p.layers * ((p.page_bytes + kPiece - 1) / kPiece) + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
@@ -237,27 +252,27 @@ unsigned move_ctas(const Pages& p, int64_t pairs, int sms) {
 
 // ---- bringing together
 //
-// With `live` pages in use, the i-th free page below `live` gets the i-th page in use from there on.  The pages are cut into kSegments
-// runs: a first kernel counts each run's pages in use, a second has every run's place from these counts and writes the two lists, a third
-// moves and renames.
+// With `live` pages in use, the i-th free page below `live` gets the i-th page in use from there on.  The pages are cut into runs, a CTA to each, up to
+// kMostRuns of them.  Every run's place follows from the counts of all of them: a kernel of their own finds these where the pages are
+// more than kCountPages; else each CTA looks at all pages itself.  A last kernel moves and renames.
 
-constexpr int kSegments = 1024;
+constexpr int kMostRuns = 1024, kRunPages = 1024, kCountPages = 16384;
 constexpr int kListThreads = 256;
 struct Lists {
-    int32_t* counts;                    // [kSegments] pages in use
+    int32_t* counts;                    // [runs] pages in use; null: not counted
     int32_t* place;                     // [pages] of the pages from `live` on: the one's place in the lists, or -1
     int32_t* src;                       // [pages / 2] pages to move
     int32_t* dst;                       // [pages / 2] and where to
-    int32_t* moved;                     // how many
+    int32_t* moved;                     // how many, and behind it: pages in use
+    int run, runs;                      // pages of a run
 };
-__device__ __forceinline__ int segment_length(int pages) { return (pages + kSegments - 1) / kSegments; }
 
 __global__ void __launch_bounds__(kListThreads) count_kernel(const int32_t* ref, int pages, Lists l) {
     __shared__ int count;
     dev::programmatic_start();
     if (threadIdx.x == 0) count = 0;
     __syncthreads();
-    const int64_t begin = static_cast<int64_t>(blockIdx.x) * segment_length(pages), end = min(begin + segment_length(pages), static_cast<int64_t>(pages));
+    const int64_t begin = static_cast<int64_t>(blockIdx.x) * l.run, end = min(begin + l.run, static_cast<int64_t>(pages));
     int mine = 0;
     for (int64_t i = begin + threadIdx.x; i < end; i += kListThreads) mine += ref[i] > 0 ? 1 : 0;
     mine = __reduce_add_sync(kAll, mine);
@@ -280,22 +295,32 @@ __device__ __forceinline__ int block_sum(int mine, int* word) {
 __global__ void __launch_bounds__(kListThreads) list_kernel(const int32_t* ref, int pages, Lists l, int32_t* live_out) {
     __shared__ int word, warp_counts[kListThreads / 32];
     dev::programmatic_start();
-    const int length = segment_length(pages);
-    const int64_t begin = static_cast<int64_t>(blockIdx.x) * length, end = min(begin + length, static_cast<int64_t>(pages));
-    int all = 0, before = 0;
-    for (int i = threadIdx.x; i < kSegments; i += kListThreads) {
-        all += l.counts[i];
-        if (i < blockIdx.x) before += l.counts[i];
+    const int64_t begin = static_cast<int64_t>(blockIdx.x) * l.run, end = min(begin + l.run, static_cast<int64_t>(pages));
+    int all = 0, before = 0, below = 0, live;                   // pages in use: all of them, before this run, below `live`
+    if (l.counts != nullptr) {
+        for (int i = threadIdx.x; i < l.runs; i += kListThreads) {
+            all += l.counts[i];
+            if (i < blockIdx.x) before += l.counts[i];
+        }
+        live = block_sum(all, &word);
+        const int cut = live / l.run;
+        for (int i = threadIdx.x; i < cut; i += kListThreads) below += l.counts[i];
+        for (int64_t i = static_cast<int64_t>(cut) * l.run + threadIdx.x; i < live; i += kListThreads) below += ref[i] > 0 ? 1 : 0;
+    } else {
+#pragma unroll 8
+        for (int i = threadIdx.x; i < pages; i += kListThreads) {
+            const int used = ref[i] > 0 ? 1 : 0;
+            all += used;
+            if (i < begin) before += used;
+        }
+        live = block_sum(all, &word);
+#pragma unroll 8
+        for (int i = threadIdx.x; i < live; i += kListThreads) below += ref[i] > 0 ? 1 : 0;
     }
-    const int live = block_sum(all, &word);
-    before = block_sum(before, &word);                          // pages in use before this run
-    int below = 0;                                              // and below `live`
-    const int cut = live / length;
-    for (int i = threadIdx.x; i < cut; i += kListThreads) below += l.counts[i];
-    for (int64_t i = static_cast<int64_t>(cut) * length + threadIdx.x; i < live; i += kListThreads) below += ref[i] > 0 ? 1 : 0;
+    before = block_sum(before, &word);
     below = block_sum(below, &word);
     if (blockIdx.x == 0 && threadIdx.x == 0) {
-        *l.moved = live - below;
+        l.moved[0] = live - below, l.moved[1] = live;
         if (live_out != nullptr) *live_out = live;
     }
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
@@ -327,13 +352,10 @@ __global__ void __launch_bounds__(kMoveThreads) compact_kernel(const Pages p, in
     dev::programmatic_start();
     const int moved = *l.moved, movers = static_cast<int>(gridDim.x) - renamers;
     if (static_cast<int>(blockIdx.x) < movers) {
-        move_pages(p, l.src, l.dst, moved, static_cast<int64_t>(blockIdx.x) * (kMoveThreads / 32) + (threadIdx.x >> 5), static_cast<int64_t>(movers) * (kMoveThreads / 32));
+        move_pages(p, [&](int64_t i) { return l.src[i]; }, [&](int64_t i) { return l.dst[i]; }, moved, my_warp(), static_cast<int64_t>(movers) * kMoveWarps);
         return;
     }
-    __shared__ int word;
-    int all = 0;
-    for (int i = threadIdx.x; i < kSegments; i += kMoveThreads) all += l.counts[i];
-    const int live = block_sum(all, &word);
+    const int live = l.moved[1];
     const int64_t at = static_cast<int64_t>(blockIdx.x - movers) * kMoveThreads + threadIdx.x, step = static_cast<int64_t>(renamers) * kMoveThreads;
     for (int64_t i = at; i < moved; i += step) {
         ref[l.dst[i]] = ref[l.src[i]];
@@ -393,22 +415,14 @@ spdp_status launch_kv_pages_copy(const KvPagesCall& c, cudaStream_t s) {
 
 spdp_status launch_kv_pages_fork(const KvPagesCall& c, cudaStream_t s) {
     int device = 0, sms = 0;
-    spdp_status st = ready(&device, &sms);
+    const spdp_status st = ready(&device, &sms);
     if (st != SPDP_OK) return st;
-    void* scratch = nullptr;
-    st = scratch_alloc(device, (2 * c.n + 1) * sizeof(int32_t), s, &scratch);
-    if (st != SPDP_OK) return st;
-    int32_t *src = static_cast<int32_t*>(scratch), *dst = src + c.n;
+    Forks f = {c.row, c.from, c.to, static_cast<int>(c.n), 0};
+    while ((1 << f.page_shift) < c.page_tokens) ++f.page_shift;
     const Pages p = pages_of(c);
-    int shift = 0;
-    while ((1 << shift) < c.page_tokens) ++shift;
     const unsigned sharers = static_cast<unsigned>(c.n < sms ? c.n : sms);
-    cudaError_t e = launch_programmatic(fork_kernel, dim3(1 + sharers), kThreads, kGiveBytes, s, c.ref, static_cast<int>(c.pages), table_of(c), c.row, c.from, c.to, static_cast<int>(c.n), shift, src, dst,
-                                        c.short_out);
-    if (e == cudaSuccess && c.n > 0) e = launch_programmatic(copy_kernel, dim3(move_ctas(p, c.n, sms)), kMoveThreads, 0, s, p, static_cast<const int32_t*>(src), static_cast<const int32_t*>(dst), c.n);
-    const cudaError_t freed = cudaFreeAsync(scratch, s);
-    SPDP_CUDA_TRY(e);
-    SPDP_CUDA_TRY(freed);
+    SPDP_CUDA_TRY(launch_programmatic(fork_kernel, dim3(1 + sharers), kThreads, kGiveBytes, s, c.ref, static_cast<int>(c.pages), table_of(c), f, c.short_out));
+    if (c.n > 0) SPDP_CUDA_TRY(launch_programmatic(copy_forks_kernel, dim3(move_ctas(p, c.n, sms)), kMoveThreads, 0, s, p, table_of(c), f));
     return SPDP_OK;
 }
 
@@ -418,18 +432,21 @@ spdp_status launch_kv_pages_compact(const KvPagesCall& c, cudaStream_t s) {
     if (st != SPDP_OK) return st;
     const int pages = static_cast<int>(c.pages);
     void* scratch = nullptr;
-    st = scratch_alloc(device, (kSegments + 1 + 2ll * pages + 2) * sizeof(int32_t), s, &scratch);
-    if (st != SPDP_OK) return st;
     Lists l;
-    l.counts = static_cast<int32_t*>(scratch);
-    l.moved = l.counts + kSegments;
-    l.place = l.moved + 1;
+    l.run = kRunPages * ((pages + kMostRuns * kRunPages - 1) / (kMostRuns * kRunPages)), l.runs = (pages + l.run - 1) / l.run;
+    st = scratch_alloc(device, (l.runs + 2 + 2ll * pages + 2) * sizeof(int32_t), s, &scratch);
+    if (st != SPDP_OK) return st;
+    l.moved = static_cast<int32_t*>(scratch);
+    l.place = l.moved + 2;
     l.src = l.place + pages;
     l.dst = l.src + pages / 2 + 1;
+    l.counts = pages > kCountPages ? l.dst + pages / 2 + 1 : nullptr;
     const Pages p = pages_of(c);
     const int renamers = 16;
-    cudaError_t e = launch_programmatic(count_kernel, dim3(kSegments), kListThreads, 0, s, static_cast<const int32_t*>(c.ref), pages, l);
-    if (e == cudaSuccess) e = launch_programmatic(list_kernel, dim3(kSegments), kListThreads, 0, s, static_cast<const int32_t*>(c.ref), pages, l, c.short_out);
+    const int32_t* ref = c.ref;
+    cudaError_t e = cudaSuccess;
+    if (l.counts != nullptr) e = launch_programmatic(count_kernel, dim3(static_cast<unsigned>(l.runs)), kListThreads, 0, s, ref, pages, l);
+    if (e == cudaSuccess) e = launch_programmatic(list_kernel, dim3(static_cast<unsigned>(l.runs)), kListThreads, 0, s, ref, pages, l, c.short_out);
     if (e == cudaSuccess) e = launch_programmatic(compact_kernel, dim3(move_ctas(p, pages / 2 + 1, sms) + renamers), kMoveThreads, 0, s, p, c.ref, table_of(c), l, renamers);
     const cudaError_t freed = cudaFreeAsync(scratch, s);
     SPDP_CUDA_TRY(e);
