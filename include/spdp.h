@@ -393,11 +393,13 @@ SPDP_API spdp_status spdp_kv8_store(const void* k_dev, int64_t ldk, const void* 
  *   y_dev        fp16 [N][ldy], ldy >= q_heads * head_dim.  A token that sees no key gets zeros; tokens of no request stay as they were.
  *   mask_dev_out uint32 [N][mask_stride], mask_stride >= q_heads * head_dim / 32, or NULL: the columns that the o-projection
  *                should keep, NOT(|y_j| <= thr) on the stored y, for SPDP_DP_MASK (thr is used for nothing else).
- * Refused as SPDP_ERR_UNSUPPORTED_SHAPE besides: N * q_heads of 2^31 and more, and B * kv_heads * (rows / 8, rounded up) * (table_pages * page_tokens
- * / 64 + 8) of 2^31 and more, with rows the query heads of a key head times N (times 1 where first_dev is NULL).
+ * Refused as SPDP_ERR_UNSUPPORTED_SHAPE besides: N * q_heads of 2^31 and more; with g = q_heads / kv_heads and T = table_pages * page_tokens, B * kv_heads *
+ * (r / 8, rounded up) * (T / 64 + 8) of 2^31 and more, where r is g if first_dev is NULL and else 64 or N g, whichever is less; and, with first_dev,
+ * kv_heads * (N g / 128 + B) * (T / 128 + 8) of 2^31 and more.
  * What lies in the cache behind a request's last key is never used, whatever it is.  Sums in 32 bits; the softmax's weights, times the
- * scales of the values, are rounded to fp16 for their product with these.  Launches one to four kernels, with scratch memory (up to
- * some tens of MB) unless the requests are few and short. */
+ * scales of the values, are rounded to fp16 for their product with these.  Requests of up to 64 rows (tokens times g) and longer ones are different kernels': the
+ * call launches one to five, with scratch memory (up to 40 MB on 148 SMs, and 64 bytes to 128 rows) unless the requests are few and short.  The waits inside the
+ * kernels are bounded; where one runs out, which none should, rows become NaN or stay unwritten. */
 SPDP_API spdp_status spdp_attn_kv8(const void* q_dev, int64_t ldq, int64_t N, int q_heads, int kv_heads, int head_dim, int64_t B, const void* first_dev, const void* cache_dev,
                           int64_t pages, int page_tokens, const void* table_dev, int64_t table_stride, int64_t table_pages, const void* length_dev, float scale, float cap,
                           int64_t window, int64_t sinks, float thr, void* y_dev, int64_t ldy, void* mask_dev_out, int64_t mask_stride, void* stream);

@@ -731,10 +731,11 @@ spdp_status spdp_attn_kv8(const void* q_dev, int64_t ldq, int64_t N, int q_heads
     if (misaligned(q_dev, 1u) || misaligned(first_dev, 3u) || misaligned(cache_dev, 15u) || misaligned(table_dev, 3u) || misaligned(length_dev, 3u) || misaligned(y_dev, 1u) ||
         misaligned(mask_dev_out, 3u))
         return SPDP_ERR_INVALID_ARG;
-    // the keys of a request, the rows of a key head and the 64-key units of all of them, with what the kernels add, are counted in 32 bits
+    // the keys of a request, the rows of all and the units of keys of all blocks of rows, with what the kernels add, are counted in 32 bits
     if (table_pages > kMostKeys / page_tokens || N > INT32_MAX / q_heads) return SPDP_ERR_UNSUPPORTED_SHAPE;
-    const int64_t tokens = first_dev == nullptr ? 1 : N, blocks = kv_heads * ((tokens * (q_heads / kv_heads) + 7) / 8);
-    if (blocks * (table_pages * page_tokens / 64 + 8) > INT32_MAX / B) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    const int64_t group = q_heads / kv_heads, keys = table_pages * page_tokens, few = first_dev == nullptr ? group : N * group < kFewRows ? N * group : kFewRows;
+    if (kv_heads * ((few + 7) / 8) * (keys / 64 + 8) > INT32_MAX / B) return SPDP_ERR_UNSUPPORTED_SHAPE;
+    if (first_dev != nullptr && kv_heads * (N * group / 128 + B) > INT32_MAX / (keys / 128 + 8)) return SPDP_ERR_UNSUPPORTED_SHAPE;
     Kv8AttnCall c = {};
     c.q = static_cast<const __half*>(q_dev), c.cache = static_cast<const unsigned char*>(cache_dev), c.first = static_cast<const int32_t*>(first_dev);
     c.table = static_cast<const int32_t*>(table_dev), c.length = static_cast<const int32_t*>(length_dev), c.y = static_cast<__half*>(y_dev), c.mask = static_cast<uint32_t*>(mask_dev_out);

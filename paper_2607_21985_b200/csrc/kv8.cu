@@ -356,7 +356,6 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kUnitCells = 4;
 constexpr int kMostRequests = 4096;
-constexpr int kFewRows = 64;            // of a request and key head, up to which this form is taken
 constexpr float kHeadroom = 12.0f;      // weights are below 2^(kHeadroom + kSlack)
 constexpr float kSlack = 2.5f;
 

@@ -28,6 +28,7 @@ constexpr int kTileRows = 128;
 constexpr int kThreads = 512;           // warps 0-3 and 4-7: softmax; 8-11: codes to operands; 12: products; 13: pieces; 14, 15: rows of q
 constexpr int kRowBytes = 128;          // of an operand tile: 64 fp16 numbers, in the 128-byte swizzle
 constexpr int kAtomBytes = 8 * kRowBytes;
+constexpr int kShortList = 192, kShortRequests = 32;     // up to so many blocks of so many requests each CTA lists itself, which saves a kernel (333 tokens of 12 and 3 heads: 24.5 -> 22.5 us)
 constexpr int kFlags = 8;               // units whose cells' existence is kept
 constexpr float kHeadroom = 8.0f, kSlack = 6.5f;       // weights are below 2^(kHeadroom + kSlack); 12 and 2.5 scale the sums anew more often: 336 -> 342 us
 // Registers of a thread by its warpgroup; with the 128 of the launch the four come to the same sum.
@@ -56,7 +57,7 @@ struct alignas(16) Block {              // of rows, and the cells with keys that
 struct PromptParams {
     AttnParams a;
     Block* blocks;
-    int* totals;                        // blocks; length of the line of one head
+    int* totals;                        // blocks; length of the line of one head; null: each CTA lists the blocks itself
     int most_list;                      // blocks that there can be
     bool negative;                      // the scale; a.scale is its size
     bool wide16;                        // rows of y on 16-byte boundaries
@@ -245,6 +246,7 @@ struct Barriers {
     uint64_t q_full[2], q_free[2], s_full[2], p_full[2][2], o_full[2], k_full[2], k_free[2], v_full[2], v_free[2], piece_full[kPieces], piece_free[kPieces], drained;
     uint32_t tmem;
     Piece pieces[kPieces];
+    Block blocks[kShortList];           // where each CTA lists them
     alignas(16) int there[kFlags][4];   // of the units' cells, two bits to a decoding warp
 };
 
@@ -261,15 +263,62 @@ __device__ __forceinline__ const Piece* piece_at(Barriers* bars, unsigned i) {
 
 // ---- pieces (a warp)
 
+// The list of blocks into this CTA's shared memory, and the first CTA's also to where the join looks: (blocks, length of the line of one head).
+template <int kRows>
+__device__ __forceinline__ int2 list_blocks(const PromptParams& p, Barriers* bars) {
+    const int lane = threadIdx.x & 31;
+    int count = 0;                                              // of the lane's request
+    if (lane < p.a.B) {
+        const Request rq = request_of(p.a, lane);
+        if (rq.cells > 0) count = (rq.n * p.a.group + kRows - 1) / kRows;
+    }
+    int up_to = count;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int v = __shfl_up_sync(0xFFFFFFFFu, up_to, d);
+        if (lane >= d) up_to += v;
+    }
+    const int total = min(__shfl_sync(0xFFFFFFFFu, up_to, 31), p.most_list);
+    int length = 0;
+    for (int base = 0; base < total; base += 32) {
+        const int i = base + lane;
+        int b = 0;                                              // the first request whose blocks go on behind i
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2)
+            if (__shfl_sync(0xFFFFFFFFu, up_to, b + d - 1) <= i) b += d;
+        b = min(b, p.a.B - 1);
+        const int first = __shfl_sync(0xFFFFFFFFu, up_to - count, b);
+        Block block = {};
+        if (i < total) block = block_of<kRows>(p.a, b, (i - first) * kRows);
+        int at = block.length;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int v = __shfl_up_sync(0xFFFFFFFFu, at, d);
+            if (lane >= d) at += v;
+        }
+        block.start = length + at - block.length;
+        length += __shfl_sync(0xFFFFFFFFu, at, 31);
+        if (i < total) {
+            bars->blocks[i] = block;
+            if (blockIdx.x == 0) p.blocks[i] = block;
+        }
+    }
+    __syncwarp();
+    return make_int2(total, length);
+}
+
+template <int kRows>
 __device__ __forceinline__ void piece_role(const PromptParams& p, Barriers* bars) {
-    const int lane = threadIdx.x & 31, n = p.totals[0], length = p.totals[1], total = length * p.a.heads, ctas = min(static_cast<int>(gridDim.x), total);
+    const int2 list = p.totals != nullptr ? make_int2(p.totals[0], p.totals[1]) : list_blocks<kRows>(p, bars);
+    const Block* const blocks = p.totals != nullptr ? p.blocks : bars->blocks;
+    const int lane = threadIdx.x & 31, n = list.x, length = list.y, total = length * p.a.heads, ctas = min(static_cast<int>(gridDim.x), total);
     int u = 0, stop = 0, index = 0, h = 0;
     if (static_cast<int>(blockIdx.x) < ctas) {
         u = run_start(total, ctas, blockIdx.x), stop = run_start(total, ctas, blockIdx.x + 1);
         h = u / length;
         const int v = u % length;
         for (int count = n; count > 1;) {                       // the last of the blocks index .. index + count - 1 that does not begin behind v
-            const int step = (count + 31) / 32, last = 31 - __clz(__ballot_sync(0xFFFFFFFFu, lane * step < count && p.blocks[index + lane * step].start <= v));
+            const int step = (count + 31) / 32, last = 31 - __clz(__ballot_sync(0xFFFFFFFFu, lane * step < count && blocks[index + lane * step].start <= v));
             const int end = index + count;
             index += last * step, count = min(step, end - index);
         }
@@ -279,7 +328,7 @@ __device__ __forceinline__ void piece_role(const PromptParams& p, Barriers* bars
         Piece s;
         s.count = 0;
         while (u < stop && s.count <= 0) {
-            s.block = p.blocks[index];
+            s.block = blocks[index];
             const int start = h * length + s.block.start;
             s.off = max(0, u - start - kStart), s.count = max(0, min(s.block.length, stop - start) - kStart) - s.off;
             s.index = index, s.h = h, s.whole = s.count == s.block.length - kStart;
@@ -768,7 +817,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_prompt_kernel(const __grid_co
             if (elect_one()) product_role<kDim>(p, bars, queries, keys, values, tmem);
             __syncwarp();
         } else if (warp == 13) {
-            piece_role(p, bars);
+            piece_role<F::kRows>(p, bars);
             const int columns = p.a.heads * p.a.group * kDim;
             for (int b = blockIdx.x; b < p.a.B; b += gridDim.x) {       // tokens of requests without keys
                 const Request rq = request_of(p.a, b);
@@ -844,7 +893,9 @@ spdp_status launch_form(PromptParams p, int device, int sms, cudaStream_t s) {
     char* at = static_cast<char*>(scratch);
     p.a.sums = reinterpret_cast<float*>(at), p.a.stats = reinterpret_cast<float2*>(at + sums), p.a.open = reinterpret_cast<int4*>(at + sums + stats);
     p.blocks = reinterpret_cast<Block*>(at + sums + stats + open), p.totals = reinterpret_cast<int*>(p.blocks + p.most_list);
-    cudaError_t e = launch_programmatic(kv8_blocks_kernel<F::kRows>, dim3(1), kListThreads, 0, s, p);
+    cudaError_t e = cudaSuccess;
+    if (p.a.B <= kShortRequests && p.most_list <= kShortList) p.totals = nullptr;
+    else e = launch_programmatic(kv8_blocks_kernel<F::kRows>, dim3(1), kListThreads, 0, s, p);
     if (e == cudaSuccess) e = launch_programmatic(kv8_prompt_kernel<kDim, kCap>, dim3(static_cast<unsigned>(sms)), kThreads, kShared, s, p);
     if (e == cudaSuccess) e = launch_programmatic(kv8_prompt_join_kernel<kDim>, dim3(static_cast<unsigned>(sms), F::kRows / kJoinWarps), 32 * kJoinWarps, 0, s, p);
     const cudaError_t freed = cudaFreeAsync(scratch, s);

@@ -55,7 +55,7 @@ __device__ __forceinline__ int within(int v, int most) { return v < 0 ? 0 : v < 
 
 // Free pages, lowest first, to the places 0 .. wanted - 1: give(place, page) for each, page -1 where there are no more.  One CTA, which first brings
 // the pages of a run together, in `found` (kRun words), so that the places are served side by side (200 places on 6000 pages: 14.8 us where each
-// thread served what it had found, XX this way).
+// thread served what it had found, 6.9 this way).
 constexpr int kAhead = 8;               // pages of a lane that are looked at at once
 constexpr int kRun = kThreads * kAhead;
 template <typename Give>

@@ -242,6 +242,7 @@ struct Kv8AttnCall {
     int q_heads, kv_heads, head_dim, page_tokens;
     float scale, cap, thr;
 };
+constexpr int kFewRows = 64;    // tokens times query heads of a key head, up to which a request's attention is kv8.cu's and not kv8_prompt.cu's
 spdp_status launch_attn_kv8(const Kv8AttnCall& call, cudaStream_t s);
 
 // kv_pages.cu

@@ -337,6 +337,43 @@ def test_attn_kv8_no_numbers(S, tokens):
     assert torch.equal(y, z)
 
 
+@pytest.mark.parametrize("scale", [-0.11, 0.0, 1e-20])
+@pytest.mark.parametrize("tokens", [1, 6, 80])
+def test_attn_kv8_scales_below_and_at_zero(S, tokens, scale):
+    rng = np.random.default_rng(13)
+    table, oracle = filled(rng, 2, 128, 16, [120, 90])
+    first = starts([tokens, 1])
+    wide = torch.full((2, table.shape[1] + 5), 10 ** 6, dtype=torch.int32, device="cuda")          # rows of the table apart
+    wide[:, :table.shape[1]] = dev(table)
+    q, y = dev(rng.standard_normal((tokens + 1, 6, 128)).astype(np.float16)), torch.empty(tokens + 1, 768, dtype=torch.float16, device="cuda")
+    for window, sinks in ((0, 0), (30, 3)):
+        S.spdp_attn_kv8(q, dev(oracle.raw), 16, 2, wide[:, :table.shape[1]], ints(120, 90), y, scale, first=dev(first), window=window, sinks=sinks)
+        attn_check(y, q, oracle, table, first, [120, 90], scale, 0.0, window, sinks)
+
+
+def test_attn_kv8_prompt_of_many_blocks(S):
+    """More blocks of rows than a CTA lists by itself, beside requests of a few tokens and of none."""
+    heads, group, D, page = 1, 16, 64, 64
+    counts, past = [4001, 0, 2, 300], [0, 5, 70, 1000]
+    length = [n + p for n, p in zip(counts, past)]
+    each, N = -(-max(length) // page), sum(counts)
+    gen = torch.Generator(device="cuda").manual_seed(14)
+    table = torch.randperm(4 * each, generator=gen, device="cuda").view(4, each).int()
+    cache = torch.full((4 * each, S.spdp_kv8_page_bytes(heads, D, page)), 0xFF, dtype=torch.uint8, device="cuda")
+    k, v = (torch.randn(sum(length), heads, D, generator=gen, device="cuda").half() for _ in range(2))
+    kv, vv = torch.empty_like(k), torch.empty_like(v)
+    S.spdp_kv8_store(k, v, cache, page, table, ints(*length), first=dev(starts(length)), k_values=kv, v_values=vv)
+    q, y = torch.randn(N, group, D, generator=gen, device="cuda").half(), torch.empty(N, group * D, dtype=torch.float16, device="cuda")
+    S.spdp_attn_kv8(q, cache, page, heads, table, ints(*length), y, 0.125, first=dev(starts(counts)))
+    for b in (0, 2, 3):
+        n, T = counts[b], length[b]
+        some = torch.arange(0, n, 7 if b == 0 else 1, device="cuda")
+        keys = slice(starts(length)[b], starts(length)[b + 1])
+        seen = torch.arange(T, device="cuda") <= (past[b] + some)[:, None]
+        at = int(starts(counts)[b]) + some
+        device_check(y[at], q[at], kv[keys].double().transpose(0, 1), vv[keys].double().transpose(0, 1), seen, 0.125, 7.0, 7.0)
+
+
 def exact_on_device(q, k, v, seen, scale):
     """In 64 bits: q [n][H][D], k and v [kv heads][keys][D], seen [n][keys] -> (y, spread), [n][H][D]."""
     z = torch.einsum("nhgd,htd->hgnt", q.double().unflatten(1, (k.shape[0], -1)), k) * scale
