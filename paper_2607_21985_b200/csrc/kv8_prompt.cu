@@ -10,6 +10,11 @@
 // first operand of the product with the values, whose sums stay in tensor memory through the block.  While one tile's scores become
 // weights the tensor cores work on the other's.  Codes times their scale are fp16 numbers, so both operands of the first product and
 // the values of the second are exact; the weights are rounded to fp16 (2^-11, the one rounding besides the result's).
+// What bounds it: the way of a tile's scores, from the products through the softmax (some 1900 cycles a unit, 1024 of them the exponentials of
+// a scheduler's 32 rows) and back, two tiles side by side: 3700 cycles a unit of 256 rows, whose products are 2048; and the power limit, at 1.89
+// GHz.  4096 tokens of 64 and 8 heads of 128: 305 us, 0.9 PFLOP/s.  Tried and not kept: units of 64 keys with scores for two of them (384 us), a pair
+// of CTAs to 512 rows (cta_group::2, 327 us against 330, with 512 rows to a block), a thread to each tile's products (382 to 410), two threads to a
+// row (359), turns at the exponentials (340 to 381), part of them by a polynomial (376 and up).
 //
 // The order of a unit's keys is what suits the operand tiles, and the same in both: row n of the keys' tile is token 2 (n % 64 / 16) + n % 2 +
 // 8 (n % 4 / 2) of cell 4 (n / 64) + 2 (n / 8 % 2) + n / 4 % 2.  So the 8 keys of a 16-byte piece of a dimension's row of the values' tile are

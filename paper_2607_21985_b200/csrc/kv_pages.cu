@@ -3,7 +3,8 @@
 // free.  What a call does follows from these alone, page by page in their order, so the same state gives the same pages; and all of it
 // may be captured together with the steps that use the pages.
 //
-// Counting and naming are integers; what takes time is moving pages (2 bytes of traffic to each byte of a page, in every layer).
+// Counting and naming are integers; what takes time is moving pages (2 bytes of traffic to each byte of a page, in every layer): 300 pages of
+// 12 layers of 16.5 KB in 18 us, 6.6 TB/s.  Calls on few pages are the latency of a kernel's loads, one after another.
 #include <mutex>
 
 #include "kv8.cuh"
