@@ -36,10 +36,6 @@ constexpr int kAtomBytes = 8 * kRowBytes;
 constexpr int kShortList = 192, kShortRequests = 32;     // up to so many blocks of so many requests each CTA lists itself, which saves a kernel (333 tokens of 12 and 3 heads: 24.5 -> 22.5 us)
 constexpr int kFlags = 8;               // units whose cells' existence is kept
 constexpr float kHeadroom = 8.0f, kSlack = 6.5f;       // weights are below 2^(kHeadroom + kSlack); 12 and 2.5 scale the sums anew more often: 336 -> 342 us
-// Registers of a thread by its warpgroup; with the 128 of the launch the four come to the same sum.
-constexpr int kSoftmaxRegs = 176, kDecodeRegs = 112, kOtherRegs = 48;
-static_assert(2 * kSoftmaxRegs + kDecodeRegs + kOtherRegs == 4 * 128, "the launch's registers");
-
 template <int kDim>
 struct Form {
     static constexpr int kTiles = kDim == 256 ? 1 : 2;
@@ -47,6 +43,10 @@ struct Form {
     static constexpr int kRows = kTiles * kTileRows;
     static constexpr int kKeyBytes = kUnitKeys * kDim * 2, kQueryBytes = kTileRows * kDim * 2;
     static constexpr int kSums = 256;                                   // first tensor-memory column of the sums; scores of tile t at 128 t
+    // Registers of a thread by its warpgroup (the second softmax warpgroup has nothing to do where there is one tile: the codes' gets them); with the
+    // 128 of the launch the four come to the same sum.
+    static constexpr int kSoftmaxRegs = 176, kSecondRegs = kTiles == 2 ? kSoftmaxRegs : 40, kDecodeRegs = kTiles == 2 ? 112 : 232, kOtherRegs = kTiles == 2 ? 48 : 64;
+    static_assert(kSoftmaxRegs + kSecondRegs + kDecodeRegs + kOtherRegs == 4 * 128, "the launch's registers");
     static constexpr int kOperands = kTiles * kQueryBytes + 2 * kStages * kKeyBytes;
 };
 
@@ -244,6 +244,11 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
     return r;
 }
 __device__ __forceinline__ float2 twice(float a) { return make_float2(a, a); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 // The lowest n bits of 16: none below 0, all from 16 on.
 __device__ __forceinline__ uint32_t low_bits(int n) { return (1u << min(max(n, 0), kCell)) - 1u; }
 
@@ -611,12 +616,9 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
         const int row = block.row0 + tile * kTileRows + min(t, rows - 1), token = p.by_group(row), position = block.before + token, count = s->count;
         // The piece's units whose every key every token of the block sees (one run of them), if the pages exist.  (Found once, in registers: a load from
         // shared memory waits behind the exponentials of the scheduler's other warps.)
-        int whole_begin = 0, whole_end = count;
-        {
-            const int off = s->off, sinks = block.sink_cells, past = a.window > 0 ? max(block.latest + 1 - a.window, 0) : 0;   // keys before `past` are behind some window
-            while (whole_begin < count && sinks + ((past + kCell - 1) / kCell - block.low_cell) > (off + whole_begin) * kUnitCells) ++whole_begin;
-            whole_end = min(count, (block.earliest + 1 < 0 ? 0 : sinks + (block.earliest + 1) / kCell - block.low_cell) / kUnitCells - off);
-        }
+        const int off = s->off, past = a.window > 0 ? max(block.latest + 1 - a.window, 0) : 0;     // keys before `past` are behind some window
+        const int whole_begin = (block.sink_cells + (past + kCell - 1) / kCell - block.low_cell + kUnitCells - 1) / kUnitCells - off;
+        const int whole_end = (block.earliest < 0 ? 0 : block.sink_cells + (block.earliest + 1) / kCell - block.low_cell) / kUnitCells - off;
         const unsigned unit0 = s->unit0;
         float top = kLowest, weight = 0.0f;
         for (int i = 0; i < count; ++i, ++units) {
@@ -652,7 +654,7 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
                 uint32_t seen[kUnitCells];
 #pragma unroll
                 for (int j = 0; j < kUnitCells; ++j) {
-                    const int from = block.cell_at((s->off + i) * kUnitCells + j) * kCell;
+                    const int from = block.cell_at((off + i) * kUnitCells + j) * kCell;
                     uint32_t m = low_bits(position + 1 - from);
                     if (a.window > 0) m &= ~low_bits(position + 1 - a.window - from) | low_bits(a.sinks - from);
                     seen[j] = bits >> j & 1 ? m : 0u;
@@ -660,15 +662,15 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
 #pragma unroll
                 for (int n = 0; n < 128; ++n) x[n] = seen[cell_of(n)] & 1u << token_of(n) ? x[n] : -INFINITY;
             }
-            float mosts[8];                                     // in chains side by side
+            float mosts[4];                                     // in chains side by side
 #pragma unroll
-            for (int n = 0; n < 8; ++n) mosts[n] = fmaxf(x[n], x[n + 8]);
+            for (int j = 0; j < 4; ++j) mosts[j] = fmaxf(x[j], x[4 + j]);
 #pragma unroll
-            for (int n = 16; n < 128; n += 16) {
+            for (int n = 8; n < 128; n += 8) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) mosts[j] = fmaxf(mosts[j], fmaxf(x[n + j], x[n + j + 8]));
+                for (int j = 0; j < 4; ++j) mosts[j] = max3(mosts[j], x[n + j], x[n + 4 + j]);
             }
-            float most = fmaxf(fmaxf(fmaxf(mosts[0], mosts[1]), fmaxf(mosts[2], mosts[3])), fmaxf(fmaxf(mosts[4], mosts[5]), fmaxf(mosts[6], mosts[7])));
+            float most = fmaxf(max3(mosts[0], mosts[1], mosts[2]), mosts[3]);
             const float factor = kCap ? 1.0f : a.scale;
             most *= factor;
             // weights as in kv8.cu: 2^(score - top), top the largest score so far less kHeadroom, or up to kSlack less
@@ -810,14 +812,17 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_prompt_kernel(const __grid_co
     const uint32_t tmem = bars->tmem, queries = smem_u32(operands), keys = queries + F::kTiles * F::kQueryBytes, values = keys + F::kStages * F::kKeyBytes;
     if (threadIdx.x == 0) p.a.open[blockIdx.x] = make_int4(-1, 0, 0, 0);
     __syncthreads();
-    if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        if (warp < 4 * F::kTiles) softmax_role<kDim, kCap>(p, bars, tmem, warp >> 2);
+    if (warp < 4 * F::kTiles) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F::kSoftmaxRegs));
+        softmax_role<kDim, kCap>(p, bars, tmem, warp >> 2);
+    } else if (warp < 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F::kSecondRegs));
     } else if (warp < 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDecodeRegs));
+        if constexpr (F::kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F::kDecodeRegs));
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(F::kDecodeRegs));
         decode_role<kDim>(p, bars, keys, values);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(F::kOtherRegs));
         if (warp == 12) {
             if (elect_one()) product_role<kDim>(p, bars, queries, keys, values, tmem);
             __syncwarp();
