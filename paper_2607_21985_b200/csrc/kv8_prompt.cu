@@ -12,13 +12,16 @@
 // the values of the second are exact; the weights are rounded to fp16 (2^-11, the one rounding besides the result's).
 // What bounds it: the way of a tile's scores, from the products through the softmax (some 1900 cycles a unit, 1024 of them the exponentials of
 // a scheduler's 32 rows) and back, two tiles side by side: 3700 cycles a unit of 256 rows, whose products are 2048; and the power limit, at 1.89
-// GHz.  4096 tokens of 64 and 8 heads of 128: 305 us, 0.9 PFLOP/s.  Tried and not kept: units of 64 keys with scores for two of them (384 us), a pair
-// of CTAs to 512 rows (cta_group::2, 327 us against 330, with 512 rows to a block), a thread to each tile's products (382 to 410), two threads to a
-// row (359), turns at the exponentials (340 to 381), part of them by a polynomial (376 and up).
+// GHz.  4096 tokens of 64 and 8 heads of 128: 305 us by itself, 0.9 PFLOP/s (327 to 343 with the store of its keys and values).  Tried and not kept:
+// units of 64 keys with scores for two of them (384 us), a pair of CTAs to 512 rows (cta_group::2, 327 us against 330, with 512 rows to a block), a
+// thread to each tile's products (382 to 410), two threads to a row (359), turns at the exponentials (340 to 381), part of them by a polynomial (376
+// and up), the softmax as two short loops over a row (332, but capped ones 209 against 185), code of its own for each softmax warpgroup (its code
+// then leaves the instruction cache: 45 % slower).
 //
 // The order of a unit's keys is what suits the operand tiles, and the same in both: row n of the keys' tile is token 2 (n % 64 / 16) + n % 2 +
 // 8 (n % 4 / 2) of cell 4 (n / 64) + 2 (n / 8 % 2) + n / 4 % 2.  So the 8 keys of a 16-byte piece of a dimension's row of the values' tile are
 // words of two cells that one lane has, and the lanes' pieces of either tile fall into different banks.
+#include <cfloat>
 #include <mutex>
 
 #include "kv8.cuh"
@@ -639,7 +642,7 @@ __device__ __forceinline__ void softmax_role(const PromptParams& p, Barriers* ba
 #pragma unroll
                     for (int n = 0; n < 128; ++n) x[n] = capped(a, x[n] * a.scale);
                 } else {                                        // as capped_near, in pairs
-                    const float f = a.scale * a.cap_inv;
+                    const float f = fminf(a.scale * a.cap_inv, FLT_MAX);       // never Inf, for a product may be 0
 #pragma unroll
                     for (int n = 0; n < 128; n += 2) {
                         const float2 z = mul2(make_float2(x[n], x[n + 1]), twice(a.scale)), y = mul2(make_float2(x[n], x[n + 1]), twice(f)), t = mul2(y, y);

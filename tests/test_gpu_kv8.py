@@ -319,6 +319,19 @@ def test_attn_kv8_caps_that_leave_nothing_of_the_scores(S, tokens):
     attn_check(y, dev(q) * 0, oracle, table, [0, tokens], [100], 0.1)
 
 
+@pytest.mark.parametrize("scale,cap", [(2.0, 1e-40), (1e16, 1e-24), (-1e16, 1e-30)])
+@pytest.mark.parametrize("tokens", [1, 70])
+def test_attn_kv8_small_caps_of_large_scales(S, tokens, scale, cap):
+    """Products of 0 under a cap that the scale divided by is beyond 32 bits: weights of 1 like those of the others."""
+    rng = np.random.default_rng(17)
+    table, oracle = filled(rng, 1, 64, 16, [100])
+    q = np.stack([np.zeros((tokens, 64)), rng.standard_normal((tokens, 64))], 1).astype(np.float16)
+    q[:tokens // 2] = 0                  # all rows of a warp, and some
+    y = torch.empty(tokens, 128, dtype=torch.float16, device="cuda")
+    S.spdp_attn_kv8(dev(q), dev(oracle.raw), 16, 1, dev(table), ints(100), y, scale, first=ints(0, tokens), cap=cap)
+    attn_check(y, dev(q) * 0, oracle, table, [0, tokens], [100], 0.1)
+
+
 @pytest.mark.parametrize("tokens", [1, 90])
 def test_attn_kv8_no_numbers(S, tokens):
     """NaN and Inf in one token's query reach that head of that token only."""
