@@ -140,8 +140,8 @@ __global__ void __launch_bounds__(256) free_kernel(int32_t* ref, int pages, Tabl
     dev::programmatic_start();
     const int i = blockIdx.x, r = row[i];
     if (r < 0 || r >= t.rows) return;
-    const int end = within(to[i], t.pages);
-    for (int e = within(from[i], t.pages) + threadIdx.x; e < end; e += blockDim.x) {
+    const int64_t end = within(to[i], t.pages);                 // a row may have nearly 2^31 entries
+    for (int64_t e = within(from[i], t.pages) + static_cast<int64_t>(threadIdx.x); e < end; e += blockDim.x) {
         const int page = atomicExch(&t.entries[r * t.stride + e], -1);      // so that an entry that is named twice is freed once
         if (page >= 0 && page < pages) atomicSub(&ref[page], 1);
     }
@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(kThreads) fork_kernel(int32_t* ref, int pages,
         for (int i = blockIdx.x - 1; i < f.n; i += gridDim.x - 1) {
             if (!f.exists(t, i)) continue;
             const int full = f.tokens(t, i) >> f.page_shift;
-            for (int e = threadIdx.x; e < full; e += kThreads) {
+            for (int64_t e = threadIdx.x; e < full; e += kThreads) {
                 const int page = t.entries[f.parent[i] * t.stride + e];
                 const bool ok = page >= 0 && page < pages;
                 t.entries[f.child[i] * t.stride + e] = ok ? page : -1;

@@ -625,6 +625,25 @@ def test_kv_pages_odd_tables_and_full_caches(S):
     assert int(short) == 0
 
 
+def test_kv_pages_longest_row(S):
+    """The last entries of a row of as many as a table may have."""
+    most, count = 2 ** 31 - 1, 3000
+    if torch.cuda.mem_get_info()[0] < 5 * most:
+        pytest.skip("needs 11 GB of device memory")
+    tab = torch.empty(1, most, dtype=torch.int32, device="cuda")
+    ref, short = torch.zeros(4000, dtype=torch.int32, device="cuda"), ints(-1)
+    tab[0, -count - 5:] = 17
+    row, start, stop = ints(0), ints(most - count), ints(most)
+    S.spdp_kv_pages_take(ref, tab, row, start, stop, short)
+    torch.cuda.synchronize()
+    assert int(short) == 0 and torch.equal(tab[0, -count:], torch.arange(count, dtype=torch.int32, device="cuda")) and int(ref.sum()) == count
+    S.spdp_kv_pages_free(ref, tab, row, start, stop)
+    torch.cuda.synchronize()
+    assert bool((tab[0, -count:] == -1).all()) and bool((tab[0, -count - 5:-count] == 17).all()) and int(ref.abs().sum()) == 0
+    del tab
+    torch.cuda.empty_cache()
+
+
 def test_kv_pages_captured(S):
     """A step's whole handling of pages in a graph, replayed on another state."""
     rng = np.random.default_rng(5)
