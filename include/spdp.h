@@ -375,7 +375,8 @@ SPDP_API spdp_status spdp_kv8_page_bytes(int kv_heads, int head_dim, int page_to
  *                they are not stored.  Rows of tokens that are passed over stay as they were.
  * A cell's first token makes the rest of it zeros.  One that joins a cell whose scale is too small for it makes the scale grow, and
  * the codes of the tokens before are rounded again (those that stand for less than 2^-6 of the new scale change, by half a step of
- * 2^-9 of it at most).  Launches one kernel. */
+ * 2^-9 of it at most).  Where a request's length has gone back, its new tokens take the places of those that are no more: a cell that still holds older ones
+ * keeps the scale it has, also where that was a lost token's.  Launches one kernel. */
 SPDP_API spdp_status spdp_kv8_store(const void* k_dev, int64_t ldk, const void* v_dev, int64_t ldv, spdp_ydtype vdt, int64_t N, int kv_heads, int head_dim, int64_t B,
                            const void* first_dev, const void* table_dev, int64_t table_stride, int64_t table_pages, const void* length_dev, void* cache_dev,
                            int64_t pages, int page_tokens, void* k_values_dev_out, int64_t ldk_values, void* v_values_dev_out, int64_t ldv_values, void* stream);

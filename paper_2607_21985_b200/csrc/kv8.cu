@@ -354,7 +354,8 @@ cudaError_t launch_store(StoreParams p, bool wide, int sms, cudaStream_t s) {
 // fp16 numbers they are.  The keys' scale multiplies the scores, the values' scale 2^e the weights: as a term of the exponent, so
 // that what is rounded to fp16 (2^-11, the one rounding besides the result's) is as large as it counts in the sum.
 // What bounds it: memory.  48 requests of up to 16384 keys, 64 and 8 heads of 128: 890 MB in 143 us (6.2 TB/s); one request of 131072: 271 MB in 51.5 us
-// (5.3 TB/s), the start and the end of a run being 4 us of it.  Issue is 33 to 39 % busy: a cell is 64 conversions (two codes each), 16 products.
+// (5.3 TB/s), the start and the end of a run being 4 us of it.  Issue is 33 to 39 % busy: a cell is 64 conversions (two codes each), 16 products.  Rows behind
+// the first 8 or 16 go through the keys again, and that is not hidden behind the bytes: one request of 131072 keys takes 76 us with 16 rows, 127 with 32, 226 with 64.
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
@@ -752,7 +753,9 @@ template <int kChunks, int kCols>
 size_t line_bytes(int B) { return base_bytes<kChunks, kCols>() + (kWarps + B + 1) * sizeof(int); }
 
 // Up to here a cluster to a triple, where all of them fit the GPU at once.  What decides is the longest that the table or the window
-// allows: a request's own length is only known on the device.
+// allows: a request's own length is only known on the device.  As a line or as clusters, us, 8 query heads to a key head: 8 triples of heads of 128 18.8 / 14.3 at 4000
+// keys, 20.8 / 20.5 at 8000, 22.8 / 30.7 at 16000; 32 triples 29.0 / 24.6 at 8000, 59.7 / 59.4 at 32000; 8 of 64 16.7 / 14.3 and 16.8 / 18.4, 4 of 256 20.8 / 20.5 and
+// 22.8 / 30.7 at 4000 and 8000.
 constexpr int kClusterKeys = 8192;
 
 template <int kChunks, int kCols>
@@ -803,8 +806,9 @@ spdp_status launch_form(AttnParams p, int device, int sms, cudaStream_t s) {
 template <int kChunks>
 spdp_status launch_dim(const AttnParams& p, int device, int sms, cudaStream_t s) {
     if constexpr (kChunks < 4) {                                // heads of 256 leave no registers for 16 columns
-        // rows of a request, on average, that make two blocks of columns worth their place; beside prompts, whose tokens the number N has too, those
-        // of one token
+        // Rows of a request, on average, that make two blocks of columns worth their place; beside prompts, whose tokens the number N has too, those
+        // of one token.  One or two, us, 8 key heads of 128: 48 requests behind 4000 keys 98 / 120 at 8 rows, 157 / 124 at 16, 218 / 202 at 24, 497 / 360 at 64;
+        // one behind 65536 43 / 50, 64 / 50, 68 / 76, 172 / 125; one behind 2000 12 / 14, 12 / 16, 13 / 16, 21 / 16.
         if (p.most_rows < INT32_MAX ? p.group > 8 : static_cast<int64_t>(p.N) * p.group > 8ll * p.B) return launch_form<kChunks, 2>(p, device, sms, s);
     }
     return launch_form<kChunks, 1>(p, device, sms, s);

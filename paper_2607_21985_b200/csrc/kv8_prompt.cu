@@ -12,7 +12,9 @@
 // the values of the second are exact; the weights are rounded to fp16 (2^-11, the one rounding besides the result's).
 // What bounds it: the way of a tile's scores, from the products through the softmax (some 1900 cycles a unit, 1024 of them the exponentials of
 // a scheduler's 32 rows) and back, two tiles side by side: 3700 cycles a unit of 256 rows, whose products are 2048; and the power limit, at 1.89
-// GHz.  4096 tokens of 64 and 8 heads of 128: 305 us by itself, 0.9 PFLOP/s (327 to 343 with the store of its keys and values).  Tried and not kept:
+// GHz.  4096 tokens of 64 and 8 heads of 128: 305 to 326 us by itself, 0.9 PFLOP/s (327 to 347 with the store of its keys and values).  Under a cap 520 while a warp's
+// scores are within a quarter of it; where they are not, 1470 to 1540 (an exponential and a quotient more to a score; 2045 tokens of 32 and 8 heads in pieces with a
+// window 118, 174 and 412).  Tried and not kept:
 // units of 64 keys with scores for two of them (384 us), a pair of CTAs to 512 rows (cta_group::2, 327 us against 330, with 512 rows to a block), a
 // thread to each tile's products (382 to 410), two threads to a row (359), turns at the exponentials (340 to 381), part of them by a polynomial (376
 // and up), the softmax as two short loops over a row (332, but capped ones 209 against 185), code of its own for each softmax warpgroup (its code

@@ -3,8 +3,9 @@
 // free.  What a call does follows from these alone, page by page in their order, so the same state gives the same pages; and all of it
 // may be captured together with the steps that use the pages.
 //
-// Counting and naming are integers; what takes time is moving pages (2 bytes of traffic to each byte of a page, in every layer): 300 pages of
-// 12 layers of 16.5 KB in 18 us, 6.6 TB/s.  Calls on few pages are the latency of a kernel's loads, one after another.
+// Counting and naming are integers; what takes time is moving pages (2 bytes of traffic to each byte of a page, in every layer): 3000 pages of
+// 12 layers of 16.5 KB in 207 us, 5.7 TB/s; 1000 of 33 KB in 141 us, 5.6 TB/s.  300 of 16.5 KB take 18 to 20 us, which is no rate of the memory's: 74 of their 119 MB
+// reach it, the rest stays in the second-level cache.  Calls on few pages are the latency of a kernel's loads, one after another.
 #include <mutex>
 
 #include "kv8.cuh"

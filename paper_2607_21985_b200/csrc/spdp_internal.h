@@ -242,7 +242,12 @@ struct Kv8AttnCall {
     int q_heads, kv_heads, head_dim, page_tokens;
     float scale, cap, thr;
 };
-constexpr int kFewRows = 64;    // tokens times query heads of a key head, up to which a request's attention is kv8.cu's and not kv8_prompt.cu's
+// Tokens times query heads of a key head, up to which a request's attention is kv8.cu's and not kv8_prompt.cu's.  kv8.cu takes 8 or 16 of these rows at a time
+// through all keys, kv8_prompt.cu 128 or 256 but has three launches.  One request by either, us: 8 key heads of 128, behind 2000 keys 16 / 31 at 64 rows, behind
+// 131072 76 / 148 at 16, 127 / 148 at 32, 172 / 148 at 40, 226 / 148 at 64; of 64, 74 / 127 at 32 and 125 / 127 at 64; 4 of 256, 150 / 148 at 24 and 303 / 150
+// at 64.  So 64 is the border behind short contexts and for heads of 64; behind long ones it would be 32 for heads of 128 and 16 for 256, but lengths are only
+// known on the device.
+constexpr int kFewRows = 64;
 spdp_status launch_attn_kv8(const Kv8AttnCall& call, cudaStream_t s);
 
 // kv_pages.cu
